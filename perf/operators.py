@@ -214,9 +214,9 @@ def prepare(case, seed):
         return s
     t, e, k = c["tokens"], c["experts"], c["top_k"]
     s.logits = _normal(seed, 21, (t, e), dtype=torch.float32)
-    if c["masked"]:                                   # experts out of service, and a token whose every expert is
+    if c["masked"]:                                   # experts out of service, and (of several) a token whose every expert is
         s.logits[torch.rand((t, e), generator=_generator(seed, 22), device=DEV) < c["masked"]] = -math.inf
-        s.logits[t // 2] = -math.inf
+        s.logits[t // 2:t // 2 + min(1, t // 2)] = -math.inf
     if c["logits"] == "bf16":
         s.logits = s.logits.bfloat16()
     s.bias = _normal(seed, 23, (e,), 0.1, torch.float32) if c["bias"] else None
