@@ -742,6 +742,56 @@ MW_API int32_t mw_relay_packets_copy_index_next(mw_ctx *ctx, const mw_recv_packe
                                          const mw_recv_packets *next_in_dev, int64_t next_child_capacity_rows,
                                          mw_relay_stats *next_stats_dev, void *stream);
 
+/* ---- the gate, and the experts of a few tokens ------------------------------------------- */
+
+/*
+ * What a gate's scores mean.  Scores l are one row of n_experts values a token (a NaN counts as -inf, +inf as the
+ * largest finite value); c is `scale`.  Experts are taken by s = l + bias, one fp32 addition (without a bias s = l; at
+ * most the largest finite value).  With n_groups > 1 the experts are n_groups runs of n_experts / n_groups; a group's
+ * score is the fp32 sum of its two best s (a group of one expert: its s), and only the kept_groups best groups' experts
+ * can be taken.  The top_k best are taken in descending order; among equals the lowest expert, the lowest group.  An
+ * expert whose s is -inf (or NaN) is never taken: where fewer than top_k are left the id is -1 and the weight 0, so a token
+ * whose experts are all masked goes nowhere.  Weights do not use the bias:
+ *   MW_GATE_SOFTMAX       w_k = c exp(l_k) / sum over all experts of exp(l_e)
+ *   MW_GATE_SOFTMAX_TOPK  w_k = c exp(l_k) / sum over the experts taken of exp(l_j)
+ *   MW_GATE_SIGMOID_TOPK  w_k = c sig(l_k) / sum over the experts taken of sig(l_j)   (0 where that sum is 0)
+ */
+#define MW_GATE_SOFTMAX      0
+#define MW_GATE_SOFTMAX_TOPK 1
+#define MW_GATE_SIGMOID_TOPK 2
+#define MW_LOGITS_F32  0
+#define MW_LOGITS_BF16 1
+#define MW_GATE_MAX_EXPERTS 1024
+#define MW_GATE_MAX_GROUPS  64
+typedef struct mw_gate {
+    int32_t score;          /* MW_GATE_* */
+    int32_t n_groups;       /* 1: no groups; divides n_experts, at most MW_GATE_MAX_GROUPS */
+    int32_t kept_groups;    /* 1..n_groups */
+    float scale;            /* finite */
+} mw_gate;                  /* 16 bytes, HOST */
+
+/*
+ * mw_route: the gate's scores -> the expert ids mw_plan takes, and their weights.  n_experts and top_k are the
+ * context's.  logits_dev [n_tokens] rows of n_experts values (MW_LOGITS_*), logit_stride elements apart; bias_dev [n_experts]
+ * fp32 or NULL; topk_ids_dev [n_tokens][top_k] int32 and topk_weights_dev [n_tokens][top_k] fp32 are written whole.
+ * 0 <= n_tokens <= max_tokens.  Uses no workspace.  More than MW_GATE_MAX_EXPERTS experts: MW_ERR_UNSUPPORTED.
+ */
+MW_API int32_t mw_route(mw_ctx *ctx, const mw_gate *gate, const void *logits_dev, int32_t logit_format, int64_t logit_stride,
+                        const float *bias_dev, int32_t n_tokens, int32_t *topk_ids_dev, float *topk_weights_dev, void *stream);
+
+/*
+ * mw_route_backward: the gradient of mw_route's weights with respect to its scores, for the experts it took (which ones
+ * it took has no gradient, so neither has the bias).  d_weights_dev [n_tokens][top_k] fp32; an id outside [0, n_experts) stands
+ * for no expert.  d_logits_dev: rows of the scores' format, d_logit_stride elements apart, written whole.  With q_k = w_k / c
+ * and M = sum over k of d_weights_k q_k:
+ *   MW_GATE_SOFTMAX       d_l_e = c p_e (d_weights_e - M), p the softmax over all experts, d_weights_e = 0 where e was not taken
+ *   MW_GATE_SOFTMAX_TOPK  d_l_k = c q_k (d_weights_k - M), 0 elsewhere
+ *   MW_GATE_SIGMOID_TOPK  d_l_k = c q_k (1 - sig(l_k)) (d_weights_k - M), 0 elsewhere
+ */
+MW_API int32_t mw_route_backward(mw_ctx *ctx, const mw_gate *gate, const void *logits_dev, int32_t logit_format, int64_t logit_stride,
+                                 const int32_t *topk_ids_dev, const float *d_weights_dev, int32_t n_tokens, void *d_logits_dev,
+                                 int64_t d_logit_stride, void *stream);
+
 /* ---- simulation and measurement helpers (not part of the dispatch path) ---------------- */
 
 /*

@@ -32,7 +32,8 @@ EXPORTS = ["mw_workspace_bytes", "mw_ctx_create", "mw_ctx_destroy", "mw_plan", "
            "mw_sim_deliver", "mw_copy_bytes", "mw_get_send_stats", "mw_get_recv_stats",
            "mw_set_forwarding", "mw_relay", "mw_relay_index", "mw_relay_copy", "mw_relay_copy_index_next", "mw_relay_packets", "mw_relay_packets_index", "mw_relay_packets_copy", "mw_relay_packets_copy_index_next", "mw_get_relay_stats",
            "mw_allgather_split_point", "mw_plan_allgather_split", "mw_unpack_allgather_split",
-           "mw_ctx_set_timing_events", "mw_status_string", "mw_plan_static", "mw_ctx_set_options", "mw_relay_batch"]
+           "mw_ctx_set_timing_events", "mw_status_string", "mw_plan_static", "mw_ctx_set_options", "mw_relay_batch",
+           "mw_route", "mw_route_backward"]
 MW_KERNEL_PLAN_RANK, MW_KERNEL_PLAN_GROUPS, MW_KERNEL_PACK, MW_KERNEL_RECV_INDEX, MW_KERNEL_EXPAND = 0, 1, 2, 3, 4
 MW_KERNEL_AG_PACK, MW_KERNEL_AG_GATHER, MW_KERNEL_RELAY_INDEX, MW_KERNEL_RELAY_COPY = 5, 6, 7, 8
 MW_KERNEL_PLAN_PACK, MW_KERNEL_PACK_QUANT, MW_KERNEL_COMBINE = 9, 10, 11
@@ -44,6 +45,9 @@ MW_FLAG_BAD_RANK = 0x80
 MW_FLAG_PLAN_TIMEOUT = 0x100
 MW_FLAG_DUPLICATE_DROPPED = 0x200
 MW_OPT_RELAY_KEEP_METADATA, MW_OPT_RECV_DEDUP = 0x1, 0x2
+MW_GATE_SOFTMAX, MW_GATE_SOFTMAX_TOPK, MW_GATE_SIGMOID_TOPK = 0, 1, 2
+MW_LOGITS_F32, MW_LOGITS_BF16 = 0, 1
+MW_GATE_MAX_EXPERTS, MW_GATE_MAX_GROUPS = 1024, 64
 
 # numpy views of the ABI records (host copies)
 DESC_DTYPE = np.dtype([("mask", "<u8", (4,)), ("row_offset", "<u4"), ("row_count", "<u4"),
@@ -103,6 +107,11 @@ class MwRelayJob(C.Structure):
                 ("child_capacity_rows", C.c_int64), ("stats_dev", C.c_void_p)]
 
 
+class MwGate(C.Structure):
+    """mw_gate (include/mw.h)."""
+    _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("kept_groups", C.c_int32), ("scale", C.c_float)]
+
+
 class MwError(RuntimeError):
     def __init__(self, status: int, where: str):
         super().__init__("%s: %s (%d)" % (where, status_string(status), status))
@@ -134,7 +143,8 @@ _KINDS = {"mw_plan": "htittttp", "mw_pack": "htttttitttp", "mw_pack_quantize": "
           "mw_unpack_allgather": "htltp", "mw_plan_allgather_split": "hllttp", "mw_unpack_allgather_split": "httlltp",
           "mw_allgather_step": "htltttttp", "mw_relay": "httltp", "mw_relay_index": "httltp", "mw_relay_copy": "htttp",
           "mw_relay_copy_index_next": "httthttltp", "mw_relay_packets": "httltp", "mw_relay_packets_index": "htltp",
-          "mw_relay_packets_copy": "htttp", "mw_relay_packets_copy_index_next": "httthtltp"}
+          "mw_relay_packets_copy": "htttp", "mw_relay_packets_copy_index_next": "httthtltp",
+          "mw_route": "hptiltittp", "mw_route_backward": "hptilttitlp"}
 _calls = None
 
 
@@ -246,6 +256,29 @@ def next_batch(next_ctx, peers, n_peers, out_capacity_rows, expert_offsets, recv
                        _addr(desc), _addr(send_stats))
 
 
+class Gate:
+    """mw_gate: how scores become expert ids and weights (include/mw.h)."""
+
+    def __init__(self, score: int, n_groups: int = 1, kept_groups: int = 1, scale: float = 1.0):
+        self.record = MwGate(score, n_groups, kept_groups, scale)
+        self.address = C.addressof(self.record)
+
+
+_LOGIT_FORMAT = {torch.float32: MW_LOGITS_F32, torch.bfloat16: MW_LOGITS_BF16}
+
+
+def _rows(t: torch.Tensor, width: int, what: str) -> int:
+    """Elements from row to row of a matrix whose rows are in one piece each."""
+    if t.dim() != 2 or t.shape[1] != width or (t.stride(1) != 1 and width > 1):
+        raise ValueError("%s: rows of %d values in one piece each, got shape %s and strides %s" % (what, width, tuple(t.shape), t.stride()))
+    return max(t.stride(0), width) if t.shape[0] < 2 else t.stride(0)
+
+
+def _whole(t: Optional[torch.Tensor], shape, dtype, what: str):
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError("%s: a contiguous tensor of %s and shape %s, got %s and %s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+
+
 MW_RELAY_BATCH_MAX = 4
 
 
@@ -305,6 +338,32 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    # ---- gate ----------------------------------------------------------------------------
+    def _logits(self, logits: torch.Tensor, what: str):
+        if logits.dtype not in _LOGIT_FORMAT:
+            raise ValueError("%s: float32 or bfloat16, got %s" % (what, logits.dtype))
+        return _LOGIT_FORMAT[logits.dtype], _rows(logits, self.n_experts, what)
+
+    def mw_route(self, gate: Gate, logits: torch.Tensor, bias: Optional[torch.Tensor], topk_ids: torch.Tensor,
+                 topk_weights: torch.Tensor):
+        n = logits.shape[0]
+        fmt, stride = self._logits(logits, "logits")
+        _whole(bias, (self.n_experts,), torch.float32, "bias")
+        _whole(topk_ids, (n, self.top_k), torch.int32, "topk_ids")
+        _whole(topk_weights, (n, self.top_k), torch.float32, "topk_weights")
+        _check(_native().mw_route(self._h, gate.address, logits, fmt, stride, bias, n, topk_ids, topk_weights, _stream_handle()), "mw_route")
+
+    def mw_route_backward(self, gate: Gate, logits: torch.Tensor, topk_ids: torch.Tensor, d_weights: torch.Tensor, d_logits: torch.Tensor):
+        n = logits.shape[0]
+        fmt, stride = self._logits(logits, "logits")
+        d_fmt, d_stride = self._logits(d_logits, "d_logits")
+        if d_fmt != fmt or d_logits.shape[0] != n:
+            raise ValueError("d_logits: as many rows as logits, of their type")
+        _whole(topk_ids, (n, self.top_k), torch.int32, "topk_ids")
+        _whole(d_weights, (n, self.top_k), torch.float32, "d_weights")
+        _check(_native().mw_route_backward(self._h, gate.address, logits, fmt, stride, topk_ids, d_weights, n, d_logits, d_stride,
+                                           _stream_handle()), "mw_route_backward")
 
     # ---- send side -----------------------------------------------------------------------
     def mw_plan(self, topk_ids: torch.Tensor, mask: torch.Tensor, perm: torch.Tensor,

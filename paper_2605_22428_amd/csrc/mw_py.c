@@ -83,6 +83,8 @@ CALL(mw_relay_packets, "httltp", P(0), P(1), P(2), L(3), P(4), P(5))
 CALL(mw_relay_packets_index, "htltp", P(0), P(1), L(2), P(3), P(4))
 CALL(mw_relay_packets_copy, "htttp", P(0), P(1), P(2), P(3), P(4))
 CALL(mw_relay_packets_copy_index_next, "httthtltp", P(0), P(1), P(2), P(3), P(4), P(5), L(6), P(7), P(8))
+CALL(mw_route, "hptiltittp", P(0), P(1), P(2), I(3), L(4), P(5), I(6), P(7), P(8), P(9))
+CALL(mw_route_backward, "hptilttitlp", P(0), P(1), P(2), I(3), L(4), P(5), P(6), I(7), P(8), L(9), P(10))
 
 // The calls, once for the module's functions and once for their addresses.
 #define CALLS(X)                                                                                                        \
@@ -91,7 +93,7 @@ CALL(mw_relay_packets_copy_index_next, "httthtltp", P(0), P(1), P(2), P(3), P(4)
     X(mw_plan_allgather) X(mw_pack_allgather) X(mw_unpack_allgather) X(mw_plan_allgather_split)                         \
     X(mw_unpack_allgather_split) X(mw_allgather_step) X(mw_relay) X(mw_relay_index) X(mw_relay_copy)                    \
     X(mw_relay_copy_index_next) X(mw_relay_packets) X(mw_relay_packets_index) X(mw_relay_packets_copy)                  \
-    X(mw_relay_packets_copy_index_next)
+    X(mw_relay_packets_copy_index_next) X(mw_route) X(mw_route_backward)
 
 #define SLOT(name) {#name, (void **)&fn_##name},
 static const struct { const char *name; void **at; } slots[] = {CALLS(SLOT)};
