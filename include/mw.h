@@ -792,6 +792,48 @@ MW_API int32_t mw_route_backward(mw_ctx *ctx, const mw_gate *gate, const void *l
                                  const int32_t *topk_ids_dev, const float *d_weights_dev, int32_t n_tokens, void *d_logits_dev,
                                  int64_t d_logit_stride, void *stream);
 
+/*
+ * The weights of this rank's experts, in the order of their ids (HOST record of device arrays).
+ *   MW_ROW_BF16               gate_up [local experts][2][inter][hidden] bf16 (gate rows, then up rows), down [local experts]
+ *                             [hidden][inter] bf16; no scales.  hidden and inter are multiples of 8.
+ *   MW_ROW_FP8_E4M3_BLOCK128  e4m3 codes in the same places, an fp32 factor per 128 x 128 block of a matrix (blocks at its edges are
+ *                             smaller): gate_up_scale [local experts][2][ceil(inter/128)][ceil(hidden/128)], down_scale
+ *                             [local experts][ceil(hidden/128)][ceil(inter/128)].  hidden and inter are multiples of 16.
+ * Arrays contiguous, weights 16-byte aligned.
+ */
+typedef struct mw_experts {
+    const void *gate_up_dev;
+    const void *down_dev;
+    const float *gate_up_scale_dev;
+    const float *down_scale_dev;
+    int32_t inter;
+    int32_t format;         /* MW_ROW_BF16 or MW_ROW_FP8_E4M3_BLOCK128 */
+} mw_experts;               /* 40 bytes */
+
+#define MW_LAYER_MAX_TOKENS 256  /* largest batch mw_moe_layer takes */
+
+/* Bytes of device workspace mw_moe_layer needs for batches of up to max_tokens (at most MW_LAYER_MAX_TOKENS). */
+MW_API int32_t mw_moe_workspace_bytes(mw_ctx *ctx, const mw_experts *experts, int32_t max_tokens, int64_t *out_bytes);
+
+/*
+ * mw_moe_layer: this rank's share of a mixture-of-experts layer for a few tokens that it already has, without a dispatch:
+ *   out[t] = sum over the token's distinct ids k that are experts of this rank (expert_to_rank) of
+ *            w_k down_k (silu(gate_k x_t) * (up_k x_t)),      silu(v) = v / (1 + exp(-v))
+ * in fp32 sums, rounded to bf16 once.  A token that goes to none of them gets zeros; ranks that share the experts add up their outputs.
+ *   gate, logits_dev, logit_format, logit_stride, bias_dev: as mw_route, which is done first and writes topk_ids_dev and
+ *     topk_weights_dev; with gate and logits_dev both NULL these two are read instead.  An id that a token names twice weighs the sum of both.
+ *   x_dev, out_dev: bf16 rows of `hidden` values, x_stride and out_stride elements apart (multiples of 8; 16-byte aligned).  They
+ *     must not overlap.
+ *   error_flags_dev: a word that MW_FLAG_BAD_EXPERT is or'ed into where an id is outside {-1} U [0, n_experts) (it is left out); or NULL.
+ *   workspace_dev: 256-byte aligned, mw_moe_workspace_bytes; needs no preparation.  Calls that share one must not overlap.
+ * 0 <= n_tokens <= min(max_tokens, MW_LAYER_MAX_TOKENS).  At most MW_GATE_MAX_EXPERTS experts; contexts of MW_ROW_BYTES have no hidden size:
+ * MW_ERR_UNSUPPORTED.
+ */
+MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const void *logits_dev, int32_t logit_format, int64_t logit_stride,
+                            const float *bias_dev, const mw_experts *experts, const void *x_dev, int64_t x_stride, int32_t n_tokens,
+                            int32_t *topk_ids_dev, float *topk_weights_dev, void *out_dev, int64_t out_stride,
+                            uint32_t *error_flags_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
 /* ---- simulation and measurement helpers (not part of the dispatch path) ---------------- */
 
 /*

@@ -33,7 +33,7 @@ EXPORTS = ["mw_workspace_bytes", "mw_ctx_create", "mw_ctx_destroy", "mw_plan", "
            "mw_set_forwarding", "mw_relay", "mw_relay_index", "mw_relay_copy", "mw_relay_copy_index_next", "mw_relay_packets", "mw_relay_packets_index", "mw_relay_packets_copy", "mw_relay_packets_copy_index_next", "mw_get_relay_stats",
            "mw_allgather_split_point", "mw_plan_allgather_split", "mw_unpack_allgather_split",
            "mw_ctx_set_timing_events", "mw_status_string", "mw_plan_static", "mw_ctx_set_options", "mw_relay_batch",
-           "mw_route", "mw_route_backward"]
+           "mw_route", "mw_route_backward", "mw_moe_workspace_bytes", "mw_moe_layer"]
 MW_KERNEL_PLAN_RANK, MW_KERNEL_PLAN_GROUPS, MW_KERNEL_PACK, MW_KERNEL_RECV_INDEX, MW_KERNEL_EXPAND = 0, 1, 2, 3, 4
 MW_KERNEL_AG_PACK, MW_KERNEL_AG_GATHER, MW_KERNEL_RELAY_INDEX, MW_KERNEL_RELAY_COPY = 5, 6, 7, 8
 MW_KERNEL_PLAN_PACK, MW_KERNEL_PACK_QUANT, MW_KERNEL_COMBINE = 9, 10, 11
@@ -48,6 +48,7 @@ MW_OPT_RELAY_KEEP_METADATA, MW_OPT_RECV_DEDUP = 0x1, 0x2
 MW_GATE_SOFTMAX, MW_GATE_SOFTMAX_TOPK, MW_GATE_SIGMOID_TOPK = 0, 1, 2
 MW_LOGITS_F32, MW_LOGITS_BF16 = 0, 1
 MW_GATE_MAX_EXPERTS, MW_GATE_MAX_GROUPS = 1024, 64
+MW_LAYER_MAX_TOKENS = 256
 
 # numpy views of the ABI records (host copies)
 DESC_DTYPE = np.dtype([("mask", "<u8", (4,)), ("row_offset", "<u4"), ("row_count", "<u4"),
@@ -112,6 +113,12 @@ class MwGate(C.Structure):
     _fields_ = [("score", C.c_int32), ("n_groups", C.c_int32), ("kept_groups", C.c_int32), ("scale", C.c_float)]
 
 
+class MwExperts(C.Structure):
+    """mw_experts (include/mw.h)."""
+    _fields_ = [("gate_up_dev", C.c_void_p), ("down_dev", C.c_void_p), ("gate_up_scale_dev", C.c_void_p), ("down_scale_dev", C.c_void_p),
+                ("inter", C.c_int32), ("format", C.c_int32)]
+
+
 class MwError(RuntimeError):
     def __init__(self, status: int, where: str):
         super().__init__("%s: %s (%d)" % (where, status_string(status), status))
@@ -144,7 +151,8 @@ _KINDS = {"mw_plan": "htittttp", "mw_pack": "htttttitttp", "mw_pack_quantize": "
           "mw_allgather_step": "htltttttp", "mw_relay": "httltp", "mw_relay_index": "httltp", "mw_relay_copy": "htttp",
           "mw_relay_copy_index_next": "httthttltp", "mw_relay_packets": "httltp", "mw_relay_packets_index": "htltp",
           "mw_relay_packets_copy": "htttp", "mw_relay_packets_copy_index_next": "httthtltp",
-          "mw_route": "hptiltittp", "mw_route_backward": "hptilttitlp"}
+          "mw_route": "hptiltittp", "mw_route_backward": "hptilttitlp",
+          "mw_moe_layer": "hptiltptlitttlttlp"}
 _calls = None
 
 
@@ -264,6 +272,35 @@ class Gate:
         self.address = C.addressof(self.record)
 
 
+class Experts:
+    """mw_experts: the weights of a rank's experts (include/mw.h), gate_up [local experts][2][inter][hidden] and down
+    [local experts][hidden][inter], bfloat16, or float8_e4m3fn with a float32 factor per 128 x 128 block of each matrix."""
+
+    def __init__(self, gate_up: torch.Tensor, down: torch.Tensor, gate_up_scale: Optional[torch.Tensor] = None,
+                 down_scale: Optional[torch.Tensor] = None):
+        n, two, inter, hidden = gate_up.shape
+        fp8 = gate_up.dtype == torch.float8_e4m3fn
+        dtype = torch.float8_e4m3fn if fp8 else torch.bfloat16
+        if two != 2:
+            raise ValueError("gate_up: [experts][2][inter][hidden], got %s" % (tuple(gate_up.shape),))
+        _whole(gate_up, (n, 2, inter, hidden), dtype, "gate_up")
+        _whole(down, (n, hidden, inter), dtype, "down")
+        if fp8 != (gate_up_scale is not None) or fp8 != (down_scale is not None):
+            raise ValueError("float8 weights come with both scales, bfloat16 weights with none")
+        _whole(gate_up_scale, (n, 2, -(-inter // 128), -(-hidden // 128)), torch.float32, "gate_up_scale")
+        _whole(down_scale, (n, -(-hidden // 128), -(-inter // 128)), torch.float32, "down_scale")
+        self._held = (gate_up, down, gate_up_scale, down_scale)
+        self.n_local, self.inter, self.hidden = n, inter, hidden
+        self.record = MwExperts(*(_addr(t) for t in self._held), inter, MW_ROW_FP8_E4M3_BLOCK128 if fp8 else MW_ROW_BF16)
+        self.address = C.addressof(self.record)
+
+
+def _workspace(n_bytes: int, device) -> torch.Tensor:
+    """A tensor of at least n_bytes that begins on 256 bytes."""
+    t = torch.empty(n_bytes + 256, dtype=torch.uint8, device=device)
+    return t[(-t.data_ptr()) % 256:][:n_bytes]
+
+
 _LOGIT_FORMAT = {torch.float32: MW_LOGITS_F32, torch.bfloat16: MW_LOGITS_BF16}
 
 
@@ -364,6 +401,32 @@ class Context:
         _whole(d_weights, (n, self.top_k), torch.float32, "d_weights")
         _check(_native().mw_route_backward(self._h, gate.address, logits, fmt, stride, topk_ids, d_weights, n, d_logits, d_stride,
                                            _stream_handle()), "mw_route_backward")
+
+    # ---- the experts of a few tokens -----------------------------------------------------
+    def moe_workspace(self, experts: Experts, max_tokens: int) -> torch.Tensor:
+        need = C.c_int64(0)
+        _check(load().mw_moe_workspace_bytes(self._h, C.byref(experts.record), C.c_int32(max_tokens), C.byref(need)), "mw_moe_workspace_bytes")
+        return _workspace(need.value, self.device)
+
+    def mw_moe_layer(self, gate: Optional[Gate], logits: Optional[torch.Tensor], bias: Optional[torch.Tensor], experts: Experts,
+                     x: torch.Tensor, topk_ids: torch.Tensor, topk_weights: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                     flags: Optional[torch.Tensor] = None):
+        n = x.shape[0]
+        fmt = stride = 0
+        if logits is not None:
+            fmt, stride = self._logits(logits, "logits")
+            if logits.shape[0] != n:
+                raise ValueError("logits: a row for each of %d tokens, got %d" % (n, logits.shape[0]))
+        _whole(bias, (self.n_experts,), torch.float32, "bias")
+        _whole(topk_ids, (n, self.top_k), torch.int32, "topk_ids")
+        _whole(topk_weights, (n, self.top_k), torch.float32, "topk_weights")
+        if x.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape[0] != n:
+            raise ValueError("x and out: bfloat16, as many rows each")
+        if (experts.n_local, experts.hidden) != (self.n_local, self.hidden):
+            raise ValueError("weights of %d experts of hidden size %d, the context has %d of %d" % (experts.n_local, experts.hidden, self.n_local, self.hidden))
+        _check(_native().mw_moe_layer(self._h, 0 if gate is None else gate.address, logits, fmt, stride, bias, experts.address, x,
+                                      _rows(x, self.hidden, "x"), n, topk_ids, topk_weights, out, _rows(out, self.hidden, "out"), flags,
+                                      workspace, workspace.numel() * workspace.element_size(), _stream_handle()), "mw_moe_layer")
 
     # ---- send side -----------------------------------------------------------------------
     def mw_plan(self, topk_ids: torch.Tensor, mask: torch.Tensor, perm: torch.Tensor,

@@ -86,3 +86,26 @@ def route_backward(logits, ids, dw, score, scale=1.0):
                 d[t, e] += f * (g[k] - mean)
                 size[t, e] += abs(f) * (abs(g[k]) + big)
     return d, size
+
+
+def silu(v):
+    with np.errstate(over="ignore"):
+        return v / (1.0 + np.exp(-v))
+
+
+def layer(x, ids, weights, gate_up, down, slots, gamma):
+    """(output, how far fp32 sums may be off) of one rank: x [T][H], gate_up [L][2][I][H], down [L][H][I] as float64; slots: id -> local
+    expert or -1.  gamma: relative error of a sum of products against the sum of their sizes."""
+    out, off = np.zeros(x.shape), np.zeros(x.shape)
+    for t in range(len(x)):
+        for e in dict.fromkeys(int(e) for e in ids[t]):
+            if e not in slots:
+                continue
+            w, (wg, wu), wd = sum(float(weights[t, k]) for k in range(ids.shape[1]) if ids[t, k] == e), gate_up[slots[e]], down[slots[e]]
+            g, u = wg @ x[t], wu @ x[t]
+            dg, du = gamma * (np.abs(wg) @ np.abs(x[t])), gamma * (np.abs(wu) @ np.abs(x[t]))
+            act = w * silu(g) * u
+            d_act = abs(w) * (1.1 * np.abs(u) * dg + np.abs(silu(g)) * du + 1.1 * dg * du) + 2.0 ** -15 * np.abs(act)
+            out[t] += wd @ act
+            off[t] += np.abs(wd) @ (d_act + gamma * np.abs(act))
+    return out, off
