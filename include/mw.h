@@ -97,6 +97,7 @@ extern "C" {
 #define MW_FLAG_DUP_SRC_TOKEN    0x40u  /* two rows of one peer carry the same source token for one expert */
 #define MW_FLAG_PLAN_TIMEOUT     0x100u /* mw_unpack_expand_index_plan_next, mw_stream_step: the riding plan gave up waiting (see there) */
 #define MW_FLAG_BAD_RANK         0x80u  /* relay: a bitmap names a rank >= n_ranks: that bit is not forwarded */
+#define MW_FLAG_BAD_ADAPTER      0x400u /* adapter id outside {-1} U [0, n_adapters): the row is taken as one without an adapter */
 #define MW_FLAG_DUPLICATE_DROPPED 0x200u /* with MW_OPT_RECV_DEDUP: a repeated row was dropped (information, not an error) */
 
 /*
@@ -833,6 +834,58 @@ MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const void *logits
                             const float *bias_dev, const mw_experts *experts, const void *x_dev, int64_t x_stride, int32_t n_tokens,
                             int32_t *topk_ids_dev, float *topk_weights_dev, void *out_dev, int64_t out_stride,
                             uint32_t *error_flags_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* ---- adapters of many requests beside a shared projection -------------------------------- */
+
+/*
+ * Low-rank adapters of one projection from n_in to n_out values (HOST record of device arrays): adapter a adds
+ * scale_a B_a A_a.  rank, n_in and n_out are multiples of 8; adapters of smaller ranks are padded with zeros.
+ */
+typedef struct mw_adapters {
+    const void *a_dev;          /* [n_adapters][rank][n_in] bf16, contiguous, 16-byte aligned */
+    const void *b_dev;          /* [n_adapters][n_out][rank] bf16, contiguous, 16-byte aligned */
+    const float *scale_dev;     /* [n_adapters] fp32, or NULL: 1 */
+    int32_t n_adapters;         /* 1..MW_ADAPT_MAX_ADAPTERS */
+    int32_t rank;               /* 8..MW_ADAPT_MAX_RANK */
+    int32_t n_in;
+    int32_t n_out;
+} mw_adapters;                  /* 40 bytes */
+
+#define MW_ADAPT_MAX_ADAPTERS 1024
+#define MW_ADAPT_MAX_RANK     128
+#define MW_ADAPT_MAX_ROWS     65536
+
+/* Bytes of device workspace mw_adapt (backward == 0) or mw_adapt_backward needs for up to max_rows rows. */
+MW_API int32_t mw_adapt_workspace_bytes(const mw_adapters *adapters, int32_t max_rows, int32_t backward, int64_t *out_bytes);
+
+/*
+ * mw_adapt: every row's own adapter beside the projection that all rows share.  With a = adapter_ids[t],
+ *   h_t = A_a x_t (fp32),   out_t = base_t + scale_a B_a h_t, rounded to bf16 once.
+ * Rows whose id is -1 have no adapter: out_t = base_t, h_t = 0.  Rows of one adapter need not stand together.
+ *   x_dev, base_dev, out_dev: bf16 rows, strides in elements (multiples of 8), 16-byte aligned.  base_dev is the shared
+ *     projection's output, or NULL (zeros); out_dev may be base_dev itself (with its stride), else none of them may overlap.
+ *   h_dev: [n_rows][rank] fp32, written for a later mw_adapt_backward; or NULL.
+ *   error_flags_dev: a word that MW_FLAG_BAD_ADAPTER is or'ed into where an id is outside {-1} U [0, n_adapters); or NULL.
+ *   workspace_dev: 256-byte aligned, mw_adapt_workspace_bytes; needs no preparation.  Calls that share one must not overlap.
+ * Runs on the current device; needs no context.  n_rows > MW_ADAPT_MAX_ROWS: MW_ERR_CAPACITY.
+ */
+MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_dev, int64_t x_stride, const int32_t *adapter_ids_dev,
+                        int32_t n_rows, const void *base_dev, int64_t base_stride, void *out_dev, int64_t out_stride,
+                        float *h_dev, uint32_t *error_flags_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/*
+ * mw_adapt_backward: from dy, the gradient of mw_adapt's out (which is also that of base), and the h it wrote,
+ *   dh_t = B_a^T dy_t,   dx_t = dx_base_t + scale_a A_a^T dh_t,
+ *   dA_a = scale_a sum over a's rows of dh_t x_t^T,   dB_a = scale_a sum over a's rows of dy_t h_t^T,
+ * in fp32 sums, each rounded to bf16 once.  dx_base_dev is the gradient that comes through the shared projection, or NULL; dx_dev
+ * may be dx_base_dev itself.  da_dev, db_dev: laid out as a_dev and b_dev, 16-byte aligned, written whole (zeros for adapters without
+ * rows).  Sums over rows have a fixed order: equal calls give equal bits.
+ */
+MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const void *x_dev, int64_t x_stride, const int32_t *adapter_ids_dev,
+                                 int32_t n_rows, const float *h_dev, const void *dy_dev, int64_t dy_stride,
+                                 const void *dx_base_dev, int64_t dx_base_stride, void *dx_dev, int64_t dx_stride,
+                                 void *da_dev, void *db_dev, uint32_t *error_flags_dev, void *workspace_dev,
+                                 int64_t workspace_bytes, void *stream);
 
 /* ---- simulation and measurement helpers (not part of the dispatch path) ---------------- */
 

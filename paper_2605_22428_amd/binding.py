@@ -33,7 +33,8 @@ EXPORTS = ["mw_workspace_bytes", "mw_ctx_create", "mw_ctx_destroy", "mw_plan", "
            "mw_set_forwarding", "mw_relay", "mw_relay_index", "mw_relay_copy", "mw_relay_copy_index_next", "mw_relay_packets", "mw_relay_packets_index", "mw_relay_packets_copy", "mw_relay_packets_copy_index_next", "mw_get_relay_stats",
            "mw_allgather_split_point", "mw_plan_allgather_split", "mw_unpack_allgather_split",
            "mw_ctx_set_timing_events", "mw_status_string", "mw_plan_static", "mw_ctx_set_options", "mw_relay_batch",
-           "mw_route", "mw_route_backward", "mw_moe_workspace_bytes", "mw_moe_layer"]
+           "mw_route", "mw_route_backward", "mw_moe_workspace_bytes", "mw_moe_layer",
+           "mw_adapt_workspace_bytes", "mw_adapt", "mw_adapt_backward"]
 MW_KERNEL_PLAN_RANK, MW_KERNEL_PLAN_GROUPS, MW_KERNEL_PACK, MW_KERNEL_RECV_INDEX, MW_KERNEL_EXPAND = 0, 1, 2, 3, 4
 MW_KERNEL_AG_PACK, MW_KERNEL_AG_GATHER, MW_KERNEL_RELAY_INDEX, MW_KERNEL_RELAY_COPY = 5, 6, 7, 8
 MW_KERNEL_PLAN_PACK, MW_KERNEL_PACK_QUANT, MW_KERNEL_COMBINE = 9, 10, 11
@@ -49,6 +50,8 @@ MW_GATE_SOFTMAX, MW_GATE_SOFTMAX_TOPK, MW_GATE_SIGMOID_TOPK = 0, 1, 2
 MW_LOGITS_F32, MW_LOGITS_BF16 = 0, 1
 MW_GATE_MAX_EXPERTS, MW_GATE_MAX_GROUPS = 1024, 64
 MW_LAYER_MAX_TOKENS = 256
+MW_ADAPT_MAX_ADAPTERS, MW_ADAPT_MAX_RANK, MW_ADAPT_MAX_ROWS = 1024, 128, 65536
+MW_FLAG_BAD_ADAPTER = 0x400
 
 # numpy views of the ABI records (host copies)
 DESC_DTYPE = np.dtype([("mask", "<u8", (4,)), ("row_offset", "<u4"), ("row_count", "<u4"),
@@ -119,6 +122,12 @@ class MwExperts(C.Structure):
                 ("inter", C.c_int32), ("format", C.c_int32)]
 
 
+class MwAdapters(C.Structure):
+    """mw_adapters (include/mw.h)."""
+    _fields_ = [("a_dev", C.c_void_p), ("b_dev", C.c_void_p), ("scale_dev", C.c_void_p), ("n_adapters", C.c_int32), ("rank", C.c_int32),
+                ("n_in", C.c_int32), ("n_out", C.c_int32)]
+
+
 class MwError(RuntimeError):
     def __init__(self, status: int, where: str):
         super().__init__("%s: %s (%d)" % (where, status_string(status), status))
@@ -152,7 +161,8 @@ _KINDS = {"mw_plan": "htittttp", "mw_pack": "htttttitttp", "mw_pack_quantize": "
           "mw_relay_copy_index_next": "httthttltp", "mw_relay_packets": "httltp", "mw_relay_packets_index": "htltp",
           "mw_relay_packets_copy": "htttp", "mw_relay_packets_copy_index_next": "httthtltp",
           "mw_route": "hptiltittp", "mw_route_backward": "hptilttitlp",
-          "mw_moe_layer": "hptiltptlitttlttlp"}
+          "mw_moe_layer": "hptiltptlitttlttlp",
+          "mw_adapt": "ptltitltltttlp", "mw_adapt_backward": "ptltittltltlttttlp"}
 _calls = None
 
 
@@ -299,6 +309,57 @@ def _workspace(n_bytes: int, device) -> torch.Tensor:
     """A tensor of at least n_bytes that begins on 256 bytes."""
     t = torch.empty(n_bytes + 256, dtype=torch.uint8, device=device)
     return t[(-t.data_ptr()) % 256:][:n_bytes]
+
+
+class Adapters:
+    """mw_adapters: low-rank adapters of one projection (include/mw.h), a [adapters][rank][n_in], b [adapters][n_out][rank]
+    bfloat16, scale [adapters] float32 or None (1)."""
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: Optional[torch.Tensor] = None):
+        (n, rank, n_in), n_out = a.shape, b.shape[1]
+        _whole(a, (n, rank, n_in), torch.bfloat16, "a")
+        _whole(b, (n, n_out, rank), torch.bfloat16, "b")
+        _whole(scale, (n,), torch.float32, "scale")
+        self._held = (a, b, scale)
+        self.n, self.rank, self.n_in, self.n_out, self.device = n, rank, n_in, n_out, a.device
+        self.record = MwAdapters(_addr(a), _addr(b), _addr(scale), n, rank, n_in, n_out)
+        self.address = C.addressof(self.record)
+
+    def workspace(self, max_rows: int, backward: bool = True) -> torch.Tensor:
+        """Workspace of calls with up to max_rows rows; without `backward` for mw_adapt only."""
+        need = C.c_int64(0)
+        _check(load().mw_adapt_workspace_bytes(C.byref(self.record), C.c_int32(max_rows), C.c_int32(backward), C.byref(need)),
+               "mw_adapt_workspace_bytes")
+        return _workspace(need.value, self.device)
+
+    def _matrix(self, t: Optional[torch.Tensor], rows: int, width: int, what: str) -> int:
+        if t is None:
+            return 0
+        if t.dtype != torch.bfloat16 or t.shape[0] != rows:
+            raise ValueError("%s: bfloat16 and %d rows, got %s and %s" % (what, rows, t.dtype, tuple(t.shape)))
+        return _rows(t, width, what)
+
+    def mw_adapt(self, x: torch.Tensor, adapter_ids: torch.Tensor, base: Optional[torch.Tensor], out: torch.Tensor,
+                 workspace: torch.Tensor, h: Optional[torch.Tensor] = None, flags: Optional[torch.Tensor] = None):
+        n = x.shape[0]
+        _whole(adapter_ids, (n,), torch.int32, "adapter_ids")
+        _whole(h, (n, self.rank), torch.float32, "h")
+        _check(_native().mw_adapt(self.address, x, self._matrix(x, n, self.n_in, "x"), adapter_ids, n, base,
+                                  self._matrix(base, n, self.n_out, "base"), out, self._matrix(out, n, self.n_out, "out"), h, flags,
+                                  workspace, workspace.numel() * workspace.element_size(), _stream_handle()), "mw_adapt")
+
+    def mw_adapt_backward(self, x: torch.Tensor, adapter_ids: torch.Tensor, h: torch.Tensor, dy: torch.Tensor,
+                          dx_base: Optional[torch.Tensor], dx: torch.Tensor, da: torch.Tensor, db: torch.Tensor,
+                          workspace: torch.Tensor, flags: Optional[torch.Tensor] = None):
+        n = x.shape[0]
+        _whole(adapter_ids, (n,), torch.int32, "adapter_ids")
+        _whole(h, (n, self.rank), torch.float32, "h")
+        _whole(da, (self.n, self.rank, self.n_in), torch.bfloat16, "da")
+        _whole(db, (self.n, self.n_out, self.rank), torch.bfloat16, "db")
+        _check(_native().mw_adapt_backward(self.address, x, self._matrix(x, n, self.n_in, "x"), adapter_ids, n, h, dy,
+                                           self._matrix(dy, n, self.n_out, "dy"), dx_base, self._matrix(dx_base, n, self.n_in, "dx_base"),
+                                           dx, self._matrix(dx, n, self.n_in, "dx"), da, db, flags, workspace,
+                                           workspace.numel() * workspace.element_size(), _stream_handle()), "mw_adapt_backward")
 
 
 _LOGIT_FORMAT = {torch.float32: MW_LOGITS_F32, torch.bfloat16: MW_LOGITS_BF16}

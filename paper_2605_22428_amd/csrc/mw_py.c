@@ -87,6 +87,9 @@ CALL(mw_route, "hptiltittp", P(0), P(1), P(2), I(3), L(4), P(5), I(6), P(7), P(8
 CALL(mw_route_backward, "hptilttitlp", P(0), P(1), P(2), I(3), L(4), P(5), P(6), I(7), P(8), L(9), P(10))
 CALL(mw_moe_layer, "hptiltptlitttlttlp", P(0), P(1), P(2), I(3), L(4), P(5), P(6), P(7), L(8), I(9), P(10), P(11), P(12), L(13), P(14), P(15),
      L(16), P(17))
+CALL(mw_adapt, "ptltitltltttlp", P(0), P(1), L(2), P(3), I(4), P(5), L(6), P(7), L(8), P(9), P(10), P(11), L(12), P(13))
+CALL(mw_adapt_backward, "ptltittltltlttttlp", P(0), P(1), L(2), P(3), I(4), P(5), P(6), L(7), P(8), L(9), P(10), L(11), P(12), P(13), P(14),
+     P(15), L(16), P(17))
 
 // The calls, once for the module's functions and once for their addresses.
 #define CALLS(X)                                                                                                        \
@@ -95,7 +98,8 @@ CALL(mw_moe_layer, "hptiltptlitttlttlp", P(0), P(1), P(2), I(3), L(4), P(5), P(6
     X(mw_plan_allgather) X(mw_pack_allgather) X(mw_unpack_allgather) X(mw_plan_allgather_split)                         \
     X(mw_unpack_allgather_split) X(mw_allgather_step) X(mw_relay) X(mw_relay_index) X(mw_relay_copy)                    \
     X(mw_relay_copy_index_next) X(mw_relay_packets) X(mw_relay_packets_index) X(mw_relay_packets_copy)                  \
-    X(mw_relay_packets_copy_index_next) X(mw_route) X(mw_route_backward) X(mw_moe_layer)
+    X(mw_relay_packets_copy_index_next) X(mw_route) X(mw_route_backward) X(mw_moe_layer) X(mw_adapt)          \
+    X(mw_adapt_backward)
 
 #define SLOT(name) {#name, (void **)&fn_##name},
 static const struct { const char *name; void **at; } slots[] = {CALLS(SLOT)};

@@ -109,3 +109,29 @@ def layer(x, ids, weights, gate_up, down, slots, gamma):
             out[t] += wd @ act
             off[t] += np.abs(wd) @ (d_act + gamma * np.abs(act))
     return out, off
+
+
+def adapt(x, ids, base, a, b, scale, gamma):
+    """(out, h, how far fp32 sums may be off, the same of h); x, base, a, b, scale as float64."""
+    h = np.zeros((len(x), a.shape[1]))
+    dh, out, off = np.zeros(h.shape), base.copy(), np.zeros(base.shape)
+    for t in range(len(x)):
+        if 0 <= ids[t] < len(a):
+            i = int(ids[t])
+            h[t], dh[t] = a[i] @ x[t], gamma * (np.abs(a[i]) @ np.abs(x[t]))
+            out[t] += scale[i] * (b[i] @ h[t])
+            off[t] = abs(scale[i]) * (np.abs(b[i]) @ (dh[t] + 2.0 ** -15 * np.abs(h[t]) + gamma * np.abs(h[t]))) + gamma * np.abs(base[t])
+    return out, h, off, dh
+
+
+def adapt_backward(x, ids, h, dy, dx_base, a, b, scale, gamma):
+    """((dx, its error), (da, its error), (db, its error))."""
+    dx, dh, ex, eh = adapt(dy, ids, dx_base, b.transpose(0, 2, 1), a.transpose(0, 2, 1), scale, gamma)
+    da, ea, db, eb = (np.zeros(v.shape) for v in (a, a, b, b))
+    for i in range(len(a)):
+        at = np.nonzero(ids == i)[0]
+        da[i], db[i] = scale[i] * dh[at].T @ x[at], scale[i] * dy[at].T @ h[at]
+        size = abs(scale[i]) * (2.0 ** -15 + gamma)
+        ea[i] = abs(scale[i]) * eh[at].T @ np.abs(x[at]) + size * np.abs(dh[at]).T @ np.abs(x[at])
+        eb[i] = size * np.abs(dy[at]).T @ np.abs(h[at])
+    return (dx, ex), (da, ea), (db, eb)
