@@ -6,13 +6,9 @@
 // Every weight of an expert that a token goes to has to be read once and is used for a few tokens only, so the weights' bytes bound both
 // kernels.  They are streamed from memory into registers in the layout that the matrix instruction takes, never through LDS: 16
 // weight rows are one side, up to 16 tokens the other, and whichever columns have no token cost nothing that counts.
-#include <float.h>
-
 #include "mw_math.h"
 
 namespace {
-
-constexpr int kChunk = 128;              // columns a wave takes at a time: a scale block of fp8 weights
 
 struct layer_args {
     const int32_t *ids;                  // [T][K]
@@ -35,82 +31,99 @@ __device__ __forceinline__ int local_slot(const layer_args &a, int32_t id)
     return (v >> 16) == a.my_rank ? (v & 0xffff) : -1;
 }
 
-// An expert that a token names twice is one pair: the first place's, with both weights.
-__device__ __forceinline__ bool first_place(const layer_args &a, int p, int32_t id)
-{
-    for (int q = p - p % a.K; q < p; ++q) if (a.ids[q] == id) return false;
-    return true;
-}
-__device__ __forceinline__ float pair_weight(const layer_args &a, int p, int32_t id)
-{
-    float w = 0.0f;
-    for (int q = p; q < p - p % a.K + a.K; ++q) if (a.ids[q] == id) w += a.weights[q];
-    return w;
-}
-
+// ---- which experts a batch goes to: every workgroup finds out for itself --------------------------------
 constexpr int kWords = MW_GATE_MAX_EXPERTS / 32;
-// The local experts that some token goes to, as bits; every thread of the workgroup.
-__device__ __forceinline__ void hit_experts(const layer_args &a, uint32_t *bits, uint32_t *bad)
+extern __shared__ int16_t le_of[];       // [T * K] a pair's local expert, -1: none (or the token named it before)
+struct hit_set { uint32_t bits[kWords], before[kWords]; };     // experts that some token goes to; how many are in the words before
+
+// Every thread of the workgroup; one round trip for the ids, one for the slots.
+__device__ __forceinline__ void find_hits(const layer_args &a, hit_set &h, uint32_t *flags)
 {
-    for (int i = threadIdx.x; i < kWords; i += blockDim.x) bits[i] = 0;
+    if (threadIdx.x < kWords) h.bits[threadIdx.x] = 0;
     __syncthreads();
     bool wrong = false;
     for (int p = threadIdx.x; p < a.T * a.K; p += blockDim.x) {
         const int32_t id = a.ids[p];
         wrong |= id < -1 || id >= a.E;
         const int le = local_slot(a, id);
-        if (le >= 0) atomicOr(&bits[le >> 5], 1u << (le & 31));
+        le_of[p] = (int16_t)le;
+        if (le >= 0) atomicOr(&h.bits[le >> 5], 1u << (le & 31));
     }
-    if (bad && wrong) atomicOr(bad, MW_FLAG_BAD_EXPERT);
+    if (flags && wrong) atomicOr(flags, MW_FLAG_BAD_EXPERT);
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const uint32_t c = threadIdx.x < kWords ? (uint32_t)__popc(h.bits[threadIdx.x]) : 0u;
+        const uint32_t incl = mw_wave_incl_scan(c);
+        if (threadIdx.x < kWords) h.before[threadIdx.x] = incl - c;
+    }
     __syncthreads();
 }
-// The n-th of them, or -1.
-__device__ __forceinline__ int nth_hit(const uint32_t *bits, int n)
+__device__ __forceinline__ int n_hits(const hit_set &h) { return (int)(h.before[kWords - 1] + (uint32_t)__popc(h.bits[kWords - 1])); }
+__device__ __forceinline__ int index_of(const hit_set &h, int le)
 {
-    for (int w = 0; w < kWords; ++w) {
-        uint32_t b = bits[w];
-        const int c = __popc(b);
-        if (n < c) {
-            for (; n > 0; --n) b &= b - 1;
-            return w * 32 + __ffs(b) - 1;
-        }
-        n -= c;
-    }
-    return -1;
+    return (int)(h.before[le >> 5] + (uint32_t)__popc(h.bits[le >> 5] & ((1u << (le & 31)) - 1)));
+}
+// The n-th expert hit, n < n_hits.
+__device__ __forceinline__ int nth_hit(const hit_set &h, int n)
+{
+    int w = 0;
+    for (int i = 1; i < kWords; ++i) w = (int)h.before[i] <= n ? i : w;
+    uint32_t b = h.bits[w];
+    for (n -= (int)h.before[w]; n > 0; --n) b &= b - 1;
+    return __builtin_amdgcn_readfirstlane(w * 32 + __ffs(b) - 1);
+}
+// An expert that a token names twice is one pair: the first place's, with both weights.
+__device__ __forceinline__ bool first_place(const layer_args &a, int p)
+{
+    for (int q = p - p % a.K; q < p; ++q) if (le_of[q] == le_of[p]) return false;
+    return true;
+}
+__device__ __forceinline__ float pair_weight(const layer_args &a, int p)
+{
+    float w = 0.0f;
+    for (int q = p; q < p - p % a.K + a.K; ++q) if (le_of[q] == le_of[p]) w += a.weights[q];
+    return w;
 }
 // The pairs of local expert `le` (their order does not matter: a pair is a column of its own everywhere).
 __device__ __forceinline__ int pairs_of(const layer_args &a, int le, int *count, uint16_t *list)
 {
     if (threadIdx.x == 0) *count = 0;
     __syncthreads();
-    for (int p = threadIdx.x; p < a.T * a.K; p += blockDim.x) {
-        const int32_t id = a.ids[p];
-        if (local_slot(a, id) == le && first_place(a, p, id)) list[atomicAdd(count, 1)] = (uint16_t)p;
-    }
+    for (int p = threadIdx.x; p < a.T * a.K; p += blockDim.x)
+        if (le_of[p] == le && first_place(a, p)) list[atomicAdd(count, 1)] = (uint16_t)p;
     __syncthreads();
     return *count;
 }
 
-// 8 weights of one lane for one matrix instruction, as bf16.  Of a span of 64 columns lane group g holds columns g * 16 .. + 15 and
-// the span takes two instructions (half 0, half 1): bf16 weights are two 16-byte loads a span, fp8 weights one.
+// ---- the stream of weights --------------------------------------------------------------------------------
+// Columns are taken in spans of 64, two matrix instructions: lane group g (of four) has columns g * 16 .. + 15 of the span, the first
+// eight in the first instruction.  bf16 weights are two 16-byte loads a span and lane, fp8 weights one.  The loads are plain: a
+// row's cache line is read by two of them, and as streaming loads they reach 5.6 TB/s where these reach 6.3 (and a copy 6.8).
+constexpr int kSpan = 64;
 template <bool kFp8> struct span;
 template <> struct span<false> {
     bf16x8 v[2];
-    __device__ __forceinline__ void load(const void *row, int at, int limit)
+    __device__ __forceinline__ void load(const char *row, int at)
     {
-        const bf16x8 zero = {};
-        const uint16_t *p = (const uint16_t *)row;
-        v[0] = at < limit ? __builtin_bit_cast(bf16x8, mw_ld16((const u32x4 *)(p + at))) : zero;
-        v[1] = at + 8 < limit ? __builtin_bit_cast(bf16x8, mw_ld16((const u32x4 *)(p + at + 8))) : zero;
+        const bf16x8 *p = (const bf16x8 *)(row + 2 * at);
+        v[0] = p[0];
+        v[1] = p[1];
+    }
+    __device__ __forceinline__ void load_part(const char *row, int at, int limit)
+    {
+        const bf16x8 zero = {}, *p = (const bf16x8 *)(row + 2 * at);
+        v[0] = at < limit ? p[0] : zero;
+        v[1] = at + 8 < limit ? p[1] : zero;
     }
     __device__ __forceinline__ bf16x8 half(int i) const { return v[i]; }
 };
 template <> struct span<true> {
     u32x4 c;
-    __device__ __forceinline__ void load(const void *row, int at, int limit)
+    __device__ __forceinline__ void load(const char *row, int at) { c = *(const u32x4 *)(row + at); }
+    __device__ __forceinline__ void load_part(const char *row, int at, int limit)
     {
         const u32x4 zero = {};
-        c = at < limit ? mw_ld16((const u32x4 *)((const uint8_t *)row + at)) : zero;
+        c = at < limit ? *(const u32x4 *)(row + at) : zero;
     }
     __device__ __forceinline__ bf16x8 half(int i) const
     {
@@ -122,232 +135,297 @@ template <> struct span<true> {
         return r;
     }
 };
-__device__ __forceinline__ bf16x8 load8(const uint16_t *row, int at, int limit, bool live)
-{
-    const bf16x8 zero = {};
-    return live && at < limit ? *(const bf16x8 *)(row + at) : zero;
-}
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x4 add_scaled(f32x4 to, f32x4 v, float s)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) to[i] += s * v[i];
-    return to;
-}
 
-// grid: (16 rows of I, hit experts).  A workgroup's waves take every kUpWaves-th chunk of the columns each.
-constexpr int kUpWaves = 4;
-template <bool kFp8, int kTiles>
-__device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, float *part)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    const int row = min(row0 + n, a.I - 1);
-    const int64_t unit = kFp8 ? 1 : 2;
-    const char *gate = (const char *)a.up + (((int64_t)le * 2) * a.I + row) * a.H * unit;
-    const char *up = gate + (int64_t)a.I * a.H * unit;
-    const int cblocks = (a.H + 127) / 128, rblocks = (a.I + 127) / 128;
-    const float *gs = kFp8 ? a.up_scale + ((int64_t)le * 2 * rblocks + row0 / 128) * cblocks : nullptr;
-    const float *us = kFp8 ? gs + (int64_t)rblocks * cblocks : nullptr;
-    const uint16_t *xr[kTiles];
-    bool live[kTiles];
+// One span of kRows tiles of 16 weight rows and kCols tiles of 16 columns (tokens); kTerms: a column is a sum of that many bf16 vectors.
+template <bool kFp8, int kRows, int kCols, int kTerms>
+struct stage {
+    span<kFp8> w[kRows];
+    bf16x8 b[kCols][kTerms][2];
+    float s[kRows];
+    __device__ __forceinline__ void load(const char *const (&row)[kRows], const uint16_t *const (&col)[kCols][kTerms],
+                                         const float *const (&scale)[kRows], int k0, int g)
+    {
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        live[i] = first + i * 16 + n < count;
-        xr[i] = a.x + (int64_t)(list[live[i] ? first + i * 16 + n : 0] / a.K) * a.x_stride;
-    }
-    f32x4 accg[kTiles] = {}, accu[kTiles] = {};
-    for (int c = wave; c * kChunk < a.H; c += kUpWaves) {
-        span<kFp8> wg[2], wu[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            wg[j].load(gate, c * kChunk + j * 64 + g * 16, a.H);
-            wu[j].load(up, c * kChunk + j * 64 + g * 16, a.H);
+        for (int r = 0; r < kRows; ++r) {
+            w[r].load(row[r], k0 + g * 16);
+            if constexpr (kFp8) s[r] = scale[r][k0 >> 7];
         }
-        f32x4 cg[kTiles] = {}, cu[kTiles] = {};
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bf16x8 ag = wg[j].half(h), au = wu[j].half(h);
+            for (int t = 0; t < kTerms; ++t)
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i) {
-                    const bf16x8 b = load8(xr[i], c * kChunk + j * 64 + g * 16 + h * 8, a.H, live[i]);
-                    if constexpr (kFp8) { cg[i] = mma(ag, b, cg[i]); cu[i] = mma(au, b, cu[i]); }
-                    else { accg[i] = mma(ag, b, accg[i]); accu[i] = mma(au, b, accu[i]); }
+                for (int h = 0; h < 2; ++h) b[c][t][h] = *(const bf16x8 *)(col[c][t] + k0 + g * 16 + h * 8);
+    }
+    __device__ __forceinline__ void load_part(const char *const (&row)[kRows], const uint16_t *const (&col)[kCols][kTerms],
+                                              const float *const (&scale)[kRows], int k0, int g, int limit)
+    {
+        const bf16x8 zero = {};
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            w[r].load_part(row[r], k0 + g * 16, limit);
+            if constexpr (kFp8) s[r] = scale[r][k0 >> 7];
+        }
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int at = k0 + g * 16 + h * 8;
+                    b[c][t][h] = at < limit ? *(const bf16x8 *)(col[c][t] + at) : zero;
+                }
+    }
+    __device__ __forceinline__ void add_to(f32x4 (&acc)[kRows][kCols]) const
+    {
+        f32x4 part[kRows][kCols];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) part[r][c] = kFp8 ? f32x4{} : acc[r][c];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const bf16x8 v = w[r].half(h);
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+#pragma unroll
+                    for (int t = kTerms - 1; t >= 0; --t) part[r][c] = mma(v, b[c][t][h], part[r][c]);
+            }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                if constexpr (kFp8) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[r][c][i] += s[r] * part[r][c][i];
+                } else {
+                    acc[r][c] = part[r][c];
                 }
             }
-        if constexpr (kFp8) {
-            const float sg = gs[c], su = us[c];
+    }
+};
+
+// acc += rows times columns; the workgroup's waves take every kWaves-th span each, kDepth of them on the way at a time.
+template <bool kFp8, int kRows, int kCols, int kTerms, int kWaves, int kDepth>
+__device__ __forceinline__ void stream(const char *const (&row)[kRows], const uint16_t *const (&col)[kCols][kTerms],
+                                       const float *const (&scale)[kRows], int limit, int wave, int g, f32x4 (&acc)[kRows][kCols])
+{
+    stage<kFp8, kRows, kCols, kTerms> st[kDepth];
+    const int full = limit / kSpan;
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) { accg[i] = add_scaled(accg[i], cg[i], sg); accu[i] = add_scaled(accu[i], cu[i], su); }
+    for (int d = 0; d < kDepth - 1; ++d)
+        if (wave + d * kWaves < full) st[d].load(row, col, scale, (wave + d * kWaves) * kSpan, g);
+    for (int s = wave; s < full; s += kWaves * kDepth) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            const int at = s + d * kWaves, next = at + (kDepth - 1) * kWaves;
+            if (next < full) st[(d + kDepth - 1) % kDepth].load(row, col, scale, next * kSpan, g);
+            if (at < full) st[d].add_to(acc);
         }
     }
-    // part [wave][gate, up][column][16 rows]
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        *(f32x4 *)&part[((wave * 2 + 0) * kTiles * 16 + i * 16 + n) * 16 + g * 4] = accg[i];
-        *(f32x4 *)&part[((wave * 2 + 1) * kTiles * 16 + i * 16 + n) * 16 + g * 4] = accu[i];
+    if (limit % kSpan != 0 && full % kWaves == wave) {
+        st[0].load_part(row, col, scale, full * kSpan, g, limit);
+        st[0].add_to(acc);
     }
-    __syncthreads();
-    for (int o = threadIdx.x; o < kTiles * 256; o += kUpWaves * 64) {
-        const int col = o >> 4, r = o & 15;
-        if (first + col >= count || row0 + r >= a.I) continue;
-        float vg = 0.0f, vu = 0.0f;
+}
+
+// ---- act = w silu(gate) * up --------------------------------------------------------------------------------
+// grid: (16 rows of I, hit experts)
+constexpr int kUpWaves = 4;
+template <bool kFp8, int kCols, int kDepth>
+__device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, float *part)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
+    const int64_t unit = kFp8 ? 1 : 2, row = min(row0 + n, a.I - 1);
+    const int cblocks = (a.H + 127) / 128, rblocks = (a.I + 127) / 128;
+    const char *rows[2];
+    const float *scale[2];
 #pragma unroll
-        for (int w = 0; w < kUpWaves; ++w) {
-            vg += part[(w * 2 + 0) * kTiles * 256 + o];
-            vu += part[(w * 2 + 1) * kTiles * 256 + o];
+    for (int r = 0; r < 2; ++r) {
+        rows[r] = (const char *)a.up + (((int64_t)le * 2 + r) * a.I + row) * a.H * unit;
+        scale[r] = kFp8 ? a.up_scale + (((int64_t)le * 2 + r) * rblocks + row0 / 128) * cblocks : nullptr;
+    }
+    const uint16_t *cols[kCols][1];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {        // (a column without a pair repeats the first one's; its sums are not used)
+        const int at = first + c * 16 + n;
+        cols[c][0] = a.x + (int64_t)(list[at < count ? at : first] / a.K) * a.x_stride;
+    }
+    f32x4 acc[2][kCols] = {};
+    stream<kFp8, 2, kCols, 1, kUpWaves, kDepth>(rows, cols, scale, a.H, wave, g, acc);
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+        // part [wave][gate, up][column][16 rows]
+#pragma unroll
+        for (int r = 0; r < 2; ++r) *(f32x4 *)&part[((wave * 2 + r) * 16 + n) * 16 + g * 4] = acc[r][c];
+        __syncthreads();
+        const int col = threadIdx.x >> 4, r = threadIdx.x & 15;
+        if (threadIdx.x < 256 && first + c * 16 + col < count && row0 + r < a.I) {
+            float vg = 0.0f, vu = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kUpWaves; ++w) {
+                vg += part[(w * 2 + 0) * 256 + threadIdx.x];
+                vu += part[(w * 2 + 1) * 256 + threadIdx.x];
+            }
+            const int p = list[first + c * 16 + col];
+            const float v = vg / (1.0f + expf(-vg)) * vu * pair_weight(a, p);
+            // Kept as a sum of two bf16 values, 16 bits of mantissa: the second costs the next kernel a matrix instruction that it has to
+            // spare, where one value alone would add as much error as the output's own rounding does.
+            const uint16_t hi = mw_f32_to_bf16(v);
+            const float rest = v - mw_bf16_to_f32(hi);
+            a.act_hi[(int64_t)p * a.I + row0 + r] = hi;
+            a.act_lo[(int64_t)p * a.I + row0 + r] = rest - rest == 0.0f ? mw_f32_to_bf16(rest) : 0;
         }
-        const int p = list[first + col];
-        const float v = vg / (1.0f + expf(-vg)) * vu * pair_weight(a, p, a.ids[p]);
-        // Kept as a sum of two bf16 values, 16 bits of mantissa: the second costs the next kernel a matrix instruction that it has to
-        // spare, where one value alone would add as much error as the output's own rounding does.
-        const uint16_t hi = mw_f32_to_bf16(v);
-        const float rest = v - mw_bf16_to_f32(hi);
-        a.act_hi[(int64_t)p * a.I + row0 + r] = hi;
-        a.act_lo[(int64_t)p * a.I + row0 + r] = fabsf(v) <= FLT_MAX && rest == rest && fabsf(rest) <= FLT_MAX ? mw_f32_to_bf16(rest) : 0;
+        __syncthreads();
     }
-    __syncthreads();
 }
 
 template <bool kFp8>
 __global__ __launch_bounds__(kUpWaves * 64) void k_layer_up(layer_args a)
 {
-    __shared__ __align__(16) float part[kUpWaves * 2 * 4 * 256];
-    __shared__ uint32_t bits[kWords];
+    __shared__ __align__(16) float part[kUpWaves * 2 * 256];
+    __shared__ hit_set hits;
     __shared__ uint16_t list[MW_LAYER_MAX_TOKENS];
     __shared__ int n_pairs;
-    hit_experts(a, bits, blockIdx.x == 0 && blockIdx.y == 0 ? a.flags : nullptr);
-    const int le = nth_hit(bits, blockIdx.y);
-    if (le < 0) return;
-    const int count = pairs_of(a, le, &n_pairs, list), row0 = blockIdx.x * 16;
+    find_hits(a, hits, blockIdx.x == 0 && blockIdx.y == 0 ? a.flags : nullptr);
+    if ((int)blockIdx.y >= n_hits(hits)) return;
+    const int le = nth_hit(hits, blockIdx.y), count = pairs_of(a, le, &n_pairs, list), row0 = blockIdx.x * 16;
     for (int first = 0; first < count;) {
         const int left = count - first;
-        if (left <= 16) { up_columns<kFp8, 1>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 32) { up_columns<kFp8, 2>(a, le, row0, list, first, count, part); first += 32; }
-        else { up_columns<kFp8, 4>(a, le, row0, list, first, count, part); first += 64; }
+        if (left <= 16) { up_columns<kFp8, 1, 4>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 32) { up_columns<kFp8, 2, 3>(a, le, row0, list, first, count, part); first += 32; }
+        else { up_columns<kFp8, 4, 2>(a, le, row0, list, first, count, part); first += 64; }
     }
 }
 
+// ---- out = sum of down act ------------------------------------------------------------------------------------
 // Batches of at most 16 tokens: a token is a column, the experts' products are one long sum.  grid: 16 rows of H.
-constexpr int kDownWaves = 4;
+constexpr int kFewWaves = 8, kFewDepth = 4;
 template <bool kFp8>
-__global__ __launch_bounds__(kDownWaves * 64) void k_layer_down_few(layer_args a)
+__global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
 {
-    __shared__ __align__(16) float part[kDownWaves * 256];
-    __shared__ uint32_t bits[kWords];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4, row0 = blockIdx.x * 16;
-    hit_experts(a, bits, nullptr);
-    const int row = min(row0 + n, a.H - 1), chunks = (a.I + kChunk - 1) / kChunk, rblocks = (a.H + 127) / 128;
+    __shared__ __align__(16) float part[kFewWaves * 256];
+    __shared__ hit_set hits;
+    int16_t *pair = le_of + (a.T * a.K + 7) / 8 * 8;          // [hit expert][16] the token's pair, -1: it does not go there
+    uint16_t *expert = (uint16_t *)(pair + min(a.T * a.K, a.L) * 16);      // [hit expert]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4, row0 = blockIdx.x * 16;
+    for (int i = threadIdx.x; i < min(a.T * a.K, a.L) * 16; i += kFewWaves * 64) pair[i] = -1;
+    find_hits(a, hits, nullptr);
+    for (int p = threadIdx.x; p < a.T * a.K; p += kFewWaves * 64)
+        if (le_of[p] >= 0 && first_place(a, p)) {
+            const int i = index_of(hits, le_of[p]);
+            pair[i * 16 + p / a.K] = (int16_t)p;
+            expert[i] = (uint16_t)le_of[p];
+        }
+    __syncthreads();
+    const int64_t unit = kFp8 ? 1 : 2, row = min(row0 + n, a.H - 1);
+    const int spans = (a.I + kSpan - 1) / kSpan, cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128, units = n_hits(hits) * spans;
+    stage<kFp8, 1, 1, 2> st[kFewDepth];
+    bool mine[kFewDepth];
     f32x4 acc = {};
-    int u = 0;
-    for (int w = 0; w < kWords; ++w)
-        for (uint32_t b = bits[w]; b; b &= b - 1) {
-            const int le = w * 32 + __ffs(b) - 1;
-            int pair = -1;                       // the column's token's place in the batch's list, if it goes to this expert
-            if (n < a.T)
-                for (int k = a.K - 1; k >= 0; --k) if (local_slot(a, a.ids[n * a.K + k]) == le) pair = n * a.K + k;
-            const uint16_t *hi = a.act_hi + (int64_t)max(pair, 0) * a.I, *lo = a.act_lo + (int64_t)max(pair, 0) * a.I;
-            const char *down = (const char *)a.down + ((int64_t)le * a.H + row) * a.I * (kFp8 ? 1 : 2);
-            for (int c = 0; c < chunks; ++c, ++u) {
-                if (u % kDownWaves != wave) continue;
-                span<kFp8> wd[2];
-                f32x4 cc = {};
+    int e = 0, s = wave;                     // the next span to load
+    auto load = [&](int d) {
+        while (s >= spans) { s -= spans; ++e; }
+        const int le = __builtin_amdgcn_readfirstlane((int)expert[e]), p = pair[e * 16 + n];
+        mine[d] = p >= 0;
+        const char *rows[1] = {(const char *)a.down + ((int64_t)le * a.H + row) * a.I * unit};
+        const int64_t at = (int64_t)max(p, 0) * a.I;
+        const uint16_t *cols[1][2] = {{a.act_hi + at, a.act_lo + at}};
+        const float *scale[1] = {kFp8 ? a.down_scale + ((int64_t)le * rblocks + row0 / 128) * cblocks : nullptr};
+        if ((s + 1) * kSpan <= a.I) st[d].load(rows, cols, scale, s * kSpan, g);
+        else st[d].load_part(rows, cols, scale, s * kSpan, g, a.I);
+        s += kFewWaves;
+    };
 #pragma unroll
-                for (int j = 0; j < 2; ++j) wd[j].load(down, c * kChunk + j * 64 + g * 16, a.I);
+    for (int d = 0; d < kFewDepth - 1; ++d)
+        if (wave + d * kFewWaves < units) load(d);
+    for (int u = wave; u < units; u += kFewWaves * kFewDepth) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int at = c * kChunk + j * 64 + g * 16 + h * 8;
-                        const bf16x8 v = wd[j].half(h);
-                        cc = mma(v, load8(hi, at, a.I, pair >= 0), cc);
-                        cc = mma(v, load8(lo, at, a.I, pair >= 0), cc);
-                    }
-                const float s = kFp8 ? a.down_scale[((int64_t)le * rblocks + row0 / 128) * chunks + c] : 1.0f;
-                if (pair >= 0) acc = add_scaled(acc, cc, s);         // (0 times a weight that is no number is not 0)
+        for (int d = 0; d < kFewDepth; ++d) {
+            const int at = u + d * kFewWaves;
+            if (at + (kFewDepth - 1) * kFewWaves < units) load((d + kFewDepth - 1) % kFewDepth);
+            if (at < units) {
+                f32x4 one[1][1] = {};
+                st[d].add_to(one);
+                if (mine[d]) acc += one[0][0];                 // (0 times a weight that is no number is not 0)
             }
         }
+    }
     *(f32x4 *)&part[wave * 256 + n * 16 + g * 4] = acc;
     __syncthreads();
     const int col = threadIdx.x >> 4, r = threadIdx.x & 15;
     if (col < a.T && row0 + r < a.H) {
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kDownWaves; ++w) v += part[w * 256 + col * 16 + r];
+        for (int w = 0; w < kFewWaves; ++w) v += part[w * 256 + threadIdx.x];
         a.out[(int64_t)col * a.out_stride + row0 + r] = mw_f32_to_bf16(v);
     }
 }
 
-// Larger batches: a pair's product by itself.  grid: (16 rows of H, hit experts).
-template <bool kFp8, int kTiles>
+// Larger batches: a pair's product by itself.  grid: (kDownRows rows of H, hit experts); two tiles of 16 rows share the columns' loads.
+constexpr int kDownWaves = 4, kDownRows = 64;
+template <bool kFp8, int kCols, int kDepth>
 __device__ __forceinline__ void down_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, float *part)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    const int row = min(row0 + n, a.H - 1), chunks = (a.I + kChunk - 1) / kChunk, rblocks = (a.H + 127) / 128;
-    const char *down = (const char *)a.down + ((int64_t)le * a.H + row) * a.I * (kFp8 ? 1 : 2);
-    const uint16_t *hi[kTiles], *lo[kTiles];
-    bool live[kTiles];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
+    const int64_t unit = kFp8 ? 1 : 2;
+    const int cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128;
+    const char *rows[2];
+    const float *scale[2];
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        live[i] = first + i * 16 + n < count;
-        const int64_t p = list[live[i] ? first + i * 16 + n : 0];
-        hi[i] = a.act_hi + p * a.I;
-        lo[i] = a.act_lo + p * a.I;
+    for (int r = 0; r < 2; ++r) {
+        rows[r] = (const char *)a.down + ((int64_t)le * a.H + min(row0 + r * 16 + n, a.H - 1)) * a.I * unit;
+        scale[r] = kFp8 ? a.down_scale + ((int64_t)le * rblocks + row0 / 128) * cblocks : nullptr;      // (32 rows from a multiple of 32)
     }
-    f32x4 acc[kTiles] = {};
-    for (int c = wave; c < chunks; c += kDownWaves) {
-        span<kFp8> wd[2];
-        f32x4 cc[kTiles] = {};
+    const uint16_t *cols[kCols][2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) wd[j].load(down, c * kChunk + j * 64 + g * 16, a.I);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int at = c * kChunk + j * 64 + g * 16 + h * 8;
-                const bf16x8 v = wd[j].half(h);
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i) {
-                    cc[i] = mma(v, load8(hi[i], at, a.I, live[i]), cc[i]);
-                    cc[i] = mma(v, load8(lo[i], at, a.I, live[i]), cc[i]);
-                }
-            }
-        const float s = kFp8 ? a.down_scale[((int64_t)le * rblocks + row0 / 128) * chunks + c] : 1.0f;
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) acc[i] = add_scaled(acc[i], cc[i], s);
+    for (int c = 0; c < kCols; ++c) {
+        const int at = first + c * 16 + n;
+        const int64_t p = list[at < count ? at : first];
+        cols[c][0] = a.act_hi + p * a.I;
+        cols[c][1] = a.act_lo + p * a.I;
     }
+    f32x4 acc[2][kCols] = {};
+    stream<kFp8, 2, kCols, 2, kDownWaves, kDepth>(rows, cols, scale, a.I, wave, g, acc);
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) *(f32x4 *)&part[wave * kTiles * 256 + (i * 16 + n) * 16 + g * 4] = acc[i];
-    __syncthreads();
-    for (int o = threadIdx.x; o < kTiles * 256; o += kDownWaves * 64) {
-        const int col = o >> 4, r = o & 15;
-        if (first + col >= count || row0 + r >= a.H) continue;
-        float v = 0.0f;
+    for (int c = 0; c < kCols; ++c) {
+        // part [wave][column][32 rows]
 #pragma unroll
-        for (int w = 0; w < kDownWaves; ++w) v += part[w * kTiles * 256 + o];
-        a.y[(int64_t)list[first + col] * a.H + row0 + r] = v;
+        for (int r = 0; r < 2; ++r) *(f32x4 *)&part[(wave * 16 + n) * 32 + r * 16 + g * 4] = acc[r][c];
+        __syncthreads();
+        const int col = threadIdx.x >> 4, r = (threadIdx.x & 15) * 2;
+        if (first + c * 16 + col < count && row0 + r < a.H) {          // (H is even)
+            float v0 = 0.0f, v1 = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kDownWaves; ++w) { v0 += part[(w * 16 + col) * 32 + r]; v1 += part[(w * 16 + col) * 32 + r + 1]; }
+            float *y = a.y + (int64_t)list[first + c * 16 + col] * a.H + row0 + r;
+            y[0] = v0;
+            y[1] = v1;
+        }
+        __syncthreads();
     }
-    __syncthreads();
 }
 
 template <bool kFp8>
 __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
 {
-    __shared__ __align__(16) float part[kDownWaves * 4 * 256];
-    __shared__ uint32_t bits[kWords];
+    __shared__ __align__(16) float part[kDownWaves * 16 * 32];
+    __shared__ hit_set hits;
     __shared__ uint16_t list[MW_LAYER_MAX_TOKENS];
     __shared__ int n_pairs;
-    hit_experts(a, bits, nullptr);
-    const int le = nth_hit(bits, blockIdx.y);
-    if (le < 0) return;
-    const int count = pairs_of(a, le, &n_pairs, list), row0 = blockIdx.x * 16;
-    for (int first = 0; first < count;) {
-        const int left = count - first;
-        if (left <= 16) { down_columns<kFp8, 1>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 32) { down_columns<kFp8, 2>(a, le, row0, list, first, count, part); first += 32; }
-        else { down_columns<kFp8, 4>(a, le, row0, list, first, count, part); first += 64; }
-    }
+    find_hits(a, hits, nullptr);
+    if ((int)blockIdx.y >= n_hits(hits)) return;
+    const int le = nth_hit(hits, blockIdx.y), count = pairs_of(a, le, &n_pairs, list);
+    for (int row0 = blockIdx.x * kDownRows; row0 < min((int)(blockIdx.x + 1) * kDownRows, a.H); row0 += 32)
+        for (int first = 0; first < count;) {
+            const int left = count - first;
+            if (left <= 16) { down_columns<kFp8, 1, 3>(a, le, row0, list, first, count, part); first += 16; }
+            else if (left <= 32) { down_columns<kFp8, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
+            else { down_columns<kFp8, 4, 2>(a, le, row0, list, first, count, part); first += 64; }
+        }
 }
 
 // out[t] = the sum of its pairs, in the order of its ids.  grid: (1024 columns, token).
@@ -355,11 +433,9 @@ __global__ __launch_bounds__(256) void k_layer_sum(layer_args a)
 {
     __shared__ int use[MW_MAX_TOPK];
     const int t = blockIdx.y;
-    if ((int)threadIdx.x < a.K) {
-        const int p = t * a.K + threadIdx.x;
-        const int32_t id = a.ids[p];
-        use[threadIdx.x] = local_slot(a, id) >= 0 && first_place(a, p, id);
-    }
+    if ((int)threadIdx.x < a.K) le_of[threadIdx.x] = (int16_t)local_slot(a, a.ids[t * a.K + threadIdx.x]);
+    __syncthreads();
+    if ((int)threadIdx.x < a.K) use[threadIdx.x] = le_of[threadIdx.x] >= 0 && first_place(a, threadIdx.x);
     __syncthreads();
     const int h = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (h >= a.H) return;                        // (H is a multiple of 8)
@@ -447,21 +523,25 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     const hipStream_t s = (hipStream_t)stream;
     const int64_t pairs = (int64_t)n_tokens * a.K;
     const uint32_t hits = (uint32_t)(a.L < 1 ? 1 : pairs < a.L ? pairs : a.L);       // experts that can be hit at most
-    const dim3 up((uint32_t)((I + 15) / 16), hits), down((uint32_t)((H + 15) / 16), n_tokens <= 16 ? 1 : hits);
+    const uint32_t ids_lds = (uint32_t)mw_align_up(2 * pairs, 16);
+    const dim3 up((uint32_t)((I + 15) / 16), hits);
     const bool fp8 = experts->format == MW_ROW_FP8_E4M3_BLOCK128;
-    if (fp8) hipLaunchKernelGGL((k_layer_up<true>), up, dim3(kUpWaves * 64), 0, s, a);
-    else hipLaunchKernelGGL((k_layer_up<false>), up, dim3(kUpWaves * 64), 0, s, a);
+    if (fp8) hipLaunchKernelGGL((k_layer_up<true>), up, dim3(kUpWaves * 64), ids_lds, s, a);
+    else hipLaunchKernelGGL((k_layer_up<false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
     if (n_tokens <= 16) {
-        if (fp8) hipLaunchKernelGGL((k_layer_down_few<true>), down, dim3(kDownWaves * 64), 0, s, a);
-        else hipLaunchKernelGGL((k_layer_down_few<false>), down, dim3(kDownWaves * 64), 0, s, a);
+        const dim3 down((uint32_t)((H + 15) / 16));
+        const uint32_t lds = ids_lds + hits * 34;
+        if (fp8) hipLaunchKernelGGL((k_layer_down_few<true>), down, dim3(kFewWaves * 64), lds, s, a);
+        else hipLaunchKernelGGL((k_layer_down_few<false>), down, dim3(kFewWaves * 64), lds, s, a);
         MW_HIP_CHECK(hipGetLastError());
         return MW_OK;
     }
-    if (fp8) hipLaunchKernelGGL((k_layer_down<true>), down, dim3(kDownWaves * 64), 0, s, a);
-    else hipLaunchKernelGGL((k_layer_down<false>), down, dim3(kDownWaves * 64), 0, s, a);
+    const dim3 down((uint32_t)((H + kDownRows - 1) / kDownRows), hits);
+    if (fp8) hipLaunchKernelGGL((k_layer_down<true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else hipLaunchKernelGGL((k_layer_down<false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL(k_layer_sum, dim3((uint32_t)((H + 1023) / 1024), (uint32_t)n_tokens), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_layer_sum, dim3((uint32_t)((H + 1023) / 1024), (uint32_t)n_tokens), dim3(256), 2 * MW_MAX_TOPK, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }
