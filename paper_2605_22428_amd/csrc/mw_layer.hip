@@ -18,7 +18,8 @@ struct layer_args {
     const uint16_t *x; int64_t x_stride; // bf16 rows
     const void *up, *down;               // [L][2][I][H], [L][H][I]
     const float *up_scale, *down_scale;  // fp8: [L][2][ceil(I/128)][ceil(H/128)], [L][ceil(H/128)][ceil(I/128)]
-    uint16_t *act_hi, *act_lo;           // [T * K][I] bf16: act rounded, and what the rounding left
+    uint16_t *act_hi, *act_lo;           // [T * K][I] bf16, act_stride apart: act rounded, and what the rounding left
+    int64_t act_stride;
     float *y;                            // [T * K][H] (batches over 16 tokens)
     uint16_t *out; int64_t out_stride;
     uint32_t *flags;                     // or null
@@ -96,59 +97,54 @@ __device__ __forceinline__ int pairs_of(const layer_args &a, int le, int *count,
 }
 
 // ---- the stream of weights --------------------------------------------------------------------------------
-// Columns are taken in spans of 64, two matrix instructions: lane group g (of four) has columns g * 16 .. + 15 of the span, the first
-// eight in the first instruction.  bf16 weights are two 16-byte loads a span and lane, fp8 weights one.  The loads are plain: a
-// row's cache line is read by two of them, and as streaming loads they reach 5.6 TB/s where these reach 6.3 (and a copy 6.8).
-constexpr int kSpan = 64;
-template <bool kFp8> struct span;
-template <> struct span<false> {
-    bf16x8 v[2];
-    __device__ __forceinline__ void load(const char *row, int at)
-    {
-        const bf16x8 *p = (const bf16x8 *)(row + 2 * at);
-        v[0] = p[0];
-        v[1] = p[1];
-    }
-    __device__ __forceinline__ void load_part(const char *row, int at, int limit)
-    {
-        const bf16x8 zero = {}, *p = (const bf16x8 *)(row + 2 * at);
-        v[0] = at < limit ? p[0] : zero;
-        v[1] = at + 8 < limit ? p[1] : zero;
-    }
-    __device__ __forceinline__ bf16x8 half(int i) const { return v[i]; }
-};
-template <> struct span<true> {
-    u32x4 c;
-    __device__ __forceinline__ void load(const char *row, int at) { c = *(const u32x4 *)(row + at); }
-    __device__ __forceinline__ void load_part(const char *row, int at, int limit)
-    {
-        const u32x4 zero = {};
-        c = at < limit ? *(const u32x4 *)(row + at) : zero;
-    }
-    __device__ __forceinline__ bf16x8 half(int i) const
-    {
-        const uint32_t a = i ? c.z : c.x, b = i ? c.w : c.y;         // (every e4m3 value is a bf16 value)
-        bf16x8 r;
-        const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
-        const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
-        r[0] = p0[0]; r[1] = p0[1]; r[2] = p1[0]; r[3] = p1[1]; r[4] = p2[0]; r[5] = p2[1]; r[6] = p3[0]; r[7] = p3[1];
-        return r;
-    }
-};
-__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// A wave takes 128 bytes of each of 16 weight rows at a time (64 bf16 or 128 fp8 columns) with two loads, eight whole cache lines
+// each, and the tokens' columns that belong to them likewise; they pass through a piece of LDS of the wave's own, out of which come the matrix
+// instruction's operands.  Loaded straight into operand layout, 16 rows by 64 bytes a load, the weights of 1.9 GB came at 6.3 TB/s with nothing
+// else to load, and tokens loaded so beside them cost as much again a load (up 5.0, down 3.25 TB/s); whole lines, streaming, come at 7.0 TB/s.
+constexpr int kPitch = 144;              // bytes from row to row in LDS: 16 rows start on different banks
+constexpr int kTileBytes = 16 * kPitch;
+template <bool kFp8> struct span { static constexpr int cols = kFp8 ? 128 : 64, pieces = kFp8 ? 2 : 1; };     // pieces of 64 columns
 
-// One span of kRows tiles of 16 weight rows and kCols tiles of 16 columns (tokens); kTerms: a column is a sum of that many bf16 vectors.
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// Eight e4m3 codes as bf16 (every e4m3 value is a bf16 value).
+__device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b)
+{
+    const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+    const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+    bf16x8 r;
+    r[0] = p0[0]; r[1] = p0[1]; r[2] = p1[0]; r[3] = p1[1]; r[4] = p2[0]; r[5] = p2[1]; r[6] = p3[0]; r[7] = p3[1];
+    return r;
+}
+// LDS written by lanes of this wave is read by others of it: the accesses stay in program order (the hardware keeps them so).
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Lane l loads 16 bytes of row l / 8 and of row 8 + l / 8 of every tile, at byte (l % 8) * 16 of the span.
 template <bool kFp8, int kRows, int kCols, int kTerms>
 struct stage {
-    span<kFp8> w[kRows];
-    bf16x8 b[kCols][kTerms][2];
+    static constexpr int kPieces = span<kFp8>::pieces;
+    u32x4 w[kRows][2];
+    u32x4 b[kCols][kTerms][kPieces][2];
     float s[kRows];
-    __device__ __forceinline__ void load(const char *const (&row)[kRows], const uint16_t *const (&col)[kCols][kTerms],
-                                         const float *const (&scale)[kRows], int k0, int g)
+    // row[r][i], col[c][t][i]: the lane's two rows, at its place of the first span; at: bytes (weights) or columns of the span's start;
+    // bytes past `limit` columns are zeros
+    template <bool kPart>
+    __device__ __forceinline__ void load(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][2],
+                                         const float *const (&scale)[kRows], int k0, int lane, int limit)
     {
+        const u32x4 zero = {};
+        const int at = (lane & 7) * 16;
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            w[r].load(row[r], k0 + g * 16);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int byte = kFp8 ? k0 : 2 * k0;
+                if (kPart && byte + at >= (kFp8 ? limit : 2 * limit)) w[r][i] = zero;
+                else w[r][i] = mw_ld16((const u32x4 *)(row[r][i] + byte));
+            }
             if constexpr (kFp8) s[r] = scale[r][k0 >> 7];
         }
 #pragma unroll
@@ -156,44 +152,58 @@ struct stage {
 #pragma unroll
             for (int t = 0; t < kTerms; ++t)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) b[c][t][h] = *(const bf16x8 *)(col[c][t] + k0 + g * 16 + h * 8);
+                for (int h = 0; h < kPieces; ++h)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int byte = 2 * k0 + h * 128;
+                        if (kPart && byte + at >= 2 * limit) b[c][t][h][i] = zero;
+                        else b[c][t][h][i] = *(const u32x4 *)(col[c][t][i] + byte);
+                    }
     }
-    __device__ __forceinline__ void load_part(const char *const (&row)[kRows], const uint16_t *const (&col)[kCols][kTerms],
-                                              const float *const (&scale)[kRows], int k0, int g, int limit)
+    __device__ __forceinline__ void add_to(f32x4 (&acc)[kRows][kCols], char *lds, int lane) const
     {
-        const bf16x8 zero = {};
+        char *to = lds + (lane >> 3) * kPitch + (lane & 7) * 16;
+        const char *from = lds + (lane & 15) * kPitch + (lane >> 4) * 16;
+        bf16x8 v[kRows][2 * kPieces];
+        wave_order();
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            w[r].load_part(row[r], k0 + g * 16, limit);
-            if constexpr (kFp8) s[r] = scale[r][k0 >> 7];
-        }
+        for (int r = 0; r < kRows; ++r)
 #pragma unroll
-        for (int c = 0; c < kCols; ++c)
+            for (int i = 0; i < 2; ++i) *(u32x4 *)(to + r * kTileBytes + i * 8 * kPitch) = w[r][i];
+        wave_order();
 #pragma unroll
-            for (int t = 0; t < kTerms; ++t)
+        for (int r = 0; r < kRows; ++r)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int at = k0 + g * 16 + h * 8;
-                    b[c][t][h] = at < limit ? *(const bf16x8 *)(col[c][t] + at) : zero;
-                }
-    }
-    __device__ __forceinline__ void add_to(f32x4 (&acc)[kRows][kCols]) const
-    {
+            for (int j = 0; j < 2; ++j) {
+                const u32x4 q = *(const u32x4 *)(from + r * kTileBytes + j * 64);
+                // bf16: columns j * 32 + g * 8 ..; fp8: columns j * 64 + g * 16 .., eight for each of two instructions
+                if constexpr (kFp8) { v[r][j * 2] = widen(q.x, q.y); v[r][j * 2 + 1] = widen(q.z, q.w); }
+                else v[r][j] = __builtin_bit_cast(bf16x8, q);
+            }
         f32x4 part[kRows][kCols];
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
 #pragma unroll
             for (int c = 0; c < kCols; ++c) part[r][c] = kFp8 ? f32x4{} : acc[r][c];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const bf16x8 v = w[r].half(h);
+            for (int t = kTerms - 1; t >= 0; --t)
 #pragma unroll
-                for (int c = 0; c < kCols; ++c)
+                for (int h = 0; h < kPieces; ++h) {
+                    char *tile = lds + kRows * kTileBytes;
+                    wave_order();
 #pragma unroll
-                    for (int t = kTerms - 1; t >= 0; --t) part[r][c] = mma(v, b[c][t][h], part[r][c]);
-            }
+                    for (int i = 0; i < 2; ++i) *(u32x4 *)(tile + (to - lds) + i * 8 * kPitch) = b[c][t][h][i];
+                    wave_order();
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const char *x = tile + (lane & 15) * kPitch + (kFp8 ? (lane >> 4) * 32 + j * 16 : (lane >> 4) * 16 + j * 64);
+                        const bf16x8 xv = *(const bf16x8 *)x;
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) part[r][c] = mma(v[r][h * 2 + j], xv, part[r][c]);
+                    }
+                }
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -207,28 +217,30 @@ struct stage {
             }
     }
 };
+template <int kRows> constexpr int kWaveLds = (kRows + 1) * kTileBytes;
 
 // acc += rows times columns; the workgroup's waves take every kWaves-th span each, kDepth of them on the way at a time.
 template <bool kFp8, int kRows, int kCols, int kTerms, int kWaves, int kDepth>
-__device__ __forceinline__ void stream(const char *const (&row)[kRows], const uint16_t *const (&col)[kCols][kTerms],
-                                       const float *const (&scale)[kRows], int limit, int wave, int g, f32x4 (&acc)[kRows][kCols])
+__device__ __forceinline__ void stream(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][2],
+                                       const float *const (&scale)[kRows], int limit, int wave, int lane, char *lds, f32x4 (&acc)[kRows][kCols])
 {
+    constexpr int kSpan = span<kFp8>::cols;
     stage<kFp8, kRows, kCols, kTerms> st[kDepth];
     const int full = limit / kSpan;
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d)
-        if (wave + d * kWaves < full) st[d].load(row, col, scale, (wave + d * kWaves) * kSpan, g);
+        if (wave + d * kWaves < full) st[d].template load<false>(row, col, scale, (wave + d * kWaves) * kSpan, lane, limit);
     for (int s = wave; s < full; s += kWaves * kDepth) {
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
             const int at = s + d * kWaves, next = at + (kDepth - 1) * kWaves;
-            if (next < full) st[(d + kDepth - 1) % kDepth].load(row, col, scale, next * kSpan, g);
-            if (at < full) st[d].add_to(acc);
+            if (next < full) st[(d + kDepth - 1) % kDepth].template load<false>(row, col, scale, next * kSpan, lane, limit);
+            if (at < full) st[d].add_to(acc, lds, lane);
         }
     }
     if (limit % kSpan != 0 && full % kWaves == wave) {
-        st[0].load_part(row, col, scale, full * kSpan, g, limit);
-        st[0].add_to(acc);
+        st[0].template load<true>(row, col, scale, full * kSpan, lane, limit);
+        st[0].add_to(acc, lds, lane);
     }
 }
 
@@ -236,26 +248,32 @@ __device__ __forceinline__ void stream(const char *const (&row)[kRows], const ui
 // grid: (16 rows of I, hit experts)
 constexpr int kUpWaves = 4;
 template <bool kFp8, int kCols, int kDepth>
-__device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, float *part)
+__device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, char *lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
-    const int64_t unit = kFp8 ? 1 : 2, row = min(row0 + n, a.I - 1);
-    const int cblocks = (a.H + 127) / 128, rblocks = (a.I + 127) / 128;
-    const char *rows[2];
+    const int64_t unit = kFp8 ? 1 : 2;
+    const int cblocks = (a.H + 127) / 128, rblocks = (a.I + 127) / 128, l8 = lane >> 3, piece = (lane & 7) * 16;
+    const char *rows[2][2];
     const float *scale[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        rows[r] = (const char *)a.up + (((int64_t)le * 2 + r) * a.I + row) * a.H * unit;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            rows[r][i] = (const char *)a.up + (((int64_t)le * 2 + r) * a.I + min(row0 + i * 8 + l8, a.I - 1)) * a.H * unit + piece;
         scale[r] = kFp8 ? a.up_scale + (((int64_t)le * 2 + r) * rblocks + row0 / 128) * cblocks : nullptr;
     }
-    const uint16_t *cols[kCols][1];
+    const char *cols[kCols][1][2];
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {        // (a column without a pair repeats the first one's; its sums are not used)
-        const int at = first + c * 16 + n;
-        cols[c][0] = a.x + (int64_t)(list[at < count ? at : first] / a.K) * a.x_stride;
-    }
+    for (int c = 0; c < kCols; ++c)          // (a column without a pair repeats the first one's; its sums are not used)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = first + c * 16 + i * 8 + l8;
+            cols[c][0][i] = (const char *)(a.x + (int64_t)(list[at < count ? at : first] / a.K) * a.x_stride) + piece;
+        }
+    float *part = (float *)lds;
     f32x4 acc[2][kCols] = {};
-    stream<kFp8, 2, kCols, 1, kUpWaves, kDepth>(rows, cols, scale, a.H, wave, g, acc);
+    stream<kFp8, 2, kCols, 1, kUpWaves, kDepth>(rows, cols, scale, a.H, wave, lane, lds + wave * kWaveLds<2>, acc);
+    __syncthreads();                         // (the partial sums take the place of the waves' pieces)
 #pragma unroll
     for (int c = 0; c < kCols; ++c) {
         // part [wave][gate, up][column][16 rows]
@@ -276,8 +294,8 @@ __device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0
             // spare, where one value alone would add as much error as the output's own rounding does.
             const uint16_t hi = mw_f32_to_bf16(v);
             const float rest = v - mw_bf16_to_f32(hi);
-            a.act_hi[(int64_t)p * a.I + row0 + r] = hi;
-            a.act_lo[(int64_t)p * a.I + row0 + r] = rest - rest == 0.0f ? mw_f32_to_bf16(rest) : 0;
+            a.act_hi[(int64_t)p * a.act_stride + row0 + r] = hi;
+            a.act_lo[(int64_t)p * a.act_stride + row0 + r] = rest - rest == 0.0f ? mw_f32_to_bf16(rest) : 0;
         }
         __syncthreads();
     }
@@ -286,7 +304,7 @@ __device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0
 template <bool kFp8>
 __global__ __launch_bounds__(kUpWaves * 64) void k_layer_up(layer_args a)
 {
-    __shared__ __align__(16) float part[kUpWaves * 2 * 256];
+    __shared__ __align__(16) char part[kUpWaves * kWaveLds<2>];
     __shared__ hit_set hits;
     __shared__ uint16_t list[MW_LAYER_MAX_TOKENS];
     __shared__ int n_pairs;
@@ -307,7 +325,7 @@ constexpr int kFewWaves = 8, kFewDepth = 4;
 template <bool kFp8>
 __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
 {
-    __shared__ __align__(16) float part[kFewWaves * 256];
+    __shared__ __align__(16) char lds[kFewWaves * kWaveLds<1>];
     __shared__ hit_set hits;
     int16_t *pair = le_of + (a.T * a.K + 7) / 8 * 8;          // [hit expert][16] the token's pair, -1: it does not go there
     uint16_t *expert = (uint16_t *)(pair + min(a.T * a.K, a.L) * 16);      // [hit expert]
@@ -321,7 +339,9 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
             expert[i] = (uint16_t)le_of[p];
         }
     __syncthreads();
-    const int64_t unit = kFp8 ? 1 : 2, row = min(row0 + n, a.H - 1);
+    constexpr int kSpan = span<kFp8>::cols;
+    const int64_t unit = kFp8 ? 1 : 2;
+    const int l8 = lane >> 3, piece = (lane & 7) * 16, row_a = min(row0 + l8, a.H - 1), row_b = min(row0 + 8 + l8, a.H - 1);
     const int spans = (a.I + kSpan - 1) / kSpan, cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128, units = n_hits(hits) * spans;
     stage<kFp8, 1, 1, 2> st[kFewDepth];
     bool mine[kFewDepth];
@@ -329,14 +349,16 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
     int e = 0, s = wave;                     // the next span to load
     auto load = [&](int d) {
         while (s >= spans) { s -= spans; ++e; }
-        const int le = __builtin_amdgcn_readfirstlane((int)expert[e]), p = pair[e * 16 + n];
-        mine[d] = p >= 0;
-        const char *rows[1] = {(const char *)a.down + ((int64_t)le * a.H + row) * a.I * unit};
-        const int64_t at = (int64_t)max(p, 0) * a.I;
-        const uint16_t *cols[1][2] = {{a.act_hi + at, a.act_lo + at}};
+        const int le = __builtin_amdgcn_readfirstlane((int)expert[e]);
+        mine[d] = pair[e * 16 + n] >= 0;
+        const char *rows[1][2] = {{(const char *)a.down + ((int64_t)le * a.H + row_a) * a.I * unit + piece,
+                                   (const char *)a.down + ((int64_t)le * a.H + row_b) * a.I * unit + piece}};
+        const int64_t at_a = (int64_t)max((int)pair[e * 16 + l8], 0) * a.act_stride, at_b = (int64_t)max((int)pair[e * 16 + 8 + l8], 0) * a.act_stride;
+        const char *cols[1][2][2] = {{{(const char *)(a.act_hi + at_a) + piece, (const char *)(a.act_hi + at_b) + piece},
+                                      {(const char *)(a.act_lo + at_a) + piece, (const char *)(a.act_lo + at_b) + piece}}};
         const float *scale[1] = {kFp8 ? a.down_scale + ((int64_t)le * rblocks + row0 / 128) * cblocks : nullptr};
-        if ((s + 1) * kSpan <= a.I) st[d].load(rows, cols, scale, s * kSpan, g);
-        else st[d].load_part(rows, cols, scale, s * kSpan, g, a.I);
+        if ((s + 1) * kSpan <= a.I) st[d].template load<false>(rows, cols, scale, s * kSpan, lane, a.I);
+        else st[d].template load<true>(rows, cols, scale, s * kSpan, lane, a.I);
         s += kFewWaves;
     };
 #pragma unroll
@@ -349,11 +371,13 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
             if (at + (kFewDepth - 1) * kFewWaves < units) load((d + kFewDepth - 1) % kFewDepth);
             if (at < units) {
                 f32x4 one[1][1] = {};
-                st[d].add_to(one);
+                st[d].add_to(one, lds + wave * kWaveLds<1>, lane);
                 if (mine[d]) acc += one[0][0];                 // (0 times a weight that is no number is not 0)
             }
         }
     }
+    float *part = (float *)lds;
+    __syncthreads();
     *(f32x4 *)&part[wave * 256 + n * 16 + g * 4] = acc;
     __syncthreads();
     const int col = threadIdx.x >> 4, r = threadIdx.x & 15;
@@ -368,28 +392,35 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
 // Larger batches: a pair's product by itself.  grid: (kDownRows rows of H, hit experts); two tiles of 16 rows share the columns' loads.
 constexpr int kDownWaves = 4, kDownRows = 64;
 template <bool kFp8, int kCols, int kDepth>
-__device__ __forceinline__ void down_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, float *part)
+__device__ __forceinline__ void down_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, char *lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
     const int64_t unit = kFp8 ? 1 : 2;
     const int cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128;
-    const char *rows[2];
+    const int l8 = lane >> 3, piece = (lane & 7) * 16;
+    float *part = (float *)lds;
+    const char *rows[2][2];
     const float *scale[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        rows[r] = (const char *)a.down + ((int64_t)le * a.H + min(row0 + r * 16 + n, a.H - 1)) * a.I * unit;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            rows[r][i] = (const char *)a.down + ((int64_t)le * a.H + min(row0 + r * 16 + i * 8 + l8, a.H - 1)) * a.I * unit + piece;
         scale[r] = kFp8 ? a.down_scale + ((int64_t)le * rblocks + row0 / 128) * cblocks : nullptr;      // (32 rows from a multiple of 32)
     }
-    const uint16_t *cols[kCols][2];
+    const char *cols[kCols][2][2];
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-        const int at = first + c * 16 + n;
-        const int64_t p = list[at < count ? at : first];
-        cols[c][0] = a.act_hi + p * a.I;
-        cols[c][1] = a.act_lo + p * a.I;
-    }
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = first + c * 16 + i * 8 + l8;
+            const int64_t p = list[at < count ? at : first];
+            cols[c][0][i] = (const char *)(a.act_hi + p * a.act_stride) + piece;
+            cols[c][1][i] = (const char *)(a.act_lo + p * a.act_stride) + piece;
+        }
     f32x4 acc[2][kCols] = {};
-    stream<kFp8, 2, kCols, 2, kDownWaves, kDepth>(rows, cols, scale, a.I, wave, g, acc);
+    stream<kFp8, 2, kCols, 2, kDownWaves, kDepth>(rows, cols, scale, a.I, wave, lane, lds + wave * kWaveLds<2>, acc);
+    __syncthreads();
 #pragma unroll
     for (int c = 0; c < kCols; ++c) {
         // part [wave][column][32 rows]
@@ -412,7 +443,7 @@ __device__ __forceinline__ void down_columns(const layer_args &a, int le, int ro
 template <bool kFp8>
 __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
 {
-    __shared__ __align__(16) float part[kDownWaves * 16 * 32];
+    __shared__ __align__(16) char part[kDownWaves * kWaveLds<2>];
     __shared__ hit_set hits;
     __shared__ uint16_t list[MW_LAYER_MAX_TOKENS];
     __shared__ int n_pairs;
@@ -449,13 +480,14 @@ __global__ __launch_bounds__(256) void k_layer_sum(layer_args a)
 }
 
 struct layer_ws { int64_t hi, lo, y, total; };
+int64_t act_stride(int64_t inter) { return mw_align_up(inter, 64) + 128; }
 layer_ws layer_layout(const mw_ctx *ctx, int64_t inter, int64_t tokens)
 {
     layer_ws w;
     int64_t o = 0;
     const int64_t pairs = tokens * ctx->cfg.top_k;
-    w.hi = o; o += mw_align_up(2 * pairs * inter, 256);
-    w.lo = o; o += mw_align_up(2 * pairs * inter, 256);
+    w.hi = o; o += mw_align_up(2 * pairs * act_stride(inter), 256);
+    w.lo = o; o += mw_align_up(2 * pairs * act_stride(inter), 256);
     w.y = o;  o += tokens > 16 ? mw_align_up(4 * pairs * ctx->cfg.hidden, 256) : 0;
     w.total = o > 0 ? o : 256;
     return w;
@@ -517,6 +549,7 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     a.x = (const uint16_t *)x_dev; a.x_stride = x_stride;
     a.up = experts->gate_up_dev; a.down = experts->down_dev;
     a.up_scale = experts->gate_up_scale_dev; a.down_scale = experts->down_scale_dev;
+    a.act_stride = act_stride(I);
     a.act_hi = (uint16_t *)(b + w.hi); a.act_lo = (uint16_t *)(b + w.lo); a.y = (float *)(b + w.y);
     a.out = (uint16_t *)out_dev; a.out_stride = out_stride;
     a.flags = error_flags_dev;
