@@ -123,16 +123,17 @@ __device__ __forceinline__ void wave_order()
 }
 
 // Lane l loads 16 bytes of row l / 8 and of row 8 + l / 8 of every tile, at byte (l % 8) * 16 of the span.
-template <bool kFp8, int kRows, int kCols, int kTerms>
+// kHalves 1: no tile has more than eight tokens, the second load of theirs is left out.
+template <bool kFp8, int kRows, int kCols, int kHalves, int kTerms>
 struct stage {
     static constexpr int kPieces = span<kFp8>::pieces;
     u32x4 w[kRows][2];
-    u32x4 b[kCols][kTerms][kPieces][2];
+    u32x4 b[kCols][kTerms][kPieces][kHalves];
     float s[kRows];
     // row[r][i], col[c][t][i]: the lane's two rows, at its place of the first span; at: bytes (weights) or columns of the span's start;
     // bytes past `limit` columns are zeros
     template <bool kPart>
-    __device__ __forceinline__ void load(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][2],
+    __device__ __forceinline__ void load(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][kHalves],
                                          const float *const (&scale)[kRows], int k0, int lane, int limit)
     {
         const u32x4 zero = {};
@@ -154,7 +155,7 @@ struct stage {
 #pragma unroll
                 for (int h = 0; h < kPieces; ++h)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < kHalves; ++i) {
                         const int byte = 2 * k0 + h * 128;
                         if (kPart && byte + at >= 2 * limit) b[c][t][h][i] = zero;
                         else b[c][t][h][i] = *(const u32x4 *)(col[c][t][i] + byte);
@@ -194,7 +195,7 @@ struct stage {
                     char *tile = lds + kRows * kTileBytes;
                     wave_order();
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) *(u32x4 *)(tile + (to - lds) + i * 8 * kPitch) = b[c][t][h][i];
+                    for (int i = 0; i < kHalves; ++i) *(u32x4 *)(tile + (to - lds) + i * 8 * kPitch) = b[c][t][h][i];
                     wave_order();
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
@@ -220,12 +221,12 @@ struct stage {
 template <int kRows> constexpr int kWaveLds = (kRows + 1) * kTileBytes;
 
 // acc += rows times columns; the workgroup's waves take every kWaves-th span each, kDepth of them on the way at a time.
-template <bool kFp8, int kRows, int kCols, int kTerms, int kWaves, int kDepth>
-__device__ __forceinline__ void stream(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][2],
+template <bool kFp8, int kRows, int kCols, int kHalves, int kTerms, int kWaves, int kDepth>
+__device__ __forceinline__ void stream(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][kHalves],
                                        const float *const (&scale)[kRows], int limit, int wave, int lane, char *lds, f32x4 (&acc)[kRows][kCols])
 {
     constexpr int kSpan = span<kFp8>::cols;
-    stage<kFp8, kRows, kCols, kTerms> st[kDepth];
+    stage<kFp8, kRows, kCols, kHalves, kTerms> st[kDepth];
     const int full = limit / kSpan;
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d)
@@ -247,7 +248,7 @@ __device__ __forceinline__ void stream(const char *const (&row)[kRows][2], const
 // ---- act = w silu(gate) * up --------------------------------------------------------------------------------
 // grid: (16 rows of I, hit experts)
 constexpr int kUpWaves = 4;
-template <bool kFp8, int kCols, int kDepth>
+template <bool kFp8, int kCols, int kHalves, int kDepth>
 __device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, char *lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
@@ -262,17 +263,17 @@ __device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0
             rows[r][i] = (const char *)a.up + (((int64_t)le * 2 + r) * a.I + min(row0 + i * 8 + l8, a.I - 1)) * a.H * unit + piece;
         scale[r] = kFp8 ? a.up_scale + (((int64_t)le * 2 + r) * rblocks + row0 / 128) * cblocks : nullptr;
     }
-    const char *cols[kCols][1][2];
+    const char *cols[kCols][1][kHalves];
 #pragma unroll
     for (int c = 0; c < kCols; ++c)          // (a column without a pair repeats the first one's; its sums are not used)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kHalves; ++i) {
             const int at = first + c * 16 + i * 8 + l8;
             cols[c][0][i] = (const char *)(a.x + (int64_t)(list[at < count ? at : first] / a.K) * a.x_stride) + piece;
         }
     float *part = (float *)lds;
     f32x4 acc[2][kCols] = {};
-    stream<kFp8, 2, kCols, 1, kUpWaves, kDepth>(rows, cols, scale, a.H, wave, lane, lds + wave * kWaveLds<2>, acc);
+    stream<kFp8, 2, kCols, kHalves, 1, kUpWaves, kDepth>(rows, cols, scale, a.H, wave, lane, lds + wave * kWaveLds<2>, acc);
     __syncthreads();                         // (the partial sums take the place of the waves' pieces)
 #pragma unroll
     for (int c = 0; c < kCols; ++c) {
@@ -313,9 +314,10 @@ __global__ __launch_bounds__(kUpWaves * 64) void k_layer_up(layer_args a)
     const int le = nth_hit(hits, blockIdx.y), count = pairs_of(a, le, &n_pairs, list), row0 = blockIdx.x * 16;
     for (int first = 0; first < count;) {
         const int left = count - first;
-        if (left <= 16) { up_columns<kFp8, 1, 4>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 32) { up_columns<kFp8, 2, 3>(a, le, row0, list, first, count, part); first += 32; }
-        else { up_columns<kFp8, 4, 2>(a, le, row0, list, first, count, part); first += 64; }
+        if (left <= 8) { up_columns<kFp8, 1, 1, 4>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 16) { up_columns<kFp8, 1, 2, 4>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 32) { up_columns<kFp8, 2, 2, 3>(a, le, row0, list, first, count, part); first += 32; }
+        else { up_columns<kFp8, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
     }
 }
 
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
     const int64_t unit = kFp8 ? 1 : 2;
     const int l8 = lane >> 3, piece = (lane & 7) * 16, row_a = min(row0 + l8, a.H - 1), row_b = min(row0 + 8 + l8, a.H - 1);
     const int spans = (a.I + kSpan - 1) / kSpan, cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128, units = n_hits(hits) * spans;
-    stage<kFp8, 1, 1, 2> st[kFewDepth];
+    stage<kFp8, 1, 1, 2, 2> st[kFewDepth];
     bool mine[kFewDepth];
     f32x4 acc = {};
     int e = 0, s = wave;                     // the next span to load
@@ -389,16 +391,16 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
     }
 }
 
-// Larger batches: a pair's product by itself.  grid: (kDownRows rows of H, hit experts); two tiles of 16 rows share the columns' loads.
-constexpr int kDownWaves = 4, kDownRows = 64;
-template <bool kFp8, int kCols, int kDepth>
+// Larger batches: a pair's product by itself.  Two tiles of 16 rows share the columns' loads.  A wave takes 32 rows by itself (kSplit 1) or
+// a workgroup's four take its columns in turn (kSplit 4).  grid: (4 / kSplit times 32 rows of H, hit experts)
+constexpr int kDownWaves = 4;
+template <bool kFp8, int kSplit, int kCols, int kHalves, int kDepth>
 __device__ __forceinline__ void down_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, char *lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
     const int64_t unit = kFp8 ? 1 : 2;
     const int cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128;
     const int l8 = lane >> 3, piece = (lane & 7) * 16;
-    float *part = (float *)lds;
     const char *rows[2][2];
     const float *scale[2];
 #pragma unroll
@@ -408,39 +410,50 @@ __device__ __forceinline__ void down_columns(const layer_args &a, int le, int ro
             rows[r][i] = (const char *)a.down + ((int64_t)le * a.H + min(row0 + r * 16 + i * 8 + l8, a.H - 1)) * a.I * unit + piece;
         scale[r] = kFp8 ? a.down_scale + ((int64_t)le * rblocks + row0 / 128) * cblocks : nullptr;      // (32 rows from a multiple of 32)
     }
-    const char *cols[kCols][2][2];
+    const char *cols[kCols][2][kHalves];
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kHalves; ++i) {
             const int at = first + c * 16 + i * 8 + l8;
             const int64_t p = list[at < count ? at : first];
             cols[c][0][i] = (const char *)(a.act_hi + p * a.act_stride) + piece;
             cols[c][1][i] = (const char *)(a.act_lo + p * a.act_stride) + piece;
         }
     f32x4 acc[2][kCols] = {};
-    stream<kFp8, 2, kCols, 2, kDownWaves, kDepth>(rows, cols, scale, a.I, wave, lane, lds + wave * kWaveLds<2>, acc);
-    __syncthreads();
+    stream<kFp8, 2, kCols, kHalves, 2, kSplit, kDepth>(rows, cols, scale, a.I, wave % kSplit, lane, lds + wave * kWaveLds<2>, acc);
+    if constexpr (kSplit == 1) {
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-        // part [wave][column][32 rows]
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-        for (int r = 0; r < 2; ++r) *(f32x4 *)&part[(wave * 16 + n) * 32 + r * 16 + g * 4] = acc[r][c];
+            for (int r = 0; r < 2; ++r) {
+                const int h = row0 + r * 16 + g * 4;            // (H is a multiple of 8)
+                if (first + c * 16 + n < count && h < a.H) *(f32x4 *)(a.y + (int64_t)list[first + c * 16 + n] * a.H + h) = acc[r][c];
+            }
+    } else {
+        float *part = (float *)lds;
         __syncthreads();
-        const int col = threadIdx.x >> 4, r = (threadIdx.x & 15) * 2;
-        if (first + c * 16 + col < count && row0 + r < a.H) {          // (H is even)
-            float v0 = 0.0f, v1 = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kDownWaves; ++w) { v0 += part[(w * 16 + col) * 32 + r]; v1 += part[(w * 16 + col) * 32 + r + 1]; }
-            float *y = a.y + (int64_t)list[first + c * 16 + col] * a.H + row0 + r;
-            y[0] = v0;
-            y[1] = v1;
+        for (int c = 0; c < kCols; ++c) {
+            // part [wave][column][32 rows]
+#pragma unroll
+            for (int r = 0; r < 2; ++r) *(f32x4 *)&part[(wave * 16 + n) * 32 + r * 16 + g * 4] = acc[r][c];
+            __syncthreads();
+            const int col = threadIdx.x >> 4, r = (threadIdx.x & 15) * 2;
+            if (first + c * 16 + col < count && row0 + r < a.H) {
+                float v0 = 0.0f, v1 = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kDownWaves; ++w) { v0 += part[(w * 16 + col) * 32 + r]; v1 += part[(w * 16 + col) * 32 + r + 1]; }
+                float *y = a.y + (int64_t)list[first + c * 16 + col] * a.H + row0 + r;
+                y[0] = v0;
+                y[1] = v1;
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
-template <bool kFp8>
+template <bool kFp8, int kSplit>
 __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
 {
     __shared__ __align__(16) char part[kDownWaves * kWaveLds<2>];
@@ -450,13 +463,15 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
     find_hits(a, hits, nullptr);
     if ((int)blockIdx.y >= n_hits(hits)) return;
     const int le = nth_hit(hits, blockIdx.y), count = pairs_of(a, le, &n_pairs, list);
-    for (int row0 = blockIdx.x * kDownRows; row0 < min((int)(blockIdx.x + 1) * kDownRows, a.H); row0 += 32)
-        for (int first = 0; first < count;) {
-            const int left = count - first;
-            if (left <= 16) { down_columns<kFp8, 1, 3>(a, le, row0, list, first, count, part); first += 16; }
-            else if (left <= 32) { down_columns<kFp8, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
-            else { down_columns<kFp8, 4, 2>(a, le, row0, list, first, count, part); first += 64; }
-        }
+    const int row0 = kSplit == 1 ? ((int)blockIdx.x * kDownWaves + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * 32 : (int)blockIdx.x * 32;
+    if (row0 >= a.H) return;                 // (a wave by itself; no barrier follows for those)
+    for (int first = 0; first < count;) {
+        const int left = count - first;
+        if (left <= 8) { down_columns<kFp8, kSplit, 1, 1, 4>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 16) { down_columns<kFp8, kSplit, 1, 2, 3>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 32) { down_columns<kFp8, kSplit, 2, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
+        else { down_columns<kFp8, kSplit, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
+    }
 }
 
 // out[t] = the sum of its pairs, in the order of its ids.  grid: (1024 columns, token).
@@ -570,9 +585,13 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
         MW_HIP_CHECK(hipGetLastError());
         return MW_OK;
     }
-    const dim3 down((uint32_t)((H + kDownRows - 1) / kDownRows), hits);
-    if (fp8) hipLaunchKernelGGL((k_layer_down<true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else hipLaunchKernelGGL((k_layer_down<false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    const int64_t groups = (H + 31) / 32;
+    const bool alone = groups * hits >= 8LL * ctx->n_cu;
+    const dim3 down((uint32_t)(alone ? (groups + kDownWaves - 1) / kDownWaves : groups), hits);
+    if (fp8 && alone) hipLaunchKernelGGL((k_layer_down<true, 1>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (fp8) hipLaunchKernelGGL((k_layer_down<true, 4>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (alone) hipLaunchKernelGGL((k_layer_down<false, 1>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else hipLaunchKernelGGL((k_layer_down<false, 4>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL(k_layer_sum, dim3((uint32_t)((H + 1023) / 1024), (uint32_t)n_tokens), dim3(256), 2 * MW_MAX_TOPK, s, a);
     MW_HIP_CHECK(hipGetLastError());
