@@ -16,6 +16,7 @@ struct gate_args {
     int64_t stride;             // elements from one token's scores to the next's
     const float *bias;
     int32_t n_tokens, n_experts, top_k, score, n_groups, kept, group_size;
+    int32_t group_lanes;        // lanes that look at a group together
     uint32_t group_mul;         // expert / group_size = expert * group_mul >> 20 (experts below 1024)
     float scale;
 };
@@ -44,7 +45,7 @@ __device__ __forceinline__ void select_keys(const gate_args &a, const float (&l)
         key[j] = s[j] > -INFINITY ? mw_order_key(s[j]) : 0u;
     }
     if (a.n_groups == 1) return;
-    // A lane a group: its two best scores, then how many groups are ahead of it.
+    // Several lanes a group, a power of two: its two best scores, then how many groups are ahead of it.
 #pragma unroll
     for (int j = 0; j < kVals; ++j) {
         const int e = j * 64 + lane;
@@ -53,17 +54,21 @@ __device__ __forceinline__ void select_keys(const gate_args &a, const float (&l)
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
     float best = -INFINITY, second = -INFINITY;
-    const int G = a.n_groups, S = a.group_size;
-    if (lane < G) {
-        int at = lane % S;                       // (lanes start apart: other banks)
-        for (int i = 0; i < S; ++i) {
-            const float v = row[lane * S + at];
+    const int G = a.n_groups, S = a.group_size, P = a.group_lanes, group = lane / P;
+    if (group < G) {
+#pragma unroll 4
+        for (int i = lane % P; i < S; i += P) {
+            const float v = row[group * S + i];
             second = fmaxf(second, fminf(best, v));
             best = fmaxf(best, v);
-            at = at + 1 == S ? 0 : at + 1;
         }
     }
-    const float mine = S > 1 ? best + second : best;
+    for (int d = 1; d < P; d *= 2) {
+        const float ob = __shfl_xor(best, d), os = __shfl_xor(second, d);
+        second = fmaxf(fmaxf(second, os), fminf(best, ob));
+        best = fmaxf(best, ob);
+    }
+    const float mine = __shfl(S > 1 ? best + second : best, min(lane * P, 63));      // lane g: group g
     int ahead = 0;
     for (int g = 0; g < G; ++g) {
         const float other = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(mine), g));
@@ -230,6 +235,8 @@ int32_t gate_ready(const mw_ctx *ctx, const mw_gate *gate, const void *logits, i
     a->n_tokens = n_tokens; a->n_experts = E; a->top_k = ctx->cfg.top_k;
     a->score = gate->score; a->n_groups = gate->n_groups; a->kept = gate->kept_groups; a->scale = gate->scale;
     a->group_size = E / gate->n_groups;
+    a->group_lanes = 1;
+    while (a->group_lanes * 2 * gate->n_groups <= 64 && a->group_lanes * 2 <= a->group_size) a->group_lanes *= 2;
     a->group_mul = ((1u << 20) + (uint32_t)a->group_size - 1) / (uint32_t)a->group_size;
     return MW_OK;
 }

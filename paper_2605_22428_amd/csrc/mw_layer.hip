@@ -25,39 +25,54 @@ struct layer_args {
     uint32_t *flags;                     // or null
 };
 
-__device__ __forceinline__ int local_slot(const layer_args &a, int32_t id)
+// Slot of an id's expert among this rank's, or -1; `eslot`: the table, wherever it is.
+__device__ __forceinline__ int local_slot(const layer_args &a, const int32_t *eslot, int32_t id)
 {
     if (id < 0 || id >= a.E) return -1;
-    const int32_t v = a.eslot[id];
+    const int32_t v = eslot[id];
     return (v >> 16) == a.my_rank ? (v & 0xffff) : -1;
 }
 
 // ---- which experts a batch goes to: every workgroup finds out for itself --------------------------------
 constexpr int kWords = MW_GATE_MAX_EXPERTS / 32;
-extern __shared__ int16_t le_of[];       // [T * K] a pair's local expert, -1: none (or the token named it before)
-struct hit_set { uint32_t bits[kWords], before[kWords]; };     // experts that some token goes to; how many are in the words before
+extern __shared__ int16_t le_of[];       // [T * K] a pair's local expert, -1: none
+struct hit_set {
+    uint32_t bits[kWords], before[kWords];      // experts that some token goes to; how many are in the words before
+    int32_t eslot[MW_GATE_MAX_EXPERTS];
+};
 
-// Every thread of the workgroup; one round trip for the ids, one for the slots.
+// Every thread of the workgroup.  The ids and the table of slots are requested together: one round trip to memory.
 __device__ __forceinline__ void find_hits(const layer_args &a, hit_set &h, uint32_t *flags)
 {
-    if (threadIdx.x < kWords) h.bits[threadIdx.x] = 0;
-    __syncthreads();
+    constexpr int kIds = 8, kSlots = 4;
+    const int tid = threadIdx.x, step = blockDim.x, pairs = a.T * a.K;
+    int32_t id[kIds], slot[kSlots];
+#pragma unroll
+    for (int i = 0; i < kIds; ++i) id[i] = tid + i * step < pairs ? a.ids[tid + i * step] : -1;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) slot[i] = tid + i * step < a.E ? a.eslot[tid + i * step] : 0;
+    if (tid < kWords) h.bits[tid] = 0;
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) if (tid + i * step < a.E) h.eslot[tid + i * step] = slot[i];
+    mw_lds_barrier();
     bool wrong = false;
-    for (int p = threadIdx.x; p < a.T * a.K; p += blockDim.x) {
-        const int32_t id = a.ids[p];
-        wrong |= id < -1 || id >= a.E;
-        const int le = local_slot(a, id);
+    auto take = [&](int p, int32_t e) {
+        wrong |= e < -1 || e >= a.E;
+        const int le = local_slot(a, h.eslot, e);
         le_of[p] = (int16_t)le;
         if (le >= 0) atomicOr(&h.bits[le >> 5], 1u << (le & 31));
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < kIds; ++i) if (tid + i * step < pairs) take(tid + i * step, id[i]);
+    for (int p = tid + kIds * step; p < pairs; p += step) take(p, a.ids[p]);
     if (flags && wrong) atomicOr(flags, MW_FLAG_BAD_EXPERT);
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        const uint32_t c = threadIdx.x < kWords ? (uint32_t)__popc(h.bits[threadIdx.x]) : 0u;
+    mw_lds_barrier();
+    if (tid < 64) {
+        const uint32_t c = tid < kWords ? (uint32_t)__popc(h.bits[tid]) : 0u;
         const uint32_t incl = mw_wave_incl_scan(c);
-        if (threadIdx.x < kWords) h.before[threadIdx.x] = incl - c;
+        if (tid < kWords) h.before[tid] = incl - c;
     }
-    __syncthreads();
+    mw_lds_barrier();
 }
 __device__ __forceinline__ int n_hits(const hit_set &h) { return (int)(h.before[kWords - 1] + (uint32_t)__popc(h.bits[kWords - 1])); }
 __device__ __forceinline__ int index_of(const hit_set &h, int le)
@@ -89,11 +104,11 @@ __device__ __forceinline__ float pair_weight(const layer_args &a, int p)
 __device__ __forceinline__ int pairs_of(const layer_args &a, int le, int *count, uint16_t *list)
 {
     if (threadIdx.x == 0) *count = 0;
-    __syncthreads();
+    mw_lds_barrier();
     for (int p = threadIdx.x; p < a.T * a.K; p += blockDim.x)
         if (le_of[p] == le && first_place(a, p)) list[atomicAdd(count, 1)] = (uint16_t)p;
-    __syncthreads();
-    return *count;
+    mw_lds_barrier();
+    return __builtin_amdgcn_readfirstlane(*count);
 }
 
 // ---- the stream of weights --------------------------------------------------------------------------------
@@ -302,7 +317,7 @@ __device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0
     }
 }
 
-template <bool kFp8>
+template <bool kFp8, bool kWide>
 __global__ __launch_bounds__(kUpWaves * 64) void k_layer_up(layer_args a)
 {
     __shared__ __align__(16) char part[kUpWaves * kWaveLds<2>];
@@ -316,8 +331,8 @@ __global__ __launch_bounds__(kUpWaves * 64) void k_layer_up(layer_args a)
         const int left = count - first;
         if (left <= 8) { up_columns<kFp8, 1, 1, 4>(a, le, row0, list, first, count, part); first += 16; }
         else if (left <= 16) { up_columns<kFp8, 1, 2, 4>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 32) { up_columns<kFp8, 2, 2, 3>(a, le, row0, list, first, count, part); first += 32; }
-        else { up_columns<kFp8, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
+        else if (!kWide || left <= 32) { up_columns<kFp8, 2, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
+        else if constexpr (kWide) { up_columns<kFp8, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
     }
 }
 
@@ -453,7 +468,7 @@ __device__ __forceinline__ void down_columns(const layer_args &a, int le, int ro
     }
 }
 
-template <bool kFp8, int kSplit>
+template <bool kFp8, int kSplit, bool kWide>
 __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
 {
     __shared__ __align__(16) char part[kDownWaves * kWaveLds<2>];
@@ -467,10 +482,10 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
     if (row0 >= a.H) return;                 // (a wave by itself; no barrier follows for those)
     for (int first = 0; first < count;) {
         const int left = count - first;
-        if (left <= 8) { down_columns<kFp8, kSplit, 1, 1, 4>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 16) { down_columns<kFp8, kSplit, 1, 2, 3>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 32) { down_columns<kFp8, kSplit, 2, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
-        else { down_columns<kFp8, kSplit, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
+        if (left <= 8) { down_columns<kFp8, kSplit, 1, 1, kFp8 ? 3 : 4>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 16) { down_columns<kFp8, kSplit, 1, 2, kFp8 ? 2 : 3>(a, le, row0, list, first, count, part); first += 16; }
+        else if (!kWide || left <= 32) { down_columns<kFp8, kSplit, 2, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
+        else if constexpr (kWide) { down_columns<kFp8, kSplit, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
     }
 }
 
@@ -479,7 +494,7 @@ __global__ __launch_bounds__(256) void k_layer_sum(layer_args a)
 {
     __shared__ int use[MW_MAX_TOPK];
     const int t = blockIdx.y;
-    if ((int)threadIdx.x < a.K) le_of[threadIdx.x] = (int16_t)local_slot(a, a.ids[t * a.K + threadIdx.x]);
+    if ((int)threadIdx.x < a.K) le_of[threadIdx.x] = (int16_t)local_slot(a, a.eslot, a.ids[t * a.K + threadIdx.x]);
     __syncthreads();
     if ((int)threadIdx.x < a.K) use[threadIdx.x] = le_of[threadIdx.x] >= 0 && first_place(a, threadIdx.x);
     __syncthreads();
@@ -574,8 +589,11 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     const uint32_t ids_lds = (uint32_t)mw_align_up(2 * pairs, 16);
     const dim3 up((uint32_t)((I + 15) / 16), hits);
     const bool fp8 = experts->format == MW_ROW_FP8_E4M3_BLOCK128;
-    if (fp8) hipLaunchKernelGGL((k_layer_up<true>), up, dim3(kUpWaves * 64), ids_lds, s, a);
-    else hipLaunchKernelGGL((k_layer_up<false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
+    // Experts with more than 32 tokens: 64 of them at a time where that is the usual case.
+    const bool wide = !fp8 && pairs >= 24LL * a.E;
+    if (fp8) hipLaunchKernelGGL((k_layer_up<true, false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
+    else if (wide) hipLaunchKernelGGL((k_layer_up<false, true>), up, dim3(kUpWaves * 64), ids_lds, s, a);
+    else hipLaunchKernelGGL((k_layer_up<false, false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
     if (n_tokens <= 16) {
         const dim3 down((uint32_t)((H + 15) / 16));
@@ -588,10 +606,12 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     const int64_t groups = (H + 31) / 32;
     const bool alone = groups * hits >= 8LL * ctx->n_cu;
     const dim3 down((uint32_t)(alone ? (groups + kDownWaves - 1) / kDownWaves : groups), hits);
-    if (fp8 && alone) hipLaunchKernelGGL((k_layer_down<true, 1>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (fp8) hipLaunchKernelGGL((k_layer_down<true, 4>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (alone) hipLaunchKernelGGL((k_layer_down<false, 1>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else hipLaunchKernelGGL((k_layer_down<false, 4>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    if (fp8 && alone) hipLaunchKernelGGL((k_layer_down<true, 1, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (fp8) hipLaunchKernelGGL((k_layer_down<true, 4, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (alone && wide) hipLaunchKernelGGL((k_layer_down<false, 1, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (wide) hipLaunchKernelGGL((k_layer_down<false, 4, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (alone) hipLaunchKernelGGL((k_layer_down<false, 1, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else hipLaunchKernelGGL((k_layer_down<false, 4, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL(k_layer_sum, dim3((uint32_t)((H + 1023) / 1024), (uint32_t)n_tokens), dim3(256), 2 * MW_MAX_TOPK, s, a);
     MW_HIP_CHECK(hipGetLastError());
