@@ -137,44 +137,53 @@ __device__ __forceinline__ void wave_order()
     __builtin_amdgcn_wave_barrier();
 }
 
-// Lane l loads 16 bytes of row l / 8 and of row 8 + l / 8 of every tile, at byte (l % 8) * 16 of the span.
+// An array whose loads past its end are zeros and cost no traffic: places are 32-bit, and kNowhere plus any place (below 2^31) is past it.
+// So every load of the stream is issued whether there is something to load or not; a load behind a branch would make each wait
+// behind the branch wait for it (the counter of loads on the way has to suit both ways), and with that for all of them.
+typedef __amdgpu_buffer_rsrc_t array;
+constexpr uint32_t kNowhere = 0x80000000u;
+__device__ __forceinline__ array array_at(const void *p) { return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)kNowhere, 0x00027000); }
+template <bool kStreaming>
+__device__ __forceinline__ u32x4 load16(array from, uint32_t at)
+{
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, at, 0, kStreaming ? 2 : 0));
+}
+
+// Rows and columns of a product.  A lane's places: of row lane / 8 and 8 + lane / 8 of every tile, at byte (lane % 8) * 16.
+template <bool kFp8, int kRows, int kCols, int kHalves, int kTerms>
+struct operands {
+    array w, scale, b[kTerms];
+    uint32_t row[kRows][2], col[kCols][kTerms][kHalves], block[kRows];      // block: byte of the rows' first scale
+    int limit;                                                              // columns
+};
+
 // kHalves 1: no tile has more than eight tokens, the second load of theirs is left out.
 template <bool kFp8, int kRows, int kCols, int kHalves, int kTerms>
 struct stage {
     static constexpr int kPieces = span<kFp8>::pieces;
     u32x4 w[kRows][2];
     u32x4 b[kCols][kTerms][kPieces][kHalves];
-    float s[kRows];
-    // row[r][i], col[c][t][i]: the lane's two rows, at its place of the first span; at: bytes (weights) or columns of the span's start;
-    // bytes past `limit` columns are zeros
-    template <bool kPart>
-    __device__ __forceinline__ void load(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][kHalves],
-                                         const float *const (&scale)[kRows], int k0, int lane, int limit)
+    uint32_t s[kRows];
+    __device__ __forceinline__ void load(const operands<kFp8, kRows, kCols, kHalves, kTerms> &o, int k0, int lane)
     {
-        const u32x4 zero = {};
-        const int at = (lane & 7) * 16;
+        const uint32_t at = (uint32_t)(lane & 7) * 16, end = kFp8 ? (uint32_t)o.limit : 2u * (uint32_t)o.limit;
+        const uint32_t byte = kFp8 ? (uint32_t)k0 : 2u * (uint32_t)k0, w_at = byte + at < end ? byte : kNowhere;
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int byte = kFp8 ? k0 : 2 * k0;
-                if (kPart && byte + at >= (kFp8 ? limit : 2 * limit)) w[r][i] = zero;
-                else w[r][i] = mw_ld16((const u32x4 *)(row[r][i] + byte));
-            }
-            if constexpr (kFp8) s[r] = scale[r][k0 >> 7];
+            for (int i = 0; i < 2; ++i) w[r][i] = load16<true>(o.w, o.row[r][i] + w_at);
+            if constexpr (kFp8) s[r] = __builtin_amdgcn_raw_buffer_load_b32(o.scale, k0 < o.limit ? o.block[r] + (uint32_t)(k0 >> 7) * 4 : kNowhere, 0, 0);
         }
 #pragma unroll
-        for (int c = 0; c < kCols; ++c)
+        for (int h = 0; h < kPieces; ++h) {
+            const uint32_t b_byte = 2u * (uint32_t)k0 + (uint32_t)h * 128, b_at = b_byte + at < 2u * (uint32_t)o.limit ? b_byte : kNowhere;
 #pragma unroll
-            for (int t = 0; t < kTerms; ++t)
+            for (int c = 0; c < kCols; ++c)
 #pragma unroll
-                for (int h = 0; h < kPieces; ++h)
+                for (int t = 0; t < kTerms; ++t)
 #pragma unroll
-                    for (int i = 0; i < kHalves; ++i) {
-                        const int byte = 2 * k0 + h * 128;
-                        if (kPart && byte + at >= 2 * limit) b[c][t][h][i] = zero;
-                        else b[c][t][h][i] = *(const u32x4 *)(col[c][t][i] + byte);
-                    }
+                    for (int i = 0; i < kHalves; ++i) b[c][t][h][i] = load16<false>(o.b[t], o.col[c][t][i] + b_at);
+        }
     }
     __device__ __forceinline__ void add_to(f32x4 (&acc)[kRows][kCols], char *lds, int lane) const
     {
@@ -202,11 +211,11 @@ struct stage {
 #pragma unroll
             for (int c = 0; c < kCols; ++c) part[r][c] = kFp8 ? f32x4{} : acc[r][c];
 #pragma unroll
-        for (int c = 0; c < kCols; ++c)
+        for (int h = 0; h < kPieces; ++h)
 #pragma unroll
-            for (int t = kTerms - 1; t >= 0; --t)
+            for (int c = 0; c < kCols; ++c)
 #pragma unroll
-                for (int h = 0; h < kPieces; ++h) {
+                for (int t = 0; t < kTerms; ++t) {
                     char *tile = lds + kRows * kTileBytes;
                     wave_order();
 #pragma unroll
@@ -226,7 +235,7 @@ struct stage {
             for (int c = 0; c < kCols; ++c) {
                 if constexpr (kFp8) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[r][c][i] += s[r] * part[r][c][i];
+                    for (int i = 0; i < 4; ++i) acc[r][c][i] += __uint_as_float(s[r]) * part[r][c][i];
                 } else {
                     acc[r][c] = part[r][c];
                 }
@@ -237,26 +246,18 @@ template <int kRows> constexpr int kWaveLds = (kRows + 1) * kTileBytes;
 
 // acc += rows times columns; the workgroup's waves take every kWaves-th span each, kDepth of them on the way at a time.
 template <bool kFp8, int kRows, int kCols, int kHalves, int kTerms, int kWaves, int kDepth>
-__device__ __forceinline__ void stream(const char *const (&row)[kRows][2], const char *const (&col)[kCols][kTerms][kHalves],
-                                       const float *const (&scale)[kRows], int limit, int wave, int lane, char *lds, f32x4 (&acc)[kRows][kCols])
+__device__ __forceinline__ void stream(const operands<kFp8, kRows, kCols, kHalves, kTerms> &o, int wave, int lane, char *lds, f32x4 (&acc)[kRows][kCols])
 {
     constexpr int kSpan = span<kFp8>::cols;
     stage<kFp8, kRows, kCols, kHalves, kTerms> st[kDepth];
-    const int full = limit / kSpan;
 #pragma unroll
-    for (int d = 0; d < kDepth - 1; ++d)
-        if (wave + d * kWaves < full) st[d].template load<false>(row, col, scale, (wave + d * kWaves) * kSpan, lane, limit);
-    for (int s = wave; s < full; s += kWaves * kDepth) {
+    for (int d = 0; d < kDepth - 1; ++d) st[d].load(o, (wave + d * kWaves) * kSpan, lane);
+    for (int k0 = wave * kSpan; k0 < o.limit; k0 += kWaves * kDepth * kSpan) {
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
-            const int at = s + d * kWaves, next = at + (kDepth - 1) * kWaves;
-            if (next < full) st[(d + kDepth - 1) % kDepth].template load<false>(row, col, scale, next * kSpan, lane, limit);
-            if (at < full) st[d].add_to(acc, lds, lane);
+            st[(d + kDepth - 1) % kDepth].load(o, k0 + (d + kDepth - 1) * kWaves * kSpan, lane);
+            if (k0 + d * kWaves * kSpan < o.limit) st[d].add_to(acc, lds, lane);
         }
-    }
-    if (limit % kSpan != 0 && full % kWaves == wave) {
-        st[0].template load<true>(row, col, scale, full * kSpan, lane, limit);
-        st[0].add_to(acc, lds, lane);
     }
 }
 
@@ -268,27 +269,29 @@ __device__ __forceinline__ void up_columns(const layer_args &a, int le, int row0
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
     const int64_t unit = kFp8 ? 1 : 2;
-    const int cblocks = (a.H + 127) / 128, rblocks = (a.I + 127) / 128, l8 = lane >> 3, piece = (lane & 7) * 16;
-    const char *rows[2][2];
-    const float *scale[2];
+    const int cblocks = (a.H + 127) / 128, rblocks = (a.I + 127) / 128, l8 = lane >> 3;
+    const uint32_t piece = (uint32_t)(lane & 7) * 16;
+    float *part = (float *)lds;
+    operands<kFp8, 2, kCols, kHalves, 1> o;
+    o.w = array_at((const char *)a.up + (int64_t)le * 2 * a.I * a.H * unit);
+    o.scale = array_at(kFp8 ? a.up_scale + (int64_t)le * 2 * rblocks * cblocks : nullptr);
+    o.b[0] = array_at(a.x);
+    o.limit = a.H;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            rows[r][i] = (const char *)a.up + (((int64_t)le * 2 + r) * a.I + min(row0 + i * 8 + l8, a.I - 1)) * a.H * unit + piece;
-        scale[r] = kFp8 ? a.up_scale + (((int64_t)le * 2 + r) * rblocks + row0 / 128) * cblocks : nullptr;
+        for (int i = 0; i < 2; ++i) o.row[r][i] = (uint32_t)((r * a.I + min(row0 + i * 8 + l8, a.I - 1)) * unit * a.H) + piece;
+        o.block[r] = (uint32_t)((r * rblocks + row0 / 128) * cblocks) * 4;
     }
-    const char *cols[kCols][1][kHalves];
 #pragma unroll
     for (int c = 0; c < kCols; ++c)          // (a column without a pair repeats the first one's; its sums are not used)
 #pragma unroll
         for (int i = 0; i < kHalves; ++i) {
             const int at = first + c * 16 + i * 8 + l8;
-            cols[c][0][i] = (const char *)(a.x + (int64_t)(list[at < count ? at : first] / a.K) * a.x_stride) + piece;
+            o.col[c][0][i] = (uint32_t)((list[at < count ? at : first] / a.K) * a.x_stride * 2) + piece;
         }
-    float *part = (float *)lds;
     f32x4 acc[2][kCols] = {};
-    stream<kFp8, 2, kCols, kHalves, 1, kUpWaves, kDepth>(rows, cols, scale, a.H, wave, lane, lds + wave * kWaveLds<2>, acc);
+    stream<kFp8, 2, kCols, kHalves, 1, kUpWaves, kDepth>(o, wave, lane, lds + wave * kWaveLds<2>, acc);
     __syncthreads();                         // (the partial sums take the place of the waves' pieces)
 #pragma unroll
     for (int c = 0; c < kCols; ++c) {
@@ -358,35 +361,42 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
     __syncthreads();
     constexpr int kSpan = span<kFp8>::cols;
     const int64_t unit = kFp8 ? 1 : 2;
-    const int l8 = lane >> 3, piece = (lane & 7) * 16, row_a = min(row0 + l8, a.H - 1), row_b = min(row0 + 8 + l8, a.H - 1);
-    const int spans = (a.I + kSpan - 1) / kSpan, cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128, units = n_hits(hits) * spans;
+    const int l8 = lane >> 3, spans = (a.I + kSpan - 1) / kSpan, cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128, n_exp = n_hits(hits);
+    const int units = n_exp * spans;
+    const uint32_t piece = (uint32_t)(lane & 7) * 16;
+    operands<kFp8, 1, 1, 2, 2> o;
+    o.b[0] = array_at(a.act_hi);
+    o.b[1] = array_at(a.act_lo);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) o.row[0][i] = (uint32_t)(min(row0 + i * 8 + l8, a.H - 1) * unit * a.I) + piece;
+    o.block[0] = (uint32_t)(row0 / 128 * cblocks) * 4;
     stage<kFp8, 1, 1, 2, 2> st[kFewDepth];
     bool mine[kFewDepth];
     f32x4 acc = {};
-    int e = 0, s = wave;                     // the next span to load
+    int e = 0, s = wave, to_load = wave;     // the next span to load
     auto load = [&](int d) {
         while (s >= spans) { s -= spans; ++e; }
-        const int le = __builtin_amdgcn_readfirstlane((int)expert[e]);
-        mine[d] = pair[e * 16 + n] >= 0;
-        const char *rows[1][2] = {{(const char *)a.down + ((int64_t)le * a.H + row_a) * a.I * unit + piece,
-                                   (const char *)a.down + ((int64_t)le * a.H + row_b) * a.I * unit + piece}};
-        const int64_t at_a = (int64_t)max((int)pair[e * 16 + l8], 0) * a.act_stride, at_b = (int64_t)max((int)pair[e * 16 + 8 + l8], 0) * a.act_stride;
-        const char *cols[1][2][2] = {{{(const char *)(a.act_hi + at_a) + piece, (const char *)(a.act_hi + at_b) + piece},
-                                      {(const char *)(a.act_lo + at_a) + piece, (const char *)(a.act_lo + at_b) + piece}}};
-        const float *scale[1] = {kFp8 ? a.down_scale + ((int64_t)le * rblocks + row0 / 128) * cblocks : nullptr};
-        if ((s + 1) * kSpan <= a.I) st[d].template load<false>(rows, cols, scale, s * kSpan, lane, a.I);
-        else st[d].template load<true>(rows, cols, scale, s * kSpan, lane, a.I);
-        s += kFewWaves;
-    };
+        const int at = min(e, n_exp - 1), le = __builtin_amdgcn_readfirstlane((int)expert[at]);
+        mine[d] = pair[at * 16 + n] >= 0;
+        o.w = array_at((const char *)a.down + (int64_t)le * a.H * a.I * unit);
+        o.scale = array_at(kFp8 ? a.down_scale + (int64_t)le * rblocks * cblocks : nullptr);
 #pragma unroll
-    for (int d = 0; d < kFewDepth - 1; ++d)
-        if (wave + d * kFewWaves < units) load(d);
+        for (int i = 0; i < 2; ++i)
+            o.col[0][0][i] = o.col[0][1][i] = (uint32_t)(max((int)pair[at * 16 + i * 8 + l8], 0) * a.act_stride * 2) + piece;
+        o.limit = to_load < units ? a.I : 0;
+        st[d].load(o, s * kSpan, lane);
+        s += kFewWaves;
+        to_load += kFewWaves;
+    };
+    if (n_exp > 0) {
+#pragma unroll
+        for (int d = 0; d < kFewDepth - 1; ++d) load(d);
+    }
     for (int u = wave; u < units; u += kFewWaves * kFewDepth) {
 #pragma unroll
         for (int d = 0; d < kFewDepth; ++d) {
-            const int at = u + d * kFewWaves;
-            if (at + (kFewDepth - 1) * kFewWaves < units) load((d + kFewDepth - 1) % kFewDepth);
-            if (at < units) {
+            load((d + kFewDepth - 1) % kFewDepth);
+            if (u + d * kFewWaves < units) {
                 f32x4 one[1][1] = {};
                 st[d].add_to(one, lds + wave * kWaveLds<1>, lane);
                 if (mine[d]) acc += one[0][0];                 // (0 times a weight that is no number is not 0)
@@ -415,28 +425,29 @@ __device__ __forceinline__ void down_columns(const layer_args &a, int le, int ro
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
     const int64_t unit = kFp8 ? 1 : 2;
     const int cblocks = (a.I + 127) / 128, rblocks = (a.H + 127) / 128;
-    const int l8 = lane >> 3, piece = (lane & 7) * 16;
-    const char *rows[2][2];
-    const float *scale[2];
+    const int l8 = lane >> 3;
+    const uint32_t piece = (uint32_t)(lane & 7) * 16;
+    operands<kFp8, 2, kCols, kHalves, 2> o;
+    o.w = array_at((const char *)a.down + (int64_t)le * a.H * a.I * unit);
+    o.scale = array_at(kFp8 ? a.down_scale + (int64_t)le * rblocks * cblocks : nullptr);
+    o.b[0] = array_at(a.act_hi);
+    o.b[1] = array_at(a.act_lo);
+    o.limit = a.I;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            rows[r][i] = (const char *)a.down + ((int64_t)le * a.H + min(row0 + r * 16 + i * 8 + l8, a.H - 1)) * a.I * unit + piece;
-        scale[r] = kFp8 ? a.down_scale + ((int64_t)le * rblocks + row0 / 128) * cblocks : nullptr;      // (32 rows from a multiple of 32)
+        for (int i = 0; i < 2; ++i) o.row[r][i] = (uint32_t)(min(row0 + r * 16 + i * 8 + l8, a.H - 1) * unit * a.I) + piece;
+        o.block[r] = (uint32_t)(row0 / 128 * cblocks) * 4;                   // (32 rows from a multiple of 32)
     }
-    const char *cols[kCols][2][kHalves];
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
         for (int i = 0; i < kHalves; ++i) {
             const int at = first + c * 16 + i * 8 + l8;
-            const int64_t p = list[at < count ? at : first];
-            cols[c][0][i] = (const char *)(a.act_hi + p * a.act_stride) + piece;
-            cols[c][1][i] = (const char *)(a.act_lo + p * a.act_stride) + piece;
+            o.col[c][0][i] = o.col[c][1][i] = (uint32_t)(list[at < count ? at : first] * a.act_stride * 2) + piece;
         }
     f32x4 acc[2][kCols] = {};
-    stream<kFp8, 2, kCols, kHalves, 2, kSplit, kDepth>(rows, cols, scale, a.I, wave % kSplit, lane, lds + wave * kWaveLds<2>, acc);
+    stream<kFp8, 2, kCols, kHalves, 2, kSplit, kDepth>(o, wave % kSplit, lane, lds + wave * kWaveLds<2>, acc);
     if constexpr (kSplit == 1) {
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
@@ -565,6 +576,9 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     if (((uintptr_t)x_dev | (uintptr_t)out_dev) & 15u) return MW_ERR_INVALID_ARG;
     if ((uintptr_t)error_flags_dev & 3u) return MW_ERR_INVALID_ARG;
     if (n_tokens > 0 && (!x_dev || !topk_ids_dev || !topk_weights_dev || !out_dev)) return MW_ERR_INVALID_ARG;
+    // places inside an expert's matrices, the tokens and their activations are 32-bit, below 2^31
+    const int64_t far = 2LL << 30, tokens = n_tokens;
+    if (4LL * H * I > far || 2 * x_stride * tokens > far || 2 * act_stride(I) * tokens * ctx->cfg.top_k > far) return MW_ERR_UNSUPPORTED;
     const layer_ws w = layer_layout(ctx, I, n_tokens);
     if (!workspace_dev || ((uintptr_t)workspace_dev & 255u) || workspace_bytes < w.total) return MW_ERR_WORKSPACE;
     if (logits_dev || gate) {
