@@ -332,8 +332,8 @@ __global__ __launch_bounds__(kUpWaves * 64) void k_layer_up(layer_args a)
     const int le = nth_hit(hits, blockIdx.y), count = pairs_of(a, le, &n_pairs, list), row0 = blockIdx.x * 16;
     for (int first = 0; first < count;) {
         const int left = count - first;
-        if (left <= 8) { up_columns<kFp8, 1, 1, 4>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 16) { up_columns<kFp8, 1, 2, 4>(a, le, row0, list, first, count, part); first += 16; }
+        if (left <= 8) { up_columns<kFp8, 1, 1, 3>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 16) { up_columns<kFp8, 1, 2, 3>(a, le, row0, list, first, count, part); first += 16; }
         else if (!kWide || left <= 32) { up_columns<kFp8, 2, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
         else if constexpr (kWide) { up_columns<kFp8, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
     }
@@ -416,8 +416,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
     }
 }
 
-// Larger batches: a pair's product by itself.  Two tiles of 16 rows share the columns' loads.  A wave takes 32 rows by itself (kSplit 1) or
-// a workgroup's four take its columns in turn (kSplit 4).  grid: (4 / kSplit times 32 rows of H, hit experts)
+// Larger batches: a pair's product by itself.  Two tiles of 16 rows share the columns' loads.  kSplit of a workgroup's four
+// waves take 32 rows, every kSplit-th span each.  grid: (4 / kSplit times 32 rows of H, hit experts)
 constexpr int kDownWaves = 4;
 template <bool kFp8, int kSplit, int kCols, int kHalves, int kDepth>
 __device__ __forceinline__ void down_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, char *lds)
@@ -437,7 +437,7 @@ __device__ __forceinline__ void down_columns(const layer_args &a, int le, int ro
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) o.row[r][i] = (uint32_t)(min(row0 + r * 16 + i * 8 + l8, a.H - 1) * unit * a.I) + piece;
-        o.block[r] = (uint32_t)(row0 / 128 * cblocks) * 4;                   // (32 rows from a multiple of 32)
+        o.block[r] = (uint32_t)(min(row0, a.H - 1) / 128 * cblocks) * 4;       // (32 rows from a multiple of 32)
     }
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
@@ -448,34 +448,30 @@ __device__ __forceinline__ void down_columns(const layer_args &a, int le, int ro
         }
     f32x4 acc[2][kCols] = {};
     stream<kFp8, 2, kCols, kHalves, 2, kSplit, kDepth>(o, wave % kSplit, lane, lds + wave * kWaveLds<2>, acc);
-    if constexpr (kSplit == 1) {
+    float *part = (float *)lds;
+    __syncthreads();
 #pragma unroll
-        for (int c = 0; c < kCols; ++c)
+    for (int c = 0; c < kCols; ++c) {
+        // part [wave][column][32 rows]
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int h = row0 + r * 16 + g * 4;            // (H is a multiple of 8)
-                if (first + c * 16 + n < count && h < a.H) *(f32x4 *)(a.y + (int64_t)list[first + c * 16 + n] * a.H + h) = acc[r][c];
-            }
-    } else {
-        float *part = (float *)lds;
+        for (int r = 0; r < 2; ++r) *(f32x4 *)&part[(wave * 16 + n) * 32 + r * 16 + g * 4] = acc[r][c];
         __syncthreads();
+        constexpr int kThreads = kSplit * 64;
+        for (int o = threadIdx.x % kThreads; o < 256; o += kThreads) {
+            const int col = o >> 4, r = (o & 15) * 2;
+            if (first + c * 16 + col >= count || row0 + r >= a.H) continue;          // (H is even)
+            float v0 = 0.0f, v1 = 0.0f;
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) {
-            // part [wave][column][32 rows]
-#pragma unroll
-            for (int r = 0; r < 2; ++r) *(f32x4 *)&part[(wave * 16 + n) * 32 + r * 16 + g * 4] = acc[r][c];
-            __syncthreads();
-            const int col = threadIdx.x >> 4, r = (threadIdx.x & 15) * 2;
-            if (first + c * 16 + col < count && row0 + r < a.H) {
-                float v0 = 0.0f, v1 = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kDownWaves; ++w) { v0 += part[(w * 16 + col) * 32 + r]; v1 += part[(w * 16 + col) * 32 + r + 1]; }
-                float *y = a.y + (int64_t)list[first + c * 16 + col] * a.H + row0 + r;
-                y[0] = v0;
-                y[1] = v1;
+            for (int w = 0; w < kSplit; ++w) {
+                const float *q = &part[((wave / kSplit * kSplit + w) * 16 + col) * 32 + r];
+                v0 += q[0];
+                v1 += q[1];
             }
-            __syncthreads();
+            float *y = a.y + (int64_t)list[first + c * 16 + col] * a.H + row0 + r;
+            y[0] = v0;
+            y[1] = v1;
         }
+        __syncthreads();
     }
 }
 
@@ -489,8 +485,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
     find_hits(a, hits, nullptr);
     if ((int)blockIdx.y >= n_hits(hits)) return;
     const int le = nth_hit(hits, blockIdx.y), count = pairs_of(a, le, &n_pairs, list);
-    const int row0 = kSplit == 1 ? ((int)blockIdx.x * kDownWaves + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * 32 : (int)blockIdx.x * 32;
-    if (row0 >= a.H) return;                 // (a wave by itself; no barrier follows for those)
+    const int row0 = ((int)blockIdx.x * (kDownWaves / kSplit) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) / kSplit) * 32;
     for (int first = 0; first < count;) {
         const int left = count - first;
         if (left <= 8) { down_columns<kFp8, kSplit, 1, 1, kFp8 ? 3 : 4>(a, le, row0, list, first, count, part); first += 16; }
@@ -618,13 +613,13 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
         return MW_OK;
     }
     const int64_t groups = (H + 31) / 32;
-    const bool alone = groups * hits >= 8LL * ctx->n_cu;
-    const dim3 down((uint32_t)(alone ? (groups + kDownWaves - 1) / kDownWaves : groups), hits);
-    if (fp8 && alone) hipLaunchKernelGGL((k_layer_down<true, 1, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    const bool two = groups * hits >= 8LL * ctx->n_cu;
+    const dim3 down((uint32_t)(two ? (groups + 1) / 2 : groups), hits);
+    if (fp8 && two) hipLaunchKernelGGL((k_layer_down<true, 2, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     else if (fp8) hipLaunchKernelGGL((k_layer_down<true, 4, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (alone && wide) hipLaunchKernelGGL((k_layer_down<false, 1, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (two && wide) hipLaunchKernelGGL((k_layer_down<false, 2, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     else if (wide) hipLaunchKernelGGL((k_layer_down<false, 4, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (alone) hipLaunchKernelGGL((k_layer_down<false, 1, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (two) hipLaunchKernelGGL((k_layer_down<false, 2, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     else hipLaunchKernelGGL((k_layer_down<false, 4, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL(k_layer_sum, dim3((uint32_t)((H + 1023) / 1024), (uint32_t)n_tokens), dim3(256), 2 * MW_MAX_TOPK, s, a);
