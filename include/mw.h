@@ -827,7 +827,8 @@ MW_API int32_t mw_moe_workspace_bytes(mw_ctx *ctx, const mw_experts *experts, in
  *     must not overlap.
  *   error_flags_dev: a word that MW_FLAG_BAD_EXPERT is or'ed into where an id is outside {-1} U [0, n_experts) (it is left out); or NULL.
  *   workspace_dev: 256-byte aligned, mw_moe_workspace_bytes; needs no preparation.  Calls that share one must not overlap.
- * 0 <= n_tokens <= min(max_tokens, MW_LAYER_MAX_TOKENS).  At most MW_GATE_MAX_EXPERTS experts; contexts of MW_ROW_BYTES have no hidden size:
+ * 0 <= n_tokens <= min(max_tokens, MW_LAYER_MAX_TOKENS).  Each of an expert's gate_up, x, and n_tokens top_k rows of inter + 192 bf16
+ * values may span at most 2 GiB, else MW_ERR_UNSUPPORTED.  At most MW_GATE_MAX_EXPERTS experts; contexts of MW_ROW_BYTES have no hidden size:
  * MW_ERR_UNSUPPORTED.
  */
 MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const void *logits_dev, int32_t logit_format, int64_t logit_stride,
@@ -867,7 +868,8 @@ MW_API int32_t mw_adapt_workspace_bytes(const mw_adapters *adapters, int32_t max
  *   h_dev: [n_rows][rank] fp32, written for a later mw_adapt_backward; or NULL.
  *   error_flags_dev: a word that MW_FLAG_BAD_ADAPTER is or'ed into where an id is outside {-1} U [0, n_adapters); or NULL.
  *   workspace_dev: 256-byte aligned, mw_adapt_workspace_bytes; needs no preparation.  Calls that share one must not overlap.
- * Runs on the current device; needs no context.  n_rows > MW_ADAPT_MAX_ROWS: MW_ERR_CAPACITY.
+ * Runs on the current device; needs no context.  n_rows > MW_ADAPT_MAX_ROWS: MW_ERR_CAPACITY.  x, base and out may each span at most
+ * 2 GiB (stride times n_rows elements): MW_ERR_UNSUPPORTED.
  */
 MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_dev, int64_t x_stride, const int32_t *adapter_ids_dev,
                         int32_t n_rows, const void *base_dev, int64_t base_stride, void *out_dev, int64_t out_stride,
@@ -879,7 +881,7 @@ MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_dev, int64_t 
  *   dA_a = scale_a sum over a's rows of dh_t x_t^T,   dB_a = scale_a sum over a's rows of dy_t h_t^T,
  * in fp32 sums, each rounded to bf16 once.  dx_base_dev is the gradient that comes through the shared projection, or NULL; dx_dev
  * may be dx_base_dev itself.  da_dev, db_dev: laid out as a_dev and b_dev, 16-byte aligned, written whole (zeros for adapters without
- * rows).  Sums over rows have a fixed order: equal calls give equal bits.
+ * rows).  Sums over rows have a fixed order: equal calls give equal bits.  dy, dx_base and dx may each span at most 2 GiB.
  */
 MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const void *x_dev, int64_t x_stride, const int32_t *adapter_ids_dev,
                                  int32_t n_rows, const float *h_dev, const void *dy_dev, int64_t dy_stride,

@@ -3,43 +3,57 @@
 //   y_t  = base_t + c_a B_a h_t,   h_t = A_a x_t                       a: the adapter of row t
 //   dh_t = B_a^T dy_t,   dx_t = dx_base_t + c_a A_a^T dh_t,   dA_a = c_a sum_t dh_t x_t^T,   dB_a = c_a sum_t dy_t h_t^T
 //
-// Rows are put in order of their adapters first (stable, so sums over an adapter's rows have one order).  A workgroup then takes up to
-// 32 rows of one adapter through both products: x once, h in LDS only, base and y once.  The gradient of the input is the same
-// walk with the transposed factors.
-#include "mw_math.h"
+// Rows are put in order of their adapters first (stable, so sums over an adapter's rows have one order) and cut into tiles of one
+// adapter each.  k_adapt_down makes h of a tile, its workgroups sharing the columns of x out where there are few tiles; k_adapt_up adds
+// up their parts and makes a slice of y.  The gradient of the input is the same walk with the transposed factors; beside it the
+// tiles' h and dh are laid out for k_adapt_grads, which goes over an adapter's rows of x and dy once more.
+#include "mw_stream.h"
 
 namespace {
 
-constexpr int kTileRows = 32;
 constexpr int kOrderBlock = 512, kOrderWaves = kOrderBlock / 64;
 constexpr int kBins = MW_ADAPT_MAX_ADAPTERS + 1;       // the last: rows without an adapter
 
 struct adapt_tile { int32_t adapter, first, count, reserved0; };      // adapter == n_adapters: rows without one
 
-// One workgroup.  order: rows by (adapter, row); start[b]: first of adapter b's in it; tiles of at most kTileRows.
-__global__ __launch_bounds__(kOrderBlock) void k_adapt_order(const int32_t *__restrict__ ids, int T, int n, int32_t *__restrict__ order,
-                                                             int32_t *__restrict__ start, adapt_tile *__restrict__ tiles,
-                                                             int32_t *__restrict__ n_tiles, uint32_t *__restrict__ flags)
+struct order_args {
+    const int32_t *ids;
+    int32_t T, n, tile_rows;
+    int32_t *order;                        // rows by (adapter, row)
+    int32_t *tile_at;                      // [n + 2] first tile of an adapter, of the rows without one, and how many there are
+    adapt_tile *tiles;
+    uint32_t *flags;
+};
+
+// One workgroup.
+__device__ __forceinline__ void make_order(const order_args &a)
 {
     __shared__ uint32_t hist[kOrderWaves][kBins];
     __shared__ uint32_t row_at[kBins + 1], tile_at[kBins + 1];
     __shared__ uint32_t scratch[17];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    for (int i = tid; i < kOrderWaves * (n + 1); i += kOrderBlock) hist[i / (n + 1)][i % (n + 1)] = 0;
-    __syncthreads();
+    constexpr int kHeld = 16;              // pieces of 64 ids a wave requests together and keeps
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.n, T = a.T;
     const int per = ((T + kOrderWaves - 1) / kOrderWaves + 63) / 64 * 64;      // a wave's rows, in pieces of 64
     const int lo = wave * per, hi = min(T, lo + per);
+    int held[kHeld];
     bool wrong = false;
-    for (int at = lo; at < hi; at += 64) {
-        const int t = at + lane;
-        if (t < hi) {
-            const int id = ids[t];
-            wrong |= id < -1 || id >= n;
-            atomicAdd(&hist[wave][id < 0 || id >= n ? n : id], 1u);
-        }
+    auto bin = [&](int id, bool live) {
+        wrong |= live && (id < -1 || id >= n);
+        return id < 0 || id >= n ? n : id;
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = lo + i * 64 + lane < hi ? a.ids[lo + i * 64 + lane] : -1;
+    for (int i = tid; i < kOrderWaves * (n + 1); i += kOrderBlock) hist[i / (n + 1)][i % (n + 1)] = 0;
+    mw_lds_barrier();
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const bool live = lo + i * 64 + lane < hi;
+        held[i] = bin(held[i], live);
+        if (live) atomicAdd(&hist[wave][held[i]], 1u);
     }
-    if (flags && wrong) atomicOr(flags, MW_FLAG_BAD_ADAPTER);
-    __syncthreads();
+    for (int t = lo + kHeld * 64 + lane; t < hi; t += 64) atomicAdd(&hist[wave][bin(a.ids[t], true)], 1u);
+    if (a.flags && wrong) atomicOr(a.flags, MW_FLAG_BAD_ADAPTER);
+    mw_lds_barrier();
     // places: bins in order, in a bin the waves in order
     constexpr int kPer = (kBins + kOrderBlock - 1) / kOrderBlock;
     uint32_t rows[kPer], rsum = 0, tsum = 0, total;
@@ -50,7 +64,7 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_order(const int32_t *__re
         if (b <= n)
             for (int w = 0; w < kOrderWaves; ++w) rows[i] += hist[w][b];
         rsum += rows[i];
-        tsum += (rows[i] + kTileRows - 1) / kTileRows;
+        tsum += (rows[i] + a.tile_rows - 1) / a.tile_rows;
     }
     uint32_t r = mw_block_exscan(rsum, scratch, &total);
     uint32_t k = mw_block_exscan(tsum, scratch, &total);
@@ -60,7 +74,7 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_order(const int32_t *__re
         if (b <= n) {
             row_at[b] = r;
             tile_at[b] = k;
-            start[b] = (int32_t)r;
+            a.tile_at[b] = (int32_t)k;
             uint32_t p = r;
             for (int w = 0; w < kOrderWaves; ++w) {
                 const uint32_t c = hist[w][b];
@@ -69,34 +83,27 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_order(const int32_t *__re
             }
         }
         r += rows[i];
-        k += (rows[i] + kTileRows - 1) / kTileRows;
+        k += (rows[i] + a.tile_rows - 1) / a.tile_rows;
     }
     if (tid == 0) {
         row_at[n + 1] = (uint32_t)T;
         tile_at[n + 1] = total;
-        start[n + 1] = T;
-        *n_tiles = (int32_t)total;
+        a.tile_at[n + 1] = (int32_t)total;
     }
-    __syncthreads();
+    mw_lds_barrier();
     for (int i = tid; i < (int)total; i += kOrderBlock) {      // the bin a tile is of: the last that starts at or before it
         int at = 0, end = n + 1;
         while (end - at > 1) {
             const int mid = (at + end) / 2;
             if (tile_at[mid] <= (uint32_t)i) at = mid; else end = mid;
         }
-        const int first = (int)row_at[at] + (i - (int)tile_at[at]) * kTileRows;
-        tiles[i] = adapt_tile{at, first, min(kTileRows, (int)row_at[at + 1] - first), 0};
+        const int first = (int)row_at[at] + (i - (int)tile_at[at]) * a.tile_rows;
+        a.tiles[i] = adapt_tile{at, first, min(a.tile_rows, (int)row_at[at + 1] - first), 0};
     }
     int bits = 0;
     while ((1 << bits) <= n) ++bits;
-    for (int at = lo; at < hi; at += 64) {
-        const int t = at + lane;
+    auto place = [&](int t, int b) {
         const bool live = t < hi;
-        int b = n;
-        if (live) {
-            b = ids[t];
-            if (b < 0 || b >= n) b = n;
-        }
         unsigned long long same = __ballot(live);              // the piece's rows of the same adapter
         for (int i = 0; i < bits; ++i) {
             const unsigned long long set = __ballot((b >> i) & 1);
@@ -104,31 +111,61 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_order(const int32_t *__re
         }
         if (live) {
             const int before = __popcll(same & ((1ull << lane) - 1));
-            const uint32_t p = hist[wave][b] + (uint32_t)before;
-            order[p] = t;
+            a.order[hist[wave][b] + (uint32_t)before] = t;
             __builtin_amdgcn_wave_barrier();
             if (before == 0) hist[wave][b] += (uint32_t)__popcll(same);
         }
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) if (lo + i * 64 < hi) place(lo + i * 64 + lane, held[i]);
+    for (int at = lo + kHeld * 64; at < hi; at += 64) place(at + lane, at + lane < hi ? bin(a.ids[at + lane], false) : n);
+}
+__global__ __launch_bounds__(kOrderBlock) void k_adapt_order(order_args a) { make_order(a); }
+
+// The order in workgroup 0; the others transpose the factors: [n][rows][cols] -> [n][cols][rows], 64 x 64 values each.
+struct transpose_args { const uint16_t *in; uint16_t *out; int32_t rows, cols; };
+__global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, transpose_args t0, transpose_args t1)
+{
+    __shared__ __align__(16) uint16_t tile[64][72];
+    if (blockIdx.x == 0) {
+        make_order(a);
+        return;
+    }
+    int64_t at = (int64_t)blockIdx.x - 1;
+    const int64_t per0 = (int64_t)((t0.rows + 63) / 64) * ((t0.cols + 63) / 64);
+    const bool first = at < per0 * a.n;
+    const transpose_args t = first ? t0 : t1;
+    if (!first) at -= per0 * a.n;
+    const int64_t wide = (t.cols + 63) / 64, per = (int64_t)((t.rows + 63) / 64) * wide, matrix = at / per;
+    const int r0 = (int)(at % per / wide) * 64, c0 = (int)(at % wide) * 64, i = threadIdx.x >> 3, q = (threadIdx.x & 7) * 8;
+    const int64_t base = matrix * t.rows * t.cols;
+    if (r0 + i < t.rows && c0 + q < t.cols) *(u32x4 *)&tile[i][q] = *(const u32x4 *)(t.in + base + (int64_t)(r0 + i) * t.cols + c0 + q);
+    __syncthreads();
+    if (c0 + i < t.cols && r0 + q < t.rows) {                  // (rows and columns are multiples of 8)
+        uint32_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = tile[q + 2 * j][i] | (uint32_t)tile[q + 2 * j + 1][i] << 16;
+        *(u32x4 *)(t.out + base + (int64_t)(c0 + i) * t.rows + r0 + q) = u32x4{v[0], v[1], v[2], v[3]};
     }
 }
 
 struct adapt_args {
-    const int32_t *order; const adapt_tile *tiles; const int32_t *n_tiles; const int32_t *start;
+    const int32_t *order, *n_tiles; const adapt_tile *tiles;
     const uint16_t *a, *b;                 // [n][rank][n_in], [n][n_out][rank]
-    const float *scale;                    // [n]
-    int32_t n, rank, n_in, n_out;
+    const float *scale;                    // [n] or null
+    int32_t T, n, rank, n_in, n_out;
     const uint16_t *x; int64_t x_stride;
     const uint16_t *base; int64_t base_stride;     // or null
     uint16_t *out; int64_t out_stride;
+    int32_t slice, n_slices;               // columns of x a workgroup of k_adapt_down takes
+    int32_t out_slice;                     // columns of y a workgroup of k_adapt_up takes
+    float *part;                           // [n_slices][T][ranks, whole tiles]: rows in order
     float *h;                              // [T][rank] or null
+    // for k_adapt_grads, or null: c h and c dh of the tiles as two bf16 terms each, [tile][ranks, whole tiles][32 rows]
+    const float *kept_h;
+    uint16_t *left_h[2], *left_dh[2];
 };
 
-__device__ __forceinline__ bf16x8 load8(const uint16_t *p, bool live)
-{
-    const bf16x8 zero = {};
-    return live ? *(const bf16x8 *)p : zero;
-}
-__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // A float as a sum of two bf16 values (16 bits of mantissa).  Where it is no number or too large the first says so alone.
 __device__ __forceinline__ void split(float v, uint16_t *hi, uint16_t *lo)
 {
@@ -137,195 +174,265 @@ __device__ __forceinline__ void split(float v, uint16_t *hi, uint16_t *lo)
     *lo = rest - rest == 0.0f ? mw_f32_to_bf16(rest) : 0;
 }
 
-constexpr int kWaves = 8, kBlock = kWaves * 64;
-constexpr int kPartTiles = 2;              // tiles of 16 ranks whose partial sums are in LDS at a time
-template <int kM>                          // tiles of 16 ranks
-__global__ __launch_bounds__(kBlock) void k_adapt(adapt_args p)
+constexpr int kWaves = 4, kBlock = kWaves * 64;
+
+// h: kM tiles of 16 ranks by kCols tiles of 16 rows.  grid: (tile, slice of n_in)
+template <int kM, int kCols>
+__global__ __launch_bounds__(kBlock) void k_adapt_down(adapt_args p)
 {
-    constexpr int kRanks = kM * 16, kStep = kRanks + 8;         // (rows of h in LDS start on different banks)
-    constexpr int kParts = kM < kPartTiles ? kM : kPartTiles;
-    __shared__ __align__(16) float part[kWaves * kParts * 16 * kTileRows];
-    __shared__ __align__(16) uint16_t h_hi[kTileRows * kStep], h_lo[kTileRows * kStep];
+    constexpr int kRanks = kM * 16, kRows = kCols * 16, kDepth = kM == 1 ? 4 : kM == 2 ? 3 : 2;
+    constexpr int kPartBytes = kWaves * kRows * kRanks * 4, kStageBytes = kWaves * kWaveLds<kM>;
+    __shared__ __align__(16) char lds[kPartBytes > kStageBytes ? kPartBytes : kStageBytes];
     if ((int)blockIdx.x >= *p.n_tiles) return;
     const adapt_tile t = p.tiles[blockIdx.x];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
-    if (t.adapter == p.n) {                                     // rows without an adapter
-        const int pieces = p.n_out / 8;
-        for (int i = tid; i < t.count * pieces; i += kBlock) {
-            const int64_t row = p.order[t.first + i / pieces];
-            const int c = i % pieces * 8;
-            *(bf16x8 *)(p.out + row * p.out_stride + c) = load8(p.base + row * p.base_stride + c, p.base != nullptr);
-        }
-        if (p.h)
-            for (int i = tid; i < t.count * p.rank; i += kBlock) p.h[(int64_t)p.order[t.first + i / p.rank] * p.rank + i % p.rank] = 0.0f;
-        return;
-    }
-    const uint16_t *a = p.a + (int64_t)t.adapter * p.rank * p.n_in, *b = p.b + (int64_t)t.adapter * p.rank * p.n_out;
-    int64_t row[2];
-    bool live[2];
+    if (t.adapter == p.n) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4, l8 = lane >> 3;
+    const int start = (int)blockIdx.y * p.slice;
+    const uint32_t piece = (uint32_t)(lane & 7) * 16 + (uint32_t)start * 2;
+    operands<false, kM, kCols, 2, 1> o;
+    o.w = array_at(p.a + (int64_t)t.adapter * p.rank * p.n_in);
+    o.b[0] = array_at(p.x);
+    o.limit = min(p.slice, p.n_in - start);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        live[i] = i * 16 + n < t.count;
-        row[i] = p.order[t.first + (live[i] ? i * 16 + n : 0)];
-    }
-    {   // h: the waves share the columns out in chunks of 128
-        f32x4 acc[kM][2] = {};
-        for (int c = wave * 128; c < p.n_in; c += kWaves * 128) {
+    for (int c = 0; c < kCols; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = c + j * 32 + g * 8;
-                bf16x8 xv[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) xv[i] = load8(p.x + row[i] * p.x_stride + k, live[i] && k < p.n_in);
-#pragma unroll
-                for (int m = 0; m < kM; ++m) {
-                    const bf16x8 av = load8(a + (int64_t)min(m * 16 + n, p.rank - 1) * p.n_in + k, k < p.n_in);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) acc[m][i] = mma(av, xv[i], acc[m][i]);
-                }
-            }
-        }
-        const float scale = p.scale ? p.scale[t.adapter] : 1.0f;
-#pragma unroll
-        for (int m0 = 0; m0 < kM; m0 += kParts) {
-            // part [wave][tile][row][16 ranks]
-#pragma unroll
-            for (int m = 0; m < kParts; ++m)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) *(f32x4 *)&part[((wave * kParts + m) * kTileRows + i * 16 + n) * 16 + g * 4] = acc[m0 + m][i];
-            __syncthreads();
-            for (int o = tid; o < kParts * kTileRows * 16; o += kBlock) {
-                float v = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kWaves; ++w) v += part[w * kParts * kTileRows * 16 + o];
-                const int r = (m0 + o / (kTileRows * 16)) * 16 + o % 16, col = o / 16 % kTileRows;
-                const bool real = r < p.rank && col < t.count;
-                if (p.h && real) p.h[(int64_t)p.order[t.first + col] * p.rank + r] = v;
-                split(real ? v * scale : 0.0f, &h_hi[col * kStep + r], &h_lo[col * kStep + r]);
-            }
-            __syncthreads();
-        }
-    }
-    // y: a wave takes 64 columns of the output at a time.  Row m of tile q is column (m / 4) * 16 + q * 4 + m % 4, so that a lane ends
-    // up with 16 neighbouring columns of its row.
-    for (int c = wave * 64; c < p.n_out; c += kWaves * 64) {
-        f32x4 acc[4][2] = {};
-        const int col = c + (n >> 2) * 16 + (n & 3);
-#pragma unroll
-        for (int k = 0; k < kRanks; k += 32) {
-            bf16x8 hv[2], lv[2], bv[4];
-            const int kk = k + g * 8;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) bv[q] = load8(b + (int64_t)(col + q * 4) * p.rank + kk, col + q * 4 < p.n_out && kk < p.rank);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                hv[i] = load8(&h_hi[(i * 16 + n) * kStep + kk], kk < kRanks);
-                lv[i] = load8(&h_lo[(i * 16 + n) * kStep + kk], kk < kRanks);
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    acc[q][i] = mma(bv[q], lv[i], acc[q][i]);
-                    acc[q][i] = mma(bv[q], hv[i], acc[q][i]);
-                }
+        for (int i = 0; i < 2; ++i) {
+            const int at = c * 16 + i * 8 + l8;
+            o.col[c][0][i] = (uint32_t)((int64_t)p.order[t.first + (at < t.count ? at : 0)] * p.x_stride * 2) + piece;
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int m = 0; m < kM; ++m)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int at = c + g * 16 + half * 8;
-                if (!live[i] || at >= p.n_out) continue;
-                const bf16x8 was = load8(p.base + row[i] * p.base_stride + at, p.base != nullptr);
-                bf16x8 v;
+        for (int i = 0; i < 2; ++i) o.row[m][i] = (uint32_t)(min(m * 16 + i * 8 + l8, p.rank - 1) * p.n_in * 2) + piece;
+    f32x4 acc[kM][kCols] = {};
+    stream<false, kM, kCols, 2, 1, kWaves, kDepth, kOnceCols>(o, wave, lane, lds + wave * kWaveLds<kM>, acc);
+    float *part = (float *)lds;             // [wave][row][rank]
+    __syncthreads();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (__bf16)((float)was[e] + acc[half * 2 + e / 4][i][e % 4]);
-                *(bf16x8 *)(p.out + row[i] * p.out_stride + at) = v;
-            }
+    for (int m = 0; m < kM; ++m)
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) *(f32x4 *)&part[((wave * kRows) + c * 16 + n) * kRanks + m * 16 + g * 4] = acc[m][c];
+    __syncthreads();
+    for (int i = threadIdx.x; i < kRows * kRanks / 4; i += kBlock) {
+        if (i / (kRanks / 4) >= t.count) break;
+        f32x4 v = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += *(const f32x4 *)&part[w * kRows * kRanks + i * 4];
+        *(f32x4 *)&p.part[((int64_t)blockIdx.y * p.T + t.first) * kRanks + i * 4] = v;
     }
 }
 
-// [n][rows][cols] -> [n][cols][rows] of 16-bit values.  grid: (64 columns, 64 rows, matrix).
-__global__ __launch_bounds__(256) void k_adapt_transpose(const uint16_t *__restrict__ in, uint16_t *__restrict__ out, int rows, int cols)
+// Writes a tile's rows-by-ranks values from LDS as ranks by 32 rows.
+template <int kRanks, int kStep>
+__device__ __forceinline__ void put_left(uint16_t *const (&to)[2], int64_t tile, const uint16_t *hi, const uint16_t *lo)
 {
-    __shared__ uint16_t tile[64][66];
-    const int64_t at = (int64_t)blockIdx.z * rows * cols;
-    const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
-    for (int i = threadIdx.x; i < 4096; i += 256) {
-        const int r = i >> 6, c = i & 63;
-        if (r0 + r < rows && c0 + c < cols) tile[r][c] = in[at + (int64_t)(r0 + r) * cols + c0 + c];
+    for (int i = threadIdx.x; i < kRanks * 4 * 2; i += kBlock) {
+        const uint16_t *from = i & 1 ? lo : hi;
+        const int r = i >> 3, q = (i >> 1 & 3) * 8;
+        uint32_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = from[(q + 2 * j) * kStep + r] | (uint32_t)from[(q + 2 * j + 1) * kStep + r] << 16;
+        *(u32x4 *)(to[i & 1] + (tile * kRanks + r) * 32 + q) = u32x4{v[0], v[1], v[2], v[3]};
+    }
+}
+
+// y: a wave takes 64 columns of the output at a time, as four tiles of rows of B; h is the other side.  What comes out goes through LDS
+// so that base and y are read and written in whole cache lines.  grid: (tile, slice of n_out)
+template <int kM, int kCols>
+__global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
+{
+    constexpr int kRanks = kM * 16, kRows = kCols * 16, kStep = kRanks + 8;      // (rows of h in LDS start on different banks)
+    constexpr int kLoads = 2 * kM;                          // 16-byte pieces a lane has of 64 rows of B, at most
+    constexpr int kOutPitch = 68;                           // floats from row to row of the result in LDS
+    constexpr int kWorkBytes = 64 * (kRanks * 2 + 16) > kRows * kOutPitch * 4 ? 64 * (kRanks * 2 + 16) : kRows * kOutPitch * 4;
+    __shared__ __align__(16) uint16_t h_hi[kRows * kStep], h_lo[kRows * kStep];
+    __shared__ __align__(16) char work[kWaves][kWorkBytes];
+    if ((int)blockIdx.x >= *p.n_tiles) return;
+    const adapt_tile t = p.tiles[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4, l8 = lane >> 3, q8 = (lane & 7) * 8;
+    const int c_from = (int)blockIdx.y * p.out_slice, c_to = min(c_from + p.out_slice, p.n_out);
+    if (t.adapter == p.n) {                                 // rows without an adapter
+        const int pieces = (c_to - c_from) / 8;
+        for (int i = tid; i < t.count * pieces; i += kBlock) {
+            const int64_t row = p.order[t.first + i / pieces];
+            const int c = c_from + i % pieces * 8;
+            const u32x4 zero = {};
+            *(u32x4 *)(p.out + row * p.out_stride + c) = p.base ? *(const u32x4 *)(p.base + row * p.base_stride + c) : zero;
+        }
+        if (p.h && blockIdx.y == 0)
+            for (int i = tid; i < t.count * p.rank; i += kBlock) p.h[(int64_t)p.order[t.first + i / p.rank] * p.rank + i % p.rank] = 0.0f;
+        return;
+    }
+    const float scale = p.scale ? p.scale[t.adapter] : 1.0f;
+    if (p.kept_h && (int)blockIdx.y == (int)gridDim.y - 1) {
+        for (int i = tid; i < kRows * kRanks; i += kBlock) {
+            const int col = i / kRanks, r = i % kRanks;
+            const bool real = r < p.rank && col < t.count;
+            split(real ? scale * p.kept_h[(int64_t)p.order[t.first + col] * p.rank + r] : 0.0f, &h_hi[col * kStep + r], &h_lo[col * kStep + r]);
+        }
+        __syncthreads();
+        put_left<kRanks, kStep>(p.left_h, blockIdx.x, h_hi, h_lo);
+        __syncthreads();
+    }
+    for (int i = tid; i < kRows * kRanks; i += kBlock) {
+        const int col = i / kRanks, r = i % kRanks;
+        const bool real = r < p.rank && col < t.count;
+        float v = 0.0f;
+        if (real)
+            for (int s = 0; s < p.n_slices; ++s) v += p.part[((int64_t)s * p.T + t.first + col) * kRanks + r];
+        if (real && p.h && blockIdx.y == 0) p.h[(int64_t)p.order[t.first + col] * p.rank + r] = v;
+        split(v * scale, &h_hi[col * kStep + r], &h_lo[col * kStep + r]);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 4096; i += 256) {
-        const int c = i >> 6, r = i & 63;
-        if (r0 + r < rows && c0 + c < cols) out[at + (int64_t)(c0 + c) * rows + r0 + r] = tile[r][c];
+    if (p.kept_h && blockIdx.y == 0) put_left<kRanks, kStep>(p.left_dh, blockIdx.x, h_hi, h_lo);
+
+    const array b = array_at(p.b + (int64_t)t.adapter * p.rank * p.n_out), base = array_at(p.base ? p.base : p.out), out = array_at(p.out);
+    char *mine = work[wave];
+    const int pitch = p.rank * 2 + 16, n_loads = p.rank / 8;
+    uint32_t to_lds[kLoads];                                // where a lane's pieces of B go in LDS
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int e = (i * 64 + lane) * 8;
+        to_lds[i] = (uint32_t)(e / p.rank * pitch + e % p.rank * 2);
+    }
+    uint32_t base_at[2 * kCols], out_at[2 * kCols];         // a lane's rows
+#pragma unroll
+    for (int i = 0; i < 2 * kCols; ++i) {
+        const bool live = i * 8 + l8 < t.count;
+        const int64_t row = p.order[t.first + (live ? i * 8 + l8 : 0)];
+        base_at[i] = p.base ? (uint32_t)(row * p.base_stride * 2) : kNowhere;
+        out_at[i] = live ? (uint32_t)(row * p.out_stride * 2) : kNowhere;
+    }
+    u32x4 bw[2][kLoads], was[2][2 * kCols];
+    auto load = [&](int c, u32x4 (&bq)[kLoads], u32x4 (&wq)[2 * kCols]) {
+        const uint32_t at = c < c_to ? 0u : kNowhere;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {                  // (past the last row of B: nothing)
+            const uint32_t e = (uint32_t)((i * 64 + lane) * 8);
+            bq[i] = load16<false>(b, at | (i < n_loads && c + (int)e / p.rank < p.n_out ? (uint32_t)(c * p.rank) * 2 + e * 2 : kNowhere));
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * kCols; ++i) wq[i] = load16<true>(base, at | (c + q8 < c_to ? base_at[i] + (uint32_t)(c + q8) * 2 : kNowhere));
+    };
+    bf16x8 hv[kCols][(kRanks + 31) / 32], lv[kCols][(kRanks + 31) / 32];
+    const bf16x8 none = {};
+#pragma unroll
+    for (int i = 0; i < kCols; ++i)
+#pragma unroll
+        for (int k = 0; k < kRanks; k += 32) {
+            const int kk = k + g * 8;
+            hv[i][k / 32] = kk < kRanks ? *(const bf16x8 *)&h_hi[(i * 16 + n) * kStep + kk] : none;
+            lv[i][k / 32] = kk < kRanks ? *(const bf16x8 *)&h_lo[(i * 16 + n) * kStep + kk] : none;
+        }
+    load(c_from + wave * 64, bw[0], was[0]);
+    for (int c0 = c_from + wave * 64; c0 < c_to; c0 += 2 * kWaves * 64) {
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            const int c = c0 + d * kWaves * 64;
+            load(c + kWaves * 64, bw[d ^ 1], was[d ^ 1]);
+            wave_order();
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) if (i < n_loads) *(u32x4 *)(mine + to_lds[i]) = bw[d][i];
+            wave_order();
+            f32x4 acc[4][kCols] = {};
+#pragma unroll
+            for (int k = 0; k < kRanks; k += 32) {
+                const int kk = k + g * 8;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bf16x8 bv = kk < p.rank ? *(const bf16x8 *)(mine + (q * 16 + n) * pitch + kk * 2) : none;
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) {
+                        acc[q][i] = mma(bv, lv[i][k / 32], acc[q][i]);
+                        acc[q][i] = mma(bv, hv[i][k / 32], acc[q][i]);
+                    }
+                }
+            }
+            float *res = (float *)mine;                     // [row][64 columns]
+            wave_order();
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < kCols; ++i) *(f32x4 *)&res[(i * 16 + n) * kOutPitch + q * 16 + g * 4] = acc[q][i];
+            wave_order();
+#pragma unroll
+            for (int i = 0; i < 2 * kCols; ++i) {
+                const f32x4 v0 = *(const f32x4 *)&res[(i * 8 + l8) * kOutPitch + q8], v1 = *(const f32x4 *)&res[(i * 8 + l8) * kOutPitch + q8 + 4];
+                const bf16x8 w = __builtin_bit_cast(bf16x8, was[d][i]);
+                bf16x8 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { y[e] = (__bf16)((float)w[e] + v0[e]); y[4 + e] = (__bf16)((float)w[4 + e] + v1[e]); }
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), out, c + q8 < c_to && out_at[i] != kNowhere ? out_at[i] + (uint32_t)(c + q8) * 2 : kNowhere, 0, 2);
+            }
+        }
     }
 }
 
 // Eight vectors of eight 16-bit values, transposed.
-__device__ __forceinline__ void transpose8(bf16x8 (&v)[8])
+__device__ __forceinline__ void transpose8(u32x4 (&v)[8])
 {
-    bf16x8 r[8];
+    bf16x8 in[8], r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) in[i] = __builtin_bit_cast(bf16x8, v[i]);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[i][j] = v[j][i];
+        for (int j = 0; j < 8; ++j) r[i][j] = in[j][i];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = r[i];
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(u32x4, r[i]);
 }
 
 struct grad_args {
-    const int32_t *order, *start;
-    const float *scale;
-    int32_t rank;
-    // z 0: d_a[m][c] = c sum_t dh[t][m] x[t][c];  z 1: d_b[c][m] = c sum_t h[t][m] dy[t][c]
-    const float *left[2];                  // [T][rank]
+    const int32_t *order, *tile_at; const adapt_tile *tiles;
+    int32_t rank, ranks;                   // ranks: whole tiles of 16
+    // side 0: d_a[m][c] = sum_t (c dh)[t][m] x[t][c];  side 1: d_b[c][m] = sum_t (c h)[t][m] dy[t][c]
+    const uint16_t *left[2][2];            // [side][term]: [tile][ranks][32 rows]
     const uint16_t *right[2]; int64_t stride[2]; int32_t width[2];
     uint16_t *out[2];
 };
 
-// grid: (128 columns, adapter, {dA, dB} x pieces of 64 ranks).  The waves take 32 of the adapter's rows at a time.
-constexpr int kGradWaves = 4;
+// grid: (128 columns, adapter, side and piece of 64 ranks).  The waves take an adapter's tiles of 32 rows in turn: a tile is one
+// matrix instruction deep.  Rows of x are loaded as they lie, 256 bytes of four rows an instruction, and turned in registers: a lane has eight
+// rows of eight columns, and the columns' vectors over the rows are operands.
+constexpr int kGradWaves = 8;
 template <int kM>
 __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
 {
     __shared__ __align__(16) float part[kGradWaves * 8 * 256];
     const int side = blockIdx.z & 1, r0 = (blockIdx.z >> 1) * 64, ad = blockIdx.y, c0 = blockIdx.x * 128, width = p.width[side];
     if (c0 >= width) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    const int first = p.start[ad], count = p.start[ad + 1] - first;
-    const float *left = p.left[side];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
+    const int tile0 = p.tile_at[ad], tile1 = p.tile_at[ad + 1];
     const uint16_t *right = p.right[side];
     const int64_t stride = p.stride[side];
     const int col = c0 + n * 8;
     f32x4 acc[kM][8] = {};
-    for (int k = wave * 32; k < count; k += kGradWaves * 32) {
-        bf16x8 v[8];
+    for (int k = tile0 + wave; k < tile1; k += kGradWaves) {
+        const adapt_tile t = p.tiles[k];
+        u32x4 v[8];
         bf16x8 hi[kM], lo[kM];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool live = k + g * 8 + j < count;
-            const int64_t row = p.order[first + (live ? k + g * 8 + j : 0)];
-            v[j] = load8(right + row * stride + col, live && col < width);
+            const bool live = g * 8 + j < t.count && col < width;
+            const int64_t row = p.order[t.first + (g * 8 + j < t.count ? g * 8 + j : 0)];
+            const u32x4 zero = {};
+            v[j] = live ? *(const u32x4 *)(right + row * stride + col) : zero;
+        }
 #pragma unroll
-            for (int m = 0; m < kM; ++m) {
-                const int r = r0 + m * 16 + n;
-                uint16_t a, b;
-                split(live && r < p.rank ? left[row * p.rank + r] : 0.0f, &a, &b);
-                hi[m][j] = __builtin_bit_cast(__bf16, a);
-                lo[m][j] = __builtin_bit_cast(__bf16, b);
-            }
+        for (int m = 0; m < kM; ++m) {
+            const int64_t at = ((int64_t)k * p.ranks + r0 + m * 16 + n) * 32 + g * 8;
+            hi[m] = *(const bf16x8 *)(p.left[side][0] + at);
+            lo[m] = *(const bf16x8 *)(p.left[side][1] + at);
         }
         transpose8(v);
 #pragma unroll
         for (int m = 0; m < kM; ++m)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                acc[m][j] = mma(lo[m], v[j], acc[m][j]);
-                acc[m][j] = mma(hi[m], v[j], acc[m][j]);
+                acc[m][j] = mma(lo[m], __builtin_bit_cast(bf16x8, v[j]), acc[m][j]);
+                acc[m][j] = mma(hi[m], __builtin_bit_cast(bf16x8, v[j]), acc[m][j]);
             }
     }
-    const float scale = p.scale ? p.scale[ad] : 1.0f;
 #pragma unroll
     for (int m = 0; m < kM; ++m) {
 #pragma unroll
@@ -346,7 +453,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
                     for (int i = 0; i < 4; ++i) {
                         bf16x8 o;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) o[j] = (__bf16)(scale * s[j][i]);
+                        for (int j = 0; j < 8; ++j) o[j] = (__bf16)s[j][i];
                         *(bf16x8 *)(p.out[0] + ((int64_t)ad * p.rank + r + i) * width + col) = o;
                     }
                 } else {
@@ -354,7 +461,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
                     for (int j = 0; j < 8; ++j) {
                         bf16x4 o;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] = (__bf16)(scale * s[j][i]);
+                        for (int i = 0; i < 4; ++i) o[i] = (__bf16)s[j][i];
                         *(bf16x4 *)(p.out[1] + ((int64_t)ad * width + col + j) * p.rank + r) = o;
                     }
                 }
@@ -364,16 +471,25 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
     }
 }
 
-struct adapt_ws { int64_t order, start, tiles, n_tiles, dh, at, bt, total; };
+int ranks_of(int32_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+constexpr int kMostSlices = 16;
+constexpr int64_t kMostCus = 512;          // (slices times rows stay below rows + 96 times the CUs: a tile has at most 32 rows)
+
+// Rows of a tile: 32 where adapters have that many rows mostly, else 16.
+int tile_rows_of(const mw_adapters *s, int64_t rows, bool backward) { return backward || rows >= 24LL * s->n_adapters ? 32 : 16; }
+int64_t most_tiles(const mw_adapters *s, int64_t rows, int tile_rows) { return rows / tile_rows + (s->n_adapters + 1LL < rows ? s->n_adapters + 1LL : rows); }
+
+struct adapt_ws { int64_t order, tile_at, tiles, part, left[4], at, bt, total; };
 adapt_ws adapt_layout(const mw_adapters *s, int64_t rows, bool backward)
 {
     adapt_ws w;
     int64_t o = 0;
+    const int64_t tiles = most_tiles(s, rows, 16), ranks = ranks_of(s->rank);
     w.order = o;   o += mw_align_up(4 * rows, 256);
-    w.start = o;   o += mw_align_up(4 * (s->n_adapters + 2LL), 256);
-    w.tiles = o;   o += mw_align_up((int64_t)sizeof(adapt_tile) * (rows / kTileRows + s->n_adapters + 1), 256);
-    w.n_tiles = o; o += 256;
-    w.dh = o;      o += backward ? mw_align_up(4 * rows * s->rank, 256) : 0;
+    w.tile_at = o; o += mw_align_up(4 * (s->n_adapters + 2LL), 256);
+    w.tiles = o;   o += mw_align_up((int64_t)sizeof(adapt_tile) * tiles, 256);
+    w.part = o;    o += mw_align_up(4 * ranks * (rows * kMostSlices < rows + 96 * kMostCus ? rows * kMostSlices : rows + 96 * kMostCus), 256);
+    for (int i = 0; i < 4; ++i) { w.left[i] = o; o += backward ? mw_align_up(2 * most_tiles(s, rows, 32) * ranks * 32, 256) : 0; }
     w.at = o;      o += backward ? mw_align_up(2LL * s->n_adapters * s->rank * s->n_in, 256) : 0;
     w.bt = o;      o += backward ? mw_align_up(2LL * s->n_adapters * s->rank * s->n_out, 256) : 0;
     w.total = o;
@@ -390,21 +506,57 @@ int32_t adapters_ready(const mw_adapters *s)
 // a bf16 matrix of rows in one piece each
 bool rows_ready(const void *p, int64_t stride, int32_t width) { return p && ((uintptr_t)p & 15u) == 0 && stride >= width && stride % 8 == 0; }
 
-void launch_order(const mw_adapters *s, const int32_t *ids, int32_t T, char *ws, const adapt_ws &w, uint32_t *flags, adapt_args *p, hipStream_t st)
+order_args order_of(const mw_adapters *s, const int32_t *ids, int32_t T, char *ws, const adapt_ws &w, int tile_rows, uint32_t *flags)
 {
-    hipLaunchKernelGGL(k_adapt_order, dim3(1), dim3(kOrderBlock), 0, st, ids, T, s->n_adapters, (int32_t *)(ws + w.order), (int32_t *)(ws + w.start),
-                       (adapt_tile *)(ws + w.tiles), (int32_t *)(ws + w.n_tiles), flags);
-    p->order = (const int32_t *)(ws + w.order); p->start = (const int32_t *)(ws + w.start);
-    p->tiles = (const adapt_tile *)(ws + w.tiles); p->n_tiles = (const int32_t *)(ws + w.n_tiles);
-    p->scale = s->scale_dev; p->n = s->n_adapters; p->rank = s->rank;
+    order_args o;
+    o.ids = ids; o.T = T; o.n = s->n_adapters; o.tile_rows = tile_rows;
+    o.order = (int32_t *)(ws + w.order); o.tile_at = (int32_t *)(ws + w.tile_at); o.tiles = (adapt_tile *)(ws + w.tiles);
+    o.flags = flags;
+    return o;
 }
-void launch_adapt(const adapt_args &p, int32_t T, hipStream_t st)
+template <int kM, int kCols>
+void launch_both(const adapt_args &p, dim3 down, dim3 up, hipStream_t st)
 {
-    const dim3 grid((uint32_t)(T / kTileRows + (p.n + 1 < T ? p.n + 1 : T)));       // tiles there can be at most
-    if (p.rank <= 16) hipLaunchKernelGGL((k_adapt<1>), grid, dim3(kBlock), 0, st, p);
-    else if (p.rank <= 32) hipLaunchKernelGGL((k_adapt<2>), grid, dim3(kBlock), 0, st, p);
-    else if (p.rank <= 64) hipLaunchKernelGGL((k_adapt<4>), grid, dim3(kBlock), 0, st, p);
-    else hipLaunchKernelGGL((k_adapt<8>), grid, dim3(kBlock), 0, st, p);
+    hipLaunchKernelGGL((k_adapt_down<kM, kCols>), down, dim3(kBlock), 0, st, p);
+    hipLaunchKernelGGL((k_adapt_up<kM, kCols>), up, dim3(kBlock), 0, st, p);
+}
+// h and y.  p.a to p.out, p.T, p.h are set; the order is that of `o`.
+int32_t launch_adapt(adapt_args p, const mw_adapters *s, const order_args &o, char *ws, const adapt_ws &w, int n_cu, hipStream_t st)
+{
+    p.order = o.order; p.tiles = o.tiles; p.n_tiles = o.tile_at + s->n_adapters + 1;
+    p.scale = s->scale_dev; p.n = s->n_adapters; p.rank = s->rank;
+    p.part = (float *)(ws + w.part);
+    const int64_t tiles = most_tiles(s, p.T, o.tile_rows);
+    // Slices that give every CU three workgroups, of whole spans; of at least 512 columns each.
+    int64_t n = (3LL * n_cu + tiles - 1) / tiles;
+    const int64_t most = (p.n_in + 511) / 512;
+    n = n < most ? n : most;
+    n = n < kMostSlices ? n : kMostSlices;
+    p.slice = (int32_t)mw_align_up((p.n_in + n - 1) / n, 64);
+    p.n_slices = (p.n_in + p.slice - 1) / p.slice;
+    int64_t m = (4LL * n_cu + tiles - 1) / tiles;
+    const int64_t most_out = (p.n_out + 255) / 256;
+    m = m < most_out ? m : most_out;
+    p.out_slice = (int32_t)mw_align_up((p.n_out + m - 1) / m, 256);
+    const dim3 down((uint32_t)tiles, (uint32_t)p.n_slices), up((uint32_t)tiles, (uint32_t)((p.n_out + p.out_slice - 1) / p.out_slice));
+    const bool wide = o.tile_rows == 32;
+    switch (ranks_of(p.rank)) {
+    case 16: if (wide) launch_both<1, 2>(p, down, up, st); else launch_both<1, 1>(p, down, up, st); break;
+    case 32: if (wide) launch_both<2, 2>(p, down, up, st); else launch_both<2, 1>(p, down, up, st); break;
+    case 64: if (wide) launch_both<4, 2>(p, down, up, st); else launch_both<4, 1>(p, down, up, st); break;
+    default: if (wide) launch_both<8, 2>(p, down, up, st); else launch_both<8, 1>(p, down, up, st); break;
+    }
+    MW_HIP_CHECK(hipGetLastError());
+    return MW_OK;
+}
+int32_t cus_of_current_device(int *n)
+{
+    int dev = -1;
+    MW_HIP_CHECK(hipGetDevice(&dev));
+    MW_HIP_CHECK(hipDeviceGetAttribute(n, hipDeviceAttributeMultiprocessorCount, dev));
+    if (*n < 1) *n = 256;
+    if (*n > kMostCus) *n = kMostCus;
+    return MW_OK;
 }
 
 }  // namespace
@@ -435,18 +587,24 @@ extern "C" MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_de
     if (((uintptr_t)h_dev | (uintptr_t)error_flags_dev | (uintptr_t)adapter_ids_dev) & 3u) return MW_ERR_INVALID_ARG;
     const adapt_ws w = adapt_layout(adapters, n_rows, false);
     if (!workspace_dev || ((uintptr_t)workspace_dev & 255u) || workspace_bytes < w.total) return MW_ERR_WORKSPACE;
+    // places in x, base and out are 32-bit, below 2^31
+    const int64_t far = 1LL << 30;
+    if (x_stride * n_rows > far || out_stride * n_rows > far || (base_dev && base_stride * n_rows > far)) return MW_ERR_UNSUPPORTED;
+    int n_cu = 0;
+    const int32_t rd = cus_of_current_device(&n_cu);
+    if (rd != MW_OK) return rd;
     const hipStream_t st = (hipStream_t)stream;
-    adapt_args p;
-    launch_order(adapters, adapter_ids_dev, n_rows, (char *)workspace_dev, w, error_flags_dev, &p, st);
+    char *ws = (char *)workspace_dev;
+    const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, tile_rows_of(adapters, n_rows, false), error_flags_dev);
+    hipLaunchKernelGGL(k_adapt_order, dim3(1), dim3(kOrderBlock), 0, st, o);
     MW_HIP_CHECK(hipGetLastError());
-    p.a = (const uint16_t *)s.a_dev; p.b = (const uint16_t *)s.b_dev; p.n_in = s.n_in; p.n_out = s.n_out;
+    adapt_args p = {};
+    p.a = (const uint16_t *)s.a_dev; p.b = (const uint16_t *)s.b_dev; p.T = n_rows; p.n_in = s.n_in; p.n_out = s.n_out;
     p.x = (const uint16_t *)x_dev; p.x_stride = x_stride;
     p.base = (const uint16_t *)base_dev; p.base_stride = base_stride;
     p.out = (uint16_t *)out_dev; p.out_stride = out_stride;
     p.h = h_dev;
-    launch_adapt(p, n_rows, st);
-    MW_HIP_CHECK(hipGetLastError());
-    return MW_OK;
+    return launch_adapt(p, adapters, o, ws, w, n_cu, st);
 }
 
 extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const void *x_dev, int64_t x_stride, const int32_t *adapter_ids_dev,
@@ -470,34 +628,41 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
     }
     const adapt_ws w = adapt_layout(adapters, n_rows, true);
     if (!workspace_dev || ((uintptr_t)workspace_dev & 255u) || workspace_bytes < w.total) return MW_ERR_WORKSPACE;
+    const int64_t far = 1LL << 30;
+    if (dy_stride * n_rows > far || dx_stride * n_rows > far || (dx_base_dev && dx_base_stride * n_rows > far)) return MW_ERR_UNSUPPORTED;
+    int n_cu = 0;
+    const int32_t rd = cus_of_current_device(&n_cu);
+    if (rd != MW_OK) return rd;
     char *ws = (char *)workspace_dev;
     const hipStream_t st = (hipStream_t)stream;
-    adapt_args p;
-    launch_order(adapters, adapter_ids_dev, n_rows, ws, w, error_flags_dev, &p, st);
+    const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, 32, error_flags_dev);
+    const transpose_args ta = {(const uint16_t *)s.a_dev, (uint16_t *)(ws + w.at), s.rank, s.n_in};
+    const transpose_args tb = {(const uint16_t *)s.b_dev, (uint16_t *)(ws + w.bt), s.n_out, s.rank};
+    const int64_t r64 = (s.rank + 63) / 64, blocks = s.n_adapters * r64 * ((s.n_in + 63) / 64 + (s.n_out + 63) / 64);
+    hipLaunchKernelGGL(k_adapt_prepare, dim3(n_rows > 0 ? (uint32_t)(1 + blocks) : 1u), dim3(kOrderBlock), 0, st, o, ta, tb);
     MW_HIP_CHECK(hipGetLastError());
-    uint16_t *at = (uint16_t *)(ws + w.at), *bt = (uint16_t *)(ws + w.bt);
-    float *dh = (float *)(ws + w.dh);
+    uint16_t *left[4];
+    for (int i = 0; i < 4; ++i) left[i] = (uint16_t *)(ws + w.left[i]);
     if (n_rows > 0) {
-        const uint32_t r64 = (uint32_t)((s.rank + 63) / 64), n = (uint32_t)s.n_adapters;
-        hipLaunchKernelGGL(k_adapt_transpose, dim3((uint32_t)((s.n_in + 63) / 64), r64, n), dim3(256), 0, st, (const uint16_t *)s.a_dev, at, s.rank, s.n_in);
-        hipLaunchKernelGGL(k_adapt_transpose, dim3(r64, (uint32_t)((s.n_out + 63) / 64), n), dim3(256), 0, st, (const uint16_t *)s.b_dev, bt, s.n_out, s.rank);
-        MW_HIP_CHECK(hipGetLastError());
-        p.a = bt; p.b = at; p.n_in = s.n_out; p.n_out = s.n_in;
+        adapt_args p = {};
+        p.a = tb.out; p.b = ta.out; p.T = n_rows; p.n_in = s.n_out; p.n_out = s.n_in;
         p.x = (const uint16_t *)dy_dev; p.x_stride = dy_stride;
         p.base = (const uint16_t *)dx_base_dev; p.base_stride = dx_base_stride;
         p.out = (uint16_t *)dx_dev; p.out_stride = dx_stride;
-        p.h = dh;
-        launch_adapt(p, n_rows, st);
-        MW_HIP_CHECK(hipGetLastError());
+        p.kept_h = h_dev;
+        for (int i = 0; i < 2; ++i) { p.left_dh[i] = left[i]; p.left_h[i] = left[2 + i]; }
+        const int32_t ra = launch_adapt(p, adapters, o, ws, w, n_cu, st);
+        if (ra != MW_OK) return ra;
     }
     grad_args q;
-    q.order = p.order; q.start = p.start; q.scale = s.scale_dev; q.rank = s.rank;
-    q.left[0] = dh; q.right[0] = (const uint16_t *)x_dev; q.stride[0] = x_stride; q.width[0] = s.n_in; q.out[0] = (uint16_t *)da_dev;
-    q.left[1] = h_dev; q.right[1] = (const uint16_t *)dy_dev; q.stride[1] = dy_stride; q.width[1] = s.n_out; q.out[1] = (uint16_t *)db_dev;
+    q.order = o.order; q.tile_at = o.tile_at; q.tiles = o.tiles; q.rank = s.rank; q.ranks = ranks_of(s.rank);
+    for (int i = 0; i < 2; ++i) { q.left[0][i] = left[i]; q.left[1][i] = left[2 + i]; }
+    q.right[0] = (const uint16_t *)x_dev; q.stride[0] = x_stride; q.width[0] = s.n_in; q.out[0] = (uint16_t *)da_dev;
+    q.right[1] = (const uint16_t *)dy_dev; q.stride[1] = dy_stride; q.width[1] = s.n_out; q.out[1] = (uint16_t *)db_dev;
     const int32_t widest = s.n_in > s.n_out ? s.n_in : s.n_out;
-    const dim3 grid((uint32_t)((widest + 127) / 128), (uint32_t)s.n_adapters, (uint32_t)(2 * ((s.rank + 63) / 64)));
-    if (s.rank <= 16) hipLaunchKernelGGL((k_adapt_grads<1>), grid, dim3(kGradWaves * 64), 0, st, q);
-    else if (s.rank <= 32) hipLaunchKernelGGL((k_adapt_grads<2>), grid, dim3(kGradWaves * 64), 0, st, q);
+    const dim3 grid((uint32_t)((widest + 127) / 128), (uint32_t)s.n_adapters, (uint32_t)(2 * ((q.ranks + 63) / 64)));
+    if (q.ranks == 16) hipLaunchKernelGGL((k_adapt_grads<1>), grid, dim3(kGradWaves * 64), 0, st, q);
+    else if (q.ranks == 32) hipLaunchKernelGGL((k_adapt_grads<2>), grid, dim3(kGradWaves * 64), 0, st, q);
     else hipLaunchKernelGGL((k_adapt_grads<4>), grid, dim3(kGradWaves * 64), 0, st, q);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
