@@ -881,7 +881,7 @@ MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_dev, int64_t 
  *   dA_a = scale_a sum over a's rows of dh_t x_t^T,   dB_a = scale_a sum over a's rows of dy_t h_t^T,
  * in fp32 sums, each rounded to bf16 once.  dx_base_dev is the gradient that comes through the shared projection, or NULL; dx_dev
  * may be dx_base_dev itself.  da_dev, db_dev: laid out as a_dev and b_dev, 16-byte aligned, written whole (zeros for adapters without
- * rows).  Sums over rows have a fixed order: equal calls give equal bits.  dy, dx_base and dx may each span at most 2 GiB.
+ * rows).  Sums over rows have a fixed order: equal calls give equal bits.  x, dy, dx_base and dx may each span at most 2 GiB.
  */
 MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const void *x_dev, int64_t x_stride, const int32_t *adapter_ids_dev,
                                  int32_t n_rows, const float *h_dev, const void *dy_dev, int64_t dy_stride,

@@ -11,7 +11,7 @@
 
 namespace {
 
-constexpr int kOrderBlock = 512, kOrderWaves = kOrderBlock / 64;
+constexpr int kOrderBlock = 1024, kOrderWaves = kOrderBlock / 64;
 constexpr int kBins = MW_ADAPT_MAX_ADAPTERS + 1;       // the last: rows without an adapter
 
 struct adapt_tile { int32_t adapter, first, count, reserved0; };      // adapter == n_adapters: rows without one
@@ -31,27 +31,29 @@ __device__ __forceinline__ void make_order(const order_args &a)
     __shared__ uint32_t hist[kOrderWaves][kBins];
     __shared__ uint32_t row_at[kBins + 1], tile_at[kBins + 1];
     __shared__ uint32_t scratch[17];
-    constexpr int kHeld = 16;              // pieces of 64 ids a wave requests together and keeps
+    constexpr int kHeld = 8;               // pieces of 64 ids a wave requests together
+    __shared__ uint16_t held[kOrderWaves][kHeld * 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.n, T = a.T;
     const int per = ((T + kOrderWaves - 1) / kOrderWaves + 63) / 64 * 64;      // a wave's rows, in pieces of 64
     const int lo = wave * per, hi = min(T, lo + per);
-    int held[kHeld];
     bool wrong = false;
-    auto bin = [&](int id, bool live) {
-        wrong |= live && (id < -1 || id >= n);
-        return id < 0 || id >= n ? n : id;
+    // Bins of the rows from `at`.  They wait in LDS for loops that are not unrolled: code that runs once is fetched at memory's pace.
+    auto hold = [&](int at) {
+        int id[kHeld];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) id[i] = at + i * 64 + lane < hi ? a.ids[at + i * 64 + lane] : -1;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            wrong |= id[i] < -1 || id[i] >= n;
+            held[wave][i * 64 + lane] = (uint16_t)(id[i] < 0 || id[i] >= n ? n : id[i]);
+        }
     };
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) held[i] = lo + i * 64 + lane < hi ? a.ids[lo + i * 64 + lane] : -1;
-    for (int i = tid; i < kOrderWaves * (n + 1); i += kOrderBlock) hist[i / (n + 1)][i % (n + 1)] = 0;
-    mw_lds_barrier();
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-        const bool live = lo + i * 64 + lane < hi;
-        held[i] = bin(held[i], live);
-        if (live) atomicAdd(&hist[wave][held[i]], 1u);
+    for (int i = lane; i <= n; i += 64) hist[wave][i] = 0;
+    for (int at = lo; at < hi; at += kHeld * 64) {
+        hold(at);
+#pragma unroll 1
+        for (int t = at + lane; t < min(hi, at + kHeld * 64); t += 64) atomicAdd(&hist[wave][held[wave][t - at]], 1u);
     }
-    for (int t = lo + kHeld * 64 + lane; t < hi; t += 64) atomicAdd(&hist[wave][bin(a.ids[t], true)], 1u);
     if (a.flags && wrong) atomicOr(a.flags, MW_FLAG_BAD_ADAPTER);
     mw_lds_barrier();
     // places: bins in order, in a bin the waves in order
@@ -102,43 +104,49 @@ __device__ __forceinline__ void make_order(const order_args &a)
     }
     int bits = 0;
     while ((1 << bits) <= n) ++bits;
-    auto place = [&](int t, int b) {
-        const bool live = t < hi;
-        unsigned long long same = __ballot(live);              // the piece's rows of the same adapter
-        for (int i = 0; i < bits; ++i) {
-            const unsigned long long set = __ballot((b >> i) & 1);
-            same &= (b >> i) & 1 ? set : ~set;
+    for (int at = lo; at < hi; at += kHeld * 64) {
+        if (hi - lo > kHeld * 64) hold(at);
+#pragma unroll 1
+        for (int t0 = at; t0 < min(hi, at + kHeld * 64); t0 += 64) {
+            const int t = t0 + lane;
+            const bool live = t < hi;
+            const int b = held[wave][t - at];
+            unsigned long long same = __ballot(live);          // the piece's rows of the same adapter
+            if (__ballot(live && b != __builtin_amdgcn_readfirstlane(b)) != 0)
+                for (int i = 0; i < bits; ++i) {
+                    const unsigned long long set = __ballot((b >> i) & 1);
+                    same &= (b >> i) & 1 ? set : ~set;
+                }
+            if (live) {
+                const int before = __popcll(same & ((1ull << lane) - 1));
+                a.order[hist[wave][b] + (uint32_t)before] = t;
+                __builtin_amdgcn_wave_barrier();
+                if (before == 0) hist[wave][b] += (uint32_t)__popcll(same);
+                __builtin_amdgcn_wave_barrier();
+            }
         }
-        if (live) {
-            const int before = __popcll(same & ((1ull << lane) - 1));
-            a.order[hist[wave][b] + (uint32_t)before] = t;
-            __builtin_amdgcn_wave_barrier();
-            if (before == 0) hist[wave][b] += (uint32_t)__popcll(same);
-        }
-    };
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) if (lo + i * 64 < hi) place(lo + i * 64 + lane, held[i]);
-    for (int at = lo + kHeld * 64; at < hi; at += 64) place(at + lane, at + lane < hi ? bin(a.ids[at + lane], false) : n);
+    }
 }
 __global__ __launch_bounds__(kOrderBlock) void k_adapt_order(order_args a) { make_order(a); }
 
-// The order in workgroup 0; the others transpose the factors: [n][rows][cols] -> [n][cols][rows], 64 x 64 values each.
+// The order in workgroup 0; the others transpose the factors: [n][rows][cols] -> [n][cols][rows], 64 x 128 values each.
 struct transpose_args { const uint16_t *in; uint16_t *out; int32_t rows, cols; };
 __global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, transpose_args t0, transpose_args t1)
 {
-    __shared__ __align__(16) uint16_t tile[64][72];
+    __shared__ __align__(16) uint16_t tiles[2][64][72];         // each half of the workgroup has its own
     if (blockIdx.x == 0) {
         make_order(a);
         return;
     }
     int64_t at = (int64_t)blockIdx.x - 1;
-    const int64_t per0 = (int64_t)((t0.rows + 63) / 64) * ((t0.cols + 63) / 64);
+    const int64_t per0 = (int64_t)((t0.rows + 63) / 64) * ((t0.cols + 127) / 128);
     const bool first = at < per0 * a.n;
     const transpose_args t = first ? t0 : t1;
     if (!first) at -= per0 * a.n;
-    const int64_t wide = (t.cols + 63) / 64, per = (int64_t)((t.rows + 63) / 64) * wide, matrix = at / per;
-    const int r0 = (int)(at % per / wide) * 64, c0 = (int)(at % wide) * 64, i = threadIdx.x >> 3, q = (threadIdx.x & 7) * 8;
+    const int64_t wide = (t.cols + 127) / 128, per = (int64_t)((t.rows + 63) / 64) * wide, matrix = at / per;
+    const int r0 = (int)(at % per / wide) * 64, c0 = (int)(at % wide) * 128 + (int)(threadIdx.x >> 9) * 64, i = threadIdx.x >> 3 & 63, q = (threadIdx.x & 7) * 8;
     const int64_t base = matrix * t.rows * t.cols;
+    uint16_t (*tile)[72] = tiles[threadIdx.x >> 9];
     if (r0 + i < t.rows && c0 + q < t.cols) *(u32x4 *)&tile[i][q] = *(const u32x4 *)(t.in + base + (int64_t)(r0 + i) * t.cols + c0 + q);
     __syncthreads();
     if (c0 + i < t.cols && r0 + q < t.rows) {                  // (rows and columns are multiples of 8)
@@ -150,7 +158,8 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, tra
 }
 
 struct adapt_args {
-    const int32_t *order, *n_tiles; const adapt_tile *tiles;
+    const int32_t *order, *n_tiles; const adapt_tile *tiles;      // null: made by every workgroup (at most kBlock rows)
+    const int32_t *ids; uint32_t *flags;
     const uint16_t *a, *b;                 // [n][rank][n_in], [n][n_out][rank]
     const float *scale;                    // [n] or null
     int32_t T, n, rank, n_in, n_out;
@@ -159,7 +168,7 @@ struct adapt_args {
     uint16_t *out; int64_t out_stride;
     int32_t slice, n_slices;               // columns of x a workgroup of k_adapt_down takes
     int32_t out_slice;                     // columns of y a workgroup of k_adapt_up takes
-    float *part;                           // [n_slices][T][ranks, whole tiles]: rows in order
+    float *part;                           // [n_slices][T][ranks, whole tiles]
     float *h;                              // [T][rank] or null
     // for k_adapt_grads, or null: c h and c dh of the tiles as two bf16 terms each, [tile][ranks, whole tiles][32 rows]
     const float *kept_h;
@@ -176,6 +185,61 @@ __device__ __forceinline__ void split(float v, uint16_t *hi, uint16_t *lo)
 
 constexpr int kWaves = 4, kBlock = kWaves * 64;
 
+// This workgroup's tile: its adapter (-1: there is no such tile) and its rows.
+struct tile_rows { int32_t adapter, count; int32_t row[32]; };
+__device__ __forceinline__ void find_tile(const adapt_args &p, int n_rows, tile_rows &t)
+{
+    const int tid = threadIdx.x, index = (int)blockIdx.x;
+    if (p.tiles) {
+        const bool some = index < *p.n_tiles;
+        adapt_tile a = {-1, 0, 0, 0};
+        if (some) a = p.tiles[index];
+        if (tid < a.count) t.row[tid] = p.order[a.first + tid];
+        if (tid == 0) { t.adapter = a.adapter; t.count = a.count; }
+        mw_lds_barrier();
+        return;
+    }
+    // Few rows, one a thread: bins counted, the bin that the index-th tile is of, and of its rows those of the tile, in order.
+    __shared__ uint32_t hist[kBins], scratch[17];
+    __shared__ uint32_t bin_of_tile, first_of_tile, in_wave[kWaves];
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = p.n;
+    int b = -1;
+    if (tid < p.T) {
+        const int id = p.ids[tid];
+        b = id < 0 || id >= n ? n : id;
+        if (p.flags && (id < -1 || id >= n) && index == 0 && blockIdx.y == 0) atomicOr(p.flags, MW_FLAG_BAD_ADAPTER);
+    }
+    for (int i = tid; i <= n; i += kBlock) hist[i] = 0;
+    if (tid == 0) { t.adapter = -1; t.count = 0; }
+    mw_lds_barrier();
+    if (b >= 0) atomicAdd(&hist[b], 1u);
+    mw_lds_barrier();
+    uint32_t before = 0;
+    for (int i0 = 0; i0 <= n; i0 += kBlock) {
+        const uint32_t c = i0 + tid <= n ? hist[i0 + tid] : 0u, k = (c + (uint32_t)n_rows - 1) / (uint32_t)n_rows;
+        uint32_t all;
+        const uint32_t at = before + mw_block_exscan(k, scratch, &all);
+        if ((uint32_t)index >= at && (uint32_t)index < at + k) {
+            const uint32_t first = ((uint32_t)index - at) * (uint32_t)n_rows;
+            bin_of_tile = (uint32_t)(i0 + tid);
+            first_of_tile = first;
+            t.adapter = i0 + tid;
+            t.count = (int)min(c - first, (uint32_t)n_rows);
+        }
+        before += all;
+    }
+    mw_lds_barrier();
+    if (t.adapter < 0) return;
+    const bool mine = b == (int)bin_of_tile;
+    const unsigned long long those = __ballot(mine);
+    if (lane == 0) in_wave[wave] = (uint32_t)__popcll(those);
+    mw_lds_barrier();
+    int rank = __popcll(those & ((1ull << lane) - 1)) - (int)first_of_tile;
+    for (int w = 0; w < wave; ++w) rank += (int)in_wave[w];
+    if (mine && rank >= 0 && rank < t.count) t.row[rank] = tid;
+    mw_lds_barrier();
+}
+
 // h: kM tiles of 16 ranks by kCols tiles of 16 rows.  grid: (tile, slice of n_in)
 template <int kM, int kCols>
 __global__ __launch_bounds__(kBlock) void k_adapt_down(adapt_args p)
@@ -183,14 +247,15 @@ __global__ __launch_bounds__(kBlock) void k_adapt_down(adapt_args p)
     constexpr int kRanks = kM * 16, kRows = kCols * 16, kDepth = kM == 1 ? 4 : kM == 2 ? 3 : 2;
     constexpr int kPartBytes = kWaves * kRows * kRanks * 4, kStageBytes = kWaves * kWaveLds<kM>;
     __shared__ __align__(16) char lds[kPartBytes > kStageBytes ? kPartBytes : kStageBytes];
-    if ((int)blockIdx.x >= *p.n_tiles) return;
-    const adapt_tile t = p.tiles[blockIdx.x];
-    if (t.adapter == p.n) return;
+    __shared__ tile_rows t;
+    find_tile(p, kRows, t);
+    const int adapter = __builtin_amdgcn_readfirstlane(t.adapter);
+    if (adapter < 0 || adapter == p.n) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4, l8 = lane >> 3;
     const int start = (int)blockIdx.y * p.slice;
     const uint32_t piece = (uint32_t)(lane & 7) * 16 + (uint32_t)start * 2;
     operands<false, kM, kCols, 2, 1> o;
-    o.w = array_at(p.a + (int64_t)t.adapter * p.rank * p.n_in);
+    o.w = array_at(p.a + (int64_t)adapter * p.rank * p.n_in);
     o.b[0] = array_at(p.x);
     o.limit = min(p.slice, p.n_in - start);
 #pragma unroll
@@ -198,7 +263,7 @@ __global__ __launch_bounds__(kBlock) void k_adapt_down(adapt_args p)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = c * 16 + i * 8 + l8;
-            o.col[c][0][i] = (uint32_t)((int64_t)p.order[t.first + (at < t.count ? at : 0)] * p.x_stride * 2) + piece;
+            o.col[c][0][i] = (uint32_t)((int64_t)t.row[at < t.count ? at : 0] * p.x_stride * 2) + piece;
         }
 #pragma unroll
     for (int m = 0; m < kM; ++m)
@@ -218,7 +283,7 @@ __global__ __launch_bounds__(kBlock) void k_adapt_down(adapt_args p)
         f32x4 v = {};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) v += *(const f32x4 *)&part[w * kRows * kRanks + i * 4];
-        *(f32x4 *)&p.part[((int64_t)blockIdx.y * p.T + t.first) * kRanks + i * 4] = v;
+        *(f32x4 *)&p.part[((int64_t)blockIdx.y * p.T + t.row[i / (kRanks / 4)]) * kRanks + i % (kRanks / 4) * 4] = v;
     }
 }
 
@@ -247,46 +312,26 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
     constexpr int kWorkBytes = 64 * (kRanks * 2 + 16) > kRows * kOutPitch * 4 ? 64 * (kRanks * 2 + 16) : kRows * kOutPitch * 4;
     __shared__ __align__(16) uint16_t h_hi[kRows * kStep], h_lo[kRows * kStep];
     __shared__ __align__(16) char work[kWaves][kWorkBytes];
-    if ((int)blockIdx.x >= *p.n_tiles) return;
-    const adapt_tile t = p.tiles[blockIdx.x];
+    __shared__ tile_rows t;
+    find_tile(p, kRows, t);
+    const int adapter = __builtin_amdgcn_readfirstlane(t.adapter);
+    if (adapter < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4, l8 = lane >> 3, q8 = (lane & 7) * 8;
     const int c_from = (int)blockIdx.y * p.out_slice, c_to = min(c_from + p.out_slice, p.n_out);
-    if (t.adapter == p.n) {                                 // rows without an adapter
+    if (adapter == p.n) {                                   // rows without an adapter
         const int pieces = (c_to - c_from) / 8;
         for (int i = tid; i < t.count * pieces; i += kBlock) {
-            const int64_t row = p.order[t.first + i / pieces];
+            const int64_t row = t.row[i / pieces];
             const int c = c_from + i % pieces * 8;
             const u32x4 zero = {};
             *(u32x4 *)(p.out + row * p.out_stride + c) = p.base ? *(const u32x4 *)(p.base + row * p.base_stride + c) : zero;
         }
         if (p.h && blockIdx.y == 0)
-            for (int i = tid; i < t.count * p.rank; i += kBlock) p.h[(int64_t)p.order[t.first + i / p.rank] * p.rank + i % p.rank] = 0.0f;
+            for (int i = tid; i < t.count * p.rank; i += kBlock) p.h[(int64_t)t.row[i / p.rank] * p.rank + i % p.rank] = 0.0f;
         return;
     }
-    const float scale = p.scale ? p.scale[t.adapter] : 1.0f;
-    if (p.kept_h && (int)blockIdx.y == (int)gridDim.y - 1) {
-        for (int i = tid; i < kRows * kRanks; i += kBlock) {
-            const int col = i / kRanks, r = i % kRanks;
-            const bool real = r < p.rank && col < t.count;
-            split(real ? scale * p.kept_h[(int64_t)p.order[t.first + col] * p.rank + r] : 0.0f, &h_hi[col * kStep + r], &h_lo[col * kStep + r]);
-        }
-        __syncthreads();
-        put_left<kRanks, kStep>(p.left_h, blockIdx.x, h_hi, h_lo);
-        __syncthreads();
-    }
-    for (int i = tid; i < kRows * kRanks; i += kBlock) {
-        const int col = i / kRanks, r = i % kRanks;
-        const bool real = r < p.rank && col < t.count;
-        float v = 0.0f;
-        if (real)
-            for (int s = 0; s < p.n_slices; ++s) v += p.part[((int64_t)s * p.T + t.first + col) * kRanks + r];
-        if (real && p.h && blockIdx.y == 0) p.h[(int64_t)p.order[t.first + col] * p.rank + r] = v;
-        split(v * scale, &h_hi[col * kStep + r], &h_lo[col * kStep + r]);
-    }
-    __syncthreads();
-    if (p.kept_h && blockIdx.y == 0) put_left<kRanks, kStep>(p.left_dh, blockIdx.x, h_hi, h_lo);
-
-    const array b = array_at(p.b + (int64_t)t.adapter * p.rank * p.n_out), base = array_at(p.base ? p.base : p.out), out = array_at(p.out);
+    const float scale = p.scale ? p.scale[adapter] : 1.0f;
+    const array b = array_at(p.b + (int64_t)adapter * p.rank * p.n_out), base = array_at(p.base ? p.base : p.out), out = array_at(p.out);
     char *mine = work[wave];
     const int pitch = p.rank * 2 + 16, n_loads = p.rank / 8;
     uint32_t to_lds[kLoads];                                // where a lane's pieces of B go in LDS
@@ -299,7 +344,7 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
 #pragma unroll
     for (int i = 0; i < 2 * kCols; ++i) {
         const bool live = i * 8 + l8 < t.count;
-        const int64_t row = p.order[t.first + (live ? i * 8 + l8 : 0)];
+        const int64_t row = t.row[live ? i * 8 + l8 : 0];
         base_at[i] = p.base ? (uint32_t)(row * p.base_stride * 2) : kNowhere;
         out_at[i] = live ? (uint32_t)(row * p.out_stride * 2) : kNowhere;
     }
@@ -314,6 +359,36 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
 #pragma unroll
         for (int i = 0; i < 2 * kCols; ++i) wq[i] = load16<true>(base, at | (c + q8 < c_to ? base_at[i] + (uint32_t)(c + q8) * 2 : kNowhere));
     };
+    load(c_from + wave * 64, bw[0], was[0]);               // (on their way while h is added up)
+    if (p.kept_h && (int)blockIdx.y == (int)gridDim.y - 1) {
+        for (int i = tid; i < kRows * kRanks; i += kBlock) {
+            const int col = i / kRanks, r = i % kRanks;
+            const bool real = r < p.rank && col < t.count;
+            split(real ? scale * p.kept_h[(int64_t)t.row[col] * p.rank + r] : 0.0f, &h_hi[col * kStep + r], &h_lo[col * kStep + r]);
+        }
+        mw_lds_barrier();
+        put_left<kRanks, kStep>(p.left_h, blockIdx.x, h_hi, h_lo);
+        mw_lds_barrier();
+    }
+    for (int i = tid * 4; i < kRows * kRanks; i += kBlock * 4) {
+        const int col = i / kRanks, r = i % kRanks;         // four ranks of a row
+        const bool real = r < p.rank && col < t.count;
+        f32x4 v = {};
+        if (real) {
+            const float *from = p.part + (int64_t)t.row[col] * kRanks + r;
+#pragma unroll 4
+            for (int k = 0; k < p.n_slices; ++k) v += *(const f32x4 *)(from + (int64_t)k * p.T * kRanks);
+            if (p.h && blockIdx.y == 0) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p.h[(int64_t)t.row[col] * p.rank + r + e] = v[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split(v[e] * scale, &h_hi[col * kStep + r + e], &h_lo[col * kStep + r + e]);
+    }
+    mw_lds_barrier();
+    if (p.kept_h && blockIdx.y == 0) put_left<kRanks, kStep>(p.left_dh, blockIdx.x, h_hi, h_lo);
+
     bf16x8 hv[kCols][(kRanks + 31) / 32], lv[kCols][(kRanks + 31) / 32];
     const bf16x8 none = {};
 #pragma unroll
@@ -324,7 +399,6 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
             hv[i][k / 32] = kk < kRanks ? *(const bf16x8 *)&h_hi[(i * 16 + n) * kStep + kk] : none;
             lv[i][k / 32] = kk < kRanks ? *(const bf16x8 *)&h_lo[(i * 16 + n) * kStep + kk] : none;
         }
-    load(c_from + wave * 64, bw[0], was[0]);
     for (int c0 = c_from + wave * 64; c0 < c_to; c0 += 2 * kWaves * 64) {
 #pragma unroll
         for (int d = 0; d < 2; ++d) {
@@ -394,7 +468,7 @@ struct grad_args {
 // grid: (128 columns, adapter, side and piece of 64 ranks).  The waves take an adapter's tiles of 32 rows in turn: a tile is one
 // matrix instruction deep.  Rows of x are loaded as they lie, 256 bytes of four rows an instruction, and turned in registers: a lane has eight
 // rows of eight columns, and the columns' vectors over the rows are operands.
-constexpr int kGradWaves = 8;
+constexpr int kGradWaves = 4;
 template <int kM>
 __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
 {
@@ -403,35 +477,45 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
     if (c0 >= width) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
     const int tile0 = p.tile_at[ad], tile1 = p.tile_at[ad + 1];
-    const uint16_t *right = p.right[side];
     const int64_t stride = p.stride[side];
     const int col = c0 + n * 8;
+    const array right = array_at(p.right[side]), hi_of = array_at(p.left[side][0]), lo_of = array_at(p.left[side][1]);
+    const uint32_t c_at = col < width ? (uint32_t)col * 2 : kNowhere;
     f32x4 acc[kM][8] = {};
-    for (int k = tile0 + wave; k < tile1; k += kGradWaves) {
-        const adapt_tile t = p.tiles[k];
-        u32x4 v[8];
-        bf16x8 hi[kM], lo[kM];
+    u32x4 v[2][8], hi[2][kM], lo[2][kM];
+    // A tile's rows, then what is loaded of them; past the last tile nothing.
+    auto load = [&](int k, u32x4 (&vq)[8], u32x4 (&hq)[kM], u32x4 (&lq)[kM]) {
+        const bool some = k < tile1;
+        const adapt_tile t = p.tiles[some ? k : tile1 - 1];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool live = g * 8 + j < t.count && col < width;
-            const int64_t row = p.order[t.first + (g * 8 + j < t.count ? g * 8 + j : 0)];
-            const u32x4 zero = {};
-            v[j] = live ? *(const u32x4 *)(right + row * stride + col) : zero;
+            const bool live = some && g * 8 + j < t.count && c_at != kNowhere;
+            const int64_t row = p.order[t.first + min(g * 8 + j, t.count - 1)];
+            vq[j] = load16<false>(right, live ? (uint32_t)(row * stride * 2) + c_at : kNowhere);
         }
 #pragma unroll
         for (int m = 0; m < kM; ++m) {
-            const int64_t at = ((int64_t)k * p.ranks + r0 + m * 16 + n) * 32 + g * 8;
-            hi[m] = *(const bf16x8 *)(p.left[side][0] + at);
-            lo[m] = *(const bf16x8 *)(p.left[side][1] + at);
+            const uint32_t at = some ? (uint32_t)((k * p.ranks + r0 + m * 16 + n) * 64 + g * 16) : kNowhere;
+            hq[m] = load16<false>(hi_of, at);
+            lq[m] = load16<false>(lo_of, at);
         }
-        transpose8(v);
+    };
+    if (tile0 < tile1) {
+        load(tile0 + wave, v[0], hi[0], lo[0]);
+        for (int k0 = tile0 + wave; k0 < tile1; k0 += 2 * kGradWaves) {
 #pragma unroll
-        for (int m = 0; m < kM; ++m)
+            for (int d = 0; d < 2; ++d) {
+                load(k0 + (d + 1) * kGradWaves, v[d ^ 1], hi[d ^ 1], lo[d ^ 1]);
+                transpose8(v[d]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                acc[m][j] = mma(lo[m], __builtin_bit_cast(bf16x8, v[j]), acc[m][j]);
-                acc[m][j] = mma(hi[m], __builtin_bit_cast(bf16x8, v[j]), acc[m][j]);
+                for (int m = 0; m < kM; ++m)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        acc[m][j] = mma(__builtin_bit_cast(bf16x8, lo[d][m]), __builtin_bit_cast(bf16x8, v[d][j]), acc[m][j]);
+                        acc[m][j] = mma(__builtin_bit_cast(bf16x8, hi[d][m]), __builtin_bit_cast(bf16x8, v[d][j]), acc[m][j]);
+                    }
             }
+        }
     }
 #pragma unroll
     for (int m = 0; m < kM; ++m) {
@@ -473,7 +557,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
 
 int ranks_of(int32_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 constexpr int kMostSlices = 16;
-constexpr int64_t kMostCus = 512;          // (slices times rows stay below rows + 96 times the CUs: a tile has at most 32 rows)
+constexpr int64_t kMostCus = 512;          // (rows times slices stay below rows + 128 times the CUs: a tile has at most 32 rows)
 
 // Rows of a tile: 32 where adapters have that many rows mostly, else 16.
 int tile_rows_of(const mw_adapters *s, int64_t rows, bool backward) { return backward || rows >= 24LL * s->n_adapters ? 32 : 16; }
@@ -488,7 +572,7 @@ adapt_ws adapt_layout(const mw_adapters *s, int64_t rows, bool backward)
     w.order = o;   o += mw_align_up(4 * rows, 256);
     w.tile_at = o; o += mw_align_up(4 * (s->n_adapters + 2LL), 256);
     w.tiles = o;   o += mw_align_up((int64_t)sizeof(adapt_tile) * tiles, 256);
-    w.part = o;    o += mw_align_up(4 * ranks * (rows * kMostSlices < rows + 96 * kMostCus ? rows * kMostSlices : rows + 96 * kMostCus), 256);
+    w.part = o;    o += mw_align_up(4 * ranks * (rows * kMostSlices < rows + 128 * kMostCus ? rows * kMostSlices : rows + 128 * kMostCus), 256);
     for (int i = 0; i < 4; ++i) { w.left[i] = o; o += backward ? mw_align_up(2 * most_tiles(s, rows, 32) * ranks * 32, 256) : 0; }
     w.at = o;      o += backward ? mw_align_up(2LL * s->n_adapters * s->rank * s->n_in, 256) : 0;
     w.bt = o;      o += backward ? mw_align_up(2LL * s->n_adapters * s->rank * s->n_out, 256) : 0;
@@ -514,32 +598,44 @@ order_args order_of(const mw_adapters *s, const int32_t *ids, int32_t T, char *w
     o.flags = flags;
     return o;
 }
+// Workgroups of the two kernels that a CU holds at once (by their LDS).
+struct resident { int down, up; };
+resident resident_of(int ranks, int tile_rows)
+{
+    const int m = ranks / 16, parts = kWaves * tile_rows * ranks * 4, stages = kWaves * (m + 1) * kTileBytes;
+    const int work = 64 * (ranks * 2 + 16) > tile_rows * 272 ? 64 * (ranks * 2 + 16) : tile_rows * 272;
+    const int down = (parts > stages ? parts : stages) + 8192, up = kWaves * work + tile_rows * (ranks + 8) * 4 + 8192;
+    const int most = 2048 / kBlock;
+    return resident{160 * 1024 / down < most ? 160 * 1024 / down : most, 160 * 1024 / up < most ? 160 * 1024 / up : most};
+}
 template <int kM, int kCols>
 void launch_both(const adapt_args &p, dim3 down, dim3 up, hipStream_t st)
 {
     hipLaunchKernelGGL((k_adapt_down<kM, kCols>), down, dim3(kBlock), 0, st, p);
     hipLaunchKernelGGL((k_adapt_up<kM, kCols>), up, dim3(kBlock), 0, st, p);
 }
-// h and y.  p.a to p.out, p.T, p.h are set; the order is that of `o`.
-int32_t launch_adapt(adapt_args p, const mw_adapters *s, const order_args &o, char *ws, const adapt_ws &w, int n_cu, hipStream_t st)
+// h and y.  p.a to p.out, p.T, p.h, and p.tiles or p.ids are set.
+int32_t launch_adapt(adapt_args p, const mw_adapters *s, int tile_rows, char *ws, const adapt_ws &w, int n_cu, hipStream_t st)
 {
-    p.order = o.order; p.tiles = o.tiles; p.n_tiles = o.tile_at + s->n_adapters + 1;
     p.scale = s->scale_dev; p.n = s->n_adapters; p.rank = s->rank;
     p.part = (float *)(ws + w.part);
-    const int64_t tiles = most_tiles(s, p.T, o.tile_rows);
-    // Slices that give every CU three workgroups, of whole spans; of at least 512 columns each.
-    int64_t n = (3LL * n_cu + tiles - 1) / tiles;
-    const int64_t most = (p.n_in + 511) / 512;
-    n = n < most ? n : most;
-    n = n < kMostSlices ? n : kMostSlices;
+    const int64_t tiles = most_tiles(s, p.T, tile_rows);
+    const resident res = resident_of(ranks_of(p.rank), tile_rows);
+    // As many slices as keep all workgroups resident at once: a few more would be a second round of their own.  Of at least 512 columns.
+    auto slices = [&](int64_t width, int64_t workgroups, int64_t least, int64_t most) {
+        int64_t n = workgroups / tiles;
+        const int64_t all = (width + least - 1) / least;
+        n = n < all ? n : all;
+        n = n < most ? n : most;
+        return n < 1 ? 1 : n;
+    };
+    const int64_t n = slices(p.n_in, (int64_t)(res.down < 4 ? res.down : 4) * n_cu, 512, kMostSlices);
     p.slice = (int32_t)mw_align_up((p.n_in + n - 1) / n, 64);
     p.n_slices = (p.n_in + p.slice - 1) / p.slice;
-    int64_t m = (4LL * n_cu + tiles - 1) / tiles;
-    const int64_t most_out = (p.n_out + 255) / 256;
-    m = m < most_out ? m : most_out;
-    p.out_slice = (int32_t)mw_align_up((p.n_out + m - 1) / m, 256);
+    const int64_t m = slices(p.n_out, (int64_t)res.up * n_cu, 256, 4096);
+    p.out_slice = (int32_t)mw_align_up((p.n_out + m - 1) / m, 64);
     const dim3 down((uint32_t)tiles, (uint32_t)p.n_slices), up((uint32_t)tiles, (uint32_t)((p.n_out + p.out_slice - 1) / p.out_slice));
-    const bool wide = o.tile_rows == 32;
+    const bool wide = tile_rows == 32;
     switch (ranks_of(p.rank)) {
     case 16: if (wide) launch_both<1, 2>(p, down, up, st); else launch_both<1, 1>(p, down, up, st); break;
     case 32: if (wide) launch_both<2, 2>(p, down, up, st); else launch_both<2, 1>(p, down, up, st); break;
@@ -595,16 +691,23 @@ extern "C" MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_de
     if (rd != MW_OK) return rd;
     const hipStream_t st = (hipStream_t)stream;
     char *ws = (char *)workspace_dev;
-    const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, tile_rows_of(adapters, n_rows, false), error_flags_dev);
-    hipLaunchKernelGGL(k_adapt_order, dim3(1), dim3(kOrderBlock), 0, st, o);
-    MW_HIP_CHECK(hipGetLastError());
     adapt_args p = {};
     p.a = (const uint16_t *)s.a_dev; p.b = (const uint16_t *)s.b_dev; p.T = n_rows; p.n_in = s.n_in; p.n_out = s.n_out;
     p.x = (const uint16_t *)x_dev; p.x_stride = x_stride;
     p.base = (const uint16_t *)base_dev; p.base_stride = base_stride;
     p.out = (uint16_t *)out_dev; p.out_stride = out_stride;
     p.h = h_dev;
-    return launch_adapt(p, adapters, o, ws, w, n_cu, st);
+    const int tile = tile_rows_of(adapters, n_rows, false);
+    if (n_rows <= kBlock) {                // every workgroup finds its tile in the ids: a launch less
+        p.ids = adapter_ids_dev;
+        p.flags = error_flags_dev;
+    } else {
+        const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, tile, error_flags_dev);
+        hipLaunchKernelGGL(k_adapt_order, dim3(1), dim3(kOrderBlock), 0, st, o);
+        MW_HIP_CHECK(hipGetLastError());
+        p.order = o.order; p.tiles = o.tiles; p.n_tiles = o.tile_at + s.n_adapters + 1;
+    }
+    return launch_adapt(p, adapters, tile, ws, w, n_cu, st);
 }
 
 extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const void *x_dev, int64_t x_stride, const int32_t *adapter_ids_dev,
@@ -629,7 +732,7 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
     const adapt_ws w = adapt_layout(adapters, n_rows, true);
     if (!workspace_dev || ((uintptr_t)workspace_dev & 255u) || workspace_bytes < w.total) return MW_ERR_WORKSPACE;
     const int64_t far = 1LL << 30;
-    if (dy_stride * n_rows > far || dx_stride * n_rows > far || (dx_base_dev && dx_base_stride * n_rows > far)) return MW_ERR_UNSUPPORTED;
+    if (x_stride * n_rows > far || dy_stride * n_rows > far || dx_stride * n_rows > far || (dx_base_dev && dx_base_stride * n_rows > far)) return MW_ERR_UNSUPPORTED;
     int n_cu = 0;
     const int32_t rd = cus_of_current_device(&n_cu);
     if (rd != MW_OK) return rd;
@@ -638,7 +741,7 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
     const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, 32, error_flags_dev);
     const transpose_args ta = {(const uint16_t *)s.a_dev, (uint16_t *)(ws + w.at), s.rank, s.n_in};
     const transpose_args tb = {(const uint16_t *)s.b_dev, (uint16_t *)(ws + w.bt), s.n_out, s.rank};
-    const int64_t r64 = (s.rank + 63) / 64, blocks = s.n_adapters * r64 * ((s.n_in + 63) / 64 + (s.n_out + 63) / 64);
+    const int64_t blocks = s.n_adapters * ((int64_t)((s.rank + 63) / 64) * ((s.n_in + 127) / 128) + (int64_t)((s.n_out + 63) / 64) * ((s.rank + 127) / 128));
     hipLaunchKernelGGL(k_adapt_prepare, dim3(n_rows > 0 ? (uint32_t)(1 + blocks) : 1u), dim3(kOrderBlock), 0, st, o, ta, tb);
     MW_HIP_CHECK(hipGetLastError());
     uint16_t *left[4];
@@ -650,8 +753,9 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
         p.base = (const uint16_t *)dx_base_dev; p.base_stride = dx_base_stride;
         p.out = (uint16_t *)dx_dev; p.out_stride = dx_stride;
         p.kept_h = h_dev;
+        p.order = o.order; p.tiles = o.tiles; p.n_tiles = o.tile_at + s.n_adapters + 1;
         for (int i = 0; i < 2; ++i) { p.left_dh[i] = left[i]; p.left_h[i] = left[2 + i]; }
-        const int32_t ra = launch_adapt(p, adapters, o, ws, w, n_cu, st);
+        const int32_t ra = launch_adapt(p, adapters, 32, ws, w, n_cu, st);
         if (ra != MW_OK) return ra;
     }
     grad_args q;
