@@ -48,11 +48,30 @@ __device__ __forceinline__ void make_order(const order_args &a)
             held[wave][i * 64 + lane] = (uint16_t)(id[i] < 0 || id[i] >= n ? n : id[i]);
         }
     };
+    // The place of every row of the piece from t0 among the wave's rows of its adapter; hist counts them.  (64 lanes' atomics to one place are
+    // one after the other for the whole workgroup: rows of few adapters took 13 us to count so, 8192 of them.)
+    int bits = 0;
+    while ((1 << bits) <= n) ++bits;
+    auto place = [&](int t, int b) {
+        const bool live = t < hi;
+        unsigned long long same = __ballot(live);              // the piece's rows of the same adapter
+        if (__ballot(live && b != __builtin_amdgcn_readfirstlane(b)) != 0)
+            for (int i = 0; i < bits; ++i) {
+                const unsigned long long set = __ballot((b >> i) & 1);
+                same &= (b >> i) & 1 ? set : ~set;
+            }
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        const uint32_t at = hist[wave][b] + (uint32_t)before;
+        __builtin_amdgcn_wave_barrier();
+        if (live && before == 0) hist[wave][b] += (uint32_t)__popcll(same);
+        __builtin_amdgcn_wave_barrier();
+        return at;
+    };
     for (int i = lane; i <= n; i += 64) hist[wave][i] = 0;
     for (int at = lo; at < hi; at += kHeld * 64) {
         hold(at);
 #pragma unroll 1
-        for (int t = at + lane; t < min(hi, at + kHeld * 64); t += 64) atomicAdd(&hist[wave][held[wave][t - at]], 1u);
+        for (int t0 = at; t0 < min(hi, at + kHeld * 64); t0 += 64) place(t0 + lane, held[wave][t0 - at + lane]);
     }
     if (a.flags && wrong) atomicOr(a.flags, MW_FLAG_BAD_ADAPTER);
     mw_lds_barrier();
@@ -102,28 +121,12 @@ __device__ __forceinline__ void make_order(const order_args &a)
         const int first = (int)row_at[at] + (i - (int)tile_at[at]) * a.tile_rows;
         a.tiles[i] = adapt_tile{at, first, min(a.tile_rows, (int)row_at[at + 1] - first), 0};
     }
-    int bits = 0;
-    while ((1 << bits) <= n) ++bits;
     for (int at = lo; at < hi; at += kHeld * 64) {
         if (hi - lo > kHeld * 64) hold(at);
 #pragma unroll 1
         for (int t0 = at; t0 < min(hi, at + kHeld * 64); t0 += 64) {
-            const int t = t0 + lane;
-            const bool live = t < hi;
-            const int b = held[wave][t - at];
-            unsigned long long same = __ballot(live);          // the piece's rows of the same adapter
-            if (__ballot(live && b != __builtin_amdgcn_readfirstlane(b)) != 0)
-                for (int i = 0; i < bits; ++i) {
-                    const unsigned long long set = __ballot((b >> i) & 1);
-                    same &= (b >> i) & 1 ? set : ~set;
-                }
-            if (live) {
-                const int before = __popcll(same & ((1ull << lane) - 1));
-                a.order[hist[wave][b] + (uint32_t)before] = t;
-                __builtin_amdgcn_wave_barrier();
-                if (before == 0) hist[wave][b] += (uint32_t)__popcll(same);
-                __builtin_amdgcn_wave_barrier();
-            }
+            const uint32_t to = place(t0 + lane, held[wave][t0 - at + lane]);
+            if (t0 + lane < hi) a.order[to] = t0 + lane;
         }
     }
 }
@@ -334,6 +337,7 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
     const array b = array_at(p.b + (int64_t)adapter * p.rank * p.n_out), base = array_at(p.base ? p.base : p.out), out = array_at(p.out);
     char *mine = work[wave];
     const int pitch = p.rank * 2 + 16, n_loads = p.rank / 8;
+    const uint32_t b_end = (uint32_t)p.n_out * (uint32_t)p.rank;
     uint32_t to_lds[kLoads];                                // where a lane's pieces of B go in LDS
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -354,7 +358,7 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {                  // (past the last row of B: nothing)
             const uint32_t e = (uint32_t)((i * 64 + lane) * 8);
-            bq[i] = load16<false>(b, at | (i < n_loads && c + (int)e / p.rank < p.n_out ? (uint32_t)(c * p.rank) * 2 + e * 2 : kNowhere));
+            bq[i] = load16<false>(b, at | (i < n_loads && (uint32_t)(c * p.rank) + e < b_end ? (uint32_t)(c * p.rank) * 2 + e * 2 : kNowhere));
         }
 #pragma unroll
         for (int i = 0; i < 2 * kCols; ++i) wq[i] = load16<true>(base, at | (c + q8 < c_to ? base_at[i] + (uint32_t)(c + q8) * 2 : kNowhere));
@@ -376,7 +380,7 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
         f32x4 v = {};
         if (real) {
             const float *from = p.part + (int64_t)t.row[col] * kRanks + r;
-#pragma unroll 4
+#pragma unroll 8
             for (int k = 0; k < p.n_slices; ++k) v += *(const f32x4 *)(from + (int64_t)k * p.T * kRanks);
             if (p.h && blockIdx.y == 0) {
 #pragma unroll
@@ -465,7 +469,7 @@ struct grad_args {
     uint16_t *out[2];
 };
 
-// grid: (128 columns, adapter, side and piece of 64 ranks).  The waves take an adapter's tiles of 32 rows in turn: a tile is one
+// grid: (128 columns, adapter, side and piece of 32 ranks).  The waves take an adapter's tiles of 32 rows in turn: a tile is one
 // matrix instruction deep.  Rows of x are loaded as they lie, 256 bytes of four rows an instruction, and turned in registers: a lane has eight
 // rows of eight columns, and the columns' vectors over the rows are operands.
 constexpr int kGradWaves = 4;
@@ -473,7 +477,7 @@ template <int kM>
 __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
 {
     __shared__ __align__(16) float part[kGradWaves * 8 * 256];
-    const int side = blockIdx.z & 1, r0 = (blockIdx.z >> 1) * 64, ad = blockIdx.y, c0 = blockIdx.x * 128, width = p.width[side];
+    const int side = blockIdx.z & 1, r0 = (blockIdx.z >> 1) * 32, ad = blockIdx.y, c0 = blockIdx.x * 128, width = p.width[side];
     if (c0 >= width) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
     const int tile0 = p.tile_at[ad], tile1 = p.tile_at[ad + 1];
@@ -483,29 +487,33 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
     const uint32_t c_at = col < width ? (uint32_t)col * 2 : kNowhere;
     f32x4 acc[kM][8] = {};
     u32x4 v[2][8], hi[2][kM], lo[2][kM];
-    // A tile's rows, then what is loaded of them; past the last tile nothing.
-    auto load = [&](int k, u32x4 (&vq)[8], u32x4 (&hq)[kM], u32x4 (&lq)[kM]) {
-        const bool some = k < tile1;
-        const adapt_tile t = p.tiles[some ? k : tile1 - 1];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool live = some && g * 8 + j < t.count && c_at != kNowhere;
-            const int64_t row = p.order[t.first + min(g * 8 + j, t.count - 1)];
-            vq[j] = load16<false>(right, live ? (uint32_t)(row * stride * 2) + c_at : kNowhere);
-        }
-#pragma unroll
-        for (int m = 0; m < kM; ++m) {
-            const uint32_t at = some ? (uint32_t)((k * p.ranks + r0 + m * 16 + n) * 64 + g * 16) : kNowhere;
-            hq[m] = load16<false>(hi_of, at);
-            lq[m] = load16<false>(lo_of, at);
-        }
-    };
     if (tile0 < tile1) {
-        load(tile0 + wave, v[0], hi[0], lo[0]);
+        const int first = p.tiles[tile0].first, end = p.tiles[tile1 - 1].first + p.tiles[tile1 - 1].count;     // the adapter's rows in the order
+        int row[2][8];
+        // A tile's rows, a step ahead of what is loaded of them; past the last tile nothing.
+        auto rows = [&](int k, int (&rq)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) rq[j] = p.order[min(first + (k - tile0) * 32 + g * 8 + j, end - 1)];
+        };
+        auto load = [&](int k, const int (&rq)[8], u32x4 (&vq)[8], u32x4 (&hq)[kM], u32x4 (&lq)[kM]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                vq[j] = load16<false>(right, first + (k - tile0) * 32 + g * 8 + j < end && c_at != kNowhere ? (uint32_t)((int64_t)rq[j] * stride * 2) + c_at : kNowhere);
+#pragma unroll
+            for (int m = 0; m < kM; ++m) {
+                const uint32_t at = k < tile1 ? (uint32_t)((k * p.ranks + r0 + m * 16 + n) * 64 + g * 16) : kNowhere;
+                hq[m] = load16<false>(hi_of, at);
+                lq[m] = load16<false>(lo_of, at);
+            }
+        };
+        rows(tile0 + wave, row[0]);
+        rows(tile0 + wave + kGradWaves, row[1]);
+        load(tile0 + wave, row[0], v[0], hi[0], lo[0]);
         for (int k0 = tile0 + wave; k0 < tile1; k0 += 2 * kGradWaves) {
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
-                load(k0 + (d + 1) * kGradWaves, v[d ^ 1], hi[d ^ 1], lo[d ^ 1]);
+                load(k0 + (d + 1) * kGradWaves, row[d ^ 1], v[d ^ 1], hi[d ^ 1], lo[d ^ 1]);
+                rows(k0 + (d + 2) * kGradWaves, row[d]);
                 transpose8(v[d]);
 #pragma unroll
                 for (int m = 0; m < kM; ++m)
@@ -764,10 +772,9 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
     q.right[0] = (const uint16_t *)x_dev; q.stride[0] = x_stride; q.width[0] = s.n_in; q.out[0] = (uint16_t *)da_dev;
     q.right[1] = (const uint16_t *)dy_dev; q.stride[1] = dy_stride; q.width[1] = s.n_out; q.out[1] = (uint16_t *)db_dev;
     const int32_t widest = s.n_in > s.n_out ? s.n_in : s.n_out;
-    const dim3 grid((uint32_t)((widest + 127) / 128), (uint32_t)s.n_adapters, (uint32_t)(2 * ((q.ranks + 63) / 64)));
+    const dim3 grid((uint32_t)((widest + 127) / 128), (uint32_t)s.n_adapters, (uint32_t)(2 * ((q.ranks + 31) / 32)));
     if (q.ranks == 16) hipLaunchKernelGGL((k_adapt_grads<1>), grid, dim3(kGradWaves * 64), 0, st, q);
-    else if (q.ranks == 32) hipLaunchKernelGGL((k_adapt_grads<2>), grid, dim3(kGradWaves * 64), 0, st, q);
-    else hipLaunchKernelGGL((k_adapt_grads<4>), grid, dim3(kGradWaves * 64), 0, st, q);
+    else hipLaunchKernelGGL((k_adapt_grads<2>), grid, dim3(kGradWaves * 64), 0, st, q);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }
