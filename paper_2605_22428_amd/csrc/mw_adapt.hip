@@ -18,7 +18,7 @@ struct adapt_tile { int32_t adapter, first, count, reserved0; };      // adapter
 
 struct order_args {
     const int32_t *ids;
-    int32_t T, n, tile_rows;
+    int32_t T, n, tile_rows, most_tiles;
     int32_t *order;                        // rows by (adapter, row)
     int32_t *tile_at;                      // [n + 2] first tile of an adapter, of the rows without one, and how many there are
     adapt_tile *tiles;
@@ -112,6 +112,7 @@ __device__ __forceinline__ void make_order(const order_args &a)
         a.tile_at[n + 1] = (int32_t)total;
     }
     mw_lds_barrier();
+    for (int i = (int)total + tid; i < a.most_tiles; i += kOrderBlock) a.tiles[i] = adapt_tile{-1, 0, 0, 0};
     for (int i = tid; i < (int)total; i += kOrderBlock) {      // the bin a tile is of: the last that starts at or before it
         int at = 0, end = n + 1;
         while (end - at > 1) {
@@ -161,7 +162,7 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, tra
 }
 
 struct adapt_args {
-    const int32_t *order, *n_tiles; const adapt_tile *tiles;      // null: made by every workgroup (at most kBlock rows)
+    const int32_t *order; const adapt_tile *tiles;      // null: every workgroup finds its tile in the ids (at most kBlock rows)
     const int32_t *ids; uint32_t *flags;
     const uint16_t *a, *b;                 // [n][rank][n_in], [n][n_out][rank]
     const float *scale;                    // [n] or null
@@ -188,23 +189,21 @@ __device__ __forceinline__ void split(float v, uint16_t *hi, uint16_t *lo)
 
 constexpr int kWaves = 4, kBlock = kWaves * 64;
 
-// This workgroup's tile: its adapter (-1: there is no such tile) and its rows.
-struct tile_rows { int32_t adapter, count; int32_t row[32]; };
+// This workgroup's tile: its adapter (-1: there is no such tile) and its rows; part: place of the first one's h, where they lie in order.
+struct tile_rows { int32_t adapter, count, part; int32_t row[32]; };
 __device__ __forceinline__ void find_tile(const adapt_args &p, int n_rows, tile_rows &t)
 {
-    const int tid = threadIdx.x, index = (int)blockIdx.x;
+    const int tid = threadIdx.x, index = (int)blockIdx.x, step = (int)blockDim.x;
     if (p.tiles) {
-        const bool some = index < *p.n_tiles;
-        adapt_tile a = {-1, 0, 0, 0};
-        if (some) a = p.tiles[index];
+        const adapt_tile a = p.tiles[index];
         if (tid < a.count) t.row[tid] = p.order[a.first + tid];
-        if (tid == 0) { t.adapter = a.adapter; t.count = a.count; }
+        if (tid == 0) { t.adapter = a.adapter; t.count = a.count; t.part = a.first; }
         mw_lds_barrier();
         return;
     }
     // Few rows, one a thread: bins counted, the bin that the index-th tile is of, and of its rows those of the tile, in order.
     __shared__ uint32_t hist[kBins], scratch[17];
-    __shared__ uint32_t bin_of_tile, first_of_tile, in_wave[kWaves];
+    __shared__ uint32_t bin_of_tile, first_of_tile, in_wave[16];
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = p.n;
     int b = -1;
     if (tid < p.T) {
@@ -212,13 +211,13 @@ __device__ __forceinline__ void find_tile(const adapt_args &p, int n_rows, tile_
         b = id < 0 || id >= n ? n : id;
         if (p.flags && (id < -1 || id >= n) && index == 0 && blockIdx.y == 0) atomicOr(p.flags, MW_FLAG_BAD_ADAPTER);
     }
-    for (int i = tid; i <= n; i += kBlock) hist[i] = 0;
-    if (tid == 0) { t.adapter = -1; t.count = 0; }
+    for (int i = tid; i <= n; i += step) hist[i] = 0;
+    if (tid == 0) { t.adapter = -1; t.count = 0; t.part = -1; }
     mw_lds_barrier();
     if (b >= 0) atomicAdd(&hist[b], 1u);
     mw_lds_barrier();
     uint32_t before = 0;
-    for (int i0 = 0; i0 <= n; i0 += kBlock) {
+    for (int i0 = 0; i0 <= n; i0 += step) {
         const uint32_t c = i0 + tid <= n ? hist[i0 + tid] : 0u, k = (c + (uint32_t)n_rows - 1) / (uint32_t)n_rows;
         uint32_t all;
         const uint32_t at = before + mw_block_exscan(k, scratch, &all);
@@ -243,11 +242,18 @@ __device__ __forceinline__ void find_tile(const adapt_args &p, int n_rows, tile_
     mw_lds_barrier();
 }
 
-// h: kM tiles of 16 ranks by kCols tiles of 16 rows.  grid: (tile, slice of n_in)
-template <int kM, int kCols>
-__global__ __launch_bounds__(kBlock) void k_adapt_down(adapt_args p)
+// Place of a row's h in the parts: rows of tiles that were found in the ids are where they are.
+__device__ __forceinline__ int64_t part_of(const tile_rows &t, int col) { return t.part >= 0 ? t.part + col : t.row[col]; }
+
+// h: kM tiles of 16 ranks by kCols tiles of 16 rows.  grid: (tile, slice of n_in).  Few tiles are cut into slices of four waves; where the
+// tiles alone fill the card as many waves share a tile's columns out as their pieces of LDS leave room for, and there is one
+// slice, or nearly.  (64 rows of 24 adapters, rank 16: 5.9 us with slices of four waves, 7.8 with 4 of sixteen.)
+template <int kM> constexpr int kManyWaves = kM <= 2 ? 16 : kM == 4 ? 8 : 4;
+template <int kM, int kCols, int kWaves>
+__global__ __launch_bounds__(kWaves * 64) void k_adapt_down(adapt_args p)
 {
-    constexpr int kRanks = kM * 16, kRows = kCols * 16, kDepth = kM == 1 ? 4 : kM == 2 ? 3 : 2;
+    constexpr int kBlock = kWaves * 64;
+    constexpr int kRanks = kM * 16, kRows = kCols * 16, kDepth = kM == 1 || kWaves == 4 && kM == 2 ? 3 : 2;
     constexpr int kPartBytes = kWaves * kRows * kRanks * 4, kStageBytes = kWaves * kWaveLds<kM>;
     __shared__ __align__(16) char lds[kPartBytes > kStageBytes ? kPartBytes : kStageBytes];
     __shared__ tile_rows t;
@@ -286,68 +292,69 @@ __global__ __launch_bounds__(kBlock) void k_adapt_down(adapt_args p)
         f32x4 v = {};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) v += *(const f32x4 *)&part[w * kRows * kRanks + i * 4];
-        *(f32x4 *)&p.part[((int64_t)blockIdx.y * p.T + t.row[i / (kRanks / 4)]) * kRanks + i % (kRanks / 4) * 4] = v;
+        *(f32x4 *)&p.part[((int64_t)blockIdx.y * p.T + part_of(t, i / (kRanks / 4))) * kRanks + i % (kRanks / 4) * 4] = v;
     }
 }
 
-// Writes a tile's rows-by-ranks values from LDS as ranks by 32 rows.
-template <int kRanks, int kStep>
-__device__ __forceinline__ void put_left(uint16_t *const (&to)[2], int64_t tile, const uint16_t *hi, const uint16_t *lo)
+// Eight ranks of a row of h as operands: the sum of the slices' parts, or what a forward pass kept, times the adapter's factor.
+__device__ __forceinline__ void operand_of(const float (&v)[8], float scale, bf16x8 *hi, bf16x8 *lo)
 {
-    for (int i = threadIdx.x; i < kRanks * 4 * 2; i += kBlock) {
-        const uint16_t *from = i & 1 ? lo : hi;
-        const int r = i >> 3, q = (i >> 1 & 3) * 8;
-        uint32_t v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = from[(q + 2 * j) * kStep + r] | (uint32_t)from[(q + 2 * j + 1) * kStep + r] << 16;
-        *(u32x4 *)(to[i & 1] + (tile * kRanks + r) * 32 + q) = u32x4{v[0], v[1], v[2], v[3]};
+    for (int e = 0; e < 8; ++e) {
+        uint16_t a, b;
+        split(v[e] * scale, &a, &b);
+        (*hi)[e] = __builtin_bit_cast(__bf16, a);
+        (*lo)[e] = __builtin_bit_cast(__bf16, b);
     }
 }
 
-// y: a wave takes 64 columns of the output at a time, as four tiles of rows of B; h is the other side.  What comes out goes through LDS
-// so that base and y are read and written in whole cache lines.  grid: (tile, slice of n_out)
+// y: a wave takes 64 columns of the output at a time, as four tiles of rows of B; h is the other side, in registers.  What comes out goes
+// through LDS so that base and y are read and written in whole cache lines.  grid: (tile, slice of n_out)
 template <int kM, int kCols>
 __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
 {
-    constexpr int kRanks = kM * 16, kRows = kCols * 16, kStep = kRanks + 8;      // (rows of h in LDS start on different banks)
+    constexpr int kRanks = kM * 16, kRows = kCols * 16, kSteps = (kRanks + 31) / 32;
     constexpr int kLoads = 2 * kM;                          // 16-byte pieces a lane has of 64 rows of B, at most
     constexpr int kOutPitch = 68;                           // floats from row to row of the result in LDS
     constexpr int kWorkBytes = 64 * (kRanks * 2 + 16) > kRows * kOutPitch * 4 ? 64 * (kRanks * 2 + 16) : kRows * kOutPitch * 4;
-    __shared__ __align__(16) uint16_t h_hi[kRows * kStep], h_lo[kRows * kStep];
     __shared__ __align__(16) char work[kWaves][kWorkBytes];
     __shared__ tile_rows t;
     find_tile(p, kRows, t);
-    const int adapter = __builtin_amdgcn_readfirstlane(t.adapter);
+    const int adapter = __builtin_amdgcn_readfirstlane(t.adapter), count = __builtin_amdgcn_readfirstlane(t.count);
     if (adapter < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4, l8 = lane >> 3, q8 = (lane & 7) * 8;
     const int c_from = (int)blockIdx.y * p.out_slice, c_to = min(c_from + p.out_slice, p.n_out);
     if (adapter == p.n) {                                   // rows without an adapter
-        const int pieces = (c_to - c_from) / 8;
-        for (int i = tid; i < t.count * pieces; i += kBlock) {
-            const int64_t row = t.row[i / pieces];
-            const int c = c_from + i % pieces * 8;
-            const u32x4 zero = {};
-            *(u32x4 *)(p.out + row * p.out_stride + c) = p.base ? *(const u32x4 *)(p.base + row * p.base_stride + c) : zero;
+        // A wave two rows, four pieces of each a lane on the way at a time.
+        for (int r = wave * 2; r < count; r += kWaves * 2) {
+            const int64_t row[2] = {__builtin_amdgcn_readfirstlane(t.row[r]), __builtin_amdgcn_readfirstlane(t.row[min(r + 1, count - 1)])};
+            for (int c0 = c_from + lane * 8; c0 < c_to; c0 += 4 * 512) {
+                u32x4 v[2][4] = {};
+                if (p.base) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[i][j] = mw_ld16((const u32x4 *)(p.base + row[i] * p.base_stride + min(c0 + j * 512, c_to - 8)));
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (c0 + j * 512 < c_to && r + i < count) *(u32x4 *)(p.out + row[i] * p.out_stride + c0 + j * 512) = v[i][j];
+            }
         }
         if (p.h && blockIdx.y == 0)
-            for (int i = tid; i < t.count * p.rank; i += kBlock) p.h[(int64_t)t.row[i / p.rank] * p.rank + i % p.rank] = 0.0f;
+            for (int i = tid; i < count * p.rank; i += kBlock) p.h[(int64_t)t.row[i / p.rank] * p.rank + i % p.rank] = 0.0f;
         return;
     }
-    const float scale = p.scale ? p.scale[adapter] : 1.0f;
     const array b = array_at(p.b + (int64_t)adapter * p.rank * p.n_out), base = array_at(p.base ? p.base : p.out), out = array_at(p.out);
     char *mine = work[wave];
     const int pitch = p.rank * 2 + 16, n_loads = p.rank / 8;
     const uint32_t b_end = (uint32_t)p.n_out * (uint32_t)p.rank;
-    uint32_t to_lds[kLoads];                                // where a lane's pieces of B go in LDS
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int e = (i * 64 + lane) * 8;
-        to_lds[i] = (uint32_t)(e / p.rank * pitch + e % p.rank * 2);
-    }
     uint32_t base_at[2 * kCols], out_at[2 * kCols];         // a lane's rows
 #pragma unroll
     for (int i = 0; i < 2 * kCols; ++i) {
-        const bool live = i * 8 + l8 < t.count;
+        const bool live = i * 8 + l8 < count;
         const int64_t row = t.row[live ? i * 8 + l8 : 0];
         base_at[i] = p.base ? (uint32_t)(row * p.base_stride * 2) : kNowhere;
         out_at[i] = live ? (uint32_t)(row * p.out_stride * 2) : kNowhere;
@@ -364,45 +371,81 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
         for (int i = 0; i < 2 * kCols; ++i) wq[i] = load16<true>(base, at | (c + q8 < c_to ? base_at[i] + (uint32_t)(c + q8) * 2 : kNowhere));
     };
     load(c_from + wave * 64, bw[0], was[0]);               // (on their way while h is added up)
-    if (p.kept_h && (int)blockIdx.y == (int)gridDim.y - 1) {
-        for (int i = tid; i < kRows * kRanks; i += kBlock) {
-            const int col = i / kRanks, r = i % kRanks;
-            const bool real = r < p.rank && col < t.count;
-            split(real ? scale * p.kept_h[(int64_t)t.row[col] * p.rank + r] : 0.0f, &h_hi[col * kStep + r], &h_lo[col * kStep + r]);
-        }
-        mw_lds_barrier();
-        put_left<kRanks, kStep>(p.left_h, blockIdx.x, h_hi, h_lo);
-        mw_lds_barrier();
-    }
-    for (int i = tid * 4; i < kRows * kRanks; i += kBlock * 4) {
-        const int col = i / kRanks, r = i % kRanks;         // four ranks of a row
-        const bool real = r < p.rank && col < t.count;
-        f32x4 v = {};
-        if (real) {
-            const float *from = p.part + (int64_t)t.row[col] * kRanks + r;
-#pragma unroll 8
-            for (int k = 0; k < p.n_slices; ++k) v += *(const f32x4 *)(from + (int64_t)k * p.T * kRanks);
-            if (p.h && blockIdx.y == 0) {
+    // h of the lane's rows: eight ranks a step.  Past the last rank or row: zeros, from past the parts' end.
+    const float scale = p.scale ? p.scale[adapter] : 1.0f;
+    const array parts = array_at(p.part);
+    bf16x8 hv[kCols][kSteps], lv[kCols][kSteps];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p.h[(int64_t)t.row[col] * p.rank + r + e] = v[e];
+    for (int i = 0; i < kCols; ++i) {
+        const int col = i * 16 + n;
+        const int64_t at = part_of(t, col < count ? col : 0);
+        float v[kSteps][8] = {};
+#pragma unroll 4
+        for (int s = 0; s < p.n_slices; ++s)
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                const int r = k * 32 + g * 8;
+                const uint32_t from = col < count && r < p.rank ? (uint32_t)((((int64_t)s * p.T + at) * kRanks + r) * 4) : kNowhere;
+                const f32x4 v0 = __builtin_bit_cast(f32x4, load16<false>(parts, from)), v1 = __builtin_bit_cast(f32x4, load16<false>(parts, from + 16));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { v[k][e] += v0[e]; v[k][4 + e] += v1[e]; }
+            }
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const int r = k * 32 + g * 8;
+            operand_of(v[k], scale, &hv[i][k], &lv[i][k]);
+            if (p.h && blockIdx.y == 0 && wave == 0 && col < count && r < p.rank) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p.h[(int64_t)t.row[col] * p.rank + r + e] = v[k][e];
             }
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split(v[e] * scale, &h_hi[col * kStep + r + e], &h_lo[col * kStep + r + e]);
     }
-    mw_lds_barrier();
-    if (p.kept_h && blockIdx.y == 0) put_left<kRanks, kStep>(p.left_dh, blockIdx.x, h_hi, h_lo);
-
-    bf16x8 hv[kCols][(kRanks + 31) / 32], lv[kCols][(kRanks + 31) / 32];
-    const bf16x8 none = {};
+    if constexpr (kCols == 2) {
+        // What k_adapt_grads needs of the tile: h and dh as [rank][32 rows], by the first and the last slice's workgroup.
+        uint16_t *left = (uint16_t *)work;                  // [term][row][rank]
+        constexpr int kStep = kRanks + 8;                   // (rows start on different banks)
+        for (int side = 0; side < 2; ++side) {
+            if (!p.kept_h || (int)blockIdx.y != (side == 0 ? 0 : (int)gridDim.y - 1)) continue;
+            if (wave == 0) {
 #pragma unroll
-    for (int i = 0; i < kCols; ++i)
+                for (int i = 0; i < kCols; ++i)
 #pragma unroll
-        for (int k = 0; k < kRanks; k += 32) {
-            const int kk = k + g * 8;
-            hv[i][k / 32] = kk < kRanks ? *(const bf16x8 *)&h_hi[(i * 16 + n) * kStep + kk] : none;
-            lv[i][k / 32] = kk < kRanks ? *(const bf16x8 *)&h_lo[(i * 16 + n) * kStep + kk] : none;
+                    for (int k = 0; k < kSteps; ++k) {
+                        const int r = k * 32 + g * 8, col = i * 16 + n;
+                        bf16x8 hi = hv[i][k], lo = lv[i][k];
+                        if (side == 1) {
+                            float v[8] = {};
+                            if (col < count && r < p.rank) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] = p.kept_h[(int64_t)t.row[col] * p.rank + r + e];
+                            }
+                            operand_of(v, scale, &hi, &lo);
+                        }
+                        if (r < kRanks) {
+                            *(bf16x8 *)&left[col * kStep + r] = hi;
+                            *(bf16x8 *)&left[(kRows + col) * kStep + r] = lo;
+                        }
+                    }
+            }
+            mw_lds_barrier();
+            for (int i = tid; i < kRanks * 4 * 2; i += kBlock) {
+                const uint16_t *from = left + (i & 1) * kRows * kStep;
+                const int r = i >> 3, q = (i >> 1 & 3) * 8;
+                uint32_t v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = from[(q + 2 * j) * kStep + r] | (uint32_t)from[(q + 2 * j + 1) * kStep + r] << 16;
+                *(u32x4 *)((side == 0 ? p.left_dh : p.left_h)[i & 1] + ((int64_t)blockIdx.x * kRanks + r) * 32 + q) = u32x4{v[0], v[1], v[2], v[3]};
+            }
+            mw_lds_barrier();
         }
+    }
+    uint32_t to_lds[kLoads];                                // where a lane's pieces of B go in LDS
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const int e = (i * 64 + lane) * 8;
+        to_lds[i] = (uint32_t)(e / p.rank * pitch + e % p.rank * 2);
+    }
+    const bf16x8 none = {};
     for (int c0 = c_from + wave * 64; c0 < c_to; c0 += 2 * kWaves * 64) {
 #pragma unroll
         for (int d = 0; d < 2; ++d) {
@@ -414,15 +457,15 @@ __global__ __launch_bounds__(kBlock) void k_adapt_up(adapt_args p)
             wave_order();
             f32x4 acc[4][kCols] = {};
 #pragma unroll
-            for (int k = 0; k < kRanks; k += 32) {
-                const int kk = k + g * 8;
+            for (int k = 0; k < kSteps; ++k) {
+                const int kk = k * 32 + g * 8;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const bf16x8 bv = kk < p.rank ? *(const bf16x8 *)(mine + (q * 16 + n) * pitch + kk * 2) : none;
 #pragma unroll
                     for (int i = 0; i < kCols; ++i) {
-                        acc[q][i] = mma(bv, lv[i][k / 32], acc[q][i]);
-                        acc[q][i] = mma(bv, hv[i][k / 32], acc[q][i]);
+                        acc[q][i] = mma(bv, lv[i][k], acc[q][i]);
+                        acc[q][i] = mma(bv, hv[i][k], acc[q][i]);
                     }
                 }
             }
@@ -564,7 +607,7 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
 }
 
 int ranks_of(int32_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
-constexpr int kMostSlices = 16;
+constexpr int kMostSlices = 8;
 constexpr int64_t kMostCus = 512;          // (rows times slices stay below rows + 128 times the CUs: a tile has at most 32 rows)
 
 // Rows of a tile: 32 where adapters have that many rows mostly, else 16.
@@ -601,25 +644,23 @@ bool rows_ready(const void *p, int64_t stride, int32_t width) { return p && ((ui
 order_args order_of(const mw_adapters *s, const int32_t *ids, int32_t T, char *ws, const adapt_ws &w, int tile_rows, uint32_t *flags)
 {
     order_args o;
-    o.ids = ids; o.T = T; o.n = s->n_adapters; o.tile_rows = tile_rows;
+    o.ids = ids; o.T = T; o.n = s->n_adapters; o.tile_rows = tile_rows; o.most_tiles = (int32_t)most_tiles(s, T, tile_rows);
     o.order = (int32_t *)(ws + w.order); o.tile_at = (int32_t *)(ws + w.tile_at); o.tiles = (adapt_tile *)(ws + w.tiles);
     o.flags = flags;
     return o;
 }
-// Workgroups of the two kernels that a CU holds at once (by their LDS).
-struct resident { int down, up; };
-resident resident_of(int ranks, int tile_rows)
+// Workgroups of k_adapt_up that a CU holds at once (by their LDS).
+int resident_up(int ranks, int tile_rows)
 {
-    const int m = ranks / 16, parts = kWaves * tile_rows * ranks * 4, stages = kWaves * (m + 1) * kTileBytes;
     const int work = 64 * (ranks * 2 + 16) > tile_rows * 272 ? 64 * (ranks * 2 + 16) : tile_rows * 272;
-    const int down = (parts > stages ? parts : stages) + 8192, up = kWaves * work + tile_rows * (ranks + 8) * 4 + 8192;
-    const int most = 2048 / kBlock;
-    return resident{160 * 1024 / down < most ? 160 * 1024 / down : most, 160 * 1024 / up < most ? 160 * 1024 / up : most};
+    const int up = 160 * 1024 / (kWaves * work + 5120);
+    return up < 1 ? 1 : up < 8 ? up : 8;
 }
 template <int kM, int kCols>
-void launch_both(const adapt_args &p, dim3 down, dim3 up, hipStream_t st)
+void launch_both(const adapt_args &p, bool few, dim3 down, dim3 up, hipStream_t st)
 {
-    hipLaunchKernelGGL((k_adapt_down<kM, kCols>), down, dim3(kBlock), 0, st, p);
+    if (few) hipLaunchKernelGGL((k_adapt_down<kM, kCols, 4>), down, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((k_adapt_down<kM, kCols, kManyWaves<kM>>), down, dim3(kManyWaves<kM> * 64), 0, st, p);
     hipLaunchKernelGGL((k_adapt_up<kM, kCols>), up, dim3(kBlock), 0, st, p);
 }
 // h and y.  p.a to p.out, p.T, p.h, and p.tiles or p.ids are set.
@@ -628,8 +669,7 @@ int32_t launch_adapt(adapt_args p, const mw_adapters *s, int tile_rows, char *ws
     p.scale = s->scale_dev; p.n = s->n_adapters; p.rank = s->rank;
     p.part = (float *)(ws + w.part);
     const int64_t tiles = most_tiles(s, p.T, tile_rows);
-    const resident res = resident_of(ranks_of(p.rank), tile_rows);
-    // As many slices as keep all workgroups resident at once: a few more would be a second round of their own.  Of at least 512 columns.
+    // As many slices as keep all workgroups resident at once (a few more would be a second round of their own).
     auto slices = [&](int64_t width, int64_t workgroups, int64_t least, int64_t most) {
         int64_t n = workgroups / tiles;
         const int64_t all = (width + least - 1) / least;
@@ -637,18 +677,20 @@ int32_t launch_adapt(adapt_args p, const mw_adapters *s, int tile_rows, char *ws
         n = n < most ? n : most;
         return n < 1 ? 1 : n;
     };
-    const int64_t n = slices(p.n_in, (int64_t)(res.down < 4 ? res.down : 4) * n_cu, 512, kMostSlices);
+    const int ranks = ranks_of(p.rank);
+    const bool few = tiles < n_cu / 2;
+    const int64_t n = few ? slices(p.n_in, 3LL * n_cu, 1024, kMostSlices) : slices(p.n_in, n_cu, 2048, kMostSlices);      // (a wave has two spans at least)
     p.slice = (int32_t)mw_align_up((p.n_in + n - 1) / n, 64);
     p.n_slices = (p.n_in + p.slice - 1) / p.slice;
-    const int64_t m = slices(p.n_out, (int64_t)res.up * n_cu, 256, 4096);
+    const int64_t m = slices(p.n_out, (int64_t)resident_up(ranks, tile_rows) * n_cu, 256, 4096);
     p.out_slice = (int32_t)mw_align_up((p.n_out + m - 1) / m, 64);
     const dim3 down((uint32_t)tiles, (uint32_t)p.n_slices), up((uint32_t)tiles, (uint32_t)((p.n_out + p.out_slice - 1) / p.out_slice));
     const bool wide = tile_rows == 32;
     switch (ranks_of(p.rank)) {
-    case 16: if (wide) launch_both<1, 2>(p, down, up, st); else launch_both<1, 1>(p, down, up, st); break;
-    case 32: if (wide) launch_both<2, 2>(p, down, up, st); else launch_both<2, 1>(p, down, up, st); break;
-    case 64: if (wide) launch_both<4, 2>(p, down, up, st); else launch_both<4, 1>(p, down, up, st); break;
-    default: if (wide) launch_both<8, 2>(p, down, up, st); else launch_both<8, 1>(p, down, up, st); break;
+    case 16: if (wide) launch_both<1, 2>(p, few, down, up, st); else launch_both<1, 1>(p, few, down, up, st); break;
+    case 32: if (wide) launch_both<2, 2>(p, few, down, up, st); else launch_both<2, 1>(p, few, down, up, st); break;
+    case 64: if (wide) launch_both<4, 2>(p, few, down, up, st); else launch_both<4, 1>(p, few, down, up, st); break;
+    default: if (wide) launch_both<8, 2>(p, few, down, up, st); else launch_both<8, 1>(p, few, down, up, st); break;
     }
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
@@ -713,7 +755,7 @@ extern "C" MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_de
         const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, tile, error_flags_dev);
         hipLaunchKernelGGL(k_adapt_order, dim3(1), dim3(kOrderBlock), 0, st, o);
         MW_HIP_CHECK(hipGetLastError());
-        p.order = o.order; p.tiles = o.tiles; p.n_tiles = o.tile_at + s.n_adapters + 1;
+        p.order = o.order; p.tiles = o.tiles;
     }
     return launch_adapt(p, adapters, tile, ws, w, n_cu, st);
 }
@@ -761,7 +803,7 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
         p.base = (const uint16_t *)dx_base_dev; p.base_stride = dx_base_stride;
         p.out = (uint16_t *)dx_dev; p.out_stride = dx_stride;
         p.kept_h = h_dev;
-        p.order = o.order; p.tiles = o.tiles; p.n_tiles = o.tile_at + s.n_adapters + 1;
+        p.order = o.order; p.tiles = o.tiles;
         for (int i = 0; i < 2; ++i) { p.left_dh[i] = left[i]; p.left_h[i] = left[2 + i]; }
         const int32_t ra = launch_adapt(p, adapters, 32, ws, w, n_cu, st);
         if (ra != MW_OK) return ra;
