@@ -1,0 +1,105 @@
+"""A rank's mixture-of-experts block around the dispatch.
+
+decode():   a few tokens of several requests, with each request's adapter on a shared projection and the rank's experts in place (no dispatch)
+prefill():  the same gate in front of a dispatch: its ids go straight into the plan
+training(): one step of the adapters and the gate's scores
+
+Run on one GPU: python examples/moe_block.py
+"""
+import os
+import sys
+
+import numpy as np
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2605_22428_amd import binding as B  # noqa: E402
+
+
+class Block:
+    """The weights of one block on rank `rank` of `n_ranks`, random; the buffers that its calls keep using."""
+
+    def __init__(self, n_ranks=8, rank=0, n_experts=64, top_k=8, hidden=4096, inter=1024, adapter_rank=16, n_adapters=12, max_tokens=256, seed=1,
+                 device="cuda:0"):
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+
+        def normal(*shape):
+            return torch.randn(shape, generator=g, device=device, dtype=torch.bfloat16) * shape[-1] ** -0.5
+
+        place = (np.arange(n_experts) * n_ranks // n_experts).astype(np.int32)
+        n_local = int((place == rank).sum())
+        self.ctx = B.Context(n_ranks, n_experts, top_k, rank, hidden, B.MW_ROW_BF16, max_tokens, 0, place, device=device)
+        self.gate = B.Gate(B.MW_GATE_SIGMOID_TOPK, n_groups=n_ranks, kept_groups=max(1, n_ranks // 2), scale=2.5)
+        self.gate_weight, self.gate_bias = normal(n_experts, hidden), torch.zeros(n_experts, device=device)
+        self.experts = B.Experts(normal(n_local, 2, inter, hidden), normal(n_local, hidden, inter))
+        self.projection = normal(hidden, hidden)
+        self.adapters = B.Adapters(normal(n_adapters, adapter_rank, hidden), normal(n_adapters, hidden, adapter_rank),
+                                   torch.full((n_adapters,), 2.0, device=device))
+        self.layer_workspace = self.ctx.moe_workspace(self.experts, max_tokens)
+        self.adapter_workspace = self.adapters.workspace(max_tokens)
+        self.top_k, self.hidden, self.device = top_k, hidden, device
+
+    def project(self, x, adapter_ids, keep_h=False):
+        """The shared projection and every row's own adapter beside it; in place on the projection's output."""
+        y = x @ self.projection.t()
+        h = torch.empty((x.shape[0], self.adapters.rank), device=self.device) if keep_h else None
+        self.adapters.mw_adapt(x, adapter_ids, y, y, self.adapter_workspace, h)
+        return (y, h) if keep_h else y
+
+    def route(self, x):
+        scores = x.float() @ self.gate_weight.float().t()
+        ids = torch.empty((x.shape[0], self.top_k), dtype=torch.int32, device=self.device)
+        weights = torch.empty((x.shape[0], self.top_k), device=self.device)
+        return scores, ids, weights
+
+    def decode(self, x, adapter_ids):
+        """(output of this rank's experts, ids, weights); ranks add their outputs up (an all-reduce, where there are several)."""
+        y = self.project(x, adapter_ids)
+        scores, ids, weights = self.route(y)
+        out = torch.empty_like(y)
+        self.ctx.mw_moe_layer(self.gate, scores, self.gate_bias, self.experts, y, ids, weights, out, self.layer_workspace)
+        return out, ids, weights
+
+    def prefill(self, x, adapter_ids):
+        """The send side of a dispatch: projection, gate, plan and pack.  Returns the packed rows and the statistics."""
+        y = self.project(x, adapter_ids)
+        scores, ids, weights = self.route(y)
+        send = B.SendBuffers(self.ctx, x.shape[0])
+        self.ctx.mw_route(self.gate, scores, self.gate_bias, ids, weights)
+        self.ctx.mw_plan(ids, send.mask, send.perm, send.desc, send.stats)
+        self.ctx.mw_pack(y, None, ids, send.perm, send.stats, send.packed, send.row_src_token, send.row_topk)
+        return send, self.ctx.mw_get_send_stats(send.stats)
+
+    def training(self, x, adapter_ids, d_y, d_weights):
+        """Gradients of the input, of both factors of every adapter, and of the gate's scores, for given gradients of the projection's output and
+        of the gate's weights."""
+        y, h = self.project(x, adapter_ids, keep_h=True)
+        scores, ids, weights = self.route(y)
+        self.ctx.mw_route(self.gate, scores, self.gate_bias, ids, weights)
+        d_scores = torch.empty_like(scores)
+        self.ctx.mw_route_backward(self.gate, scores, ids, d_weights, d_scores)
+        d_y = d_y + (d_scores @ self.gate_weight.float()).bfloat16()
+        a, b, _ = self.adapters._held
+        d_x, d_a, d_b = d_y @ self.projection, torch.empty_like(a), torch.empty_like(b)
+        self.adapters.mw_adapt_backward(x, adapter_ids, h, d_y, d_x, d_x, d_a, d_b, self.adapter_workspace)
+        return d_x, d_a, d_b, d_scores
+
+
+def main():
+    block, g = Block(), torch.Generator(device="cuda:0")
+    g.manual_seed(2)
+    for n in (1, 64, 256):
+        x = torch.randn((n, block.hidden), generator=g, device="cuda:0", dtype=torch.bfloat16)
+        requests = torch.randint(-1, block.adapters.n, (n,), generator=g, device="cuda:0").int()
+        out, ids, _ = block.decode(x, requests)
+        send, stats = block.prefill(x, requests)
+        d = block.training(x, requests, torch.randn(x.shape, generator=g, device="cuda:0", dtype=torch.bfloat16),
+                           torch.randn(ids.shape, generator=g, device="cuda:0"))
+        torch.cuda.synchronize()
+        print("%3d tokens: |out| %.3f, %d rows packed for %d ranks, |d_x| %.1f, |d_a| %.1f, |d_b| %.1f" % (
+            n, out.float().norm(), stats["n_rows"], (np.asarray(stats["rows_per_dest"]) > 0).sum(), *(t.float().norm() for t in d[:3])), flush=True)
+
+
+if __name__ == "__main__":
+    main()

@@ -26,16 +26,18 @@ struct order_args {
 };
 
 // One workgroup.
-__device__ __forceinline__ void make_order(const order_args &a)
+__device__ __forceinline__ void make_order(const order_args &a, char *order_stage)
 {
-    __shared__ uint32_t hist[kOrderWaves][kBins];
-    __shared__ uint32_t row_at[kBins + 1], tile_at[kBins + 1];
+    extern __shared__ uint32_t order_lds[];                   // (by the adapters there are: the transposing workgroups are given it too)
     __shared__ uint32_t scratch[17];
+    const int n_bins = a.n + 1;
+    uint32_t *row_at = order_lds, *tile_at = row_at + n_bins + 1, *hists = tile_at + n_bins + 1;
     constexpr int kHeld = 8;               // pieces of 64 ids a wave requests together
-    __shared__ uint16_t held[kOrderWaves][kHeld * 64];
+    uint16_t (*held)[kHeld * 64] = (uint16_t (*)[kHeld * 64])order_stage;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.n, T = a.T;
     const int per = ((T + kOrderWaves - 1) / kOrderWaves + 63) / 64 * 64;      // a wave's rows, in pieces of 64
     const int lo = wave * per, hi = min(T, lo + per);
+    uint32_t *hist = hists + wave * n_bins;
     bool wrong = false;
     // Bins of the rows from `at`.  They wait in LDS for loops that are not unrolled: code that runs once is fetched at memory's pace.
     auto hold = [&](int at) {
@@ -61,13 +63,13 @@ __device__ __forceinline__ void make_order(const order_args &a)
                 same &= (b >> i) & 1 ? set : ~set;
             }
         const int before = __popcll(same & ((1ull << lane) - 1));
-        const uint32_t at = hist[wave][b] + (uint32_t)before;
+        const uint32_t at = hist[b] + (uint32_t)before;
         __builtin_amdgcn_wave_barrier();
-        if (live && before == 0) hist[wave][b] += (uint32_t)__popcll(same);
+        if (live && before == 0) hist[b] += (uint32_t)__popcll(same);
         __builtin_amdgcn_wave_barrier();
         return at;
     };
-    for (int i = lane; i <= n; i += 64) hist[wave][i] = 0;
+    for (int i = lane; i <= n; i += 64) hist[i] = 0;
     for (int at = lo; at < hi; at += kHeld * 64) {
         hold(at);
 #pragma unroll 1
@@ -83,7 +85,7 @@ __device__ __forceinline__ void make_order(const order_args &a)
         const int b = tid * kPer + i;
         rows[i] = 0;
         if (b <= n)
-            for (int w = 0; w < kOrderWaves; ++w) rows[i] += hist[w][b];
+            for (int w = 0; w < kOrderWaves; ++w) rows[i] += hists[w * n_bins + b];
         rsum += rows[i];
         tsum += (rows[i] + a.tile_rows - 1) / a.tile_rows;
     }
@@ -98,8 +100,8 @@ __device__ __forceinline__ void make_order(const order_args &a)
             a.tile_at[b] = (int32_t)k;
             uint32_t p = r;
             for (int w = 0; w < kOrderWaves; ++w) {
-                const uint32_t c = hist[w][b];
-                hist[w][b] = p;
+                const uint32_t c = hists[w * n_bins + b];
+                hists[w * n_bins + b] = p;
                 p += c;
             }
         }
@@ -131,15 +133,22 @@ __device__ __forceinline__ void make_order(const order_args &a)
         }
     }
 }
-__global__ __launch_bounds__(kOrderBlock) void k_adapt_order(order_args a) { make_order(a); }
+constexpr int kStageBytes = kOrderWaves * 8 * 64 * 2;      // ids that wait
+__global__ __launch_bounds__(kOrderBlock) void k_adapt_order(order_args a)
+{
+    __shared__ __align__(16) char stage[kStageBytes];
+    make_order(a, stage);
+}
+uint32_t order_lds_bytes(int32_t n) { return (uint32_t)((n + 2) * 2 + (n + 1) * kOrderWaves) * 4; }
 
 // The order in workgroup 0; the others transpose the factors: [n][rows][cols] -> [n][cols][rows], 64 x 128 values each.
 struct transpose_args { const uint16_t *in; uint16_t *out; int32_t rows, cols; };
 __global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, transpose_args t0, transpose_args t1)
 {
     __shared__ __align__(16) uint16_t tiles[2][64][72];         // each half of the workgroup has its own
+    static_assert(sizeof(tiles) >= kStageBytes, "room for the ids");
     if (blockIdx.x == 0) {
-        make_order(a);
+        make_order(a, (char *)tiles);
         return;
     }
     int64_t at = (int64_t)blockIdx.x - 1;
@@ -520,6 +529,8 @@ template <int kM>
 __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
 {
     __shared__ __align__(16) float part[kGradWaves * 8 * 256];
+    constexpr int kTurned = kM * 16 + 8;                        // [128 columns][ranks]
+    __shared__ __align__(16) uint16_t turned[128 * kTurned];
     const int side = blockIdx.z & 1, r0 = (blockIdx.z >> 1) * 32, ad = blockIdx.y, c0 = blockIdx.x * 128, width = p.width[side];
     if (c0 >= width) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
@@ -597,12 +608,19 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
                         bf16x4 o;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) o[i] = (__bf16)s[j][i];
-                        *(bf16x4 *)(p.out[1] + ((int64_t)ad * width + col + j) * p.rank + r) = o;
+                        *(bf16x4 *)&turned[(n * 8 + j) * kTurned + m * 16 + g * 4] = o;
                     }
                 }
             }
         }
         __syncthreads();
+    }
+    if (side == 1) {                                            // a column's ranks lie together: 16-byte pieces of them
+        constexpr int kPieces = kM * 2;
+        for (int i = threadIdx.x; i < 128 * kPieces; i += kGradWaves * 64) {
+            const int at = i / kPieces, r = i % kPieces * 8;
+            if (c0 + at < width && r0 + r < p.rank) *(u32x4 *)(p.out[1] + ((int64_t)ad * width + c0 + at) * p.rank + r0 + r) = *(const u32x4 *)&turned[at * kTurned + r];
+        }
     }
 }
 
@@ -678,7 +696,7 @@ int32_t launch_adapt(adapt_args p, const mw_adapters *s, int tile_rows, char *ws
         return n < 1 ? 1 : n;
     };
     const int ranks = ranks_of(p.rank);
-    const bool few = tiles < n_cu / 2;
+    const bool few = tiles * 8 <= n_cu;
     const int64_t n = few ? slices(p.n_in, 3LL * n_cu, 1024, kMostSlices) : slices(p.n_in, n_cu, 2048, kMostSlices);      // (a wave has two spans at least)
     p.slice = (int32_t)mw_align_up((p.n_in + n - 1) / n, 64);
     p.n_slices = (p.n_in + p.slice - 1) / p.slice;
@@ -753,7 +771,7 @@ extern "C" MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_de
         p.flags = error_flags_dev;
     } else {
         const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, tile, error_flags_dev);
-        hipLaunchKernelGGL(k_adapt_order, dim3(1), dim3(kOrderBlock), 0, st, o);
+        hipLaunchKernelGGL(k_adapt_order, dim3(1), dim3(kOrderBlock), order_lds_bytes(o.n), st, o);
         MW_HIP_CHECK(hipGetLastError());
         p.order = o.order; p.tiles = o.tiles;
     }
@@ -792,7 +810,7 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
     const transpose_args ta = {(const uint16_t *)s.a_dev, (uint16_t *)(ws + w.at), s.rank, s.n_in};
     const transpose_args tb = {(const uint16_t *)s.b_dev, (uint16_t *)(ws + w.bt), s.n_out, s.rank};
     const int64_t blocks = s.n_adapters * ((int64_t)((s.rank + 63) / 64) * ((s.n_in + 127) / 128) + (int64_t)((s.n_out + 63) / 64) * ((s.rank + 127) / 128));
-    hipLaunchKernelGGL(k_adapt_prepare, dim3(n_rows > 0 ? (uint32_t)(1 + blocks) : 1u), dim3(kOrderBlock), 0, st, o, ta, tb);
+    hipLaunchKernelGGL(k_adapt_prepare, dim3(n_rows > 0 ? (uint32_t)(1 + blocks) : 1u), dim3(kOrderBlock), order_lds_bytes(o.n), st, o, ta, tb);
     MW_HIP_CHECK(hipGetLastError());
     uint16_t *left[4];
     for (int i = 0; i < 4; ++i) left[i] = (uint16_t *)(ws + w.left[i]);
