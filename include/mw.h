@@ -43,8 +43,9 @@
  *     mw_sim_deliver.  Calls of one part race if they
  *     overlap on the device; calls of different parts, and the packers
  *     (mw_pack, mw_pack_quantize, mw_pack_packets, mw_plan_pack, the
- *     AllGather calls), which use no workspace, may run on different streams
- *     at once.  The host-side context is not locked: one host thread at a
+ *     AllGather calls), mw_route and mw_route_backward, which use no
+ *     workspace, may run on different streams at once.  mw_moe_layer,
+ *     mw_adapt and mw_adapt_backward use a workspace of the call's own.  The host-side context is not locked: one host thread at a
  *     time per context.
  *   - A context belongs to the device that was current at mw_ctx_create; an
  *     entry point called with another device current returns

@@ -7,6 +7,12 @@
 // adapter each.  k_adapt_down makes h of a tile, its workgroups sharing the columns of x out where there are few tiles; k_adapt_up adds
 // up their parts and makes a slice of y.  The gradient of the input is the same walk with the transposed factors; beside it the
 // tiles' h and dh are laid out for k_adapt_grads, which goes over an adapter's rows of x and dy once more.
+//
+// Each row of x, base and y is touched once, the factors come out of the caches: bytes bound large calls, launches and chains of round
+// trips small ones.  Measured on one MI355X: 8192 rows, 8 adapters of rank 32, 7168 to 4096 (246 MB): order 11 us, k_adapt_down 26 us (4.5
+// TB/s of x), k_adapt_up 31 us (4.3 TB/s of base and y), the call 68 us.  64 rows of 24 adapters, rank 16, 7168 to 7168: 5.6 and 8.8 us,
+// the call 13.4 us.  Backward of 4096 rows, 4 adapters of rank 64, 4096 to 4096 (144 MB): prepare 8, down 16, up 31, k_adapt_grads 32 us
+// (2.1 TB/s), the call 85 us.
 #include "mw_stream.h"
 
 namespace {
@@ -256,7 +262,8 @@ __device__ __forceinline__ int64_t part_of(const tile_rows &t, int col) { return
 
 // h: kM tiles of 16 ranks by kCols tiles of 16 rows.  grid: (tile, slice of n_in).  Few tiles are cut into slices of four waves; where the
 // tiles alone fill the card as many waves share a tile's columns out as their pieces of LDS leave room for, and there is one
-// slice, or nearly.  (64 rows of 24 adapters, rank 16: 5.9 us with slices of four waves, 7.8 with 4 of sixteen.)
+// slice, or nearly.  us of mw_adapt, four waves / many: 300 rows of 4 adapters, rank 16, 17.4 / 19.6; 700 of 8 19.8 / 22.3; 1500 of 8, rank 32,
+// 32.2 / 32.1; 2443 of 8, rank 64, 7168 to 7168, 75.9 / 62.3.
 template <int kM> constexpr int kManyWaves = kM <= 2 ? 16 : kM == 4 ? 8 : 4;
 template <int kM, int kCols, int kWaves>
 __global__ __launch_bounds__(kWaves * 64) void k_adapt_down(adapt_args p)
@@ -537,11 +544,24 @@ __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
     const int tile0 = p.tile_at[ad], tile1 = p.tile_at[ad + 1];
     const int64_t stride = p.stride[side];
     const int col = c0 + n * 8;
+    if (tile0 == tile1) {                                       // an adapter without rows: zeros
+        const u32x4 zero = {};
+        for (int i = threadIdx.x; i < 128 * kM * 2; i += kGradWaves * 64) {
+            if (side == 0) {
+                const int r = r0 + i / 16, c = c0 + i % 16 * 8;
+                if (r < p.rank && c < width) *(u32x4 *)(p.out[0] + ((int64_t)ad * p.rank + r) * width + c) = zero;
+            } else {
+                const int c = c0 + i / (kM * 2), r = r0 + i % (kM * 2) * 8;
+                if (c < width && r < p.rank) *(u32x4 *)(p.out[1] + ((int64_t)ad * width + c) * p.rank + r) = zero;
+            }
+        }
+        return;
+    }
     const array right = array_at(p.right[side]), hi_of = array_at(p.left[side][0]), lo_of = array_at(p.left[side][1]);
     const uint32_t c_at = col < width ? (uint32_t)col * 2 : kNowhere;
     f32x4 acc[kM][8] = {};
     u32x4 v[2][8], hi[2][kM], lo[2][kM];
-    if (tile0 < tile1) {
+    {
         const int first = p.tiles[tile0].first, end = p.tiles[tile1 - 1].first + p.tiles[tile1 - 1].count;     // the adapter's rows in the order
         int row[2][8];
         // A tile's rows, a step ahead of what is loaded of them; past the last tile nothing.
@@ -628,8 +648,9 @@ int ranks_of(int32_t rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 
 constexpr int kMostSlices = 8;
 constexpr int64_t kMostCus = 512;          // (rows times slices stay below rows + 128 times the CUs: a tile has at most 32 rows)
 
-// Rows of a tile: 32 where adapters have that many rows mostly, else 16.
-int tile_rows_of(const mw_adapters *s, int64_t rows, bool backward) { return backward || rows >= 24LL * s->n_adapters ? 32 : 16; }
+// Rows of a tile: 32 where adapters have 96 rows on average, and where the gradients want tiles one matrix instruction deep; else 16.  us of
+// mw_adapt, 24 adapters of rank 16, 4096 to 4096, 16 / 32: 300 rows 18.6 / 21.9, 600 20.3 / 23.3, 1200 24.8 / 26.7, 2400 31.0 / 30.9.
+int tile_rows_of(const mw_adapters *s, int64_t rows, bool backward) { return backward || rows >= 96LL * s->n_adapters ? 32 : 16; }
 int64_t most_tiles(const mw_adapters *s, int64_t rows, int tile_rows) { return rows / tile_rows + (s->n_adapters + 1LL < rows ? s->n_adapters + 1LL : rows); }
 
 struct adapt_ws { int64_t order, tile_at, tiles, part, left[4], at, bt, total; };
@@ -766,7 +787,9 @@ extern "C" MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_de
     p.out = (uint16_t *)out_dev; p.out_stride = out_stride;
     p.h = h_dev;
     const int tile = tile_rows_of(adapters, n_rows, false);
-    if (n_rows <= kBlock) {                // every workgroup finds its tile in the ids: a launch less
+    // Up to 256 rows every workgroup finds its tile in the ids: a launch less.  us, so / with the order first: 1 row 10.1 / 13.0, 64 rows of 24
+    // adapters 11.6 / 15.3, 256 of 64 16.5 / 20.2 (rank 16, 4096 to 4096).
+    if (n_rows <= kBlock) {
         p.ids = adapter_ids_dev;
         p.flags = error_flags_dev;
     } else {

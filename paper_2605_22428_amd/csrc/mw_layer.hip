@@ -4,8 +4,11 @@
 //   out[t]    = sum over the token's pairs of Wd act[pair]                                    (k_layer_down)
 //
 // Every weight of an expert that a token goes to has to be read once and is used for a few tokens only, so the weights' bytes bound both
-// kernels.  They are streamed from memory into registers in the layout that the matrix instruction takes, never through LDS: 16
-// weight rows are one side, up to 16 tokens the other, and whichever columns have no token cost nothing that counts.
+// kernels.  16 weight rows are one side of the matrix instruction and up to 16 tokens the other; whichever columns have no token cost nothing
+// that counts.  Measured on one MI355X (weights of hidden 7168, inter 2048): 256 tokens of 256 experts, 32 bf16 ones here (2.8 GB):
+// k_layer_up 295 us, 6.4 TB/s, k_layer_down 173 us, 5.4 TB/s, the layer 469 us, 6.0 TB/s (a plain copy: 6.8).  64 tokens, four fp8 experts
+// (155 MB): 44 to 50 us; k_layer_up 22 us, 5.3 TB/s, k_layer_down 17 us, 3.4 TB/s, launches and their first round trips the rest.  One
+// token, eight of 64 experts of 4096 x 1024 (201 MB): 26 us, 5.1 TB/s, and 16 us, 4.2 TB/s, the layer 44.5 us.
 #include "mw_stream.h"
 
 namespace {
@@ -266,10 +269,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void k_layer_down_few(layer_args a)
     }
 }
 
-// Larger batches: a pair's product by itself.  Two tiles of 16 rows share the columns' loads.  kSplit of a workgroup's four
-// waves take 32 rows, every kSplit-th span each.  grid: (4 / kSplit times 32 rows of H, hit experts)
-constexpr int kDownWaves = 4;
-template <bool kFp8, int kSplit, int kCols, int kHalves, int kDepth>
+// Larger batches: a pair's product by itself.  Two tiles of 16 rows share the columns' loads; two of a workgroup's four waves take
+// 32 rows, every second span each.  grid: (64 rows of H, hit experts).  us of the layer with one / two / four waves to 32 rows: 256 tokens of
+// 256 experts, 32 of them here, 7168 x 2048, 480 / 471 / 495; four / two: 64 tokens, four fp8 experts 46.0 / 43.9, 128 tokens of 32 experts,
+// 4096 x 1024, 266 / 235.
+constexpr int kDownWaves = 4, kSplit = 2;
+template <bool kFp8, int kCols, int kHalves, int kDepth>
 __device__ __forceinline__ void down_columns(const layer_args &a, int le, int row0, const uint16_t *list, int first, int count, char *lds)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), n = lane & 15, g = lane >> 4;
@@ -325,7 +330,7 @@ __device__ __forceinline__ void down_columns(const layer_args &a, int le, int ro
     }
 }
 
-template <bool kFp8, int kSplit, bool kWide>
+template <bool kFp8, bool kWide>
 __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
 {
     __shared__ __align__(16) char part[kDownWaves * kWaveLds<2>];
@@ -338,10 +343,10 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_layer_down(layer_args a)
     const int row0 = ((int)blockIdx.x * (kDownWaves / kSplit) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) / kSplit) * 32;
     for (int first = 0; first < count;) {
         const int left = count - first;
-        if (left <= 8) { down_columns<kFp8, kSplit, 1, 1, kFp8 ? 3 : 4>(a, le, row0, list, first, count, part); first += 16; }
-        else if (left <= 16) { down_columns<kFp8, kSplit, 1, 2, kFp8 ? 2 : 3>(a, le, row0, list, first, count, part); first += 16; }
-        else if (!kWide || left <= 32) { down_columns<kFp8, kSplit, 2, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
-        else if constexpr (kWide) { down_columns<kFp8, kSplit, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
+        if (left <= 8) { down_columns<kFp8, 1, 1, kFp8 ? 3 : 4>(a, le, row0, list, first, count, part); first += 16; }
+        else if (left <= 16) { down_columns<kFp8, 1, 2, kFp8 ? 2 : 3>(a, le, row0, list, first, count, part); first += 16; }
+        else if (!kWide || left <= 32) { down_columns<kFp8, 2, 2, 2>(a, le, row0, list, first, count, part); first += 32; }
+        else if constexpr (kWide) { down_columns<kFp8, 4, 2, 2>(a, le, row0, list, first, count, part); first += 64; }
     }
 }
 
@@ -448,12 +453,17 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     const uint32_t ids_lds = (uint32_t)mw_align_up(2 * pairs, 16);
     const dim3 up((uint32_t)((I + 15) / 16), hits);
     const bool fp8 = experts->format == MW_ROW_FP8_E4M3_BLOCK128;
-    // Experts with more than 32 tokens: 64 of them at a time where that is the usual case.
+    // An expert's weights are read once for up to 32 of its tokens, or (bf16) for up to 64 at half the waves a CU holds, where experts have
+    // 24 tokens on average.  us, 32 / 64: 256 tokens, 8 experts, top-2, 4096 x 2048 227 / 177; 16 experts, top-2 258 / 209; 16 experts, top-4,
+    // 4096 x 1024 239 / 184.
     const bool wide = !fp8 && pairs >= 24LL * a.E;
     if (fp8) hipLaunchKernelGGL((k_layer_up<true, false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     else if (wide) hipLaunchKernelGGL((k_layer_up<false, true>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     else hipLaunchKernelGGL((k_layer_up<false, false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
+    // Up to 16 tokens the second product adds an output up over its experts; beyond, and for any batch so: pairs, then k_layer_sum.  us: 1 token, 64
+    // experts, top-8, 4096 x 1024 45.0, the other way 51.4; 4 tokens, 16 experts, top-2 39.8, 42.2; 16 tokens, top-4 77.6, 78.8; 16 tokens,
+    // 64 fp8 experts, top-8, 2048 x 512 72.7, 70.6.
     if (n_tokens <= 16) {
         const dim3 down((uint32_t)((H + 15) / 16));
         const uint32_t lds = ids_lds + hits * 34;
@@ -462,15 +472,10 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
         MW_HIP_CHECK(hipGetLastError());
         return MW_OK;
     }
-    const int64_t groups = (H + 31) / 32;
-    const bool two = groups * hits >= 8LL * ctx->n_cu;
-    const dim3 down((uint32_t)(two ? (groups + 1) / 2 : groups), hits);
-    if (fp8 && two) hipLaunchKernelGGL((k_layer_down<true, 2, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (fp8) hipLaunchKernelGGL((k_layer_down<true, 4, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (two && wide) hipLaunchKernelGGL((k_layer_down<false, 2, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (wide) hipLaunchKernelGGL((k_layer_down<false, 4, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else if (two) hipLaunchKernelGGL((k_layer_down<false, 2, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
-    else hipLaunchKernelGGL((k_layer_down<false, 4, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    const dim3 down((uint32_t)((H + 63) / 64), hits);
+    if (fp8) hipLaunchKernelGGL((k_layer_down<true, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else if (wide) hipLaunchKernelGGL((k_layer_down<false, true>), down, dim3(kDownWaves * 64), ids_lds, s, a);
+    else hipLaunchKernelGGL((k_layer_down<false, false>), down, dim3(kDownWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL(k_layer_sum, dim3((uint32_t)((H + 1023) / 1024), (uint32_t)n_tokens), dim3(256), 2 * MW_MAX_TOPK, s, a);
     MW_HIP_CHECK(hipGetLastError());

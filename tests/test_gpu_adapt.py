@@ -268,11 +268,11 @@ def test_refusals():
     I, CAP, WS, UN = B.MW_ERR_INVALID_ARG, B.MW_ERR_CAPACITY, B.MW_ERR_WORKSPACE, B.MW_ERR_UNSUPPORTED
     call, good = B._native().mw_adapt, [s.dev.address, x, 64, ids, T, None, 0, out, 32, None, None, ws, ws.numel(), 0]
     assert call(*good) == B.MW_OK
-    for at, bad, status in ((0, 0, I), (1, None, I), (1, wide[4:], I), (2, 56, I), (2, 68, I), (3, None, I), (4, -1, I), (4, 65537, CAP), (5, wide[1:], I), (5, out, I),
+    for at, bad, status in ((2, 1 << 29, UN), (8, 1 << 29, UN), (0, 0, I), (1, None, I), (1, wide[4:], I), (2, 56, I), (2, 68, I), (3, None, I), (4, -1, I), (4, 65537, CAP), (5, wide[1:], I), (5, out, I),
                             (7, None, I), (8, 24, I), (11, None, WS), (11, ws[8:], WS), (12, 100, WS)):
         assert call(*(good[:at] + [bad] + good[at + 1:])) == status, (at, bad)
     back, good_b = B._native().mw_adapt_backward, [s.dev.address, x, 64, ids, T, h, out, 32, None, 0, x, 64, da, db, None, ws, ws.numel(), 0]
-    for at, bad, status in ((0, 0, I), (1, None, I), (2, 56, I), (3, None, I), (4, -1, I), (4, 65537, CAP), (5, None, I), (6, None, I), (7, 28, I), (8, x, I), (10, None, I),
+    for at, bad, status in ((2, 1 << 29, UN), (7, 1 << 29, UN), (11, 1 << 29, UN), (0, 0, I), (1, None, I), (2, 56, I), (3, None, I), (4, -1, I), (4, 65537, CAP), (5, None, I), (6, None, I), (7, 28, I), (8, x, I), (10, None, I),
                             (11, 0, I), (12, None, I), (13, None, I), (13, wide[1:], I), (15, None, WS), (16, 0, WS)):
         assert back(*(good_b[:at] + [bad] + good_b[at + 1:])) == status, (at, bad)
     for change, status in ((dict(rank=12), UN), (dict(rank=136), UN), (dict(rank=0), I), (dict(n_in=60), UN), (dict(n_out=36), UN), (dict(n_adapters=0), I),

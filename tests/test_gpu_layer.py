@@ -216,7 +216,7 @@ def test_refusals():
                             (7, wide[1:], B.MW_ERR_INVALID_ARG), (8, 127, B.MW_ERR_INVALID_ARG), (8, 132, B.MW_ERR_INVALID_ARG), (9, -1, B.MW_ERR_INVALID_ARG),
                             (9, 101, B.MW_ERR_CAPACITY), (10, None, B.MW_ERR_INVALID_ARG), (11, None, B.MW_ERR_INVALID_ARG), (12, None, B.MW_ERR_INVALID_ARG),
                             (12, wide[4:], B.MW_ERR_INVALID_ARG), (13, 120, B.MW_ERR_INVALID_ARG), (15, None, B.MW_ERR_WORKSPACE), (15, ws[16:], B.MW_ERR_WORKSPACE),
-                            (16, 255, B.MW_ERR_WORKSPACE)):
+                            (16, 255, B.MW_ERR_WORKSPACE), (8, 1 << 29, B.MW_ERR_UNSUPPORTED)):
         assert call(*(good[:at] + [bad] + good[at + 1:])) == status, (at, bad)
     held = r.experts._held
     for change, status in ((dict(inter=0), B.MW_ERR_INVALID_ARG), (dict(inter=60), B.MW_ERR_UNSUPPORTED), (dict(format=2), B.MW_ERR_INVALID_ARG),
