@@ -367,13 +367,14 @@ _LOGIT_FORMAT = {torch.float32: MW_LOGITS_F32, torch.bfloat16: MW_LOGITS_BF16}
 
 def _rows(t: torch.Tensor, width: int, what: str) -> int:
     """Elements from row to row of a matrix whose rows are in one piece each."""
-    if t.dim() != 2 or t.shape[1] != width or (t.stride(1) != 1 and width > 1):
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != width or (t.stride(1) != 1 and width > 1):
         raise ValueError("%s: rows of %d values in one piece each, got shape %s and strides %s" % (what, width, tuple(t.shape), t.stride()))
-    return max(t.stride(0), width) if t.shape[0] < 2 else t.stride(0)
+    return t.stride(0) if shape[0] > 1 else max(t.stride(0), width)
 
 
-def _whole(t: Optional[torch.Tensor], shape, dtype, what: str):
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+def _whole(t: Optional[torch.Tensor], shape: tuple, dtype, what: str):
+    if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
         raise ValueError("%s: a contiguous tensor of %s and shape %s, got %s and %s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape)))
 
 

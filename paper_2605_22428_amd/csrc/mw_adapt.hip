@@ -39,7 +39,7 @@ __device__ __forceinline__ void make_order(const order_args &a, char *order_stag
     const int n_bins = a.n + 1;
     uint32_t *row_at = order_lds, *tile_at = row_at + n_bins + 1, *hists = tile_at + n_bins + 1;
     constexpr int kHeld = 8;               // pieces of 64 ids a wave requests together
-    uint16_t (*held)[kHeld * 64] = (uint16_t (*)[kHeld * 64])order_stage;
+    uint16_t (*held)[kHeld * 64] = (uint16_t (*)[kHeld * 64])order_stage, (*placed)[kHeld * 64] = held + kOrderWaves;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.n, T = a.T;
     const int per = ((T + kOrderWaves - 1) / kOrderWaves + 63) / 64 * 64;      // a wave's rows, in pieces of 64
     const int lo = wave * per, hi = min(T, lo + per);
@@ -79,7 +79,10 @@ __device__ __forceinline__ void make_order(const order_args &a, char *order_stag
     for (int at = lo; at < hi; at += kHeld * 64) {
         hold(at);
 #pragma unroll 1
-        for (int t0 = at; t0 < min(hi, at + kHeld * 64); t0 += 64) place(t0 + lane, held[wave][t0 - at + lane]);
+        for (int t0 = at; t0 < min(hi, at + kHeld * 64); t0 += 64) {
+            const int i = t0 - at + lane;
+            placed[wave][i] = (uint16_t)place(t0 + lane, held[wave][i]);
+        }
     }
     if (a.flags && wrong) atomicOr(a.flags, MW_FLAG_BAD_ADAPTER);
     mw_lds_barrier();
@@ -130,8 +133,12 @@ __device__ __forceinline__ void make_order(const order_args &a, char *order_stag
         const int first = (int)row_at[at] + (i - (int)tile_at[at]) * a.tile_rows;
         a.tiles[i] = adapt_tile{at, first, min(a.tile_rows, (int)row_at[at + 1] - first), 0};
     }
+    if (hi - lo <= kHeld * 64) {           // the wave's rows and their places are still there
+        for (int t = lo + lane; t < hi; t += 64) a.order[hist[held[wave][t - lo]] + placed[wave][t - lo]] = t;
+        return;
+    }
     for (int at = lo; at < hi; at += kHeld * 64) {
-        if (hi - lo > kHeld * 64) hold(at);
+        hold(at);
 #pragma unroll 1
         for (int t0 = at; t0 < min(hi, at + kHeld * 64); t0 += 64) {
             const uint32_t to = place(t0 + lane, held[wave][t0 - at + lane]);
@@ -139,7 +146,7 @@ __device__ __forceinline__ void make_order(const order_args &a, char *order_stag
         }
     }
 }
-constexpr int kStageBytes = kOrderWaves * 8 * 64 * 2;      // ids that wait
+constexpr int kStageBytes = 2 * kOrderWaves * 8 * 64 * 2;  // ids that wait, and their places
 __global__ __launch_bounds__(kOrderBlock) void k_adapt_order(order_args a)
 {
     __shared__ __align__(16) char stage[kStageBytes];
@@ -151,10 +158,11 @@ uint32_t order_lds_bytes(int32_t n) { return (uint32_t)((n + 2) * 2 + (n + 1) * 
 struct transpose_args { const uint16_t *in; uint16_t *out; int32_t rows, cols; };
 __global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, transpose_args t0, transpose_args t1)
 {
-    __shared__ __align__(16) uint16_t tiles[2][64][72];         // each half of the workgroup has its own
-    static_assert(sizeof(tiles) >= kStageBytes, "room for the ids");
+    __shared__ __align__(16) char stage[kStageBytes];
+    uint16_t (*tiles)[64][72] = (uint16_t (*)[64][72])stage;    // each half of the workgroup has its own
+    static_assert(2 * 64 * 72 * 2 <= kStageBytes, "room for two of them");
     if (blockIdx.x == 0) {
-        make_order(a, (char *)tiles);
+        make_order(a, stage);
         return;
     }
     int64_t at = (int64_t)blockIdx.x - 1;
