@@ -9,8 +9,8 @@
 // tiles' h and dh are laid out for k_adapt_grads, which goes over an adapter's rows of x and dy once more.
 //
 // Each row of x, base and y is touched once, the factors come out of the caches: bytes bound large calls, launches and chains of round
-// trips small ones.  Measured on one MI355X: 8192 rows, 8 adapters of rank 32, 7168 to 4096 (246 MB): order 11 us, k_adapt_down 26 us (4.5
-// TB/s of x), k_adapt_up 31 us (4.3 TB/s of base and y), the call 68 us.  64 rows of 24 adapters, rank 16, 7168 to 7168: 5.6 and 8.8 us,
+// trips small ones.  Measured on one MI355X: 8192 rows, 8 adapters of rank 32, 7168 to 4096 (246 MB): order 9 us, k_adapt_down 26 us (4.5
+// TB/s of x), k_adapt_up 31 us (4.3 TB/s of base and y), the call 65 us.  64 rows of 24 adapters, rank 16, 7168 to 7168: 5.6 and 8.8 us,
 // the call 13.4 us.  Backward of 4096 rows, 4 adapters of rank 64, 4096 to 4096 (144 MB): prepare 8, down 16, up 31, k_adapt_grads 32 us
 // (2.1 TB/s), the call 85 us.
 #include "mw_stream.h"
