@@ -3,8 +3,8 @@
 // One wave a token, its scores in registers (lane l holds experts l, l + 64, ...).  The K best are taken one by one: a wave-wide
 // maximum of keys that order like the scores, the lowest expert among equals.  Nothing but one float addition decides which experts
 // are taken, so the ids are the same whatever the order of the sums in the weights.  Measured on one MI355X: 8192 tokens, 256 experts in 8
-// groups, top-8 (8.9 MB) 10.8 us: eight rounds of a wave's maximum are some 700 instructions a token, which bound it, not the bytes
-// (1.3 us of them); backward of 4096 tokens (4.5 MB) 6.6 us, 5 of them the kernel.  Smaller calls are a launch, 5.7 us in a stream of them.
+// groups, top-8 (8.9 MB) 10.4 us: eight rounds of a wave's maximum are some 700 instructions a token, which bound it, not the bytes
+// (1.3 us of them); backward of 4096 tokens (4.5 MB) 6.6 us, 5 of them the kernel.  Smaller calls are a launch, 5 to 6 us in a stream of them.
 #include <float.h>
 
 #include "mw_math.h"
@@ -100,15 +100,13 @@ __global__ __launch_bounds__(kBlock) void k_route(gate_args a, int32_t *__restri
     }
     select_keys<kVals>(a, l, key, lane, rows[wave]);
 
-    int my_id = -1;                              // lane k: the k-th choice and its score
-    float my_l = -INFINITY;
+    int my_id = -1;                              // lane k: the k-th choice
     for (int k = 0; k < a.top_k; ++k) {
         uint32_t best = key[0];
         int at = 0;
-        float best_l = l[0];
 #pragma unroll
         for (int j = 1; j < kVals; ++j)
-            if (key[j] > best) { best = key[j]; at = j; best_l = l[j]; }
+            if (key[j] > best) { best = key[j]; at = j; }
         const uint32_t top = mw_wave_max(best);
         if (top == 0u) break;
         const unsigned long long equal = __ballot(best == top);
@@ -118,11 +116,19 @@ __global__ __launch_bounds__(kBlock) void k_route(gate_args a, int32_t *__restri
             owner = (int)((0xffffu - low) & 63u);
         }
         const int id = __builtin_amdgcn_readlane(at, owner) * 64 + owner;
-        const float ll = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(best_l), owner));
-        if (lane == k) { my_id = id; my_l = ll; }
+        if (lane == k) my_id = id;
+        const int gone = lane == owner ? at : -1;
 #pragma unroll
-        for (int j = 0; j < kVals; ++j) if (lane == owner && j == at) key[j] = 0u;
+        for (int j = 0; j < kVals; ++j) key[j] = j == gone ? 0u : key[j];
     }
+    // The choices' scores, by way of LDS: carried through the rounds they would be three instructions of each.
+    float *row = rows[wave];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < kVals; ++j) row[j * 64 + lane] = l[j];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+    __builtin_amdgcn_wave_barrier();
+    const float my_l = my_id >= 0 ? row[my_id] : -INFINITY;
 
     float v, total;
     if (a.score == MW_GATE_SIGMOID_TOPK) {
