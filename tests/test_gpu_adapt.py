@@ -173,7 +173,7 @@ def test_gradients_against_the_formulas(T, n, rank, n_in, n_out):
         assert (got[1][a] == 0).all() and (got[2][a] == 0).all()
 
 
-@pytest.mark.parametrize("T,n,rank,n_in,n_out", [(3000, 2, 64, 136, 264), (5, 2, 16, 7168, 4096), (700, 1, 128, 256, 512)])
+@pytest.mark.parametrize("T,n,rank,n_in,n_out", [(3000, 2, 64, 136, 264), (5, 2, 16, 7168, 4096), (700, 1, 128, 256, 512), (70, 1024, 8, 24, 16)])
 def test_gradients_of_many_rows_and_long_rows(T, n, rank, n_in, n_out):
     s = Set(n, rank, n_in, n_out)
     x, dy, ids, h = normal(5, T, n_in).bfloat16(), normal(6, T, n_out).bfloat16(), mixed(T, T, n, 0.1), normal(8, T, rank).numpy()

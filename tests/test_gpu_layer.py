@@ -75,7 +75,7 @@ def draw_ids(seed, T, E, K, none=0.0):
 
 SIZES = [(1, 1, 1, 1, 8, 8), (1, 4, 16, 2, 256, 256), (2, 1, 8, 2, 328, 1000), (5, 2, 6, 3, 1000, 136), (13, 2, 16, 2, 512, 264), (16, 1, 4, 4, 128, 128),
          (16, 8, 64, 8, 256, 48), (17, 1, 4, 2, 264, 72), (33, 1, 1, 1, 256, 40), (64, 4, 16, 4, 136, 128), (65, 1, 2, 2, 128, 200), (130, 8, 32, 8, 64, 64),
-         (256, 1, 2, 1, 256, 32), (256, 2, 8, 8, 40, 24)]
+         (256, 1, 2, 1, 256, 32), (256, 2, 8, 8, 40, 24), (256, 1, 64, 64, 64, 16), (16, 2, 1024, 64, 64, 16)]
 
 
 @pytest.mark.parametrize("fp8", [False, True])
