@@ -757,6 +757,7 @@ MW_API int32_t mw_relay_packets_copy_index_next(mw_ctx *ctx, const mw_recv_packe
  *   MW_GATE_SOFTMAX       w_k = c exp(l_k) / sum over all experts of exp(l_e)
  *   MW_GATE_SOFTMAX_TOPK  w_k = c exp(l_k) / sum over the experts taken of exp(l_j)
  *   MW_GATE_SIGMOID_TOPK  w_k = c sig(l_k) / sum over the experts taken of sig(l_j)   (0 where that sum is 0)
+ * sig(l) counts as 0 where it is below 2^-1022 (l < -708): finite values that stand for a mask weigh nothing.
  */
 #define MW_GATE_SOFTMAX      0
 #define MW_GATE_SOFTMAX_TOPK 1

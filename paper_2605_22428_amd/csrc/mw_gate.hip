@@ -31,6 +31,17 @@ __device__ __forceinline__ float load_score(const void *p, int64_t at)
     return v != v ? -INFINITY : fminf(v, FLT_MAX);
 }
 
+// The largest of the lanes' scores, no lower than the lowest finite value; every lane active.
+__device__ __forceinline__ float wave_top(float l) { return mw_key_value(mw_wave_max(mw_order_key(fmaxf(l, -FLT_MAX)))); }
+
+// sig(l) / exp(min(top, 0)), top the largest score taken.  Shares are quotients of these, the factor cancels; sig itself is 0 in 32 bits from l = -104
+// down and has lost bits from -87, where shares of a token whose scores are all that low still are ordinary numbers.  Below -708 sig is
+// under the smallest normal number of 64 bits and counts as 0: such scores stand for masks (-1e4, a type's lowest value).
+__device__ __forceinline__ float scaled_sigmoid(float l, float top)
+{
+    return l < -708.0f ? 0.0f : expf(fminf(l, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(l)));
+}
+
 // Keys of the scores that selection goes by, 0 where an expert cannot be taken.
 template <int kVals>
 __device__ __forceinline__ void select_keys(const gate_args &a, const float (&l)[kVals], uint32_t (&key)[kVals], int lane, float *row)
@@ -132,7 +143,8 @@ __global__ __launch_bounds__(kBlock) void k_route(gate_args a, int32_t *__restri
 
     float v, total;
     if (a.score == MW_GATE_SIGMOID_TOPK) {
-        v = my_id >= 0 ? 1.0f / (1.0f + expf(-my_l)) : 0.0f;
+        const float top = wave_top(my_l);
+        v = my_id >= 0 ? scaled_sigmoid(my_l, top) : 0.0f;
         total = mw_wave_sum_f32(v);
     } else {
         float m = my_id >= 0 ? my_l : -INFINITY;
@@ -140,7 +152,7 @@ __global__ __launch_bounds__(kBlock) void k_route(gate_args a, int32_t *__restri
 #pragma unroll
             for (int j = 0; j < kVals; ++j) m = fmaxf(m, l[j]);
         }
-        m = mw_key_value(mw_wave_max(mw_order_key(fmaxf(m, -FLT_MAX))));
+        m = wave_top(m);
         v = my_id >= 0 ? expf(my_l - m) : 0.0f;
         float sum = v;
         if (a.score == MW_GATE_SOFTMAX) {
@@ -184,16 +196,17 @@ __global__ __launch_bounds__(kBlock) void k_route_backward(gate_args a, const in
     // q: the weight before the factor; `add` goes to the expert's place
     float q, add, inv = 0.0f, m = 0.0f;
     if (a.score == MW_GATE_SIGMOID_TOPK) {
-        const float sig = id >= 0 ? 1.0f / (1.0f + expf(-my_l)) : 0.0f;
-        const float total = mw_wave_sum_f32(sig);
-        q = total > 0.0f ? sig / total : 0.0f;
+        const float top = wave_top(my_l);
+        const float v = id >= 0 ? scaled_sigmoid(my_l, top) : 0.0f;
+        const float total = mw_wave_sum_f32(v);
+        q = total > 0.0f ? v / total : 0.0f;
         add = q * (1.0f / (1.0f + expf(my_l)));             // (1 - sigmoid, with small ones kept)
         if (id < 0) add = 0.0f;
     } else {
         m = my_l;
 #pragma unroll
         for (int j = 0; j < kVals; ++j) m = fmaxf(m, l[j]);
-        m = mw_key_value(mw_wave_max(mw_order_key(fmaxf(m, -FLT_MAX))));
+        m = wave_top(m);
         const float v = id >= 0 ? expf(my_l - m) : 0.0f;
         float sum = v;
         if (a.score == MW_GATE_SOFTMAX) {
