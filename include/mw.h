@@ -751,7 +751,8 @@ MW_API int32_t mw_relay_packets_copy_index_next(mw_ctx *ctx, const mw_recv_packe
  * largest finite value); c is `scale`.  Experts are taken by s = l + bias, one fp32 addition (without a bias s = l; at
  * most the largest finite value).  With n_groups > 1 the experts are n_groups runs of n_experts / n_groups; a group's
  * score is the fp32 sum of its two best s (a group of one expert: its s), and only the kept_groups best groups' experts
- * can be taken.  The top_k best are taken in descending order; among equals the lowest expert, the lowest group.  An
+ * can be taken; a group without an expert that can be taken comes after every other, also after one whose score is -inf because it has
+ * one such expert only.  The top_k best are taken in descending order; among equals the lowest expert, the lowest group.  An
  * expert whose s is -inf (or NaN) is never taken: where fewer than top_k are left the id is -1 and the weight 0, so a token
  * whose experts are all masked goes nowhere.  Weights do not use the bias:
  *   MW_GATE_SOFTMAX       w_k = c exp(l_k) / sum over all experts of exp(l_e)

@@ -81,10 +81,12 @@ __device__ __forceinline__ void select_keys(const gate_args &a, const float (&l)
         second = fmaxf(fmaxf(second, os), fminf(best, ob));
         best = fmaxf(best, ob);
     }
-    const float mine = __shfl(S > 1 ? best + second : best, min(lane * P, 63));      // lane g: group g
+    // A group's rank as a key; 0, behind every score, for one none of whose experts can be taken (a score can be -inf with one that can).
+    const uint32_t rank = best > -INFINITY ? mw_order_key(S > 1 ? best + second : best) : 0u;
+    const uint32_t mine = (uint32_t)__shfl((int)rank, min(lane * P, 63));      // lane g: group g
     int ahead = 0;
     for (int g = 0; g < G; ++g) {
-        const float other = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(mine), g));
+        const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)mine, g);
         ahead += other > mine || (other == mine && g < lane) ? 1 : 0;
     }
     const unsigned long long kept = __ballot(lane < G && ahead < a.kept);
