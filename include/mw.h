@@ -749,7 +749,7 @@ MW_API int32_t mw_relay_packets_copy_index_next(mw_ctx *ctx, const mw_recv_packe
 /*
  * What a gate's scores mean.  Scores l are one row of n_experts values a token (a NaN counts as -inf, +inf as the
  * largest finite value); c is `scale`.  Experts are taken by s = l + bias, one fp32 addition (without a bias s = l; at
- * most the largest finite value).  With n_groups > 1 the experts are n_groups runs of n_experts / n_groups; a group's
+ * most the largest finite value), or by shares, see below.  With n_groups > 1 the experts are n_groups runs of n_experts / n_groups; a group's
  * score is the fp32 sum of its two best s (a group of one expert: its s), and only the kept_groups best groups' experts
  * can be taken; a group without an expert that can be taken comes after every other, also after one whose score is -inf because it has
  * one such expert only.  The top_k best are taken in descending order; among equals the lowest expert, the lowest group.  An
@@ -759,16 +759,22 @@ MW_API int32_t mw_relay_packets_copy_index_next(mw_ctx *ctx, const mw_recv_packe
  *   MW_GATE_SOFTMAX_TOPK  w_k = c exp(l_k) / sum over the experts taken of exp(l_j)
  *   MW_GATE_SIGMOID_TOPK  w_k = c sig(l_k) / sum over the experts taken of sig(l_j)   (0 where that sum is 0)
  * sig(l) counts as 0 where it is below 2^-1022 (l < -708): finite values that stand for a mask weigh nothing.
+ * With MW_GATE_BY_SHARE or'ed into `score` experts are taken by s = share + bias, as gates do whose bias was trained or balanced beside
+ * probabilities: share is sig(l) (MW_GATE_SIGMOID_TOPK) or the softmax over all experts, in fp32; an expert with l = -inf or NaN or a bias of -inf
+ * or NaN is never taken.  A group's score is then the fp32 sum of its two best s (MW_GATE_SIGMOID_TOPK; its best where only one can be
+ * taken) or its best s (softmax).  Without bias and groups both rules take the same experts.  Shares are rounded: experts or groups whose s are
+ * closer than that may change places, and shares that round to one value are equals.
  */
 #define MW_GATE_SOFTMAX      0
 #define MW_GATE_SOFTMAX_TOPK 1
 #define MW_GATE_SIGMOID_TOPK 2
+#define MW_GATE_BY_SHARE     0x10
 #define MW_LOGITS_F32  0
 #define MW_LOGITS_BF16 1
 #define MW_GATE_MAX_EXPERTS 1024
 #define MW_GATE_MAX_GROUPS  64
 typedef struct mw_gate {
-    int32_t score;          /* MW_GATE_* */
+    int32_t score;          /* MW_GATE_SOFTMAX .. MW_GATE_SIGMOID_TOPK, with or without MW_GATE_BY_SHARE */
     int32_t n_groups;       /* 1: no groups; divides n_experts, at most MW_GATE_MAX_GROUPS */
     int32_t kept_groups;    /* 1..n_groups */
     float scale;            /* finite */

@@ -47,6 +47,7 @@ MW_FLAG_PLAN_TIMEOUT = 0x100
 MW_FLAG_DUPLICATE_DROPPED = 0x200
 MW_OPT_RELAY_KEEP_METADATA, MW_OPT_RECV_DEDUP = 0x1, 0x2
 MW_GATE_SOFTMAX, MW_GATE_SOFTMAX_TOPK, MW_GATE_SIGMOID_TOPK = 0, 1, 2
+MW_GATE_BY_SHARE = 0x10
 MW_LOGITS_F32, MW_LOGITS_BF16 = 0, 1
 MW_GATE_MAX_EXPERTS, MW_GATE_MAX_GROUPS = 1024, 64
 MW_LAYER_MAX_TOKENS = 256
@@ -275,10 +276,11 @@ def next_batch(next_ctx, peers, n_peers, out_capacity_rows, expert_offsets, recv
 
 
 class Gate:
-    """mw_gate: how scores become expert ids and weights (include/mw.h)."""
+    """mw_gate: how scores become expert ids and weights (include/mw.h).  by_share: experts are taken by sigmoid or softmax plus bias, not by
+    score plus bias."""
 
-    def __init__(self, score: int, n_groups: int = 1, kept_groups: int = 1, scale: float = 1.0):
-        self.record = MwGate(score, n_groups, kept_groups, scale)
+    def __init__(self, score: int, n_groups: int = 1, kept_groups: int = 1, scale: float = 1.0, by_share: bool = False):
+        self.record = MwGate(score | MW_GATE_BY_SHARE if by_share else score, n_groups, kept_groups, scale)
         self.address = C.addressof(self.record)
 
 

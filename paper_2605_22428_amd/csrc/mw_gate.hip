@@ -1,8 +1,9 @@
 // mw_route, mw_route_backward: a token's gate scores -> the K experts it goes to and their weights, and the way back.
 //
 // One wave a token, its scores in registers (lane l holds experts l, l + 64, ...).  The K best are taken one by one: a wave-wide
-// maximum of keys that order like the scores, the lowest expert among equals.  Nothing but one float addition decides which experts
-// are taken, so the ids are the same whatever the order of the sums in the weights.  Measured on one MI355X: 8192 tokens, 256 experts in 8
+// maximum of keys that order like the scores, the lowest expert among equals.  By score and bias nothing but one float addition decides which
+// experts are taken, so the ids are the same whatever the order of the sums in the weights; by share a sigmoid or an exponential and a sum
+// decide as well, in fp32, and experts closer than their rounding may change places.  Measured on one MI355X: 8192 tokens, 256 experts in 8
 // groups, top-8 (8.9 MB) 10.4 us: eight rounds of a wave's maximum are some 700 instructions a token, which bound it, not the bytes
 // (1.3 us of them); backward of 4096 tokens (4.5 MB) 6.6 us, 5 of them the kernel.  Smaller calls are a launch, 5 to 6 us in a stream of them.
 #include <float.h>
@@ -17,7 +18,7 @@ struct gate_args {
     const void *logits;
     int64_t stride;             // elements from one token's scores to the next's
     const float *bias;
-    int32_t n_tokens, n_experts, top_k, score, n_groups, kept, group_size;
+    int32_t n_tokens, n_experts, top_k, score, by_share, n_groups, kept, group_size;
     int32_t group_lanes;        // lanes that look at a group together
     uint32_t group_mul;         // expert / group_size = expert * group_mul >> 20 (experts below 1024)
     float scale;
@@ -42,17 +43,44 @@ __device__ __forceinline__ float scaled_sigmoid(float l, float top)
     return l < -708.0f ? 0.0f : expf(fminf(l, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(l)));
 }
 
+// What selection goes by, before the bias, where the gate takes experts by their shares: sigmoids, or the softmax over all experts.  An expert
+// that cannot be taken keeps -inf.
+template <int kVals>
+__device__ __forceinline__ void shares(const gate_args &a, const float (&l)[kVals], float (&share)[kVals])
+{
+    if (a.score == MW_GATE_SIGMOID_TOPK) {
+#pragma unroll
+        for (int j = 0; j < kVals; ++j) share[j] = l[j] > -INFINITY ? 1.0f / (1.0f + expf(-l[j])) : -INFINITY;
+        return;
+    }
+    float m = l[0], sum = 0.0f;
+#pragma unroll
+    for (int j = 1; j < kVals; ++j) m = fmaxf(m, l[j]);
+    m = wave_top(m);
+#pragma unroll
+    for (int j = 0; j < kVals; ++j) {
+        share[j] = expf(l[j] - m);
+        sum += share[j];
+    }
+    const float total = mw_wave_sum_f32(sum);
+#pragma unroll
+    for (int j = 0; j < kVals; ++j) share[j] = l[j] > -INFINITY ? share[j] / total : -INFINITY;
+}
+
 // Keys of the scores that selection goes by, 0 where an expert cannot be taken.
 template <int kVals>
 __device__ __forceinline__ void select_keys(const gate_args &a, const float (&l)[kVals], uint32_t (&key)[kVals], int lane, float *row)
 {
-    float s[kVals];
+    float s[kVals], by[kVals];
+#pragma unroll
+    for (int j = 0; j < kVals; ++j) by[j] = l[j];
+    if (a.by_share) shares<kVals>(a, l, by);
 #pragma unroll
     for (int j = 0; j < kVals; ++j) {
         const int e = j * 64 + lane;
         s[j] = -INFINITY;
         if (e < a.n_experts) {
-            s[j] = a.bias ? l[j] + a.bias[e] : l[j];
+            s[j] = a.bias ? by[j] + a.bias[e] : by[j];
             s[j] = s[j] != s[j] ? -INFINITY : fminf(s[j], FLT_MAX) + 0.0f;      // (+ 0: -0 and 0 are one value)
         }
         key[j] = s[j] > -INFINITY ? mw_order_key(s[j]) : 0u;
@@ -82,7 +110,9 @@ __device__ __forceinline__ void select_keys(const gate_args &a, const float (&l)
         best = fmaxf(best, ob);
     }
     // A group's rank as a key; 0, behind every score, for one none of whose experts can be taken (a score can be -inf with one that can).
-    const uint32_t rank = best > -INFINITY ? mw_order_key(S > 1 ? best + second : best) : 0u;
+    // By shares the scores of the experts that can be taken count: two of a sigmoid gate, one of a softmax gate.
+    const bool one = a.by_share ? a.score != MW_GATE_SIGMOID_TOPK || !(second > -INFINITY) : S == 1;
+    const uint32_t rank = best > -INFINITY ? mw_order_key(one ? best : best + second) : 0u;
     const uint32_t mine = (uint32_t)__shfl((int)rank, min(lane * P, 63));      // lane g: group g
     int ahead = 0;
     for (int g = 0; g < G; ++g) {
@@ -246,7 +276,8 @@ int32_t gate_ready(const mw_ctx *ctx, const mw_gate *gate, const void *logits, i
     const int32_t E = ctx->cfg.n_experts;
     if (E > MW_GATE_MAX_EXPERTS) return MW_ERR_UNSUPPORTED;
     if (n_tokens > ctx->cfg.max_tokens) return MW_ERR_CAPACITY;
-    if (gate->score < MW_GATE_SOFTMAX || gate->score > MW_GATE_SIGMOID_TOPK) return MW_ERR_INVALID_ARG;
+    const int32_t score = gate->score & ~MW_GATE_BY_SHARE;
+    if (score < MW_GATE_SOFTMAX || score > MW_GATE_SIGMOID_TOPK) return MW_ERR_INVALID_ARG;
     if (format != MW_LOGITS_F32 && format != MW_LOGITS_BF16) return MW_ERR_INVALID_ARG;
     if (gate->n_groups < 1 || gate->kept_groups < 1 || gate->kept_groups > gate->n_groups || E % gate->n_groups != 0) return MW_ERR_INVALID_ARG;
     if (gate->n_groups > MW_GATE_MAX_GROUPS) return MW_ERR_UNSUPPORTED;
@@ -256,7 +287,7 @@ int32_t gate_ready(const mw_ctx *ctx, const mw_gate *gate, const void *logits, i
     if (n_tokens > 0 && (!logits || ((uintptr_t)logits & unit))) return MW_ERR_INVALID_ARG;
     a->logits = logits; a->stride = stride; a->bias = nullptr;
     a->n_tokens = n_tokens; a->n_experts = E; a->top_k = ctx->cfg.top_k;
-    a->score = gate->score; a->n_groups = gate->n_groups; a->kept = gate->kept_groups; a->scale = gate->scale;
+    a->score = score; a->by_share = gate->score != score; a->n_groups = gate->n_groups; a->kept = gate->kept_groups; a->scale = gate->scale;
     a->group_size = E / gate->n_groups;
     a->group_lanes = 1;
     while (a->group_lanes * 2 * gate->n_groups <= 64 && a->group_lanes * 2 <= a->group_size) a->group_lanes *= 2;
