@@ -35,12 +35,18 @@ __device__ __forceinline__ float load_score(const void *p, int64_t at)
 // The largest of the lanes' scores, no lower than the lowest finite value; every lane active.
 __device__ __forceinline__ float wave_top(float l) { return mw_key_value(mw_wave_max(mw_order_key(fmaxf(l, -FLT_MAX)))); }
 
-// sig(l) / exp(min(top, 0)), top the largest score taken.  Shares are quotients of these, the factor cancels; sig itself is 0 in 32 bits from l = -104
-// down and has lost bits from -87, where shares of a token whose scores are all that low still are ordinary numbers.  Below -708 sig is
-// under the smallest normal number of 64 bits and counts as 0: such scores stand for masks (-1e4, a type's lowest value).
-__device__ __forceinline__ float scaled_sigmoid(float l, float top)
+// What the experts taken weigh in a sigmoid gate, up to a factor: lane k the k-th, 0 where there is none.  That is sig(l), or, where one is below -87,
+// sig(l) / exp(min(top, 0)) with the largest score: from there down sig has lost bits in 32 bits, and from -104 down it is 0, where shares of a token
+// whose scores are all that low still are ordinary numbers.  Below -708 sig is under the smallest normal number of 64 bits and counts as 0: such
+// scores stand for masks (-1e4, a type's lowest value).  8192 tokens, top-8: 10.5 us, always divided 10.8.
+__device__ __forceinline__ float sigmoids(float l, bool taken)
 {
-    return l < -708.0f ? 0.0f : expf(fminf(l, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(l)));
+    float v = taken ? 1.0f / (1.0f + expf(-l)) : 0.0f;
+    if (__ballot(taken && l < -87.0f)) {
+        const float top = wave_top(l);
+        v = taken && l >= -708.0f ? expf(fminf(l, 0.0f) - fminf(top, 0.0f)) / (1.0f + expf(-fabsf(l))) : 0.0f;
+    }
+    return v;
 }
 
 // What selection goes by, before the bias, where the gate takes experts by their shares: sigmoids, or the softmax over all experts.  An expert
@@ -175,8 +181,7 @@ __global__ __launch_bounds__(kBlock) void k_route(gate_args a, int32_t *__restri
 
     float v, total;
     if (a.score == MW_GATE_SIGMOID_TOPK) {
-        const float top = wave_top(my_l);
-        v = my_id >= 0 ? scaled_sigmoid(my_l, top) : 0.0f;
+        v = sigmoids(my_l, my_id >= 0);
         total = mw_wave_sum_f32(v);
     } else {
         float m = my_id >= 0 ? my_l : -INFINITY;
@@ -228,8 +233,7 @@ __global__ __launch_bounds__(kBlock) void k_route_backward(gate_args a, const in
     // q: the weight before the factor; `add` goes to the expert's place
     float q, add, inv = 0.0f, m = 0.0f;
     if (a.score == MW_GATE_SIGMOID_TOPK) {
-        const float top = wave_top(my_l);
-        const float v = id >= 0 ? scaled_sigmoid(my_l, top) : 0.0f;
+        const float v = sigmoids(my_l, id >= 0);
         const float total = mw_wave_sum_f32(v);
         q = total > 0.0f ? v / total : 0.0f;
         add = q * (1.0f / (1.0f + expf(my_l)));             // (1 - sigmoid, with small ones kept)
