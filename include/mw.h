@@ -809,7 +809,7 @@ MW_API int32_t mw_route_backward(mw_ctx *ctx, const mw_gate *gate, const void *l
  *   MW_ROW_FP8_E4M3_BLOCK128  e4m3 codes in the same places, an fp32 factor per 128 x 128 block of a matrix (blocks at its edges are
  *                             smaller): gate_up_scale [local experts][2][ceil(inter/128)][ceil(hidden/128)], down_scale
  *                             [local experts][ceil(hidden/128)][ceil(inter/128)].  hidden and inter are multiples of 16.
- * Arrays contiguous, weights 16-byte aligned.
+ * Arrays contiguous, weights 16-byte aligned; all NULL on a rank without experts.
  */
 typedef struct mw_experts {
     const void *gate_up_dev;

@@ -390,7 +390,8 @@ int32_t experts_ready(const mw_ctx *ctx, const mw_experts *e)
     if (ctx->cfg.n_experts > MW_GATE_MAX_EXPERTS || ctx->cfg.row_format == MW_ROW_BYTES) return MW_ERR_UNSUPPORTED;
     const bool fp8 = e->format == MW_ROW_FP8_E4M3_BLOCK128;
     if (!fp8 && e->format != MW_ROW_BF16) return MW_ERR_INVALID_ARG;
-    if (fp8 != (e->gate_up_scale_dev != nullptr) || fp8 != (e->down_scale_dev != nullptr)) return MW_ERR_INVALID_ARG;
+    if (!fp8 && (e->gate_up_scale_dev || e->down_scale_dev)) return MW_ERR_INVALID_ARG;
+    if (fp8 && ctx->n_local > 0 && (!e->gate_up_scale_dev || !e->down_scale_dev)) return MW_ERR_INVALID_ARG;      // (a rank without experts has no arrays)
     const int32_t unit = fp8 ? 16 : 8;           // rows of whole 16-byte pieces
     if (ctx->cfg.hidden % unit != 0 || e->inter % unit != 0 || e->inter > (1 << 20)) return MW_ERR_UNSUPPORTED;
     if (ctx->n_local > 0 && (!e->gate_up_dev || !e->down_dev)) return MW_ERR_INVALID_ARG;
