@@ -368,11 +368,11 @@ _LOGIT_FORMAT = {torch.float32: MW_LOGITS_F32, torch.bfloat16: MW_LOGITS_BF16}
 
 
 def _rows(t: torch.Tensor, width: int, what: str) -> int:
-    """Elements from row to row of a matrix whose rows are in one piece each."""
+    """Elements from row to row of a matrix whose rows are in one piece each; a single row's stride says nothing and is not looked at."""
     shape = t.shape
     if len(shape) != 2 or shape[1] != width or (t.stride(1) != 1 and width > 1):
         raise ValueError("%s: rows of %d values in one piece each, got shape %s and strides %s" % (what, width, tuple(t.shape), t.stride()))
-    return t.stride(0) if shape[0] > 1 else max(t.stride(0), width)
+    return t.stride(0) if shape[0] > 1 else width
 
 
 def _whole(t: Optional[torch.Tensor], shape: tuple, dtype, what: str):
