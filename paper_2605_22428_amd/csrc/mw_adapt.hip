@@ -687,6 +687,8 @@ int32_t adapters_ready(const mw_adapters *s)
 }
 // a bf16 matrix of rows in one piece each
 bool rows_ready(const void *p, int64_t stride, int32_t width) { return p && ((uintptr_t)p & 15u) == 0 && stride >= width && stride % 8 == 0; }
+// Places in such a matrix are 32-bit, below 2^31 bytes.  (Divided: a product of any stride with the rows may pass 64 bits.)
+bool too_far(int64_t stride, int32_t rows) { return rows > 0 && stride > (1LL << 30) / rows; }
 
 order_args order_of(const mw_adapters *s, const int32_t *ids, int32_t T, char *ws, const adapt_ws &w, int tile_rows, uint32_t *flags)
 {
@@ -780,9 +782,7 @@ extern "C" MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_de
     if (((uintptr_t)h_dev | (uintptr_t)error_flags_dev | (uintptr_t)adapter_ids_dev) & 3u) return MW_ERR_INVALID_ARG;
     const adapt_ws w = adapt_layout(adapters, n_rows, false);
     if (!workspace_dev || ((uintptr_t)workspace_dev & 255u) || workspace_bytes < w.total) return MW_ERR_WORKSPACE;
-    // places in x, base and out are 32-bit, below 2^31
-    const int64_t far = 1LL << 30;
-    if (x_stride * n_rows > far || out_stride * n_rows > far || (base_dev && base_stride * n_rows > far)) return MW_ERR_UNSUPPORTED;
+    if (too_far(x_stride, n_rows) || too_far(out_stride, n_rows) || (base_dev && too_far(base_stride, n_rows))) return MW_ERR_UNSUPPORTED;
     int n_cu = 0;
     const int32_t rd = cus_of_current_device(&n_cu);
     if (rd != MW_OK) return rd;
@@ -830,8 +830,7 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
     }
     const adapt_ws w = adapt_layout(adapters, n_rows, true);
     if (!workspace_dev || ((uintptr_t)workspace_dev & 255u) || workspace_bytes < w.total) return MW_ERR_WORKSPACE;
-    const int64_t far = 1LL << 30;
-    if (x_stride * n_rows > far || dy_stride * n_rows > far || dx_stride * n_rows > far || (dx_base_dev && dx_base_stride * n_rows > far)) return MW_ERR_UNSUPPORTED;
+    if (too_far(x_stride, n_rows) || too_far(dy_stride, n_rows) || too_far(dx_stride, n_rows) || (dx_base_dev && too_far(dx_base_stride, n_rows))) return MW_ERR_UNSUPPORTED;
     int n_cu = 0;
     const int32_t rd = cus_of_current_device(&n_cu);
     if (rd != MW_OK) return rd;

@@ -429,7 +429,7 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     if (n_tokens > 0 && (!x_dev || !topk_ids_dev || !topk_weights_dev || !out_dev)) return MW_ERR_INVALID_ARG;
     // places inside an expert's matrices, the tokens and their activations are 32-bit, below 2^31
     const int64_t far = 2LL << 30, tokens = n_tokens, unit = experts->format == MW_ROW_FP8_E4M3_BLOCK128 ? 1 : 2;
-    if (2 * unit * H * I > far || 2 * x_stride * tokens > far || 2 * act_stride(I) * tokens * ctx->cfg.top_k > far) return MW_ERR_UNSUPPORTED;
+    if (2 * unit * H * I > far || (tokens > 0 && x_stride > far / 2 / tokens) || 2 * act_stride(I) * tokens * ctx->cfg.top_k > far) return MW_ERR_UNSUPPORTED;
     const layer_ws w = layer_layout(ctx, I, n_tokens);
     if (!workspace_dev || ((uintptr_t)workspace_dev & 255u) || workspace_bytes < w.total) return MW_ERR_WORKSPACE;
     if (logits_dev || gate) {
