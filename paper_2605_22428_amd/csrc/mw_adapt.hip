@@ -154,8 +154,11 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_order(order_args a)
 }
 uint32_t order_lds_bytes(int32_t n) { return (uint32_t)((n + 2) * 2 + (n + 1) * kOrderWaves) * 4; }
 
-// The order in workgroup 0; the others transpose the factors: [n][rows][cols] -> [n][cols][rows], 64 x 128 values each.
+// The order in workgroup 0; the others transpose the factors: [n][rows][cols] -> [n][cols][rows], 64 x 128 values a piece.  As many workgroups
+// as there are pieces, or kMostPieces, each then a piece every so many (a grid holds less than 2^32 threads: 1024 adapters of 262144 values have more).
 struct transpose_args { const uint16_t *in; uint16_t *out; int32_t rows, cols; };
+constexpr int64_t kMostPieces = 1 << 20;
+__host__ __device__ __forceinline__ int64_t pieces_of(const transpose_args &t) { return (int64_t)((t.rows + 63) / 64) * ((t.cols + 127) / 128); }
 __global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, transpose_args t0, transpose_args t1)
 {
     __shared__ __align__(16) char stage[kStageBytes];
@@ -165,22 +168,24 @@ __global__ __launch_bounds__(kOrderBlock) void k_adapt_prepare(order_args a, tra
         make_order(a, stage);
         return;
     }
-    int64_t at = (int64_t)blockIdx.x - 1;
-    const int64_t per0 = (int64_t)((t0.rows + 63) / 64) * ((t0.cols + 127) / 128);
-    const bool first = at < per0 * a.n;
-    const transpose_args t = first ? t0 : t1;
-    if (!first) at -= per0 * a.n;
-    const int64_t wide = (t.cols + 127) / 128, per = (int64_t)((t.rows + 63) / 64) * wide, matrix = at / per;
-    const int r0 = (int)(at % per / wide) * 64, c0 = (int)(at % wide) * 128 + (int)(threadIdx.x >> 9) * 64, i = threadIdx.x >> 3 & 63, q = (threadIdx.x & 7) * 8;
-    const int64_t base = matrix * t.rows * t.cols;
-    uint16_t (*tile)[72] = tiles[threadIdx.x >> 9];
-    if (r0 + i < t.rows && c0 + q < t.cols) *(u32x4 *)&tile[i][q] = *(const u32x4 *)(t.in + base + (int64_t)(r0 + i) * t.cols + c0 + q);
-    __syncthreads();
-    if (c0 + i < t.cols && r0 + q < t.rows) {                  // (rows and columns are multiples of 8)
-        uint32_t v[4];
+    const int64_t per0 = pieces_of(t0), all = (per0 + pieces_of(t1)) * a.n;
+    for (int64_t piece = (int64_t)blockIdx.x - 1; piece < all; piece += (int64_t)gridDim.x - 1) {
+        const bool first = piece < per0 * a.n;
+        const transpose_args t = first ? t0 : t1;
+        const int64_t at = first ? piece : piece - per0 * a.n;
+        const int64_t wide = (t.cols + 127) / 128, per = pieces_of(t), matrix = at / per;
+        const int r0 = (int)(at % per / wide) * 64, c0 = (int)(at % wide) * 128 + (int)(threadIdx.x >> 9) * 64, i = threadIdx.x >> 3 & 63, q = (threadIdx.x & 7) * 8;
+        const int64_t base = matrix * t.rows * t.cols;
+        uint16_t (*tile)[72] = tiles[threadIdx.x >> 9];
+        if (r0 + i < t.rows && c0 + q < t.cols) *(u32x4 *)&tile[i][q] = *(const u32x4 *)(t.in + base + (int64_t)(r0 + i) * t.cols + c0 + q);
+        __syncthreads();
+        if (c0 + i < t.cols && r0 + q < t.rows) {              // (rows and columns are multiples of 8)
+            uint32_t v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = tile[q + 2 * j][i] | (uint32_t)tile[q + 2 * j + 1][i] << 16;
-        *(u32x4 *)(t.out + base + (int64_t)(c0 + i) * t.rows + r0 + q) = u32x4{v[0], v[1], v[2], v[3]};
+            for (int j = 0; j < 4; ++j) v[j] = tile[q + 2 * j][i] | (uint32_t)tile[q + 2 * j + 1][i] << 16;
+            *(u32x4 *)(t.out + base + (int64_t)(c0 + i) * t.rows + r0 + q) = u32x4{v[0], v[1], v[2], v[3]};
+        }
+        __syncthreads();
     }
 }
 
@@ -839,7 +844,7 @@ extern "C" MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const v
     const order_args o = order_of(adapters, adapter_ids_dev, n_rows, ws, w, 32, error_flags_dev);
     const transpose_args ta = {(const uint16_t *)s.a_dev, (uint16_t *)(ws + w.at), s.rank, s.n_in};
     const transpose_args tb = {(const uint16_t *)s.b_dev, (uint16_t *)(ws + w.bt), s.n_out, s.rank};
-    const int64_t blocks = s.n_adapters * ((int64_t)((s.rank + 63) / 64) * ((s.n_in + 127) / 128) + (int64_t)((s.n_out + 63) / 64) * ((s.rank + 127) / 128));
+    const int64_t pieces = s.n_adapters * (pieces_of(ta) + pieces_of(tb)), blocks = pieces < kMostPieces ? pieces : kMostPieces;
     hipLaunchKernelGGL(k_adapt_prepare, dim3(n_rows > 0 ? (uint32_t)(1 + blocks) : 1u), dim3(kOrderBlock), order_lds_bytes(o.n), st, o, ta, tb);
     MW_HIP_CHECK(hipGetLastError());
     uint16_t *left[4];
