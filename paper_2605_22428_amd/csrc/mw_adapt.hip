@@ -703,16 +703,34 @@ order_args order_of(const mw_adapters *s, const int32_t *ids, int32_t T, char *w
     o.flags = flags;
     return o;
 }
-// Workgroups of k_adapt_up that a CU holds at once (by their LDS).
-int resident_up(int ranks, int tile_rows)
+// Slices of a tile's `width` columns, so that all workgroups are resident at once.
+int64_t slices(int64_t width, int64_t workgroups, int64_t tiles, int64_t least, int64_t most)
 {
-    const int work = 64 * (ranks * 2 + 16) > tile_rows * 272 ? 64 * (ranks * 2 + 16) : tile_rows * 272;
-    const int up = 160 * 1024 / (kWaves * work + 5120);
-    return up < 1 ? 1 : up < 8 ? up : 8;
+    int64_t n = workgroups / tiles;
+    const int64_t all = (width + least - 1) / least;
+    n = n < all ? n : all;
+    n = n < most ? n : most;
+    return n < 1 ? 1 : n;
+}
+// Workgroups of k_adapt_up that a CU holds at once, by their registers and LDS.
+template <int kM, int kCols>
+int resident_up()
+{
+    static const int n = [] {
+        int most = 0;
+        return hipOccupancyMaxActiveBlocksPerMultiprocessor(&most, k_adapt_up<kM, kCols>, kBlock, 0) == hipSuccess && most > 0 ? most : 1;
+    }();
+    return n;
 }
 template <int kM, int kCols>
-void launch_both(const adapt_args &p, bool few, dim3 down, dim3 up, hipStream_t st)
+void launch_both(adapt_args p, bool few, int64_t tiles, int n_cu, hipStream_t st)
 {
+    // A sixteenth more than a CU holds: `tiles` counts the most there can be, and a few that come later cost less than a slice fewer of all.  us with / without
+    // it, and by LDS alone: 8192 rows of 8 adapters, rank 32, 7168 to 4096, 66.2 / 70.4 / 66.0; 5000 of 16, rank 64, 2880 to 5120, 59.9 / 65.0 / 67.2; 2000 of 4, rank
+    // 128, 4096 to 4096, 42.6 / 46.2 / 57.9; 2443 of 8, rank 64, 7168 to 7168, 54.2 / 54.1 / 61.7.
+    const int64_t m = slices(p.n_out, (int64_t)resident_up<kM, kCols>() * n_cu * 17 / 16, tiles, 256, 4096);
+    p.out_slice = (int32_t)mw_align_up((p.n_out + m - 1) / m, 64);
+    const dim3 down((uint32_t)tiles, (uint32_t)p.n_slices), up((uint32_t)tiles, (uint32_t)((p.n_out + p.out_slice - 1) / p.out_slice));
     if (few) hipLaunchKernelGGL((k_adapt_down<kM, kCols, 4>), down, dim3(256), 0, st, p);
     else hipLaunchKernelGGL((k_adapt_down<kM, kCols, kManyWaves<kM>>), down, dim3(kManyWaves<kM> * 64), 0, st, p);
     hipLaunchKernelGGL((k_adapt_up<kM, kCols>), up, dim3(kBlock), 0, st, p);
@@ -723,28 +741,15 @@ int32_t launch_adapt(adapt_args p, const mw_adapters *s, int tile_rows, char *ws
     p.scale = s->scale_dev; p.n = s->n_adapters; p.rank = s->rank;
     p.part = (float *)(ws + w.part);
     const int64_t tiles = most_tiles(s, p.T, tile_rows);
-    // As many slices as keep all workgroups resident at once (a few more would be a second round of their own).
-    auto slices = [&](int64_t width, int64_t workgroups, int64_t least, int64_t most) {
-        int64_t n = workgroups / tiles;
-        const int64_t all = (width + least - 1) / least;
-        n = n < all ? n : all;
-        n = n < most ? n : most;
-        return n < 1 ? 1 : n;
-    };
-    const int ranks = ranks_of(p.rank);
-    const bool few = tiles * 8 <= n_cu;
-    const int64_t n = few ? slices(p.n_in, 3LL * n_cu, 1024, kMostSlices) : slices(p.n_in, n_cu, 2048, kMostSlices);      // (a wave has two spans at least)
+    const bool few = tiles * 8 <= n_cu, wide = tile_rows == 32;
+    const int64_t n = few ? slices(p.n_in, 3LL * n_cu, tiles, 1024, kMostSlices) : slices(p.n_in, n_cu, tiles, 2048, kMostSlices);      // (a wave has two spans at least)
     p.slice = (int32_t)mw_align_up((p.n_in + n - 1) / n, 64);
     p.n_slices = (p.n_in + p.slice - 1) / p.slice;
-    const int64_t m = slices(p.n_out, (int64_t)resident_up(ranks, tile_rows) * n_cu, 256, 4096);
-    p.out_slice = (int32_t)mw_align_up((p.n_out + m - 1) / m, 64);
-    const dim3 down((uint32_t)tiles, (uint32_t)p.n_slices), up((uint32_t)tiles, (uint32_t)((p.n_out + p.out_slice - 1) / p.out_slice));
-    const bool wide = tile_rows == 32;
     switch (ranks_of(p.rank)) {
-    case 16: if (wide) launch_both<1, 2>(p, few, down, up, st); else launch_both<1, 1>(p, few, down, up, st); break;
-    case 32: if (wide) launch_both<2, 2>(p, few, down, up, st); else launch_both<2, 1>(p, few, down, up, st); break;
-    case 64: if (wide) launch_both<4, 2>(p, few, down, up, st); else launch_both<4, 1>(p, few, down, up, st); break;
-    default: if (wide) launch_both<8, 2>(p, few, down, up, st); else launch_both<8, 1>(p, few, down, up, st); break;
+    case 16: if (wide) launch_both<1, 2>(p, few, tiles, n_cu, st); else launch_both<1, 1>(p, few, tiles, n_cu, st); break;
+    case 32: if (wide) launch_both<2, 2>(p, few, tiles, n_cu, st); else launch_both<2, 1>(p, few, tiles, n_cu, st); break;
+    case 64: if (wide) launch_both<4, 2>(p, few, tiles, n_cu, st); else launch_both<4, 1>(p, few, tiles, n_cu, st); break;
+    default: if (wide) launch_both<8, 2>(p, few, tiles, n_cu, st); else launch_both<8, 1>(p, few, tiles, n_cu, st); break;
     }
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
