@@ -227,6 +227,14 @@ def _stream_handle() -> int:
     return _raw_stream(torch.cuda.current_device())
 
 
+def _stream_on(device: torch.device, where: str) -> int:
+    """The same for arrays of `device`; refused where another device is current, as the calls of a context are."""
+    index = torch.cuda.current_device()
+    if index != device.index:
+        raise MwError(MW_ERR_INVALID_ARG, "%s: arrays on %s, current device %d" % (where, device, index))
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(index)
+
+
 def _stream() -> C.c_void_p:
     return C.c_void_p(_stream_handle())
 
@@ -302,7 +310,7 @@ class Experts:
         _whole(gate_up_scale, (n, 2, -(-inter // 128), -(-hidden // 128)), torch.float32, "gate_up_scale")
         _whole(down_scale, (n, -(-hidden // 128), -(-inter // 128)), torch.float32, "down_scale")
         self._held = (gate_up, down, gate_up_scale, down_scale)
-        self.n_local, self.inter, self.hidden = n, inter, hidden
+        self.n_local, self.inter, self.hidden, self.device = n, inter, hidden, gate_up.device
         self.record = MwExperts(*(_addr(t) for t in self._held), inter, MW_ROW_FP8_E4M3_BLOCK128 if fp8 else MW_ROW_BF16)
         self.address = C.addressof(self.record)
 
@@ -348,7 +356,7 @@ class Adapters:
         _whole(h, (n, self.rank), torch.float32, "h")
         _check(_native().mw_adapt(self.address, x, self._matrix(x, n, self.n_in, "x"), adapter_ids, n, base,
                                   self._matrix(base, n, self.n_out, "base"), out, self._matrix(out, n, self.n_out, "out"), h, flags,
-                                  workspace, workspace.numel() * workspace.element_size(), _stream_handle()), "mw_adapt")
+                                  workspace, workspace.numel() * workspace.element_size(), _stream_on(self.device, "mw_adapt")), "mw_adapt")
 
     def mw_adapt_backward(self, x: torch.Tensor, adapter_ids: torch.Tensor, h: torch.Tensor, dy: torch.Tensor,
                           dx_base: Optional[torch.Tensor], dx: torch.Tensor, da: torch.Tensor, db: torch.Tensor,
@@ -361,7 +369,8 @@ class Adapters:
         _check(_native().mw_adapt_backward(self.address, x, self._matrix(x, n, self.n_in, "x"), adapter_ids, n, h, dy,
                                            self._matrix(dy, n, self.n_out, "dy"), dx_base, self._matrix(dx_base, n, self.n_in, "dx_base"),
                                            dx, self._matrix(dx, n, self.n_in, "dx"), da, db, flags, workspace,
-                                           workspace.numel() * workspace.element_size(), _stream_handle()), "mw_adapt_backward")
+                                           workspace.numel() * workspace.element_size(), _stream_on(self.device, "mw_adapt_backward")),
+               "mw_adapt_backward")
 
 
 _LOGIT_FORMAT = {torch.float32: MW_LOGITS_F32, torch.bfloat16: MW_LOGITS_BF16}
@@ -488,6 +497,8 @@ class Context:
             raise ValueError("x and out: bfloat16, as many rows each")
         if (experts.n_local, experts.hidden) != (self.n_local, self.hidden):
             raise ValueError("weights of %d experts of hidden size %d, the context has %d of %d" % (experts.n_local, experts.hidden, self.n_local, self.hidden))
+        if experts.device != self.workspace.device:
+            raise ValueError("weights on %s, the context is of %s" % (experts.device, self.workspace.device))
         _check(_native().mw_moe_layer(self._h, 0 if gate is None else gate.address, logits, fmt, stride, bias, experts.address, x,
                                       _rows(x, self.hidden, "x"), n, topk_ids, topk_weights, out, _rows(out, self.hidden, "out"), flags,
                                       workspace, workspace.numel() * workspace.element_size(), _stream_handle()), "mw_moe_layer")
