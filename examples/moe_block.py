@@ -80,8 +80,7 @@ class Block:
         d_scores = torch.empty_like(scores)
         self.ctx.mw_route_backward(self.gate, scores, ids, d_weights, d_scores)
         d_y = d_y + (d_scores @ self.gate_weight.float()).bfloat16()
-        a, b, _ = self.adapters._held
-        d_x, d_a, d_b = d_y @ self.projection, torch.empty_like(a), torch.empty_like(b)
+        d_x, d_a, d_b = d_y @ self.projection, torch.empty_like(self.adapters.a), torch.empty_like(self.adapters.b)
         self.adapters.mw_adapt_backward(x, adapter_ids, h, d_y, d_x, d_x, d_a, d_b, self.adapter_workspace)
         return d_x, d_a, d_b, d_scores
 

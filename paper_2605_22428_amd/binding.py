@@ -323,14 +323,14 @@ def _workspace(n_bytes: int, device) -> torch.Tensor:
 
 class Adapters:
     """mw_adapters: low-rank adapters of one projection (include/mw.h), a [adapters][rank][n_in], b [adapters][n_out][rank]
-    bfloat16, scale [adapters] float32 or None (1)."""
+    bfloat16, scale [adapters] float32 or None (1); the calls read these tensors, `a`, `b` and `scale` of this object."""
 
     def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: Optional[torch.Tensor] = None):
         (n, rank, n_in), n_out = a.shape, b.shape[1]
         _whole(a, (n, rank, n_in), torch.bfloat16, "a")
         _whole(b, (n, n_out, rank), torch.bfloat16, "b")
         _whole(scale, (n,), torch.float32, "scale")
-        self._held = (a, b, scale)
+        self.a, self.b, self.scale = self._held = (a, b, scale)
         self.n, self.rank, self.n_in, self.n_out, self.device = n, rank, n_in, n_out, a.device
         self.record = MwAdapters(_addr(a), _addr(b), _addr(scale), n, rank, n_in, n_out)
         self.address = C.addressof(self.record)
