@@ -17,10 +17,11 @@ from paper_2605_22428_amd import binding as B  # noqa: E402
 
 
 class Block:
-    """The weights of one block on rank `rank` of `n_ranks`, random; the buffers that its calls keep using."""
+    """The weights of one block on rank `rank` of `n_ranks`, random; the buffers that its calls keep using.  by_share: the gate of a model whose
+    bias stands beside sigmoids, else beside scores; another choice of experts, so it has to be the one the weights were trained with."""
 
     def __init__(self, n_ranks=8, rank=0, n_experts=64, top_k=8, hidden=4096, inter=1024, adapter_rank=16, n_adapters=12, max_tokens=256, seed=1,
-                 device="cuda:0"):
+                 device="cuda:0", by_share=False):
         g = torch.Generator(device=device)
         g.manual_seed(seed)
 
@@ -30,7 +31,7 @@ class Block:
         place = (np.arange(n_experts) * n_ranks // n_experts).astype(np.int32)
         n_local = int((place == rank).sum())
         self.ctx = B.Context(n_ranks, n_experts, top_k, rank, hidden, B.MW_ROW_BF16, max_tokens, 0, place, device=device)
-        self.gate = B.Gate(B.MW_GATE_SIGMOID_TOPK, n_groups=n_ranks, kept_groups=max(1, n_ranks // 2), scale=2.5)
+        self.gate = B.Gate(B.MW_GATE_SIGMOID_TOPK, n_groups=n_ranks, kept_groups=max(1, n_ranks // 2), scale=2.5, by_share=by_share)
         self.gate_weight, self.gate_bias = normal(n_experts, hidden), torch.zeros(n_experts, device=device)
         self.experts = B.Experts(normal(n_local, 2, inter, hidden), normal(n_local, hidden, inter))
         self.projection = normal(hidden, hidden)

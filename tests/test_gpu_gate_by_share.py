@@ -146,3 +146,19 @@ def test_the_constant_is_the_headers():
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "mw.h")).read()
     line, = [l.split() for l in text.splitlines() if l.startswith("#define MW_GATE_BY_SHARE ")]
     assert int(line[2], 0) == B.MW_GATE_BY_SHARE
+
+
+def test_the_example_with_such_a_gate():
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("moe_block", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "moe_block.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    block = module.Block(n_ranks=4, rank=1, n_experts=16, top_k=4, hidden=256, inter=128, adapter_rank=8, n_adapters=3, max_tokens=64, by_share=True)
+    g = torch.Generator().manual_seed(1)
+    x, requests = torch.randn((40, 256), generator=g).bfloat16().to(DEV), torch.randint(-1, 3, (40,), generator=g).int().to(DEV)
+    _, ids, _ = block.decode(x, requests)
+    scores = block.route(block.project(x, requests))[0].cpu().numpy()
+    want = [taken(row, np.zeros(16), 4, 4, 2, P.SIGMOID_TOPK) for row in scores]
+    assert all(gap <= GAP or list(got) == i for got, (i, gap) in zip(ids.cpu().numpy(), want))
+    send, stats = block.prefill(x, requests)
+    assert int(stats["n_rows"]) == 40 and int(stats["error_flags"]) == 0
