@@ -829,7 +829,9 @@ MW_API int32_t mw_moe_workspace_bytes(mw_ctx *ctx, const mw_experts *experts, in
  * mw_moe_layer: this rank's share of a mixture-of-experts layer for a few tokens that it already has, without a dispatch:
  *   out[t] = sum over the token's distinct ids k that are experts of this rank (expert_to_rank) of
  *            w_k down_k (silu(gate_k x_t) * (up_k x_t)),      silu(v) = v / (1 + exp(-v))
- * in fp32 sums, rounded to bf16 once.  A token that goes to none of them gets zeros; ranks that share the experts add up their outputs.
+ * in fp32 sums, rounded to bf16 once.  Between the two products w_k silu(gate_k x_t) (up_k x_t) is held as the sum of two bf16 values, 16 bits of
+ * mantissa (an infinite weight of down_k can therefore give a NaN where one product would be infinite).  A token that goes to none of
+ * them gets zeros; ranks that share the experts add up their outputs.
  *   gate, logits_dev, logit_format, logit_stride, bias_dev: as mw_route, which is done first and writes topk_ids_dev and
  *     topk_weights_dev; with gate and logits_dev both NULL these two are read instead.  An id that a token names twice weighs the sum of both.
  *   x_dev, out_dev: bf16 rows of `hidden` values, x_stride and out_stride elements apart (multiples of 8; 16-byte aligned).  They
@@ -870,7 +872,9 @@ MW_API int32_t mw_adapt_workspace_bytes(const mw_adapters *adapters, int32_t max
 
 /*
  * mw_adapt: every row's own adapter beside the projection that all rows share.  With a = adapter_ids[t],
- *   h_t = A_a x_t (fp32),   out_t = base_t + scale_a B_a h_t, rounded to bf16 once.
+ *   h_t = A_a x_t (fp32),   out_t = base_t + B_a (scale_a h_t), rounded to bf16 once.
+ * Sums are fp32; scale_a h_t goes into its product as the sum of two bf16 values, 16 bits of mantissa (an infinite value of B can therefore
+ * give a NaN where one product would be infinite).  h_dev gets all of fp32.
  * Rows whose id is -1 have no adapter: out_t = base_t, h_t = 0.  Rows of one adapter need not stand together.
  *   x_dev, base_dev, out_dev: bf16 rows, strides in elements (multiples of 8), 16-byte aligned.  base_dev is the shared
  *     projection's output, or NULL (zeros); out_dev may be base_dev itself (with its stride), else none of them may overlap.
@@ -886,9 +890,9 @@ MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_dev, int64_t 
 
 /*
  * mw_adapt_backward: from dy, the gradient of mw_adapt's out (which is also that of base), and the h it wrote,
- *   dh_t = B_a^T dy_t,   dx_t = dx_base_t + scale_a A_a^T dh_t,
- *   dA_a = scale_a sum over a's rows of dh_t x_t^T,   dB_a = scale_a sum over a's rows of dy_t h_t^T,
- * in fp32 sums, each rounded to bf16 once.  dx_base_dev is the gradient that comes through the shared projection, or NULL; dx_dev
+ *   dh_t = B_a^T dy_t,   dx_t = dx_base_t + A_a^T (scale_a dh_t),
+ *   dA_a = sum over a's rows of (scale_a dh_t) x_t^T,   dB_a = sum over a's rows of dy_t (scale_a h_t)^T,
+ * in fp32 sums, each rounded to bf16 once; scale_a dh_t and scale_a h_t go into their products as sums of two bf16 values, as in mw_adapt.  dx_base_dev is the gradient that comes through the shared projection, or NULL; dx_dev
  * may be dx_base_dev itself.  da_dev, db_dev: laid out as a_dev and b_dev, 16-byte aligned, written whole (zeros for adapters without
  * rows).  Sums over rows have a fixed order: equal calls give equal bits.  x, dy, dx_base and dx may each span at most 2 GiB.
  */

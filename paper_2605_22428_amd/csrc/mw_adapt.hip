@@ -8,8 +8,8 @@
 // up their parts and makes a slice of y.  The gradient of the input is the same walk with the transposed factors; beside it the
 // tiles' h and dh are laid out for k_adapt_grads, which goes over an adapter's rows of x and dy once more.
 //
-// Each row of x, base and y is touched once, the factors come out of the caches: bytes bound large calls, launches and chains of round
-// trips small ones.  Measured on one MI355X: 8192 rows, 8 adapters of rank 32, 7168 to 4096 (246 MB): order 9 us, k_adapt_down 26 us (4.5
+// Forward each row of x, base and y is touched once, the factors come out of the caches: bytes bound large calls, launches and chains of round
+// trips small ones.  Backward goes over x and dy again for every 32 ranks, out of the caches where they hold them, and is bound by that.  Measured on one MI355X: 8192 rows, 8 adapters of rank 32, 7168 to 4096 (246 MB): order 9 us, k_adapt_down 26 us (4.5
 // TB/s of x), k_adapt_up 31 us (4.3 TB/s of base and y), the call 65 us.  64 rows of 24 adapters, rank 16, 7168 to 7168: 5.6 and 8.8 us,
 // the call 13.4 us.  Backward of 4096 rows, 4 adapters of rank 64, 4096 to 4096 (144 MB): prepare 8, down 16, up 31, k_adapt_grads 32 us
 // (2.1 TB/s), the call 85 us.
@@ -207,7 +207,8 @@ struct adapt_args {
     uint16_t *left_h[2], *left_dh[2];
 };
 
-// A float as a sum of two bf16 values (16 bits of mantissa).  Where it is no number or too large the first says so alone.
+// A float as a sum of two bf16 values (16 bits of mantissa).  Where it is no number or too large the first says so alone.  One value would add an
+// error as large as the results' own rounding; the second costs a matrix instruction, which kernels that wait for memory have to spare.
 __device__ __forceinline__ void split(float v, uint16_t *hi, uint16_t *lo)
 {
     *hi = mw_f32_to_bf16(v);
@@ -543,7 +544,8 @@ struct grad_args {
 
 // grid: (128 columns, adapter, side and piece of 32 ranks).  The waves take an adapter's tiles of 32 rows in turn: a tile is one
 // matrix instruction deep.  Rows of x are loaded as they lie, 256 bytes of four rows an instruction, and turned in registers: a lane has eight
-// rows of eight columns, and the columns' vectors over the rows are operands.
+// rows of eight columns, and the columns' vectors over the rows are operands.  The instance of 32 ranks has 264 registers, 96 of them sums: one
+// workgroup a CU, with nothing beside it while it waits for its loads.  That bounds it, and rows that are one workgroup's alone.
 constexpr int kGradWaves = 4;
 template <int kM>
 __global__ __launch_bounds__(kGradWaves * 64) void k_adapt_grads(grad_args p)
@@ -662,7 +664,8 @@ constexpr int kMostSlices = 8;
 constexpr int64_t kMostCus = 512;          // (rows times slices stay below rows + 128 times the CUs: a tile has at most 32 rows)
 
 // Rows of a tile: 32 where adapters have 96 rows on average, and where the gradients want tiles one matrix instruction deep; else 16.  us of
-// mw_adapt, 24 adapters of rank 16, 4096 to 4096, 16 / 32: 300 rows 18.6 / 21.9, 600 20.3 / 23.3, 1200 24.8 / 26.7, 2400 31.0 / 30.9.
+// mw_adapt, 24 adapters of rank 16, 4096 to 4096, 16 / 32: 300 rows 19.0 / 22.1, 1200 22.9 / 26.2, 2400 29.8 / 30.0; of rank 64, 7168 to 4096: 1200 37.6 /
+// 38.0, 2400 57.1 / 48.6; 40 of rank 128, 4000 rows 155 / 85.  8 of rank 32, 4096 to 7168, 800 rows 25.0 / 28.1: on the wrong side.
 int tile_rows_of(const mw_adapters *s, int64_t rows, bool backward) { return backward || rows >= 96LL * s->n_adapters ? 32 : 16; }
 int64_t most_tiles(const mw_adapters *s, int64_t rows, int tile_rows) { return rows / tile_rows + (s->n_adapters + 1LL < rows ? s->n_adapters + 1LL : rows); }
 
@@ -805,8 +808,9 @@ extern "C" MW_API int32_t mw_adapt(const mw_adapters *adapters, const void *x_de
     p.out = (uint16_t *)out_dev; p.out_stride = out_stride;
     p.h = h_dev;
     const int tile = tile_rows_of(adapters, n_rows, false);
-    // Up to 256 rows every workgroup finds its tile in the ids: a launch less.  us, so / with the order first: 1 row 10.1 / 13.0, 64 rows of 24
-    // adapters 11.6 / 15.3, 256 of 64 16.5 / 20.2 (rank 16, 4096 to 4096).
+    // Up to 256 rows every workgroup finds its tile in the ids: a launch less.  us, so / with the order first: 1 row 10.9 / 14.3, 256 of 64 adapters 17.0 /
+    // 20.3 (rank 16, 4096 to 4096); 64 of 24, rank 16, 7168 to 7168, 14.2 / 17.9; 64 of 24, rank 64, 16.9 / 20.5; 256 of 4, rank 32, 7168 to 4096, 17.0 /
+    // 20.2; 200 of 16, rank 128, 24.4 / 27.9.
     if (n_rows <= kBlock) {
         p.ids = adapter_ids_dev;
         p.flags = error_flags_dev;

@@ -456,15 +456,18 @@ extern "C" MW_API int32_t mw_moe_layer(mw_ctx *ctx, const mw_gate *gate, const v
     const bool fp8 = experts->format == MW_ROW_FP8_E4M3_BLOCK128;
     // An expert's weights are read once for up to 32 of its tokens, or (bf16) for up to 64 at half the waves a CU holds, where experts have
     // 24 tokens on average.  us, 32 / 64: 256 tokens, 8 experts, top-2, 4096 x 2048 227 / 177; 16 experts, top-2 258 / 209; 16 experts, top-4,
-    // 4096 x 1024 239 / 184.
+    // 4096 x 1024 239 / 184.  fp8 would need 272 and 423 registers for 64: the same three 166 / 169, 184 / 207, 177 / 192; 128 tokens, 32 experts,
+    // top-8, 213 / 277.
     const bool wide = !fp8 && pairs >= 24LL * a.E;
     if (fp8) hipLaunchKernelGGL((k_layer_up<true, false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     else if (wide) hipLaunchKernelGGL((k_layer_up<false, true>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     else hipLaunchKernelGGL((k_layer_up<false, false>), up, dim3(kUpWaves * 64), ids_lds, s, a);
     MW_HIP_CHECK(hipGetLastError());
-    // Up to 16 tokens the second product adds an output up over its experts; beyond, and for any batch so: pairs, then k_layer_sum.  us: 1 token, 64
-    // experts, top-8, 4096 x 1024 45.0, the other way 51.4; 4 tokens, 16 experts, top-2 39.8, 42.2; 16 tokens, top-4 77.6, 78.8; 16 tokens,
-    // 64 fp8 experts, top-8, 2048 x 512 72.7, 70.6.
+    // Up to 16 tokens the second product adds an output up over its experts; beyond it, or for any batch: pairs, then k_layer_sum.  us, this way / that
+    // way, bf16: 1 token, 64 experts, top-8, 4096 x 1024 45.2 / 49.5; 4 tokens, 16 experts, top-2 40.7 / 43.3; 16 tokens, top-4 74.7 / 77.1.  By tokens
+    // alone it is a coarse rule: over 60 sizes of 1 to 16 tokens it wins up to 20 % (1 token, top-6 of 128, 2048 x 768 18.7 / 22.6) where few experts
+    // are hit, and loses where many are or in fp8: 16 tokens, top-8 of 64, 2048 x 512 88.8 / 82.8, in fp8 71.6 / 69.7; 32 fp8 experts of 256 here, 7168 x
+    // 2048, 16 tokens 118 / 104, 2 tokens 34.5 / 30.6.
     if (n_tokens <= 16) {
         const dim3 down((uint32_t)((H + 15) / 16));
         const uint32_t lds = ids_lds + hits * 34;
