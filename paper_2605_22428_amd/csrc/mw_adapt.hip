@@ -9,10 +9,10 @@
 // tiles' h and dh are laid out for k_adapt_grads, which goes over an adapter's rows of x and dy once more.
 //
 // Forward each row of x, base and y is touched once, the factors come out of the caches: bytes bound large calls, launches and chains of round
-// trips small ones.  Backward goes over x and dy again for every 32 ranks, out of the caches where they hold them, and is bound by that.  Measured on one MI355X: 8192 rows, 8 adapters of rank 32, 7168 to 4096 (246 MB): order 9 us, k_adapt_down 26 us (4.5
-// TB/s of x), k_adapt_up 31 us (4.3 TB/s of base and y), the call 65 us.  64 rows of 24 adapters, rank 16, 7168 to 7168: 5.6 and 8.8 us,
-// the call 13.4 us.  Backward of 4096 rows, 4 adapters of rank 64, 4096 to 4096 (144 MB): prepare 8, down 16, up 31, k_adapt_grads 32 us
-// (2.1 TB/s), the call 85 us.
+// trips small ones.  Backward goes over x and dy again for every 32 ranks, out of the caches where they hold them, and is bound by that.  Measured
+// on one MI355X: 8192 rows, 8 adapters of rank 32, 7168 to 4096 (246 MB): order 9 us, k_adapt_down 26 us (4.5 TB/s of x), k_adapt_up 31 us (4.3
+// TB/s of base and y), the call 66 us.  64 rows of 24 adapters, rank 16, 7168 to 7168: 5.6 and 8.6 us, the call 13.5 us.  Backward of 4096 rows, 4
+// adapters of rank 64, 4096 to 4096 (144 MB): prepare 7.5, down 16, up 30, k_adapt_grads 32.5 us (2.1 TB/s), the call 82 to 85 us.
 #include "mw_stream.h"
 
 namespace {

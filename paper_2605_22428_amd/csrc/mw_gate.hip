@@ -4,8 +4,8 @@
 // maximum of keys that order like the scores, the lowest expert among equals.  By score and bias nothing but one float addition decides which
 // experts are taken, so the ids are the same whatever the order of the sums in the weights; by share a sigmoid or an exponential and a sum
 // decide as well, in fp32, and experts closer than their rounding may change places.  Measured on one MI355X: 8192 tokens, 256 experts in 8
-// groups, top-8 (8.9 MB) 10.4 us: eight rounds of a wave's maximum are some 700 instructions a token, which bound it, not the bytes
-// (1.3 us of them); backward of 4096 tokens (4.5 MB) 6.6 us, 5 of them the kernel.  Smaller calls are a launch, 5 to 6 us in a stream of them.
+// groups, top-8 (8.9 MB) 10.5 us: eight rounds of a wave's maximum are some 700 instructions a token, which bound it, not the bytes
+// (1.3 us of them); by share 11.6, of a softmax gate 12.7 (by score 11.1); backward of 4096 tokens (4.5 MB) 6.4 us, 5 of them the kernel.  Smaller calls are a launch, 5 to 6 us in a stream of them.
 #include <float.h>
 
 #include "mw_math.h"

@@ -6,9 +6,10 @@
 // Every weight of an expert that a token goes to has to be read once and is used for a few tokens only, so the weights' bytes bound both
 // kernels.  16 weight rows are one side of the matrix instruction and up to 16 tokens the other; whichever columns have no token cost nothing
 // that counts.  Measured on one MI355X (weights of hidden 7168, inter 2048): 256 tokens of 256 experts, 32 bf16 ones here (2.8 GB):
-// k_layer_up 295 us, 6.4 TB/s, k_layer_down 173 us, 5.4 TB/s, the layer 469 us, 6.0 TB/s (a plain copy: 6.8).  64 tokens, four fp8 experts
-// (155 MB): 44 to 50 us; k_layer_up 22 us, 5.3 TB/s, k_layer_down 17 us, 3.4 TB/s, launches and their first round trips the rest.  One
-// token, eight of 64 experts of 4096 x 1024 (201 MB): 26 us, 5.1 TB/s, and 16 us, 4.2 TB/s, the layer 44.5 us.
+// k_layer_up 295 us, 6.4 TB/s, k_layer_down 173 us, 5.4 TB/s, the layer 467 to 473 us, 6.0 TB/s (a plain copy: 6.8).  64 tokens, four fp8 experts
+// (155 MB): 44 to 50 us; k_layer_up 22 us, 4.8 TB/s, k_layer_down 15 us, 3.4 TB/s, launches and their first round trips the rest.  One
+// token, eight of 64 experts of 4096 x 1024 (201 MB): 26 us, 5.2 TB/s, and 16 us, 4.2 TB/s, the layer 45 us.  With many tokens an expert the
+// tokens' way through LDS, once for every 16 or 32 rows, takes longer than the weights: 256 tokens of 8 experts, top-2, 4096 x 2048 (403 MB) 180 us.
 #include "mw_stream.h"
 
 namespace {
