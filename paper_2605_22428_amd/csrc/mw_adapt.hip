@@ -283,7 +283,7 @@ template <int kM, int kCols, int kWaves>
 __global__ __launch_bounds__(kWaves * 64) void k_adapt_down(adapt_args p)
 {
     constexpr int kBlock = kWaves * 64;
-    constexpr int kRanks = kM * 16, kRows = kCols * 16, kDepth = kM == 1 || kWaves == 4 && kM == 2 ? 3 : 2;
+    constexpr int kRanks = kM * 16, kRows = kCols * 16, kDepth = kM == 1 || (kWaves == 4 && kM == 2) ? 3 : 2;
     constexpr int kPartBytes = kWaves * kRows * kRanks * 4, kStageBytes = kWaves * kWaveLds<kM>;
     __shared__ __align__(16) char lds[kPartBytes > kStageBytes ? kPartBytes : kStageBytes];
     __shared__ tile_rows t;
