@@ -809,15 +809,19 @@ MW_API int32_t mw_route_backward(mw_ctx *ctx, const mw_gate *gate, const void *l
  *   MW_ROW_FP8_E4M3_BLOCK128  e4m3 codes in the same places, an fp32 factor per 128 x 128 block of a matrix (blocks at its edges are
  *                             smaller): gate_up_scale [local experts][2][ceil(inter/128)][ceil(hidden/128)], down_scale
  *                             [local experts][ceil(hidden/128)][ceil(inter/128)].  hidden and inter are multiples of 16.
+ *   MW_WEIGHT_INT8_CHANNEL    (mw_ffn only) 8-bit codes in the same places, an fp32 factor per row of a matrix (output channel): gate_up_scale
+ *                             [local experts][2][inter], down_scale [local experts][hidden].  hidden and inter are multiples of 16, at most
+ *                             MW_INT8_MAX_IN.
  * Arrays contiguous, weights 16-byte aligned; all NULL on a rank without experts.
  */
+#define MW_WEIGHT_INT8_CHANNEL 3
 typedef struct mw_experts {
     const void *gate_up_dev;
     const void *down_dev;
     const float *gate_up_scale_dev;
     const float *down_scale_dev;
     int32_t inter;
-    int32_t format;         /* MW_ROW_BF16 or MW_ROW_FP8_E4M3_BLOCK128 */
+    int32_t format;         /* MW_ROW_BF16, MW_ROW_FP8_E4M3_BLOCK128 or MW_WEIGHT_INT8_CHANNEL */
 } mw_experts;               /* 40 bytes */
 
 #define MW_LAYER_MAX_TOKENS 256  /* largest batch mw_moe_layer takes */
@@ -901,6 +905,86 @@ MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const void *x_dev,
                                  const void *dx_base_dev, int64_t dx_base_stride, void *dx_dev, int64_t dx_stride,
                                  void *da_dev, void *db_dev, uint32_t *error_flags_dev, void *workspace_dev,
                                  int64_t workspace_bytes, void *stream);
+
+/* ---- products in 8-bit integers, and the experts of dispatched rows ----------------------- */
+
+#define MW_FFN_MAX_ROWS (1 << 24)
+#define MW_MAX_STRIDE   (1 << 21) /* most elements from row to row in the calls of this section: more is MW_ERR_UNSUPPORTED */
+#define MW_INT8_MAX_IN  65536     /* sums of 65536 products of two codes fit 32 bits */
+
+/*
+ * mw_quantize_rows: bf16 rows -> 8-bit codes and an fp32 scale a row.  With a the row's largest |x|:
+ *   scale = a / 127,   code = 127 x / a to the nearest whole number, halves to even
+ * (exactly: the quotient of the values, not of rounded ones).  A row of zeros gets scale 0 and codes 0; a row that holds a NaN or an infinity gets the scale
+ * NaN and codes 0, so whatever is made of it is NaN and other rows are not touched.
+ *   x_dev: n_rows rows of n_cols values, x_stride elements apart (a multiple of 8; 16-byte aligned).  codes_dev: rows of n_cols bytes, codes_stride
+ *   apart (a multiple of 16; 16-byte aligned).  scales_dev [n_rows].  n_cols is a multiple of 16, at most MW_INT8_MAX_IN.
+ * Runs on the current device; needs no context.  n_rows > MW_FFN_MAX_ROWS: MW_ERR_CAPACITY.
+ */
+MW_API int32_t mw_quantize_rows(const void *x_dev, int64_t x_stride, int64_t n_rows, int32_t n_cols, int8_t *codes_dev, int64_t codes_stride,
+                                float *scales_dev, void *stream);
+
+/* Matrices from n_in to n_out values in 8-bit codes (HOST record of device arrays): value = code * scale of its output channel. */
+typedef struct mw_matrices_int8 {
+    const int8_t *codes_dev;    /* [n_matrices][n_out][n_in], contiguous, 16-byte aligned */
+    const float *scale_dev;     /* [n_matrices][n_out] fp32 */
+    int32_t n_matrices;         /* at least 1 */
+    int32_t n_in;               /* a multiple of 16, at most MW_INT8_MAX_IN */
+    int32_t n_out;              /* a multiple of 16, at most 2^20 */
+    int32_t reserved0;
+} mw_matrices_int8;             /* 32 bytes */
+
+/*
+ * mw_matmul_int8: out_r = (sum of code products, exact) scale_r matrix scale of the column, in fp32, rounded to the output's type once.
+ *   codes_dev: n_rows rows of n_in codes, codes_stride apart (a multiple of 16; 16-byte aligned); scales_dev [n_rows]: as mw_quantize_rows makes them.
+ *   offsets_dev: [n_matrices + 1] ascending, on the device: rows offsets[m] .. offsets[m + 1] - 1 go through matrix m (what mw_unpack writes as
+ *     expert_offsets); a value outside [0, n_rows] counts as the nearest one inside.  NULL: all rows go through the only matrix.
+ *   out_dev: rows of n_out values, fp32 (MW_LOGITS_F32) or bf16 (MW_LOGITS_BF16), out_stride elements apart (a multiple of 8; 16-byte aligned);
+ *     rows of no matrix are left as they were.  Must not overlap the inputs.
+ * Runs on the current device; needs no context and no workspace.  n_rows > MW_FFN_MAX_ROWS: MW_ERR_CAPACITY.
+ */
+MW_API int32_t mw_matmul_int8(const mw_matrices_int8 *matrices, const int8_t *codes_dev, int64_t codes_stride, const float *scales_dev,
+                              const int64_t *offsets_dev, int64_t n_rows, void *out_dev, int32_t out_format, int64_t out_stride, void *stream);
+
+/* Bytes of device workspace mw_ffn (backward == 0) or mw_ffn_backward needs for up to max_rows rows. */
+MW_API int32_t mw_ffn_workspace_bytes(mw_ctx *ctx, const mw_experts *experts, int64_t max_rows, int32_t backward, int64_t *out_bytes);
+
+/*
+ * mw_ffn: the experts' gated feed-forward blocks over the rows that a dispatch brought, between mw_unpack and mw_combine_gather.  For a row r of
+ * local expert e, with silu(v) = v / (1 + exp(-v)):
+ *   g = gate_e x_r,   u = up_e x_r,   h = silu(g) u,   y_r = w_r (down_e h)
+ * in fp32 sums; h is rounded to bf16 between the two products, y once.
+ *   experts: bf16 or MW_WEIGHT_INT8_CHANNEL (fp8: MW_ERR_UNSUPPORTED).  With 8-bit experts x, and h after its rounding to bf16, are held in codes as
+ *     mw_quantize_rows makes them, and products are mw_matmul_int8's.
+ *   x_dev, y_dev: bf16 rows of `hidden` values in the order of their experts (mw_unpack's out_rows), x_stride and y_stride elements apart (multiples of 8;
+ *     16-byte aligned).  They must not overlap.
+ *   expert_offsets_dev: [local experts + 1] on the device, as mw_unpack writes it: ascending; a value outside [0, n_rows] counts as the nearest one
+ *     inside.  n_rows is the room of the arrays (mw_unpack's out_capacity_rows); rows of no expert are left as they were.
+ *   row_weights_dev [n_rows] fp32: the rows' gate weights w_r, or NULL: 1.
+ *   kept_dev [n_rows][2][inter] bf16, 16-byte aligned: g and u of every row, rounded once, for a later mw_ffn_backward; or NULL.  With 8-bit experts NULL.
+ *   workspace_dev: 256-byte aligned, mw_ffn_workspace_bytes; needs no preparation.  Calls that share one must not overlap.
+ * An expert's gate_up may span at most 2 GiB: MW_ERR_UNSUPPORTED.  n_rows > MW_FFN_MAX_ROWS: MW_ERR_CAPACITY.  Contexts of MW_ROW_BYTES have no hidden
+ * size: MW_ERR_UNSUPPORTED.
+ */
+MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const void *x_dev, int64_t x_stride, const int64_t *expert_offsets_dev,
+                      int64_t n_rows, const float *row_weights_dev, void *y_dev, int64_t y_stride, void *kept_dev,
+                      void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/*
+ * mw_ffn_backward: the gradients of mw_ffn with bf16 experts, from dy and the g and u that it kept.  With sig(g) = 1 / (1 + exp(-g)):
+ *   da = down_e^T dy_r,   dw_r = da . h,   dg = w_r da u sig(g) (1 + g (1 - sig(g))),   du = w_r da silu(g),
+ *   dx_r = gate_e^T dg + up_e^T du,   d_gate_e = sum over e's rows of dg x_r^T,   d_up_e likewise of du x_r^T,   d_down_e of dy_r (w_r h)^T
+ * in fp32 sums; dg, du and w_r h are rounded to bf16 where they go into a product, dx and the matrices' gradients once, dw_r (fp32) not at all.
+ *   x, expert_offsets, n_rows, row_weights, kept: as in mw_ffn.  dy_dev, dx_dev: rows like x and y.
+ *   dx_dev, d_gate_up_dev, d_down_dev, d_row_weights_dev: any of them may be NULL and is then not computed.  d_gate_up_dev and d_down_dev are laid out as the
+ *     weights, 16-byte aligned, written whole (zeros for experts without rows).  dx_dev and d_row_weights_dev [n_rows] are left as they were for rows
+ *     of no expert.  No output may overlap an input or another output.
+ * Sums have a fixed order: equal calls give equal bits.
+ */
+MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts, const void *x_dev, int64_t x_stride, const int64_t *expert_offsets_dev,
+                               int64_t n_rows, const float *row_weights_dev, const void *kept_dev, const void *dy_dev, int64_t dy_stride,
+                               void *dx_dev, int64_t dx_stride, void *d_gate_up_dev, void *d_down_dev, float *d_row_weights_dev,
+                               void *workspace_dev, int64_t workspace_bytes, void *stream);
 
 /* ---- simulation and measurement helpers (not part of the dispatch path) ---------------- */
 

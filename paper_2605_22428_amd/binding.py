@@ -34,7 +34,8 @@ EXPORTS = ["mw_workspace_bytes", "mw_ctx_create", "mw_ctx_destroy", "mw_plan", "
            "mw_allgather_split_point", "mw_plan_allgather_split", "mw_unpack_allgather_split",
            "mw_ctx_set_timing_events", "mw_status_string", "mw_plan_static", "mw_ctx_set_options", "mw_relay_batch",
            "mw_route", "mw_route_backward", "mw_moe_workspace_bytes", "mw_moe_layer",
-           "mw_adapt_workspace_bytes", "mw_adapt", "mw_adapt_backward"]
+           "mw_adapt_workspace_bytes", "mw_adapt", "mw_adapt_backward",
+           "mw_quantize_rows", "mw_matmul_int8", "mw_ffn_workspace_bytes", "mw_ffn", "mw_ffn_backward"]
 MW_KERNEL_PLAN_RANK, MW_KERNEL_PLAN_GROUPS, MW_KERNEL_PACK, MW_KERNEL_RECV_INDEX, MW_KERNEL_EXPAND = 0, 1, 2, 3, 4
 MW_KERNEL_AG_PACK, MW_KERNEL_AG_GATHER, MW_KERNEL_RELAY_INDEX, MW_KERNEL_RELAY_COPY = 5, 6, 7, 8
 MW_KERNEL_PLAN_PACK, MW_KERNEL_PACK_QUANT, MW_KERNEL_COMBINE = 9, 10, 11
@@ -53,6 +54,8 @@ MW_GATE_MAX_EXPERTS, MW_GATE_MAX_GROUPS = 1024, 64
 MW_LAYER_MAX_TOKENS = 256
 MW_ADAPT_MAX_ADAPTERS, MW_ADAPT_MAX_RANK, MW_ADAPT_MAX_ROWS = 1024, 128, 65536
 MW_FLAG_BAD_ADAPTER = 0x400
+MW_WEIGHT_INT8_CHANNEL = 3
+MW_FFN_MAX_ROWS, MW_MAX_STRIDE, MW_INT8_MAX_IN = 1 << 24, 1 << 21, 65536
 
 # numpy views of the ABI records (host copies)
 DESC_DTYPE = np.dtype([("mask", "<u8", (4,)), ("row_offset", "<u4"), ("row_count", "<u4"),
@@ -129,6 +132,12 @@ class MwAdapters(C.Structure):
                 ("n_in", C.c_int32), ("n_out", C.c_int32)]
 
 
+class MwMatricesInt8(C.Structure):
+    """mw_matrices_int8 (include/mw.h)."""
+    _fields_ = [("codes_dev", C.c_void_p), ("scale_dev", C.c_void_p), ("n_matrices", C.c_int32), ("n_in", C.c_int32), ("n_out", C.c_int32),
+                ("reserved0", C.c_int32)]
+
+
 class MwError(RuntimeError):
     def __init__(self, status: int, where: str):
         super().__init__("%s: %s (%d)" % (where, status_string(status), status))
@@ -163,7 +172,8 @@ _KINDS = {"mw_plan": "htittttp", "mw_pack": "htttttitttp", "mw_pack_quantize": "
           "mw_relay_packets_copy": "htttp", "mw_relay_packets_copy_index_next": "httthtltp",
           "mw_route": "hptiltittp", "mw_route_backward": "hptilttitlp",
           "mw_moe_layer": "hptiltptlitttlttlp",
-          "mw_adapt": "ptltitltltttlp", "mw_adapt_backward": "ptltittltltlttttlp"}
+          "mw_adapt": "ptltitltltttlp", "mw_adapt_backward": "ptltittltltlttttlp",
+          "mw_quantize_rows": "tllitltp", "mw_matmul_int8": "ptlttltilp", "mw_ffn": "hptltlttlttlp", "mw_ffn_backward": "hptltltttltlttttlp"}
 _calls = None
 
 
@@ -294,24 +304,26 @@ class Gate:
 
 class Experts:
     """mw_experts: the weights of a rank's experts (include/mw.h), gate_up [local experts][2][inter][hidden] and down
-    [local experts][hidden][inter], bfloat16, or float8_e4m3fn with a float32 factor per 128 x 128 block of each matrix."""
+    [local experts][hidden][inter], bfloat16, or float8_e4m3fn with a float32 factor per 128 x 128 block of each matrix, or (mw_ffn only) int8 with a
+    float32 factor per row of each matrix, gate_up_scale [local experts][2][inter] and down_scale [local experts][hidden]."""
 
     def __init__(self, gate_up: torch.Tensor, down: torch.Tensor, gate_up_scale: Optional[torch.Tensor] = None,
                  down_scale: Optional[torch.Tensor] = None):
         n, two, inter, hidden = gate_up.shape
-        fp8 = gate_up.dtype == torch.float8_e4m3fn
-        dtype = torch.float8_e4m3fn if fp8 else torch.bfloat16
+        fp8, int8 = gate_up.dtype == torch.float8_e4m3fn, gate_up.dtype == torch.int8
+        dtype = gate_up.dtype if fp8 or int8 else torch.bfloat16
         if two != 2:
             raise ValueError("gate_up: [experts][2][inter][hidden], got %s" % (tuple(gate_up.shape),))
         _whole(gate_up, (n, 2, inter, hidden), dtype, "gate_up")
         _whole(down, (n, hidden, inter), dtype, "down")
-        if fp8 != (gate_up_scale is not None) or fp8 != (down_scale is not None):
-            raise ValueError("float8 weights come with both scales, bfloat16 weights with none")
-        _whole(gate_up_scale, (n, 2, -(-inter // 128), -(-hidden // 128)), torch.float32, "gate_up_scale")
-        _whole(down_scale, (n, -(-hidden // 128), -(-inter // 128)), torch.float32, "down_scale")
+        if (fp8 or int8) != (gate_up_scale is not None) or (fp8 or int8) != (down_scale is not None):
+            raise ValueError("float8 and int8 weights come with both scales, bfloat16 weights with none")
+        _whole(gate_up_scale, (n, 2, inter) if int8 else (n, 2, -(-inter // 128), -(-hidden // 128)), torch.float32, "gate_up_scale")
+        _whole(down_scale, (n, hidden) if int8 else (n, -(-hidden // 128), -(-inter // 128)), torch.float32, "down_scale")
         self._held = (gate_up, down, gate_up_scale, down_scale)
         self.n_local, self.inter, self.hidden, self.device = n, inter, hidden, gate_up.device
-        self.record = MwExperts(*(_addr(t) for t in self._held), inter, MW_ROW_FP8_E4M3_BLOCK128 if fp8 else MW_ROW_BF16)
+        self.record = MwExperts(*(_addr(t) for t in self._held), inter,
+                                MW_ROW_FP8_E4M3_BLOCK128 if fp8 else MW_WEIGHT_INT8_CHANNEL if int8 else MW_ROW_BF16)
         self.address = C.addressof(self.record)
 
 
@@ -371,6 +383,37 @@ class Adapters:
                                            dx, self._matrix(dx, n, self.n_in, "dx"), da, db, flags, workspace,
                                            workspace.numel() * workspace.element_size(), _stream_on(self.device, "mw_adapt_backward")),
                "mw_adapt_backward")
+
+
+class MatricesInt8:
+    """mw_matrices_int8: matrices in 8-bit codes (include/mw.h), w [matrices][n_out][n_in] int8, scale [matrices][n_out] float32."""
+
+    def __init__(self, w: torch.Tensor, scale: torch.Tensor):
+        n, n_out, n_in = w.shape
+        _whole(w, (n, n_out, n_in), torch.int8, "w")
+        _whole(scale, (n, n_out), torch.float32, "scale")
+        self._held = (w, scale)
+        self.n, self.n_in, self.n_out, self.device = n, n_in, n_out, w.device
+        self.record = MwMatricesInt8(_addr(w), _addr(scale), n, n_in, n_out, 0)
+        self.address = C.addressof(self.record)
+
+    def mw_matmul_int8(self, codes: torch.Tensor, scales: torch.Tensor, offsets: Optional[torch.Tensor], out: torch.Tensor):
+        n = codes.shape[0]
+        if codes.dtype != torch.int8 or out.dtype not in _LOGIT_FORMAT or out.shape[0] != n:
+            raise ValueError("codes int8, out float32 or bfloat16, as many rows each")
+        _whole(scales, (n,), torch.float32, "scales")
+        _whole(offsets, (self.n + 1,), torch.int64, "offsets")
+        _check(_native().mw_matmul_int8(self.address, codes, _rows(codes, self.n_in, "codes"), scales, offsets, n, out, _LOGIT_FORMAT[out.dtype],
+                                        _rows(out, self.n_out, "out"), _stream_on(self.device, "mw_matmul_int8")), "mw_matmul_int8")
+
+
+def mw_quantize_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor):
+    """bfloat16 rows -> int8 codes and a float32 scale a row."""
+    if x.dtype != torch.bfloat16 or codes.dtype != torch.int8 or codes.shape != x.shape:
+        raise ValueError("x bfloat16, codes int8 of the same shape")
+    _whole(scales, (x.shape[0],), torch.float32, "scales")
+    _check(_native().mw_quantize_rows(x, _rows(x, x.shape[1], "x"), x.shape[0], x.shape[1], codes, _rows(codes, x.shape[1], "codes"), scales,
+                                      _stream_on(x.device, "mw_quantize_rows")), "mw_quantize_rows")
 
 
 _LOGIT_FORMAT = {torch.float32: MW_LOGITS_F32, torch.bfloat16: MW_LOGITS_BF16}
@@ -502,6 +545,50 @@ class Context:
         _check(_native().mw_moe_layer(self._h, 0 if gate is None else gate.address, logits, fmt, stride, bias, experts.address, x,
                                       _rows(x, self.hidden, "x"), n, topk_ids, topk_weights, out, _rows(out, self.hidden, "out"), flags,
                                       workspace, workspace.numel() * workspace.element_size(), _stream_handle()), "mw_moe_layer")
+
+    # ---- the experts of the rows that a dispatch brought ----------------------------------
+    def ffn_workspace(self, experts: Experts, max_rows: int, backward: bool = False) -> torch.Tensor:
+        """Workspace of mw_ffn, or with `backward` of mw_ffn_backward, for up to max_rows rows."""
+        need = C.c_int64(0)
+        _check(load().mw_ffn_workspace_bytes(self._h, C.byref(experts.record), C.c_int64(max_rows), C.c_int32(backward), C.byref(need)),
+               "mw_ffn_workspace_bytes")
+        return _workspace(need.value, self.device)
+
+    def _ffn_matrix(self, t: Optional[torch.Tensor], rows: int, what: str) -> int:
+        if t is None:
+            return self.hidden
+        if t.dtype != torch.bfloat16 or t.shape[0] != rows:
+            raise ValueError("%s: bfloat16 and %d rows, got %s and %s" % (what, rows, t.dtype, tuple(t.shape)))
+        return _rows(t, self.hidden, what)
+
+    def _ffn_check(self, experts: Experts, n: int, expert_offsets, row_weights, kept):
+        if (experts.n_local, experts.hidden) != (self.n_local, self.hidden):
+            raise ValueError("weights of %d experts of hidden size %d, the context has %d of %d" % (experts.n_local, experts.hidden, self.n_local, self.hidden))
+        if experts.device != self.workspace.device:
+            raise ValueError("weights on %s, the context is of %s" % (experts.device, self.workspace.device))
+        _whole(expert_offsets, (self.n_local + 1,), torch.int64, "expert_offsets")
+        _whole(row_weights, (n,), torch.float32, "row_weights")
+        _whole(kept, (n, 2, experts.inter), torch.bfloat16, "kept")
+
+    def mw_ffn(self, experts: Experts, x: torch.Tensor, expert_offsets: torch.Tensor, y: torch.Tensor, workspace: torch.Tensor,
+               row_weights: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None):
+        n = x.shape[0]
+        self._ffn_check(experts, n, expert_offsets, row_weights, kept)
+        _check(_native().mw_ffn(self._h, experts.address, x, self._ffn_matrix(x, n, "x"), expert_offsets, n, row_weights, y,
+                                self._ffn_matrix(y, n, "y"), kept, workspace, workspace.numel() * workspace.element_size(),
+                                _stream_handle()), "mw_ffn")
+
+    def mw_ffn_backward(self, experts: Experts, x: torch.Tensor, expert_offsets: torch.Tensor, kept: torch.Tensor, dy: torch.Tensor,
+                        dx: Optional[torch.Tensor], d_gate_up: Optional[torch.Tensor], d_down: Optional[torch.Tensor], workspace: torch.Tensor,
+                        row_weights: Optional[torch.Tensor] = None, d_row_weights: Optional[torch.Tensor] = None):
+        n = x.shape[0]
+        self._ffn_check(experts, n, expert_offsets, row_weights, kept)
+        _whole(d_gate_up, (self.n_local, 2, experts.inter, self.hidden), torch.bfloat16, "d_gate_up")
+        _whole(d_down, (self.n_local, self.hidden, experts.inter), torch.bfloat16, "d_down")
+        _whole(d_row_weights, (n,), torch.float32, "d_row_weights")
+        _check(_native().mw_ffn_backward(self._h, experts.address, x, self._ffn_matrix(x, n, "x"), expert_offsets, n, row_weights, kept, dy,
+                                         self._ffn_matrix(dy, n, "dy"), dx, self._ffn_matrix(dx, n, "dx"), d_gate_up, d_down, d_row_weights,
+                                         workspace, workspace.numel() * workspace.element_size(), _stream_handle()), "mw_ffn_backward")
 
     # ---- send side -----------------------------------------------------------------------
     def mw_plan(self, topk_ids: torch.Tensor, mask: torch.Tensor, perm: torch.Tensor,
