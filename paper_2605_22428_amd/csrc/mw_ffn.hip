@@ -5,68 +5,54 @@
 namespace {
 
 // ---- h = silu(x Wg^T) * (x Wu^T) --------------------------------------------------------------------------------
-struct up_args {
-    row_groups g;
-    const uint16_t *x; int64_t x_stride;
-    const uint16_t *w;                      // [n][2][I][H]
-    uint16_t *h, *kept;                     // [rows][I], [rows][2][I] or null
-    int32_t H, I, p_tiles;
-};
 // Half of a tile's columns are gate rows, half the up rows beside them: a lane then holds both values of an element.
-template <int kP, int kQ>
-__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_ffn_up(up_args a)
-{
-    typedef tile_product<kP, kQ, false, false, false> product;
-    __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
-    tile_at at;
-    if (!find_tile<kQ>(a.g, a.p_tiles, at)) return;
-    const int col0 = at.p * (kP / 2);
-    tile_feed<kP, false, false> fp;
-    tile_feed<kQ, false, false> fq;
-    fp.rows((const char *)(a.w + ((int64_t)at.e * 2 * a.I + col0) * a.H), a.H, [&](int r) {
-        const int in = r % (kP / 2), up = in / (kP / 4), col = r / (kP / 2) * (kP / 4) + tile_column(in % (kP / 4));
-        return col0 + col < a.I ? (uint32_t)(up * a.I + col) * (uint32_t)a.H * 2 : kNowhereAt;
-    });
-    fq.rows((const char *)(a.x + at.first * a.x_stride), a.H, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
-    product t;
-    t.run(fp, fq, (a.H + 63) / 64, (lds_char *)lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int j = 0; j < product::kNQ; ++j) {
-        const int row = (wave >> 1) * (kQ / 2) + j * 32 + (lane & 31);
-        if (row >= at.rows) continue;
+template <int kCols, int kRows>
+struct up_op {
+    static constexpr int kP = kCols, kQ = kRows;
+    static constexpr bool kTrP = false, kInt8 = false, kPair = true;
+    struct args {
+        row_groups g;
+        const uint16_t *x; int64_t x_stride;
+        const uint16_t *w;                      // [n][2][I][H]
+        uint16_t *h, *kept;                     // [rows][I], [rows][2][I] or null
+        float *parts;
+        int32_t K, I, p_tiles;
+    };
+    static __device__ __forceinline__ void feeds(const args &a, const tile_at &at, tile_feed<kP, false, false> &fp, tile_feed<kQ, false, false> &fq)
+    {
+        const int col0 = at.p * (kP / 2);
+        fp.rows((const char *)(a.w + ((int64_t)at.e * 2 * a.I + col0) * a.K), a.K, [&](int r) {
+            const int in = r % (kP / 2), up = in / (kP / 4), col = r / (kP / 2) * (kP / 4) + tile_column(in % (kP / 4));
+            return col0 + col < a.I ? (uint32_t)(up * a.I + col) * (uint32_t)a.K * 2 : kNowhereAt;
+        });
+        fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
+    }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const f32x16 &g, const f32x16 &u)
+    {
+        const int row = piece_row<kQ>(j);
+        if (row >= at.rows) return;
         uint16_t *h = a.h + (at.first + row) * a.I, *kept = a.kept ? a.kept + (at.first + row) * 2 * a.I : nullptr;
 #pragma unroll
-        for (int i = 0; i < product::kNP / 2; ++i)
+        for (int s = 0; s < 16; s += 8) {
+            const int col = at.p * (kP / 2) + piece_column<kP / 2>(i) + lane_half() * 16 + s;
+            if (col >= a.I) continue;
+            float gate[8], up[8], v[8];
 #pragma unroll
-            for (int s = 0; s < 16; s += 8) {
-                const int col = col0 + (wave & 1) * (kP / 4) + i * 32 + (lane >> 5) * 16 + s;
-                if (col >= a.I) continue;
-                float gate[8], up[8], v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    gate[e] = t.acc[i][j][s + e];
-                    up[e] = t.acc[i + product::kNP / 2][j][s + e];
-                    v[e] = gate[e] * tile_sigmoid(gate[e]) * up[e];
-                }
-                store_bf16<8>(h + col, v);
-                if (kept) {
-                    store_bf16<8>(kept + col, gate);
-                    store_bf16<8>(kept + a.I + col, up);
-                }
+            for (int e = 0; e < 8; ++e) {
+                gate[e] = g[s + e];
+                up[e] = u[s + e];
+                v[e] = gate[e] * tile_sigmoid(gate[e]) * up[e];
             }
+            store_bf16<8>(h + col, v);
+            if (kept) {
+                store_bf16<8>(kept + col, gate);
+                store_bf16<8>(kept + a.I + col, up);
+            }
+        }
     }
-}
+};
 
 // ---- rows times a matrix: y = w h Wd^T, dx = [dg du] [Wg; Wu] ---------------------------------------------------
-struct rows_args {
-    row_groups g;
-    const uint16_t *x; int64_t x_stride;    // [rows][K]
-    const uint16_t *w;                      // [n][N][K], kTr: [n][K][N]
-    const float *row_weights;               // or null
-    uint16_t *y; int64_t y_stride;
-    int32_t K, N, p_tiles;
-};
 template <int kP>
 __device__ __forceinline__ void columns_from(tile_feed<kP, true, false> &fp, const uint16_t *w, int col0, int K, int N)
 {
@@ -80,106 +66,103 @@ __device__ __forceinline__ void columns_from(tile_feed<kP, false, false> &fp, co
         return col0 + col < N ? (uint32_t)col * (uint32_t)K * 2 : kNowhereAt;
     });
 }
-template <int kP, int kQ, bool kTr>
-__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_ffn_rows(rows_args a)
-{
-    typedef tile_product<kP, kQ, kTr, false, false> product;
-    __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
-    tile_at at;
-    if (!find_tile<kQ>(a.g, a.p_tiles, at)) return;
-    const int col0 = at.p * kP;
-    const uint16_t *w = a.w + (int64_t)at.e * a.N * a.K;
-    tile_feed<kP, kTr, false> fp;
-    tile_feed<kQ, false, false> fq;
-    columns_from(fp, w, col0, a.K, a.N);
-    fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
-    product t;
-    t.run(fp, fq, (a.K + 63) / 64, (lds_char *)lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int j = 0; j < product::kNQ; ++j) {
-        const int row = (wave >> 1) * (kQ / 2) + j * 32 + (lane & 31);
-        if (row >= at.rows) continue;
+template <int kCols, int kRows, bool kTr>
+struct rows_op {
+    static constexpr int kP = kCols, kQ = kRows;
+    static constexpr bool kTrP = kTr, kInt8 = false, kPair = false;
+    struct args {
+        row_groups g;
+        const uint16_t *x; int64_t x_stride;    // [rows][K]
+        const uint16_t *w;                      // [n][N][K], kTr: [n][K][N]
+        const float *row_weights;               // or null
+        uint16_t *y; int64_t y_stride;
+        float *parts;
+        int32_t K, N, p_tiles;
+    };
+    static __device__ __forceinline__ void feeds(const args &a, const tile_at &at, tile_feed<kP, kTr, false> &fp, tile_feed<kQ, false, false> &fq)
+    {
+        columns_from(fp, a.w + (int64_t)at.e * a.N * a.K, at.p * kP, a.K, a.N);
+        fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
+    }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const f32x16 &t, const f32x16 &)
+    {
+        const int row = piece_row<kQ>(j);
+        if (row >= at.rows) return;
         const float weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
         uint16_t *y = a.y + (at.first + row) * a.y_stride;
+        constexpr int kPiece = kTr ? 4 : 8;
 #pragma unroll
-        for (int i = 0; i < product::kNP; ++i) {
-            constexpr int kPiece = kTr ? 4 : 8;
+        for (int s = 0; s < 16; s += kPiece) {
+            const int col = at.p * kP + piece_column<kP>(i) + (kTr ? s * 2 + lane_half() * 4 : lane_half() * 16 + s);
+            if (col >= a.N) continue;
+            float v[kPiece];
 #pragma unroll
-            for (int s = 0; s < 16; s += kPiece) {
-                const int col = col0 + (wave & 1) * (kP / 2) + i * 32 + (kTr ? s * 2 + (lane >> 5) * 4 : (lane >> 5) * 16 + s);
-                if (col >= a.N) continue;
-                float v[kPiece];
-#pragma unroll
-                for (int e = 0; e < kPiece; ++e) v[e] = a.row_weights ? weight * t.acc[i][j][s + e] : t.acc[i][j][s + e];
-                store_bf16<kPiece>(y + col, v);
-            }
+            for (int e = 0; e < kPiece; ++e) v[e] = a.row_weights ? weight * t[s + e] : t[s + e];
+            store_bf16<kPiece>(y + col, v);
         }
     }
-}
+};
 
 // ---- da = dy Wd, and what follows from it element by element ------------------------------------------------------
-struct act_args {
-    row_groups g;
-    const uint16_t *dy; int64_t dy_stride;
-    const uint16_t *down;                   // [n][H][I]
-    const float *row_weights;               // or null
-    const uint16_t *kept;                   // [rows][2][I]
-    uint16_t *act, *d_gate_up;              // [rows][I], [rows][2][I]
-    float *parts;                           // [parts][part_rows] or null: sums of da h over a wave's columns
-    int64_t part_rows;
-    int32_t H, I, p_tiles;
-};
-template <int kP, int kQ>
-__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_ffn_act(act_args a)
-{
-    typedef tile_product<kP, kQ, true, false, false> product;
-    __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
-    tile_at at;
-    if (!find_tile<kQ>(a.g, a.p_tiles, at)) return;
-    const int col0 = at.p * kP;
-    tile_feed<kP, true, false> fp;
-    tile_feed<kQ, false, false> fq;
-    fp.lines((const char *)(a.down + (int64_t)at.e * a.H * a.I + col0), a.H, (int64_t)a.I * 2, a.I - col0);
-    fq.rows((const char *)(a.dy + at.first * a.dy_stride), a.H, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.dy_stride * 2 : kNowhereAt; });
-    product t;
-    t.run(fp, fq, (a.H + 63) / 64, (lds_char *)lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int j = 0; j < product::kNQ; ++j) {
-        const int row = (wave >> 1) * (kQ / 2) + j * 32 + (lane & 31);
+template <int kCols, int kRows>
+struct act_op {
+    static constexpr int kP = kCols, kQ = kRows;
+    static constexpr bool kTrP = true, kInt8 = false, kPair = false;
+    struct args {
+        row_groups g;
+        const uint16_t *dy; int64_t dy_stride;
+        const uint16_t *down;                   // [n][H][I]
+        const float *row_weights;               // or null
+        const uint16_t *kept;                   // [rows][2][I]
+        uint16_t *act, *d_gate_up;              // [rows][I], [rows][2][I]
+        float *sums;                            // [ceil(I / 32)][rows] or null: sums of da h over 32 columns
+        float *parts;
+        int32_t K, I, p_tiles;
+    };
+    static __device__ __forceinline__ void feeds(const args &a, const tile_at &at, tile_feed<kP, true, false> &fp, tile_feed<kQ, false, false> &fq)
+    {
+        fp.lines((const char *)(a.down + (int64_t)at.e * a.K * a.I + at.p * kP), a.K, (int64_t)a.I * 2, a.I - at.p * kP);
+        fq.rows((const char *)(a.dy + at.first * a.dy_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.dy_stride * 2 : kNowhereAt; });
+    }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const f32x16 &t, const f32x16 &)
+    {
+        const int row = piece_row<kQ>(j), col0 = at.p * kP + piece_column<kP>(i);
         float sum = 0.0f;
         if (row < at.rows) {
             const float weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
             const uint16_t *kept = a.kept + (at.first + row) * 2 * a.I;
             uint16_t *act = a.act + (at.first + row) * a.I, *d = a.d_gate_up + (at.first + row) * 2 * a.I;
+            bf16x4 gate[4], up[4];
 #pragma unroll
-            for (int i = 0; i < product::kNP; ++i)
+            for (int s = 0; s < 4; ++s) {
+                const int col = col0 + s * 8 + lane_half() * 4;
+                gate[s] = col < a.I ? *(const bf16x4 *)(kept + col) : bf16x4{};
+                up[s] = col < a.I ? *(const bf16x4 *)(kept + a.I + col) : bf16x4{};
+            }
 #pragma unroll
-                for (int s = 0; s < 16; s += 4) {
-                    const int col = col0 + (wave & 1) * (kP / 2) + i * 32 + s * 2 + (lane >> 5) * 4;
-                    if (col >= a.I) continue;
-                    const bf16x4 gate = *(const bf16x4 *)(kept + col), up = *(const bf16x4 *)(kept + a.I + col);
-                    float h[4], dg[4], du[4];
+            for (int s = 0; s < 4; ++s) {
+                const int col = col0 + s * 8 + lane_half() * 4;
+                if (col >= a.I) continue;
+                float h[4], dg[4], du[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float g = (float)gate[e], u = (float)up[e], sig = tile_sigmoid(g), silu = g * sig, da = t.acc[i][j][s + e], dh = weight * da;
-                        sum += da * silu * u;
-                        h[e] = weight * silu * u;
-                        dg[e] = dh * u * (sig + silu * (1.0f - sig));
-                        du[e] = dh * silu;
-                    }
-                    store_bf16<4>(act + col, h);
-                    store_bf16<4>(d + col, dg);
-                    store_bf16<4>(d + a.I + col, du);
+                for (int e = 0; e < 4; ++e) {
+                    const float g = (float)gate[s][e], u = (float)up[s][e], sig = tile_sigmoid(g), silu = g * sig, da = t[s * 4 + e], dh = weight * da;
+                    sum += da * silu * u;
+                    h[e] = weight * silu * u;
+                    dg[e] = dh * u * (sig + silu * (1.0f - sig));
+                    du[e] = dh * silu;
                 }
+                store_bf16<4>(act + col, h);
+                store_bf16<4>(d + col, dg);
+                store_bf16<4>(d + a.I + col, du);
+            }
         }
-        if (a.parts) {
+        if (a.sums) {
             sum += __shfl_xor(sum, 32);
-            if (row < at.rows && lane < 32) a.parts[(int64_t)(at.p * 2 + (wave & 1)) * a.part_rows + at.first + row] = sum;
+            if (row < at.rows && lane_half() == 0 && col0 < a.I) a.sums[(int64_t)(col0 / 32) * a.g.n_rows + at.first + row] = sum;
         }
     }
-}
+};
 // d_row_weights: a row's sums, in the order of their columns.
 __global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, const float *parts, int n_parts, float *out)
 {
@@ -197,50 +180,65 @@ struct grads_args {
     uint16_t *out;                          // [n][M][N]
     int32_t M, N, p_tiles, q_tiles;
 };
+// Tiles of a matrix take as long as its run is: the XCDs get an eighth of every matrix's tiles each, and those of the longest run first.
 template <int kP, int kQ>
 __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_ffn_grads(grads_args a)
 {
     typedef tile_product<kP, kQ, true, true, false> product;
     __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
-    const uint32_t each = (uint32_t)a.p_tiles * (uint32_t)a.q_tiles;
-    uint32_t tile, pt, qt;
-    if (!tile_of_workgroup(each * (uint32_t)a.g.n, tile)) return;
-    const int e = (int)(tile / each);
-    tile_in_block(tile - (uint32_t)e * each, a.p_tiles, a.q_tiles, pt, qt);
-    const int q0 = (int)qt * kQ, p0 = (int)pt * kP;
+    const uint32_t each = (uint32_t)a.p_tiles * (uint32_t)a.q_tiles, per = (each + 7) / 8, at = blockIdx.x >> 3;
+    const uint32_t tile = (blockIdx.x & 7) * per + at % per;
+    int e = (int)(at / per);
+    if (tile >= each || e >= a.g.n) return;
     int64_t first, end;
+    if (a.g.n <= 64) {
+        const int lane = threadIdx.x & 63;
+        int64_t f = 0, l = 0;
+        if (lane < a.g.n) group_bounds(a.g, lane, f, l);
+        const int mine = lane < a.g.n ? (int)(l - f) : -1;
+        int place = 0;
+        for (int n = 0; n < a.g.n; ++n) {
+            const int other = __builtin_amdgcn_readlane(mine, n);
+            place += other > mine || (other == mine && n < lane);
+        }
+        e = __ffsll((unsigned long long)__ballot(lane < a.g.n && place == e)) - 1;
+    }
     group_bounds(a.g, e, first, end);
-    const int rows = (int)(end - first);
+    uint32_t pt, qt;
+    tile_in_block(tile, a.p_tiles, a.q_tiles, pt, qt);
+    const int q0 = (int)qt * kQ, p0 = (int)pt * kP, rows = (int)(end - first);
     tile_feed<kP, true, false> fp;
     tile_feed<kQ, true, false> fq;
     fp.lines((const char *)(a.p + first * a.p_stride + p0), rows, a.p_stride * 2, a.N - p0);
     fq.lines((const char *)(a.q + first * a.q_stride + q0), rows, a.q_stride * 2, a.M - q0);
     product t;
     t.run(fp, fq, (rows + 63) / 64, (lds_char *)lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint16_t *out = a.out + (int64_t)e * a.M * a.N;
 #pragma unroll
     for (int j = 0; j < product::kNQ; ++j) {
-        const int row = q0 + (wave >> 1) * (kQ / 2) + j * 32 + (lane & 31);
+        const int row = q0 + piece_row<kQ>(j);
         if (row >= a.M) continue;
 #pragma unroll
         for (int i = 0; i < product::kNP; ++i)
 #pragma unroll
             for (int s = 0; s < 16; s += 4) {
-                const int col = p0 + (wave & 1) * (kP / 2) + i * 32 + s * 2 + (lane >> 5) * 4;
+                const int col = p0 + piece_column<kP>(i) + s * 2 + lane_half() * 4;
                 if (col >= a.N) continue;
                 float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = t.acc[i][j][s + e];
+                for (int c = 0; c < 4; ++c) v[c] = t.acc[i][j][s + c];
                 store_bf16<4>(out + (int64_t)row * a.N + col, v);
             }
     }
 }
 
 // ---- entry points -----------------------------------------------------------------------------------------------------
+// The two tile sizes' arguments are alike.
+template <class To, class From> To as(const From &f) { static_assert(sizeof(To) == sizeof(From), ""); return __builtin_bit_cast(To, f); }
+constexpr int64_t kPartsBytes = 256LL * 256 * 256 * 4;          // sums of a round of the large tiles; of the small ones less
 int64_t pieces(int64_t n, int64_t each) { return (n + each - 1) / each; }
 
-struct ffn_ws { int64_t act, d_gate_up, parts, codes, scales, total; };
+struct ffn_ws { int64_t act, d_gate_up, sums, parts, codes, scales, total; };
 ffn_ws ffn_layout(const mw_experts *e, int32_t hidden, int64_t rows, bool backward)
 {
     ffn_ws w = {};
@@ -249,12 +247,13 @@ ffn_ws ffn_layout(const mw_experts *e, int32_t hidden, int64_t rows, bool backwa
     w.act = take(2 * rows * e->inter);
     if (backward) {
         w.d_gate_up = take(4 * rows * e->inter);
-        w.parts = take(4 * rows * pieces(e->inter, 64));
+        w.sums = take(4 * rows * pieces(e->inter, 32));
     }
     if (e->format == MW_WEIGHT_INT8_CHANNEL) {
         w.codes = take(rows * (hidden > e->inter ? hidden : e->inter));
         w.scales = take(4 * rows);
     }
+    if (rows > 0) w.parts = take(kPartsBytes);
     w.total = o > 0 ? o : 256;
     return w;
 }
@@ -279,44 +278,13 @@ int32_t ffn_ready(const mw_ctx *ctx, const mw_experts *e, bool backward)
 // A matrix of bf16 rows of the caller's.
 bool rows_fit(const void *p, int64_t stride, int64_t width) { return p && !((uintptr_t)p & 15u) && stride >= width && stride % 8 == 0; }
 template <int kP, int kQ>
-int32_t launch_up(up_args a, hipStream_t s)
-{
-    a.p_tiles = (int32_t)pieces(a.I, kP / 2);
-    const uint32_t grid = tile_grid(most_tiles(a.g.n_rows, a.g.n, kQ) * a.p_tiles);
-    if (!grid) return MW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((k_ffn_up<kP, kQ>), dim3(grid), dim3(kTileThreads), 0, s, a);
-    MW_HIP_CHECK(hipGetLastError());
-    return MW_OK;
-}
-template <int kP, int kQ, bool kTr>
-int32_t launch_rows(rows_args a, hipStream_t s)
-{
-    a.p_tiles = (int32_t)pieces(a.N, kP);
-    const uint32_t grid = tile_grid(most_tiles(a.g.n_rows, a.g.n, kQ) * a.p_tiles);
-    if (!grid) return MW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((k_ffn_rows<kP, kQ, kTr>), dim3(grid), dim3(kTileThreads), 0, s, a);
-    MW_HIP_CHECK(hipGetLastError());
-    return MW_OK;
-}
-template <int kP, int kQ>
-int32_t launch_act(act_args a, hipStream_t s, int *n_parts)
-{
-    a.p_tiles = (int32_t)pieces(a.I, kP);
-    const uint32_t grid = tile_grid(most_tiles(a.g.n_rows, a.g.n, kQ) * a.p_tiles);
-    if (!grid) return MW_ERR_UNSUPPORTED;
-    *n_parts = a.p_tiles * 2;
-    hipLaunchKernelGGL((k_ffn_act<kP, kQ>), dim3(grid), dim3(kTileThreads), 0, s, a);
-    MW_HIP_CHECK(hipGetLastError());
-    return MW_OK;
-}
-template <int kP, int kQ>
 int32_t launch_grads(grads_args a, hipStream_t s)
 {
     a.p_tiles = (int32_t)pieces(a.N, kP);
     a.q_tiles = (int32_t)pieces(a.M, kQ);
-    const uint32_t grid = tile_grid((int64_t)a.p_tiles * a.q_tiles * a.g.n);
-    if (!grid) return MW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), dim3(grid), dim3(kTileThreads), 0, s, a);
+    const int64_t grid = pieces((int64_t)a.p_tiles * a.q_tiles, 8) * 8 * a.g.n;
+    if (grid > 0x7ffffff0LL) return MW_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), dim3((uint32_t)grid), dim3(kTileThreads), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }
@@ -354,12 +322,12 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     char *b = (char *)workspace_dev;
     const row_groups g = {expert_offsets_dev, n_rows, ctx->n_local};
     const hipStream_t s = (hipStream_t)stream;
-    if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), s);
-    up_args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, H, I, 0};
-    rows_args d = {g, (const uint16_t *)(b + w.act), I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, I, H, 0};
+    if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), (float *)(b + w.parts), s);
     const bool large = n_rows >= 192LL * g.n;
-    rc = large ? launch_up<256, 256>(u, s) : launch_up<128, 64>(u, s);
-    if (rc == MW_OK) rc = large ? launch_rows<256, 256, false>(d, s) : launch_rows<128, 64, false>(d, s);
+    const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
+    const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
+    rc = large ? launch_tiles<up_op<256, 256>>(u, I, s) : launch_tiles<up_op<128, 64>>(as<up_op<128, 64>::args>(u), I, s);
+    if (rc == MW_OK) rc = large ? launch_tiles<rows_op<256, 256, false>>(d, H, s) : launch_tiles<rows_op<128, 64, false>>(as<rows_op<128, 64, false>::args>(d), H, s);
     return rc;
 }
 
@@ -385,20 +353,19 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
     const row_groups g = {expert_offsets_dev, n_rows, ctx->n_local};
     const hipStream_t s = (hipStream_t)stream;
     uint16_t *act = (uint16_t *)(b + w.act), *d_act = (uint16_t *)(b + w.d_gate_up);
-    float *parts = d_row_weights_dev ? (float *)(b + w.parts) : nullptr;
+    float *sums = d_row_weights_dev ? (float *)(b + w.sums) : nullptr, *parts = (float *)(b + w.parts);
     const bool large = n_rows >= 192LL * g.n;
     if (n_rows > 0) {
-        act_args a = {g, (const uint16_t *)dy_dev, dy_stride, (const uint16_t *)experts->down_dev, row_weights_dev, (const uint16_t *)kept_dev, act, d_act, parts, n_rows, H, I, 0};
-        int n_parts = 0;
-        rc = large ? launch_act<256, 256>(a, s, &n_parts) : launch_act<128, 64>(a, s, &n_parts);
+        const act_op<256, 256>::args a = {g, (const uint16_t *)dy_dev, dy_stride, (const uint16_t *)experts->down_dev, row_weights_dev, (const uint16_t *)kept_dev, act, d_act, sums, parts, H, I, 0};
+        rc = large ? launch_tiles<act_op<256, 256>>(a, I, s) : launch_tiles<act_op<128, 64>>(as<act_op<128, 64>::args>(a), I, s);
         if (rc != MW_OK) return rc;
-        if (parts) {
-            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 256)), dim3(256), 0, s, g, parts, n_parts, d_row_weights_dev);
+        if (sums) {
+            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 256)), dim3(256), 0, s, g, sums, (int)pieces(I, 32), d_row_weights_dev);
             MW_HIP_CHECK(hipGetLastError());
         }
         if (dx_dev) {
-            rows_args d = {g, d_act, 2 * (int64_t)I, (const uint16_t *)experts->gate_up_dev, nullptr, (uint16_t *)dx_dev, dx_stride, 2 * I, H, 0};
-            rc = large ? launch_rows<256, 256, true>(d, s) : launch_rows<128, 64, true>(d, s);
+            const rows_op<256, 256, true>::args d = {g, d_act, 2 * (int64_t)I, (const uint16_t *)experts->gate_up_dev, nullptr, (uint16_t *)dx_dev, dx_stride, parts, 2 * I, H, 0};
+            rc = large ? launch_tiles<rows_op<256, 256, true>>(d, H, s) : launch_tiles<rows_op<128, 64, true>>(as<rows_op<128, 64, true>::args>(d), H, s);
             if (rc != MW_OK) return rc;
         }
     }

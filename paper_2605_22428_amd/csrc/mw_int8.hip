@@ -57,98 +57,71 @@ __global__ __launch_bounds__(256) void k_quantize(quant_args a)
 }
 
 // ---- rows of codes times matrices of codes ------------------------------------------------------------------------
-struct int8_args {
-    row_groups g;
-    const int8_t *x; int64_t x_stride;
-    const float *x_scale;
-    const int8_t *w;                        // [n][N][K]; kGated: [n][2][N][K]
-    const float *w_scale;                   // [n][N]; [n][2][N]
-    const float *row_weights;               // or null
-    void *y; int64_t y_stride;              // bf16 or fp32 rows
-    int32_t K, N, p_tiles;
-};
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-// kGated: y = silu(gate) * up, columns as in k_ffn_up.
-template <int kP, int kQ, bool kGated, bool kF32>
-__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_int8(int8_args a)
-{
-    typedef tile_product<kP, kQ, false, false, true> product;
-    __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
-    tile_at at;
-    if (!find_tile<kQ>(a.g, a.p_tiles, at)) return;
-    constexpr int kHalf = kGated ? kP / 4 : kP / 2;             // columns of half the waves
-    const int col0 = at.p * 2 * kHalf;
-    const int64_t matrix = (int64_t)at.e * (kGated ? 2 : 1) * a.N;
-    tile_feed<kP, false, true> fp;
-    tile_feed<kQ, false, true> fq;
-    fp.rows((const char *)(a.w + (matrix + col0) * a.K), a.K, [&](int r) {
-        const int in = r % (kP / 2), up = in / kHalf, col = r / (kP / 2) * kHalf + tile_column(in % kHalf);
-        return col0 + col < a.N ? (uint32_t)(up * a.N + col) * (uint32_t)a.K : kNowhereAt;
-    });
-    fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride : kNowhereAt; });
-    product t;
-    t.run(fp, fq, (a.K + 127) / 128, (lds_char *)lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int j = 0; j < product::kNQ; ++j) {
-        const int row = (wave >> 1) * (kQ / 2) + j * 32 + (lane & 31);
-        if (row >= at.rows) continue;
+// kGated: y = silu(gate) * up, columns as in the bf16 experts'.
+template <int kCols, int kRows, bool kGated, bool kF32>
+struct int8_op {
+    static constexpr int kP = kCols, kQ = kRows;
+    static constexpr bool kTrP = false, kInt8 = true, kPair = kGated;
+    struct args {
+        row_groups g;
+        const int8_t *x; int64_t x_stride;
+        const float *x_scale;
+        const int8_t *w;                        // [n][N][K]; kGated: [n][2][N][K]
+        const float *w_scale;                   // [n][N]; [n][2][N]
+        const float *row_weights;               // or null
+        void *y; int64_t y_stride;              // bf16 or fp32 rows
+        float *parts;
+        int32_t K, N, p_tiles;
+    };
+    static constexpr int kHalf = kGated ? kP / 4 : kP / 2;              // columns of half the waves
+    static __device__ __forceinline__ void feeds(const args &a, const tile_at &at, tile_feed<kP, false, true> &fp, tile_feed<kQ, false, true> &fq)
+    {
+        const int col0 = at.p * 2 * kHalf;
+        fp.rows((const char *)(a.w + ((int64_t)at.e * (kGated ? 2 : 1) * a.N + col0) * a.K), a.K, [&](int r) {
+            const int in = r % (kP / 2), up = in / kHalf, col = r / (kP / 2) * kHalf + tile_column(in % kHalf);
+            return col0 + col < a.N ? (uint32_t)(up * a.N + col) * (uint32_t)a.K : kNowhereAt;
+        });
+        fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride : kNowhereAt; });
+    }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const i32x16 &t, const i32x16 &u)
+    {
+        const int row = piece_row<kQ>(j);
+        if (row >= at.rows) return;
         const float scale = a.x_scale[at.first + row], weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
-        constexpr int kN = product::kNP / (kGated ? 2 : 1);
 #pragma unroll
-        for (int i = 0; i < kN; ++i)
+        for (int s = 0; s < 16; s += 8) {
+            const int col = at.p * 2 * kHalf + piece_column<2 * kHalf>(i) + lane_half() * 16 + s;
+            if (col >= a.N) continue;
+            float v[8];
+            const float *ws = a.w_scale + (int64_t)at.e * (kGated ? 2 : 1) * a.N + col;
 #pragma unroll
-            for (int s = 0; s < 16; s += 8) {
-                const int col = col0 + (wave & 1) * kHalf + i * 32 + (lane >> 5) * 16 + s;
-                if (col >= a.N) continue;
-                float v[8];
-                const float *ws = a.w_scale + matrix + col;
-                auto value = [&](int frag, int e, f32x4 w) { return (float)t.acc[frag][j][s + e] * scale * w[e & 3]; };
-                if constexpr (kGated) {
+            for (int e = 0; e < 8; e += 4) {
+                const f32x4 w = *(const f32x4_any *)(ws + e), wu = kGated ? *(const f32x4_any *)(ws + a.N + e) : w;
 #pragma unroll
-                    for (int e = 0; e < 8; e += 4) {
-                        const f32x4 wg = *(const f32x4_any *)(ws + e), wu = *(const f32x4_any *)(ws + a.N + e);
-#pragma unroll
-                        for (int q = e; q < e + 4; ++q) {
-                            const float gate = value(i, q, wg);
-                            v[q] = gate * tile_sigmoid(gate) * value(i + kN, q, wu);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; e += 4) {
-                        const f32x4 w = *(const f32x4_any *)(ws + e);
-#pragma unroll
-                        for (int q = e; q < e + 4; ++q) v[q] = a.row_weights ? weight * value(i, q, w) : value(i, q, w);
-                    }
-                }
-                if constexpr (kF32) {
-                    float *y = (float *)a.y + (at.first + row) * a.y_stride + col;
-                    *(f32x4 *)y = f32x4{v[0], v[1], v[2], v[3]};
-                    *(f32x4 *)(y + 4) = f32x4{v[4], v[5], v[6], v[7]};
-                } else {
-                    store_bf16<8>((uint16_t *)a.y + (at.first + row) * a.y_stride + col, v);
+                for (int q = 0; q < 4; ++q) {
+                    const float value = (float)t[s + e + q] * scale * w[q];
+                    if constexpr (kGated) v[e + q] = value * tile_sigmoid(value) * ((float)u[s + e + q] * scale * wu[q]);
+                    else v[e + q] = a.row_weights ? weight * value : value;
                 }
             }
+            if constexpr (kF32) {
+                float *y = (float *)a.y + (at.first + row) * a.y_stride + col;
+                *(f32x4 *)y = f32x4{v[0], v[1], v[2], v[3]};
+                *(f32x4 *)(y + 4) = f32x4{v[4], v[5], v[6], v[7]};
+            } else {
+                store_bf16<8>((uint16_t *)a.y + (at.first + row) * a.y_stride + col, v);
+            }
+        }
     }
-}
+};
 
-int64_t pieces(int64_t n, int64_t each) { return (n + each - 1) / each; }
-
-template <int kP, int kQ, bool kGated, bool kF32>
-int32_t launch_tiles(int8_args a, hipStream_t s)
-{
-    a.p_tiles = (int32_t)pieces(a.N, kGated ? kP / 2 : kP);
-    const uint32_t grid = tile_grid(most_tiles(a.g.n_rows, a.g.n, kQ) * a.p_tiles);
-    if (!grid) return MW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((k_int8<kP, kQ, kGated, kF32>), dim3(grid), dim3(kTileThreads), 0, s, a);
-    MW_HIP_CHECK(hipGetLastError());
-    return MW_OK;
-}
 template <bool kGated, bool kF32>
-int32_t launch_int8(const int8_args &a, hipStream_t s)
+int32_t launch_int8(const typename int8_op<256, 256, kGated, kF32>::args &a, hipStream_t s)
 {
-    return a.g.n_rows >= 192LL * a.g.n ? launch_tiles<256, 256, kGated, kF32>(a, s) : launch_tiles<128, 64, kGated, kF32>(a, s);
+    typedef int8_op<128, 64, kGated, kF32> small;
+    if (a.g.n_rows >= 192LL * a.g.n) return launch_tiles<int8_op<256, 256, kGated, kF32>>(a, a.N, s);
+    return launch_tiles<small>(__builtin_bit_cast(typename small::args, a), a.N, s);
 }
 int32_t launch_quantize(const quant_args &a, hipStream_t s)
 {
@@ -160,17 +133,17 @@ int32_t launch_quantize(const quant_args &a, hipStream_t s)
 }  // namespace
 
 int32_t mw_ffn_int8(const mw_experts *experts, int32_t hidden, const void *x, int64_t x_stride, const int64_t *offsets, int32_t n_local,
-                    int64_t n_rows, const float *row_weights, void *y, int64_t y_stride, void *act, int8_t *codes, float *scales, hipStream_t s)
+                    int64_t n_rows, const float *row_weights, void *y, int64_t y_stride, void *act, int8_t *codes, float *scales, float *parts, hipStream_t s)
 {
     const int32_t I = experts->inter;
     const row_groups g = {offsets, n_rows, n_local};
     int32_t rc = launch_quantize({(const uint16_t *)x, x_stride, codes, hidden, scales, n_rows, offsets + n_local, hidden}, s);
     if (rc != MW_OK) return rc;
-    rc = launch_int8<true, false>({g, codes, hidden, scales, (const int8_t *)experts->gate_up_dev, experts->gate_up_scale_dev, nullptr, act, I, hidden, I, 0}, s);
+    rc = launch_int8<true, false>({g, codes, hidden, scales, (const int8_t *)experts->gate_up_dev, experts->gate_up_scale_dev, nullptr, act, I, parts, hidden, I, 0}, s);
     if (rc != MW_OK) return rc;
     rc = launch_quantize({(const uint16_t *)act, I, codes, I, scales, n_rows, offsets + n_local, I}, s);
     if (rc != MW_OK) return rc;
-    return launch_int8<false, false>({g, codes, I, scales, (const int8_t *)experts->down_dev, experts->down_scale_dev, row_weights, y, y_stride, I, hidden, 0}, s);
+    return launch_int8<false, false>({g, codes, I, scales, (const int8_t *)experts->down_dev, experts->down_scale_dev, row_weights, y, y_stride, parts, I, hidden, 0}, s);
 }
 
 extern "C" MW_API int32_t mw_quantize_rows(const void *x_dev, int64_t x_stride, int64_t n_rows, int32_t n_cols, int8_t *codes_dev, int64_t codes_stride,
@@ -200,7 +173,8 @@ extern "C" MW_API int32_t mw_matmul_int8(const mw_matrices_int8 *matrices, const
     if (!codes_dev || !scales_dev || !out_dev || (((uintptr_t)codes_dev | (uintptr_t)out_dev) & 15u) || ((uintptr_t)scales_dev & 3u)) return MW_ERR_INVALID_ARG;
     if (codes_stride < m->n_in || codes_stride % 16 != 0 || out_stride < m->n_out || out_stride % 8 != 0) return MW_ERR_INVALID_ARG;
     if (codes_stride > MW_MAX_STRIDE || out_stride > MW_MAX_STRIDE) return MW_ERR_UNSUPPORTED;
-    const int8_args a = {{offsets_dev, n_rows, m->n_matrices}, codes_dev, codes_stride, scales_dev, m->codes_dev, m->scale_dev, nullptr, out_dev, out_stride,
-                         m->n_in, m->n_out, 0};
-    return out_format == MW_LOGITS_F32 ? launch_int8<false, true>(a, (hipStream_t)stream) : launch_int8<false, false>(a, (hipStream_t)stream);
+    const int8_op<256, 256, false, false>::args a = {{offsets_dev, n_rows, m->n_matrices}, codes_dev, codes_stride, scales_dev, m->codes_dev, m->scale_dev, nullptr, out_dev, out_stride,
+                                                     nullptr, m->n_in, m->n_out, 0};
+    typedef int8_op<256, 256, false, true>::args wide;
+    return out_format == MW_LOGITS_F32 ? launch_int8<false, true>(__builtin_bit_cast(wide, a), (hipStream_t)stream) : launch_int8<false, false>(a, (hipStream_t)stream);
 }

@@ -1,14 +1,16 @@
 // Products of tiles that stay in registers: the experts' products over many rows.
 //
 // A workgroup of four waves makes a tile of kP columns times kQ rows of an output, one wave a quarter of it, kP / 2 by kQ / 2, in the accumulators
-// of 32 x 32 matrix instructions.  Steps of 128 bytes along the sum (64 bf16 values, 128 codes) come from memory straight into LDS, two steps' room; a step's
-// four parts go from LDS to registers one ahead of the instructions that use them.  The matrix instruction's first operand is the tile of columns (weights), so a
-// lane's results are neighbours in a row of the output.
+// of 32 x 32 matrix instructions.  Steps of 128 bytes along the sum (64 bf16 values, 128 codes) come from memory straight into LDS, two steps' room.  A step's
+// first quarter is in registers when the step begins; beside its products the other three come from LDS, then the stage is free and the step after the next is loaded into
+// it while two more quarters are multiplied, and beside the last one the next step's first quarter comes.  A load has four fifths of two steps
+// to arrive that way; with the stage free only after a step's last quarter had been read it had two fifths: 16384 x 4096, sums of 7168, 795 us instead of 740 (columns by
+// lines), 8192^3 867 instead of 792.  The matrix instruction's first operand is the tile of columns (weights), so a lane's results are neighbours in a row of the output.
 //
 // LDS holds an operand as it comes, a kilobyte a load and wave, so places change only with what each lane asks for.  Where the sum runs along the
-// operand's rows, a row is 128 bytes and its 16-byte chunks are exchanged by the row's number (chunk ^ row % 8): eight lanes of a read are on different banks.  Where it runs
+// operand's rows, a row is 128 bytes and its 16-byte chunks are exchanged by the row's number: a read of 32 rows uses all banks evenly.  Where it runs
 // across them (kTr), 64 lines of kR values are there, a line's 32-byte chunks exchanged by the line's number, and a read that transposes four lines of sixteen values makes
-// the operand.
+// the operand.  Neither has a bank conflict (counted).
 #ifndef MW_TILE_H_
 #define MW_TILE_H_
 
@@ -16,7 +18,7 @@
 
 namespace {
 
-typedef __amdgpu_buffer_rsrc_t tile_array;
+typedef u32x4 tile_array;
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -37,11 +39,22 @@ template <> struct tile_kind<true> {
     static __device__ __forceinline__ acc mma(frag a, frag b, acc c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
 
-// 16 bytes a lane from memory to LDS, the wave's kilobyte in lane order; kNowhereAt: zeros.  (The host's pass does not know these two instructions.)
+__device__ __forceinline__ int exchange(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int exchange_lines(int line) { return (line & 3) << 1; }
+
+// An array of 2 GiB whose loads past its end are zeros and cost no traffic.
+__device__ __forceinline__ tile_array tile_array_at(const char *p)
+{
+    const uint64_t a = (uint64_t)p;
+    return tile_array{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffffu, kNowhereAt, 0x00027000u};
+}
+// 16 bytes a lane from memory to LDS, the wave's kilobyte in lane order; kNowhereAt: zeros.  Written out, because the compiler lets a transposing read wait
+// for every such load on the way, whichever part of LDS it goes to.  It has no result in registers; who reads what it brings waits with tile_wait.
+// M0 is used for nothing else in these kernels.
 __device__ __forceinline__ void load_to_lds(tile_array from, lds_char *to, uint32_t at)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, at, 0, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"((uint32_t)(uintptr_t)to), "v"(at), "s"(from) : "memory");
 #endif
 }
 // Four values each of sixteen lanes, a row of sixteen to every four lanes -> every lane has its column's four.
@@ -62,6 +75,7 @@ struct tile_feed {
     int64_t step;
     int limit;                                                  // K
     int lane_k;
+    int piece0;                                                 // byte of the wave's first piece
     uint32_t at[kPieces];
     // kTr == false: place(r) gives the byte of row r of the tile, or kNowhereAt
     template <class F>
@@ -69,8 +83,8 @@ struct tile_feed {
     {
         static_assert(!kTr, "");
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-        base = from; step = kStep; limit = k;
-        const int chunk = (lane & 7) ^ (lane >> 3);
+        base = from; step = kStep; limit = k; piece0 = wave * 1024;
+        const int chunk = (lane & 7) ^ exchange((wave & 1) * 8 + (lane >> 3));
         lane_k = chunk * (kInt8 ? 16 : 8);
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
@@ -82,23 +96,29 @@ struct tile_feed {
     {
         static_assert(kTr && !kInt8, "");
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-        base = from; step = 64 * stride_bytes; limit = k;
+        base = from; step = 64 * stride_bytes; limit = k; piece0 = wave * 1024;
         lane_k = wave * kLines + lane / (kR / 8);
         const int u = lane % (kR / 8);
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-            const int kk = lane_k + j * kTileWaves * kLines, s = ((kk & 3) | ((kk >> 3) & 1) << 2) & (kR / 16 - 1);
+            const int kk = lane_k + j * kTileWaves * kLines, s = exchange_lines(kk) & (kR / 16 - 1);
             const int mn = ((u >> 1) ^ s) * 16 + (u & 1) * 8;
             at[j] = mn < width ? (uint32_t)kk * (uint32_t)stride_bytes + 2u * (uint32_t)mn : kNowhereAt;
         }
+    }
+    // Steps first .. first + n - 1 only.
+    __device__ __forceinline__ void part(int first, int n)
+    {
+        constexpr int kEach = kTr ? 64 : kStep / (kInt8 ? 1 : 2);
+        base += (int64_t)first * step;
+        limit = min(limit - first * kEach, n * kEach);
     }
     // What step k's loads share, and one of them (of kPieces).
     struct step_of { tile_array r; int left; lds_char *to; };
     __device__ __forceinline__ step_of at_step(int k, lds_char *to) const
     {
-        const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-        return step_of{__builtin_amdgcn_make_buffer_rsrc((void *)(base + (int64_t)k * step), 0, (int)kNowhereAt, 0x00027000),
-                       limit - k * (kTr ? 64 : kStep / (kInt8 ? 1 : 2)), to + wave * 1024};
+        return step_of{tile_array_at(base + (int64_t)k * step),
+                       limit - k * (kTr ? 64 : kStep / (kInt8 ? 1 : 2)), to + piece0};
     }
     __device__ __forceinline__ void issue(const step_of &s, int j) const
     {
@@ -124,14 +144,14 @@ struct tile_frags {
         const int lane = threadIdx.x & 63;
         if constexpr (!kTr) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) from[kk] = (uint32_t)(half * (kR / 2) + (lane & 31)) * kStep + (((kk * 2 + (lane >> 5)) ^ (lane & 7)) * 16);
+            for (int kk = 0; kk < 4; ++kk) from[kk] = (uint32_t)(half * (kR / 2) + (lane & 31)) * kStep + (((kk * 2 + (lane >> 5)) ^ exchange(lane & 15)) * 16);
         } else {
             // sixteen lanes take four rows of 16 values: row (lane / 4) % 4, values (lane % 4) * 4 ..; the rows' 32-byte chunks change places with the row
             const int k = (lane >> 5) * 8 + ((lane >> 2) & 3), chunk = half * (kR / 32) + ((lane >> 4) & 1);
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
                 // (k + 4 and k + 16 have the same two bits: one place for each of the piece's two reads and of the four steps)
-                const int s = ((k & 3) | ((k >> 3) & 1) << 2) & (kR / 16 - 1);
+                const int s = exchange_lines(k) & (kR / 16 - 1);
                 from[kk] = (uint32_t)(k * kR * 2 + (chunk ^ s) * 32 + (lane & 3) * 8);
             }
         }
@@ -153,20 +173,24 @@ __device__ __forceinline__ void tile_barrier()
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
-template <int kN> __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt((kN & 15) | (kN >> 4) << 14 | 0x0f70); }
-
-// kN times: one read of LDS, kM matrix instructions; whatever is left of them after that.
-template <int kReads, int kLoads, int kMfma>
-__device__ __forceinline__ void tile_mix()
+// Until at most kN of this wave's loads are on the way; kReads: and all its reads of LDS are done.
+template <int kN, bool kReads = false>
+__device__ __forceinline__ void tile_wait()
 {
-#pragma unroll
-    for (int n = 0; n < kMfma; ++n) {
-        if (n < kLoads) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
-        if (n < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (kReads) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(kN) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kN) : "memory");
+#endif
 }
+
+__device__ __forceinline__ void tile_reads_done()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+#endif
+    tile_barrier();
+}
+
 template <int kP, int kQ, bool kTrP, bool kTrQ, bool kInt8>
 struct tile_product {
     typedef tile_kind<kInt8> kind;
@@ -180,49 +204,72 @@ struct tile_product {
         tile_frags<kQ, kTrQ, kInt8> fq;
         fp.begin(wave & 1);
         fq.begin(wave >> 1);
-        frag a[2][kNP], b[2][kNQ];
-        auto read = [&](int set, const lds_char *stage, int kk, int n) {
-            if (n < kNP) a[set][n] = fp.read(stage, kk, n);
-            else b[set][n - kNP] = fq.read(stage + kP * kStep, kk, n - kNP);
+        frag a[4][kNP], b[4][kNQ];
+        auto read = [&](const lds_char *stage, int kk, int n) {
+            if (n < kNP) a[kk][n] = fp.read(stage, kk, n);
+            else b[kk][n - kNP] = fq.read(stage + kP * kStep, kk, n - kNP);
         };
-        auto multiply = [&](int set, int n) {
+        auto multiply = [&](int kk, int n) {
             const int i = n / kNQ, j = n % kNQ;
-            acc[i][j] = kind::mma(a[set][i], b[set][j], acc[i][j]);
+            acc[i][j] = kind::mma(a[kk][i], b[kk][j], acc[i][j]);
         };
-        constexpr int kReads = kNP + kNQ, kMfma = kNP * kNQ, kInstr = kNP * (kTrP ? 2 : 1) + kNQ * (kTrQ ? 2 : 1);
+        constexpr int kReads = kNP + kNQ, kMfma = kNP * kNQ;
 #pragma unroll
         for (int n = 0; n < kMfma; ++n) acc[n / kNQ][n % kNQ] = typename kind::acc{};
         p.issue_all(0, lds); q.issue_all(0, lds + kP * kStep);
         p.issue_all(1, lds + kStage); q.issue_all(1, lds + kStage + kP * kStep);
-        wait_loads<kLoads>();
+        tile_wait<kLoads>();
         tile_barrier();
 #pragma unroll
-        for (int n = 0; n < kReads; ++n) read(0, lds, 0, n);
+        for (int n = 0; n < kReads; ++n) read(lds, 0, n);
         for (int k = 0; k < steps; ++k) {
             lds_char *here = lds + (k & 1) * kStage, *next = lds + ((k + 1) & 1) * kStage;
+            // the step's other three parts come to registers beside the first part's products, in the first three quarters of them
+            constexpr int kEarly = (kMfma * 3 + 3) / 4;
 #pragma unroll
-            for (int kk = 0; kk < 3; ++kk) {
+            for (int n = 0; n < kMfma; ++n) {
 #pragma unroll
-                for (int n = 0; n < kReads; ++n) read((kk + 1) & 1, here, kk + 1, n);
-#pragma unroll
-                for (int n = 0; n < kMfma; ++n) multiply(kk & 1, n);
-                tile_mix<kInstr, 0, kMfma>();
+                for (int r = n * 3 * kReads / kEarly; r < (n + 1) * 3 * kReads / kEarly; ++r)
+                    if (r < 3 * kReads) read(here, 1 + r / kReads, r % kReads);
+                multiply(0, n);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_s_waitcnt(0x0070);         // this wave has read its last of this stage, and its part of the next one is there
-            tile_barrier();
+            tile_reads_done();                          // every wave has read this stage: it is loaded again, for the step after the next
             const auto sp = p.at_step(k + 2, here);
             const auto sq = q.at_step(k + 2, here + kP * kStep);
-            constexpr int kSlots = kLoads > kMfma ? kLoads : kMfma;
 #pragma unroll
-            for (int n = 0; n < kSlots; ++n) {
-                if (n < kReads) read(0, next, 0, n);
-                if (n < kP / 32) p.issue(sp, n);
-                else if (n < kLoads) q.issue(sq, n - kP / 32);
-                if (n < kMfma) multiply(1, n);
+            for (int n = 0; n < 2 * kMfma; ++n) {
+#pragma unroll
+                for (int l = n * kLoads / (2 * kMfma); l < (n + 1) * kLoads / (2 * kMfma); ++l) {
+                    if (l < kP / 32) p.issue(sp, l);
+                    else q.issue(sq, l - kP / 32);
+                }
+                multiply(1 + n / kMfma, n % kMfma);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            tile_wait<kLoads>();                        // the next step's loads, every wave's
+            tile_barrier();
+#pragma unroll
+            for (int n = 0; n < kMfma; ++n) {
+#pragma unroll
+                for (int r = n * kReads / kEarly; r < (n + 1) * kReads / kEarly; ++r)
+                    if (r < kReads) read(next, 0, r);
+                multiply(3, n);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        wait_loads<0>();
+        tile_wait<0>();
+        stay();
+    }
+    // The accumulators stay where the matrix instructions left them until a piece is used: brought to ordinary registers together, they are spilled.
+    __device__ __forceinline__ void stay()
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        if constexpr (kNP * kNQ == 16) {
+#pragma unroll
+            for (int n = 0; n < kNP * kNQ; ++n) asm volatile("" : "+a"(acc[n / kNQ][n % kNQ]));
+        }
+#endif
     }
 };
 
@@ -244,66 +291,187 @@ struct tile_at {
     int rows;                   // rows of the run from there on (at least one)
     int p;                      // tile of columns
 };
-// Runs of consecutive tiles go to one of the eight XCDs each, whose L2 then holds what they share.  Workgroups are dealt out to XCDs in turn.
-__device__ __forceinline__ bool tile_of_workgroup(uint32_t total, uint32_t &t)
+// Work is cut into units: a whole tile, or a part of a tile's sum.  kRound workgroups run at a time, so T tiles of one duration take ceil(T / kRound) rounds; the tiles of
+// a last round that is at most half full are cut into as many parts as fill it.  The parts' sums go to memory, and k_join adds them up in their order.
+struct tile_split { uint32_t whole, rest, parts; };             // tiles in one piece, tiles in parts, parts of each (1: rest are in one piece too)
+constexpr uint32_t kMostParts = 16;
+__device__ __forceinline__ tile_split split_tiles(uint32_t total, uint32_t round, uint32_t steps, uint32_t least_steps, bool may)
 {
-    const uint32_t per = (total + 7) / 8, at = blockIdx.x >> 3;
-    t = (blockIdx.x & 7) * per + at;
-    return at < per && t < total;
+    tile_split s = {total - total % round, total % round, 1};
+    if (may && s.rest > 0) s.parts = max(1u, min(min(round / s.rest, kMostParts), steps / least_steps));
+    return s;
 }
-// Inside a run (or matrix) tiles go down kBlock tiles of rows before the next tile of columns.
-constexpr uint32_t kBlock = 8;
+struct tile_unit { uint32_t tile, part; };
+// Runs of consecutive units go to one of the eight XCDs each, whose L2 then holds what they share.  Workgroups are dealt out to XCDs in turn.
+__device__ __forceinline__ bool unit_of_workgroup(const tile_split &s, tile_unit &u)
+{
+    uint32_t id = blockIdx.x;
+    const bool whole = id < s.whole;
+    if (!whole) id -= s.whole;                                  // (a multiple of eight)
+    const uint32_t n = whole ? s.whole : s.rest * s.parts, per = (n + 7) / 8, at = id >> 3, t = (id & 7) * per + at;
+    if (at >= per || t >= n) return false;
+    u.part = whole ? 0 : t / s.rest;
+    u.tile = whole ? t : s.whole + t % s.rest;
+    return true;
+}
+// Inside a run (or matrix) tiles go down kBlock tiles of rows before the next tile of columns.  us, 4 / 8 / 16: 8192^3 codes 465 / 600 / 704, bf16 805 / 816 / 865.
+constexpr uint32_t kBlock = 4;
 __device__ __forceinline__ void tile_in_block(uint32_t t, uint32_t p_tiles, uint32_t q_tiles, uint32_t &p, uint32_t &q)
 {
     const uint32_t block = t / (kBlock * p_tiles), left = t - block * kBlock * p_tiles, high = min(kBlock, q_tiles - block * kBlock);
     p = left / high;
     q = block * kBlock + left % high;
 }
+// The runs' tiles of kQ rows, one run a lane; the first 64 stay in registers.
 template <int kQ>
-__device__ __forceinline__ bool find_tile(const row_groups &g, uint32_t p_tiles, tile_at &at)
+struct tile_runs {
+    int64_t first, end;
+    uint32_t tiles, total;
+    __device__ __forceinline__ void load(const row_groups &g, int c)
+    {
+        const int e = c + (int)(threadIdx.x & 63);
+        first = end = 0;
+        if (e < g.n) group_bounds(g, e, first, end);
+        tiles = (uint32_t)((end - first + kQ - 1) / kQ);
+    }
+    __device__ __forceinline__ void count(const row_groups &g)
+    {
+        total = 0;
+        for (int c = (g.n - 1) / 64 * 64; c >= 0; c -= 64) {
+            load(g, c);
+            total += mw_wave_sum(tiles);
+        }
+    }
+    // Tile t of p_tiles for each tile of rows, after count().
+    __device__ __forceinline__ bool find(const row_groups &g, uint32_t p_tiles, uint32_t t, tile_at &at)
+    {
+        uint32_t before = 0;
+        const uint32_t want = t / p_tiles;
+        for (int c = 0; c < g.n; c += 64) {
+            if (c > 0) load(g, c);
+            const uint32_t incl = before + mw_wave_incl_scan(tiles);
+            const uint64_t behind = __ballot(incl > want);
+            if (behind == 0) {
+                before = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+                continue;
+            }
+            const int l = __ffsll((unsigned long long)behind) - 1;
+            const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)tiles, l), start = (uint32_t)__builtin_amdgcn_readlane((int)incl, l) - mine;
+            const int64_t f = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)first, l) |
+                                        (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(first >> 32), l) << 32);
+            const int rows = __builtin_amdgcn_readlane((int)(end - first), l);
+            uint32_t p, q;
+            tile_in_block(t - start * p_tiles, p_tiles, mine, p, q);
+            at.e = c + l; at.first = f + (int64_t)q * kQ; at.rows = rows - (int)q * kQ; at.p = (int)p;
+            return true;
+        }
+        return false;
+    }
+};
+
+// A product's kernels.  Op has: args (with g, p_tiles, K and parts, memory for kRound tiles' sums or null); kP, kQ, kTrP, kInt8; kPair: pieces i and i + half of a wave's
+// columns are used together; feeds(): what is loaded; emit(): what becomes of a piece of 32 columns and 32 rows, a lane's sixteen sums.
+template <class Op>
+struct tile_op : Op {
+    typedef tile_product<Op::kP, Op::kQ, Op::kTrP, false, Op::kInt8> product;
+    typedef typename product::kind::acc acc;
+    // Workgroups that run at a time: LDS holds one of the large tiles a CU, three of the small ones.
+    static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : 768, kLeastSteps = 8;
+    static constexpr int kNP = product::kNP, kNQ = product::kNQ, kPieces = kNP * kNQ, kEmits = Op::kPair ? kPieces / 2 : kPieces;
+    static constexpr int64_t kTileBytes = (int64_t)Op::kP * Op::kQ * 4;
+    static __device__ __forceinline__ int steps(const typename Op::args &a) { return (a.K + (Op::kInt8 ? 127 : 63)) / (Op::kInt8 ? 128 : 64); }
+    static __device__ __forceinline__ acc *place(const typename Op::args &a, uint32_t slot, int piece)
+    {
+        return (acc *)((char *)a.parts + slot * kTileBytes) + piece * kTileThreads + threadIdx.x;
+    }
+};
+template <class Op>
+__global__ __launch_bounds__(kTileThreads, Op::kP * Op::kQ > 128 * 128 ? 1 : 2) void k_tiles(typename Op::args a)
 {
-    const int lane = threadIdx.x & 63;
-    int64_t first = 0, end = 0;
-    if (lane < g.n) group_bounds(g, lane, first, end);
-    uint32_t tiles = (uint32_t)((end - first + kQ - 1) / kQ), total = mw_wave_sum(tiles);
-    for (int c = 64; c < g.n; c += 64) {
-        int64_t f = 0, l = 0;
-        if (c + lane < g.n) group_bounds(g, c + lane, f, l);
-        total += mw_wave_sum((uint32_t)((l - f + kQ - 1) / kQ));
+    typedef tile_op<Op> op;
+    typedef typename op::product product;
+    __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
+    tile_runs<Op::kQ> runs;
+    runs.count(a.g);
+    const int steps = op::steps(a);
+    const tile_split split = split_tiles(runs.total * (uint32_t)a.p_tiles, op::kRound, (uint32_t)steps, op::kLeastSteps, a.parts != nullptr);
+    tile_unit u;
+    tile_at at;
+    if (!unit_of_workgroup(split, u) || !runs.find(a.g, (uint32_t)a.p_tiles, u.tile, at)) return;
+    tile_feed<Op::kP, Op::kTrP, Op::kInt8> fp;
+    tile_feed<Op::kQ, false, Op::kInt8> fq;
+    Op::feeds(a, at, fp, fq);
+    const bool part = u.tile >= split.whole && split.parts > 1;
+    const int k0 = part ? (int)(u.part * (uint32_t)steps / split.parts) : 0, n = (part ? (int)((u.part + 1) * (uint32_t)steps / split.parts) : steps) - k0;
+    if (part) {
+        fp.part(k0, n);
+        fq.part(k0, n);
     }
-    uint32_t t;
-    if (!tile_of_workgroup(total * p_tiles, t)) return false;
-    uint32_t before = 0;
-    const uint32_t want = t / p_tiles;
-    for (int c = 0;; c += 64) {
-        if (c > 0) {
-            first = end = 0;
-            if (c + lane < g.n) group_bounds(g, c + lane, first, end);
-            tiles = (uint32_t)((end - first + kQ - 1) / kQ);
+    product t;
+    t.run(fp, fq, n, (lds_char *)lds);
+    const uint32_t slot = u.part * split.rest + u.tile - split.whole;
+    constexpr int kHalf = Op::kPair ? op::kNP / 2 : op::kNP;
+#pragma unroll
+    for (int j = 0; j < op::kNQ; ++j)
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+            const int second = Op::kPair ? i + kHalf : i;
+            if (part) {
+                *op::place(a, slot, i * op::kNQ + j) = t.acc[i][j];
+                if constexpr (Op::kPair) *op::place(a, slot, second * op::kNQ + j) = t.acc[second][j];
+            } else {
+                Op::emit(a, at, i, j, t.acc[i][j], t.acc[second][j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);          // (a piece at a time: all of them at once take more registers than there are)
         }
-        const uint32_t incl = before + mw_wave_incl_scan(tiles);
-        const uint64_t behind = __ballot(incl > want);
-        if (behind == 0) {
-            before = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
-            continue;
-        }
-        const int l = __ffsll((unsigned long long)behind) - 1;
-        const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)tiles, l), start = (uint32_t)__builtin_amdgcn_readlane((int)incl, l) - mine;
-        const int64_t f = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)first, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(first >> 32), l) << 32);
-        const int rows = __builtin_amdgcn_readlane((int)(end - first), l);
-        uint32_t p, q;
-        tile_in_block(t - start * p_tiles, p_tiles, mine, p, q);
-        at.e = c + l; at.first = f + (int64_t)q * kQ; at.rows = rows - (int)q * kQ; at.p = (int)p;
-        return true;
+}
+// grid: (pieces of a tile, tiles in parts at most)
+template <class Op>
+__global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
+{
+    typedef tile_op<Op> op;
+    tile_runs<Op::kQ> runs;
+    runs.count(a.g);
+    const tile_split split = split_tiles(runs.total * (uint32_t)a.p_tiles, op::kRound, (uint32_t)op::steps(a), op::kLeastSteps, true);
+    tile_at at;
+    if (split.parts == 1 || blockIdx.y >= split.rest || !runs.find(a.g, (uint32_t)a.p_tiles, split.whole + blockIdx.y, at)) return;
+    constexpr int kHalf = Op::kPair ? op::kNP / 2 : op::kNP;
+    const int i = (int)blockIdx.x / op::kNQ, j = (int)blockIdx.x % op::kNQ, second = Op::kPair ? i + kHalf : i;
+    typename op::acc v = *op::place(a, blockIdx.y, i * op::kNQ + j), w = v;
+    if constexpr (Op::kPair) w = *op::place(a, blockIdx.y, second * op::kNQ + j);
+    for (uint32_t n = 1; n < split.parts; ++n) {
+        v += *op::place(a, n * split.rest + blockIdx.y, i * op::kNQ + j);
+        if constexpr (Op::kPair) w += *op::place(a, n * split.rest + blockIdx.y, second * op::kNQ + j);
     }
+    Op::emit(a, at, i, j, v, w);
 }
 static inline int64_t most_tiles(int64_t n_rows, int64_t n, int rows_a_tile) { return n_rows / rows_a_tile + (n < n_rows ? n : n_rows); }
-// Workgroups of a launch for `tiles` tiles; 0: too many.
-static inline uint32_t tile_grid(int64_t tiles) { return tiles > 0x7ffffff0LL ? 0u : (uint32_t)((tiles + 7) / 8 * 8); }
+// The most tiles in parts there are: two parts each at least.
+template <class Op>
+int32_t launch_tiles(typename Op::args a, int columns, hipStream_t s)
+{
+    typedef tile_op<Op> op;
+    a.p_tiles = (columns + (Op::kPair ? Op::kP / 2 : Op::kP) - 1) / (Op::kPair ? Op::kP / 2 : Op::kP);
+    const int64_t tiles = most_tiles(a.g.n_rows, a.g.n, Op::kQ) * a.p_tiles, round = a.parts ? op::kRound : 0;
+    if (tiles > 0x7ff00000LL) return MW_ERR_UNSUPPORTED;
+    // T tiles are at most T - rest + kRound units, eights of them
+    hipLaunchKernelGGL((k_tiles<Op>), dim3((uint32_t)((tiles + round + 15) / 8 * 8)), dim3(kTileThreads), 0, s, a);
+    MW_HIP_CHECK(hipGetLastError());
+    if (a.parts) {
+        hipLaunchKernelGGL((k_join<Op>), dim3(op::kEmits, (uint32_t)(tiles < round / 2 ? tiles : round / 2)), dim3(kTileThreads), 0, s, a);
+        MW_HIP_CHECK(hipGetLastError());
+    }
+    return MW_OK;
+}
 
 // Row r of a tile of columns in LDS -> column of the tile: lanes then hold sixteen columns in a row of each 32 (the matrix instruction's result
 // has eights of rows, the lower four of each in the lower half of the wave).
 __device__ __forceinline__ int tile_column(int r) { return (r & ~31) | ((r >> 2) & 1) << 4 | ((r >> 3) & 3) << 2 | (r & 3); }
+
+// A lane's place in a piece: the row of the tile, and the column (of the tile's) that its first sum belongs to.
+template <int kQ> __device__ __forceinline__ int piece_row(int j) { return ((int)threadIdx.x >> 7) * (kQ / 2) + j * 32 + ((int)threadIdx.x & 31); }
+template <int kColumns> __device__ __forceinline__ int piece_column(int i) { return ((int)threadIdx.x >> 6 & 1) * (kColumns / 2) + i * 32; }
+__device__ __forceinline__ int lane_half() { return (int)threadIdx.x >> 5 & 1; }
 
 __device__ __forceinline__ float tile_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 template <int kN>

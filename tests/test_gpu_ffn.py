@@ -107,7 +107,7 @@ class Set:
 
 # counts, hidden, inter: one row, few rows, rows that end a tile or begin one, experts without rows, sizes that are no multiples of a tile or a step
 SIZES = [([1], 8, 8), ([1], 256, 264), ([0, 1, 0], 72, 136), ([3, 0, 5], 328, 72), ([16], 64, 64), ([17, 15, 1], 136, 200), ([33, 64, 65], 264, 328), ([31, 0, 127, 1], 128, 256),
-         ([129], 520, 40), ([255], 200, 392), ([256], 256, 128), ([257, 200], 264, 136), ([600], 72, 520), ([300, 500, 0, 31], 328, 264), ([0, 0], 64, 64), ([700, 1, 2], 128, 64)]
+         ([129], 520, 40), ([255], 200, 392), ([256], 256, 128), ([257, 200], 264, 136), ([600], 72, 520), ([300, 500, 0, 31], 328, 264), ([0, 0], 64, 64), ([700, 1, 2], 128, 64), ([400, 0, 300], 1032, 1048), ([20, 40], 1544, 2056), ([520], 2056, 264)]
 
 
 @pytest.mark.parametrize("counts,hidden,inter", SIZES)

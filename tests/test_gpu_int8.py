@@ -164,7 +164,7 @@ class Experts:
             near(y[at], want, np.abs(w)[:, None] * (off_h @ np.abs(down).T) + 6 * P.U * np.abs(want))
 
 
-@pytest.mark.parametrize("counts,hidden,inter", [([1], 16, 16), ([2, 0, 1], 256, 144), ([9, 5], 1040, 272), ([40, 0, 70], 272, 400), ([300], 400, 144), ([257, 400], 144, 256)])
+@pytest.mark.parametrize("counts,hidden,inter", [([1], 16, 16), ([2, 0, 1], 256, 144), ([9, 5], 1040, 272), ([40, 0, 70], 272, 400), ([300], 400, 144), ([257, 400], 144, 256), ([300, 0, 290], 2064, 1040), ([3, 60], 2064, 2080)])
 def test_experts(counts, hidden, inter):
     Experts(counts, hidden, inter, spare=3).check()
     Experts(counts, hidden, inter, weighted=False, seed=5).check()
