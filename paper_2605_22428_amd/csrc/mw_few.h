@@ -1,0 +1,164 @@
+// Products of matrices with a few rows each: the matrices' bytes bound them, every matrix row is read once and used for sixteen rows at a time.
+#ifndef MW_FEW_H_
+#define MW_FEW_H_
+
+#include "mw_stream.h"
+#include "mw_tile.h"
+
+namespace {
+
+// Sixteen matrix rows are one side of the matrix instruction, up to sixteen rows the other.  A workgroup's waves take every kFewWaves-th 128 bytes along the sum, kDepth of
+// them on the way at a time, as mw_stream.h does and for its reasons; bf16 values and codes differ in the instruction only.
+template <bool kInt8> struct few_kind;
+template <> struct few_kind<false> {
+    typedef f32x4 acc;
+    static __device__ __forceinline__ acc mma(u32x4 a, u32x4 b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0); }
+};
+template <> struct few_kind<true> {
+    typedef i32x4 acc;
+    static __device__ __forceinline__ acc mma(u32x4 a, u32x4 b, acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0); }
+};
+constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kSpanBytes = 128;
+
+template <int kCols> struct few_operands {
+    array w, x;
+    uint32_t row[2], col[kCols][2], limit;       // bytes; a lane's rows are lane / 8 and 8 + lane / 8, its piece byte (lane % 8) * 16
+};
+template <bool kInt8, int kCols>
+struct few_stage {
+    u32x4 w[2], x[kCols][2];
+    __device__ __forceinline__ void load(const few_operands<kCols> &o, uint32_t byte, int lane)
+    {
+        const bool in = byte + (uint32_t)(lane & 7) * 16 < o.limit;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = load16<true>(o.w, in && o.row[i] != kNowhere ? o.row[i] + byte : kNowhere);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[c][i] = load16<false>(o.x, in && o.col[c][i] != kNowhere ? o.col[c][i] + byte : kNowhere);
+    }
+    __device__ __forceinline__ void add_to(typename few_kind<kInt8>::acc (&acc)[kCols], char *lds, int lane) const
+    {
+        char *to = lds + (lane >> 3) * kPitch + (lane & 7) * 16;
+        const char *from = lds + (lane & 15) * kPitch + (lane >> 4) * 16;
+        u32x4 v[2];
+        wave_order();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *(u32x4 *)(to + i * 8 * kPitch) = w[i];
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) *(u32x4 *)(to + (c + 1) * kTileBytes + i * 8 * kPitch) = x[c][i];
+        wave_order();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) v[j] = *(const u32x4 *)(from + j * 64);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[c] = few_kind<kInt8>::mma(v[j], *(const u32x4 *)(from + (c + 1) * kTileBytes + j * 64), acc[c]);
+    }
+};
+
+// Sixteen matrix rows of tile `tile` times rows first .. of run e (count of them left).
+template <class Op, int kCols, int kDepth>
+__device__ __forceinline__ void few_columns(const typename Op::args &a, int e, int tile, int64_t first, int count, char *lds)
+{
+    typedef few_kind<Op::kInt8> kind;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l8 = lane >> 3;
+    const uint32_t piece = (uint32_t)(lane & 7) * 16;
+    few_operands<kCols> o;
+    o.w = array_at(Op::few_matrix(a, e));
+    o.x = array_at(Op::few_x(a, first));
+    o.limit = (uint32_t)a.K * (Op::kInt8 ? 1 : 2);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t at = Op::few_row(a, tile, i * 8 + l8);
+        o.row[i] = at == kNowhere ? at : at + piece;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+            const int r = c * 16 + i * 8 + l8;
+            o.col[c][i] = r < count ? (uint32_t)r * (uint32_t)a.x_stride * (Op::kInt8 ? 1 : 2) + piece : kNowhere;
+        }
+    }
+    typename kind::acc acc[kCols] = {};
+    few_stage<Op::kInt8, kCols> st[kDepth];
+    char *mine = lds + wave * (kCols + 1) * kTileBytes;
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) st[d].load(o, (uint32_t)(wave + d * kFewWaves) * kSpanBytes, lane);
+    for (uint32_t byte = (uint32_t)wave * kSpanBytes; byte < o.limit; byte += kFewWaves * kDepth * kSpanBytes) {
+#pragma unroll
+        for (int d = 0; d < kDepth; ++d) {
+            st[(d + kDepth - 1) % kDepth].load(o, byte + (uint32_t)(d + kDepth - 1) * kFewWaves * kSpanBytes, lane);
+            if (byte + (uint32_t)d * kFewWaves * kSpanBytes < o.limit) st[d].add_to(acc, mine, lane);
+        }
+    }
+    typedef decltype(acc[0][0] + acc[0][0]) value;
+    value *part = (value *)lds;                  // [wave][column][16 rows]
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+        __syncthreads();                         // (the sums take the place of the waves' pieces)
+        *(typename kind::acc *)&part[(wave * 16 + (lane & 15)) * 16 + (lane >> 4) * 4] = acc[c];
+        __syncthreads();
+        constexpr int kEach = Op::kPair ? 8 : 16;
+        const int col = (int)threadIdx.x / kEach, r = (int)threadIdx.x % kEach;
+        if (col < 16 && c * 16 + col < count) {
+            value v = 0, w = 0;
+#pragma unroll
+            for (int n = 0; n < kFewWaves; ++n) {
+                v += part[(n * 16 + col) * 16 + r];
+                if constexpr (Op::kPair) w += part[(n * 16 + col) * 16 + 8 + r];
+            }
+            Op::few_emit(a, e, first + c * 16 + col, tile * kEach + r, v, w);
+        }
+    }
+    __syncthreads();
+}
+// grid: (tiles of sixteen matrix rows, runs)
+template <class Op>
+__global__ __launch_bounds__(kFewThreads) void k_few(typename Op::args a)
+{
+    __shared__ __align__(16) char lds[kFewWaves * 3 * kTileBytes];
+    const int e = blockIdx.y, tile = blockIdx.x;
+    int64_t first, end;
+    group_bounds(a.g, e, first, end);
+    while (first < end) {
+        const int left = (int)(end - first);
+        if (left <= 16) few_columns<Op, 1, 4>(a, e, tile, first, left, lds);
+        else few_columns<Op, 2, 3>(a, e, tile, first, left, lds);
+        first += left <= 16 ? 16 : 32;
+    }
+}
+template <class Op>
+int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
+{
+    hipLaunchKernelGGL((k_few<Op>), dim3((uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), (uint32_t)a.g.n), dim3(kFewThreads), 0, s, a);
+    MW_HIP_CHECK(hipGetLastError());
+    return MW_OK;
+}
+
+// How a product of rows with n matrices of `columns` rows of `bytes` is cut.
+enum { kFew, kSmall, kMiddle, kLarge };
+static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t bytes)
+{
+    if (n_rows <= 16 * n) return kFew;
+    const double size = (double)n_rows * (double)columns * (double)bytes;
+    return n_rows >= 192 * n && size >= 7e10 ? kLarge : n_rows >= 96 * n && size >= 2.4e10 ? kMiddle : kSmall;
+}
+// The tile sizes' arguments are alike.
+template <class To, class From> To as(const From &f)
+{
+    static_assert(sizeof(To) == sizeof(From), "");
+    return __builtin_bit_cast(To, f);
+}
+// Large, Middle, Small: one product with tiles of 256 x 256, 128 x 128 and 128 x 64.  kHasFew: the product has few_emit().
+template <class Large, class Middle, class Small, bool kHasFew>
+int32_t launch_product(int form, const typename Large::args &a, int columns, hipStream_t s)
+{
+    if constexpr (kHasFew) if (form == kFew) return launch_few<Large>(a, columns, s);
+    if (form == kLarge) return launch_tiles<Large>(a, columns, s);
+    if (form == kMiddle) return launch_tiles<Middle>(as<typename Middle::args>(a), columns, s);
+    return launch_tiles<Small>(as<typename Small::args>(a), columns, s);
+}
+
+}  // namespace
+#endif  // MW_FEW_H_

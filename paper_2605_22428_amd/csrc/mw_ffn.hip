@@ -1,5 +1,5 @@
 // mw_ffn, mw_ffn_backward: the experts of the rows that a dispatch brought.
-#include "mw_tile.h"
+#include "mw_few.h"
 #include "mw_ffn.h"
 
 namespace {
@@ -48,6 +48,21 @@ struct up_op {
                 store_bf16<8>(kept + col, gate);
                 store_bf16<8>(kept + a.I + col, up);
             }
+        }
+    }
+    // A few rows: eight gate rows and the eight up rows beside them.
+    static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * 2 * a.I * a.K; }
+    static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
+    static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)          // (I is a multiple of eight)
+    {
+        return (uint32_t)((r >> 3) * a.I + tile * 8 + (r & 7)) * (uint32_t)a.K * 2;
+    }
+    static __device__ __forceinline__ void few_emit(const args &a, int, int64_t row, int col, float gate, float up)
+    {
+        a.h[row * a.I + col] = mw_f32_to_bf16(gate * tile_sigmoid(gate) * up);
+        if (a.kept) {
+            a.kept[row * 2 * a.I + col] = mw_f32_to_bf16(gate);
+            a.kept[row * 2 * a.I + a.I + col] = mw_f32_to_bf16(up);
         }
     }
 };
@@ -100,6 +115,16 @@ struct rows_op {
             for (int e = 0; e < kPiece; ++e) v[e] = a.row_weights ? weight * t[s + e] : t[s + e];
             store_bf16<kPiece>(y + col, v);
         }
+    }
+    static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * a.N * a.K; }
+    static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
+    static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)
+    {
+        return tile * 16 + r < a.N ? (uint32_t)(tile * 16 + r) * (uint32_t)a.K * 2 : kNowhere;
+    }
+    static __device__ __forceinline__ void few_emit(const args &a, int, int64_t row, int col, float v, float)
+    {
+        if (col < a.N) a.y[row * a.y_stride + col] = mw_f32_to_bf16(a.row_weights ? a.row_weights[row] * v : v);
     }
 };
 
@@ -163,13 +188,23 @@ struct act_op {
         }
     }
 };
-// d_row_weights: a row's sums, in the order of their columns.
-__global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, const float *parts, int n_parts, float *out)
+// d_row_weights: a row's sums, sixteen rows a workgroup; sixteen lanes' sums of every sixteenth each, then of these, in a fixed order.
+__global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, const float *sums, int n_sums, float *out)
 {
-    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x, end = min(max(g.offsets[g.n], (int64_t)0), g.n_rows);
-    if (row >= end) return;
+    __shared__ float part[16][17];
+    const int r = threadIdx.x & 15, n = threadIdx.x >> 4;
+    const int64_t row = (int64_t)blockIdx.x * 16 + r, end = min(max(g.offsets[g.n], (int64_t)0), g.n_rows);
     float v = 0.0f;
-    for (int i = 0; i < n_parts; ++i) v += parts[(int64_t)i * g.n_rows + row];
+    if (row < end) {
+#pragma unroll 4
+        for (int i = n; i < n_sums; i += 16) v += sums[(int64_t)i * g.n_rows + row];
+    }
+    part[n][r] = v;
+    __syncthreads();
+    if (n > 0 || row >= end) return;
+    v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v += part[i][r];
     out[row] = v;
 }
 
@@ -233,8 +268,6 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_f
 }
 
 // ---- entry points -----------------------------------------------------------------------------------------------------
-// The two tile sizes' arguments are alike.
-template <class To, class From> To as(const From &f) { static_assert(sizeof(To) == sizeof(From), ""); return __builtin_bit_cast(To, f); }
 constexpr int64_t kPartsBytes = 256LL * 256 * 256 * 4;          // sums of a round of the large tiles; of the small ones less
 int64_t pieces(int64_t n, int64_t each) { return (n + each - 1) / each; }
 
@@ -323,11 +356,11 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     const row_groups g = {expert_offsets_dev, n_rows, ctx->n_local};
     const hipStream_t s = (hipStream_t)stream;
     if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), (float *)(b + w.parts), s);
-    const bool large = n_rows >= 192LL * g.n;
+    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, 2 * (int64_t)H);
     const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
     const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
-    rc = large ? launch_tiles<up_op<256, 256>>(u, I, s) : launch_tiles<up_op<128, 64>>(as<up_op<128, 64>::args>(u), I, s);
-    if (rc == MW_OK) rc = large ? launch_tiles<rows_op<256, 256, false>>(d, H, s) : launch_tiles<rows_op<128, 64, false>>(as<rows_op<128, 64, false>::args>(d), H, s);
+    rc = launch_product<up_op<256, 256>, up_op<128, 128>, up_op<128, 64>, true>(form, u, I, s);
+    if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<128, 128, false>, rows_op<128, 64, false>, true>(form, d, H, s);
     return rc;
 }
 
@@ -354,18 +387,18 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
     const hipStream_t s = (hipStream_t)stream;
     uint16_t *act = (uint16_t *)(b + w.act), *d_act = (uint16_t *)(b + w.d_gate_up);
     float *sums = d_row_weights_dev ? (float *)(b + w.sums) : nullptr, *parts = (float *)(b + w.parts);
-    const bool large = n_rows >= 192LL * g.n;
+    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, 2 * (int64_t)H);
     if (n_rows > 0) {
         const act_op<256, 256>::args a = {g, (const uint16_t *)dy_dev, dy_stride, (const uint16_t *)experts->down_dev, row_weights_dev, (const uint16_t *)kept_dev, act, d_act, sums, parts, H, I, 0};
-        rc = large ? launch_tiles<act_op<256, 256>>(a, I, s) : launch_tiles<act_op<128, 64>>(as<act_op<128, 64>::args>(a), I, s);
+        rc = launch_product<act_op<256, 256>, act_op<128, 128>, act_op<128, 64>, false>(form, a, I, s);
         if (rc != MW_OK) return rc;
         if (sums) {
-            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 256)), dim3(256), 0, s, g, sums, (int)pieces(I, 32), d_row_weights_dev);
+            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 16)), dim3(256), 0, s, g, sums, (int)pieces(I, 32), d_row_weights_dev);
             MW_HIP_CHECK(hipGetLastError());
         }
         if (dx_dev) {
             const rows_op<256, 256, true>::args d = {g, d_act, 2 * (int64_t)I, (const uint16_t *)experts->gate_up_dev, nullptr, (uint16_t *)dx_dev, dx_stride, parts, 2 * I, H, 0};
-            rc = large ? launch_tiles<rows_op<256, 256, true>>(d, H, s) : launch_tiles<rows_op<128, 64, true>>(as<rows_op<128, 64, true>::args>(d), H, s);
+            rc = launch_product<rows_op<256, 256, true>, rows_op<128, 128, true>, rows_op<128, 64, true>, false>(form, d, H, s);
             if (rc != MW_OK) return rc;
         }
     }

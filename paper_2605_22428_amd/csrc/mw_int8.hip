@@ -1,6 +1,6 @@
 // mw_quantize_rows, mw_matmul_int8: products in 8-bit integers with a scale for each row and each output channel, and the experts that use them.
 #include "mw_ffn.h"
-#include "mw_tile.h"
+#include "mw_few.h"
 
 namespace {
 
@@ -114,14 +114,27 @@ struct int8_op {
             }
         }
     }
+    static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * (kGated ? 2 : 1) * a.N * a.K; }
+    static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
+    static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)          // (N is a multiple of sixteen)
+    {
+        return (uint32_t)(kGated ? (r >> 3) * a.N + tile * 8 + (r & 7) : tile * 16 + r) * (uint32_t)a.K;
+    }
+    static __device__ __forceinline__ void few_emit(const args &a, int e, int64_t row, int col, int t, int u)
+    {
+        const float scale = a.x_scale[row], *w = a.w_scale + (int64_t)e * (kGated ? 2 : 1) * a.N + col, value = (float)t * scale * w[0];
+        float v;
+        if constexpr (kGated) v = value * tile_sigmoid(value) * ((float)u * scale * w[a.N]);
+        else v = a.row_weights ? a.row_weights[row] * value : value;
+        if constexpr (kF32) ((float *)a.y)[row * a.y_stride + col] = v;
+        else ((uint16_t *)a.y)[row * a.y_stride + col] = mw_f32_to_bf16(v);
+    }
 };
 
 template <bool kGated, bool kF32>
 int32_t launch_int8(const typename int8_op<256, 256, kGated, kF32>::args &a, hipStream_t s)
 {
-    typedef int8_op<128, 64, kGated, kF32> small;
-    if (a.g.n_rows >= 192LL * a.g.n) return launch_tiles<int8_op<256, 256, kGated, kF32>>(a, a.N, s);
-    return launch_tiles<small>(__builtin_bit_cast(typename small::args, a), a.N, s);
+    return launch_product<int8_op<256, 256, kGated, kF32>, int8_op<128, 128, kGated, kF32>, int8_op<128, 64, kGated, kF32>, true>(rows_form(a.g.n_rows, a.g.n, kGated ? 2 * (int64_t)a.N : a.N, a.K), a, a.N, s);
 }
 int32_t launch_quantize(const quant_args &a, hipStream_t s)
 {

@@ -375,14 +375,37 @@ template <class Op>
 struct tile_op : Op {
     typedef tile_product<Op::kP, Op::kQ, Op::kTrP, false, Op::kInt8> product;
     typedef typename product::kind::acc acc;
-    // Workgroups that run at a time: LDS holds one of the large tiles a CU, three of the small ones.
-    static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : 768, kLeastSteps = 8;
+    // Workgroups that run at a time: LDS holds one of the large tiles a CU, two of 128 x 128, three of 128 x 64.
+    static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : Op::kP * Op::kQ == 128 * 128 ? 512 : 768, kLeastSteps = 8;
     static constexpr int kNP = product::kNP, kNQ = product::kNQ, kPieces = kNP * kNQ, kEmits = Op::kPair ? kPieces / 2 : kPieces;
     static constexpr int64_t kTileBytes = (int64_t)Op::kP * Op::kQ * 4;
     static __device__ __forceinline__ int steps(const typename Op::args &a) { return (a.K + (Op::kInt8 ? 127 : 63)) / (Op::kInt8 ? 128 : 64); }
-    static __device__ __forceinline__ acc *place(const typename Op::args &a, uint32_t slot, int piece)
+    // A piece's sums in memory: sixteen bytes a lane, four times.
+    typedef decltype(__builtin_shufflevector(acc{}, acc{}, 0, 1, 2, 3)) quarter;
+    static __device__ __forceinline__ quarter *place(const typename Op::args &a, uint32_t slot, int piece)
     {
-        return (acc *)((char *)a.parts + slot * kTileBytes) + piece * kTileThreads + threadIdx.x;
+        return (quarter *)((char *)a.parts + slot * kTileBytes) + piece * 4 * kTileThreads + threadIdx.x;
+    }
+    static __device__ __forceinline__ void put(const typename Op::args &a, uint32_t slot, int piece, const acc &v)
+    {
+        quarter *to = place(a, slot, piece);
+        to[0] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+        to[kTileThreads] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+        to[2 * kTileThreads] = __builtin_shufflevector(v, v, 8, 9, 10, 11);
+        to[3 * kTileThreads] = __builtin_shufflevector(v, v, 12, 13, 14, 15);
+    }
+    // The parts' sums of a piece, in their order.
+    static __device__ __forceinline__ acc sum(const typename Op::args &a, const tile_split &split, uint32_t tile, int piece)
+    {
+        quarter v[4] = {};
+#pragma unroll 4
+        for (uint32_t n = 0; n < split.parts; ++n) {
+            const quarter *from = place(a, n * split.rest + tile, piece);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += from[i * kTileThreads];
+        }
+        const auto low = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), high = __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
     }
 };
 template <class Op>
@@ -417,8 +440,8 @@ __global__ __launch_bounds__(kTileThreads, Op::kP * Op::kQ > 128 * 128 ? 1 : 2) 
         for (int i = 0; i < kHalf; ++i) {
             const int second = Op::kPair ? i + kHalf : i;
             if (part) {
-                *op::place(a, slot, i * op::kNQ + j) = t.acc[i][j];
-                if constexpr (Op::kPair) *op::place(a, slot, second * op::kNQ + j) = t.acc[second][j];
+                op::put(a, slot, i * op::kNQ + j, t.acc[i][j]);
+                if constexpr (Op::kPair) op::put(a, slot, second * op::kNQ + j, t.acc[second][j]);
             } else {
                 Op::emit(a, at, i, j, t.acc[i][j], t.acc[second][j]);
             }
@@ -437,12 +460,7 @@ __global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
     if (split.parts == 1 || blockIdx.y >= split.rest || !runs.find(a.g, (uint32_t)a.p_tiles, split.whole + blockIdx.y, at)) return;
     constexpr int kHalf = Op::kPair ? op::kNP / 2 : op::kNP;
     const int i = (int)blockIdx.x / op::kNQ, j = (int)blockIdx.x % op::kNQ, second = Op::kPair ? i + kHalf : i;
-    typename op::acc v = *op::place(a, blockIdx.y, i * op::kNQ + j), w = v;
-    if constexpr (Op::kPair) w = *op::place(a, blockIdx.y, second * op::kNQ + j);
-    for (uint32_t n = 1; n < split.parts; ++n) {
-        v += *op::place(a, n * split.rest + blockIdx.y, i * op::kNQ + j);
-        if constexpr (Op::kPair) w += *op::place(a, n * split.rest + blockIdx.y, second * op::kNQ + j);
-    }
+    const typename op::acc v = op::sum(a, split, blockIdx.y, i * op::kNQ + j), w = Op::kPair ? op::sum(a, split, blockIdx.y, second * op::kNQ + j) : v;
     Op::emit(a, at, i, j, v, w);
 }
 static inline int64_t most_tiles(int64_t n_rows, int64_t n, int rows_a_tile) { return n_rows / rows_a_tile + (n < n_rows ? n : n_rows); }
