@@ -22,32 +22,23 @@ struct up_op {
     {
         const int col0 = at.p * (kP / 2);
         fp.rows((const char *)(a.w + ((int64_t)at.e * 2 * a.I + col0) * a.K), a.K, [&](int r) {
-            const int in = r % (kP / 2), up = in / (kP / 4), col = r / (kP / 2) * (kP / 4) + tile_column(in % (kP / 4));
+            const int in = r % (kP / 2), up = in / (kP / 4), col = r / (kP / 2) * (kP / 4) + in % (kP / 4);
             return col0 + col < a.I ? (uint32_t)(up * a.I + col) * (uint32_t)a.K * 2 : kNowhereAt;
         });
         fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const f32x16 &g, const f32x16 &u)
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&gate)[8], const float (&up)[8])
     {
-        const int row = piece_row<kQ>(j);
-        if (row >= at.rows) return;
-        uint16_t *h = a.h + (at.first + row) * a.I, *kept = a.kept ? a.kept + (at.first + row) * 2 * a.I : nullptr;
+        const int col = at.p * (kP / 2) + column;
+        if (row >= at.rows || col >= a.I) return;               // (I is a multiple of eight)
+        float v[8];
 #pragma unroll
-        for (int s = 0; s < 16; s += 8) {
-            const int col = at.p * (kP / 2) + piece_column<kP / 2>(i) + lane_half() * 16 + s;
-            if (col >= a.I) continue;
-            float gate[8], up[8], v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                gate[e] = g[s + e];
-                up[e] = u[s + e];
-                v[e] = gate[e] * tile_sigmoid(gate[e]) * up[e];
-            }
-            store_bf16<8>(h + col, v);
-            if (kept) {
-                store_bf16<8>(kept + col, gate);
-                store_bf16<8>(kept + a.I + col, up);
-            }
+        for (int e = 0; e < 8; ++e) v[e] = gate[e] * tile_sigmoid(gate[e]) * up[e];
+        store_bf16(a.h + (at.first + row) * a.I + col, v);
+        if (a.kept) {
+            uint16_t *kept = a.kept + (at.first + row) * 2 * a.I + col;
+            store_bf16(kept, gate);
+            store_bf16(kept + a.I, up);
         }
     }
     // A few rows: eight gate rows and the eight up rows beside them.
@@ -77,8 +68,7 @@ template <int kP>
 __device__ __forceinline__ void columns_from(tile_feed<kP, false, false> &fp, const uint16_t *w, int col0, int K, int N)
 {
     fp.rows((const char *)(w + (int64_t)col0 * K), K, [&](int r) {
-        const int col = tile_column(r);
-        return col0 + col < N ? (uint32_t)col * (uint32_t)K * 2 : kNowhereAt;
+        return col0 + r < N ? (uint32_t)r * (uint32_t)K * 2 : kNowhereAt;
     });
 }
 template <int kCols, int kRows, bool kTr>
@@ -99,22 +89,15 @@ struct rows_op {
         columns_from(fp, a.w + (int64_t)at.e * a.N * a.K, at.p * kP, a.K, a.N);
         fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const f32x16 &t, const f32x16 &)
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&t)[8], const float (&)[8])
     {
-        const int row = piece_row<kQ>(j);
-        if (row >= at.rows) return;
+        const int col = at.p * kP + column;
+        if (row >= at.rows || col >= a.N) return;
         const float weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
-        uint16_t *y = a.y + (at.first + row) * a.y_stride;
-        constexpr int kPiece = kTr ? 4 : 8;
+        float v[8];
 #pragma unroll
-        for (int s = 0; s < 16; s += kPiece) {
-            const int col = at.p * kP + piece_column<kP>(i) + (kTr ? s * 2 + lane_half() * 4 : lane_half() * 16 + s);
-            if (col >= a.N) continue;
-            float v[kPiece];
-#pragma unroll
-            for (int e = 0; e < kPiece; ++e) v[e] = a.row_weights ? weight * t[s + e] : t[s + e];
-            store_bf16<kPiece>(y + col, v);
-        }
+        for (int e = 0; e < 8; ++e) v[e] = a.row_weights ? weight * t[e] : t[e];
+        store_bf16(a.y + (at.first + row) * a.y_stride + col, v);
     }
     static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * a.N * a.K; }
     static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
@@ -129,6 +112,7 @@ struct rows_op {
 };
 
 // ---- da = dy Wd, and what follows from it element by element ------------------------------------------------------
+constexpr int kSum = 64;
 template <int kCols, int kRows>
 struct act_op {
     static constexpr int kP = kCols, kQ = kRows;
@@ -140,7 +124,7 @@ struct act_op {
         const float *row_weights;               // or null
         const uint16_t *kept;                   // [rows][2][I]
         uint16_t *act, *d_gate_up;              // [rows][I], [rows][2][I]
-        float *sums;                            // [ceil(I / 32)][rows] or null: sums of da h over 32 columns
+        float *sums;                            // [ceil(I / kSum)][rows] or null: sums of da h over kSum columns
         float *parts;
         int32_t K, I, p_tiles;
     };
@@ -149,42 +133,33 @@ struct act_op {
         fp.lines((const char *)(a.down + (int64_t)at.e * a.K * a.I + at.p * kP), a.K, (int64_t)a.I * 2, a.I - at.p * kP);
         fq.rows((const char *)(a.dy + at.first * a.dy_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.dy_stride * 2 : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const f32x16 &t, const f32x16 &)
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&da)[8], const float (&)[8])
     {
-        const int row = piece_row<kQ>(j), col0 = at.p * kP + piece_column<kP>(i);
+        const int col = at.p * kP + column;
+        const bool mine = row < at.rows && col < a.I;
         float sum = 0.0f;
-        if (row < at.rows) {
+        if (mine) {
             const float weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
-            const uint16_t *kept = a.kept + (at.first + row) * 2 * a.I;
-            uint16_t *act = a.act + (at.first + row) * a.I, *d = a.d_gate_up + (at.first + row) * 2 * a.I;
-            bf16x4 gate[4], up[4];
+            const uint16_t *kept = a.kept + (at.first + row) * 2 * a.I + col;
+            uint16_t *act = a.act + (at.first + row) * a.I + col, *d = a.d_gate_up + (at.first + row) * 2 * a.I + col;
+            const bf16x8 gate = *(const bf16x8 *)kept, up = *(const bf16x8 *)(kept + a.I);
+            float h[8], dg[8], du[8];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int col = col0 + s * 8 + lane_half() * 4;
-                gate[s] = col < a.I ? *(const bf16x4 *)(kept + col) : bf16x4{};
-                up[s] = col < a.I ? *(const bf16x4 *)(kept + a.I + col) : bf16x4{};
+            for (int e = 0; e < 8; ++e) {
+                const float g = (float)gate[e], u = (float)up[e], sig = tile_sigmoid(g), silu = g * sig, dh = weight * da[e];
+                sum += da[e] * silu * u;
+                h[e] = weight * silu * u;
+                dg[e] = dh * u * (sig + silu * (1.0f - sig));
+                du[e] = dh * silu;
             }
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int col = col0 + s * 8 + lane_half() * 4;
-                if (col >= a.I) continue;
-                float h[4], dg[4], du[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float g = (float)gate[s][e], u = (float)up[s][e], sig = tile_sigmoid(g), silu = g * sig, da = t[s * 4 + e], dh = weight * da;
-                    sum += da * silu * u;
-                    h[e] = weight * silu * u;
-                    dg[e] = dh * u * (sig + silu * (1.0f - sig));
-                    du[e] = dh * silu;
-                }
-                store_bf16<4>(act + col, h);
-                store_bf16<4>(d + col, dg);
-                store_bf16<4>(d + a.I + col, du);
-            }
+            store_bf16(act, h);
+            store_bf16(d, dg);
+            store_bf16(d + a.I, du);
         }
-        if (a.sums) {
-            sum += __shfl_xor(sum, 32);
-            if (row < at.rows && lane_half() == 0 && col0 < a.I) a.sums[(int64_t)(col0 / 32) * a.g.n_rows + at.first + row] = sum;
+        if (a.sums) {                                           // over the lanes that have kSum columns of the row: a fixed order
+#pragma unroll
+            for (int n = 1; n < kSum / 8; n *= 2) sum += __shfl_xor(sum, n);
+            if (mine && column % kSum == 0) a.sums[(int64_t)(col / kSum) * a.g.n_rows + at.first + row] = sum;
         }
     }
 };
@@ -220,7 +195,8 @@ template <int kP, int kQ>
 __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_ffn_grads(grads_args a)
 {
     typedef tile_product<kP, kQ, true, true, false> product;
-    __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
+    typedef tile_out<kP, kQ, false> out_form;
+    __shared__ __attribute__((aligned(1024))) char lds[product::kLds > kTileWaves * out_form::kBytes ? product::kLds : kTileWaves * out_form::kBytes];
     const uint32_t each = (uint32_t)a.p_tiles * (uint32_t)a.q_tiles, per = (each + 7) / 8, at = blockIdx.x >> 3;
     const uint32_t tile = (blockIdx.x & 7) * per + at % per;
     int e = (int)(at / per);
@@ -249,22 +225,9 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_f
     product t;
     t.run(fp, fq, (rows + 63) / 64, (lds_char *)lds);
     uint16_t *out = a.out + (int64_t)e * a.M * a.N;
-#pragma unroll
-    for (int j = 0; j < product::kNQ; ++j) {
-        const int row = q0 + piece_row<kQ>(j);
-        if (row >= a.M) continue;
-#pragma unroll
-        for (int i = 0; i < product::kNP; ++i)
-#pragma unroll
-            for (int s = 0; s < 16; s += 4) {
-                const int col = p0 + piece_column<kP>(i) + s * 2 + lane_half() * 4;
-                if (col >= a.N) continue;
-                float v[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = t.acc[i][j][s + c];
-                store_bf16<4>(out + (int64_t)row * a.N + col, v);
-            }
-    }
+    tile_results<kP, kQ, false>(t, (lds_char *)lds, [&](int row, int column, const float (&v)[8], const float (&)[8]) {
+        if (q0 + row < a.M && p0 + column < a.N) store_bf16(out + (int64_t)(q0 + row) * a.N + p0 + column, v);
+    });
 }
 
 // ---- entry points -----------------------------------------------------------------------------------------------------
@@ -280,7 +243,7 @@ ffn_ws ffn_layout(const mw_experts *e, int32_t hidden, int64_t rows, bool backwa
     w.act = take(2 * rows * e->inter);
     if (backward) {
         w.d_gate_up = take(4 * rows * e->inter);
-        w.sums = take(4 * rows * pieces(e->inter, 32));
+        w.sums = take(4 * rows * pieces(e->inter, kSum));
     }
     if (e->format == MW_WEIGHT_INT8_CHANNEL) {
         w.codes = take(rows * (hidden > e->inter ? hidden : e->inter));
@@ -393,7 +356,7 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
         rc = launch_product<act_op<256, 256>, act_op<128, 128>, act_op<128, 64>, false>(form, a, I, s);
         if (rc != MW_OK) return rc;
         if (sums) {
-            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 16)), dim3(256), 0, s, g, sums, (int)pieces(I, 32), d_row_weights_dev);
+            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 16)), dim3(256), 0, s, g, sums, (int)pieces(I, kSum), d_row_weights_dev);
             MW_HIP_CHECK(hipGetLastError());
         }
         if (dx_dev) {

@@ -79,39 +79,34 @@ struct int8_op {
     {
         const int col0 = at.p * 2 * kHalf;
         fp.rows((const char *)(a.w + ((int64_t)at.e * (kGated ? 2 : 1) * a.N + col0) * a.K), a.K, [&](int r) {
-            const int in = r % (kP / 2), up = in / kHalf, col = r / (kP / 2) * kHalf + tile_column(in % kHalf);
+            const int in = r % (kP / 2), up = in / kHalf, col = r / (kP / 2) * kHalf + in % kHalf;
             return col0 + col < a.N ? (uint32_t)(up * a.N + col) * (uint32_t)a.K : kNowhereAt;
         });
         fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int i, int j, const i32x16 &t, const i32x16 &u)
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const int (&t)[8], const int (&u)[8])
     {
-        const int row = piece_row<kQ>(j);
-        if (row >= at.rows) return;
+        const int col = at.p * 2 * kHalf + column;
+        if (row >= at.rows || col >= a.N) return;               // (N is a multiple of sixteen)
         const float scale = a.x_scale[at.first + row], weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
+        const float *ws = a.w_scale + (int64_t)at.e * (kGated ? 2 : 1) * a.N + col;
+        float v[8];
 #pragma unroll
-        for (int s = 0; s < 16; s += 8) {
-            const int col = at.p * 2 * kHalf + piece_column<2 * kHalf>(i) + lane_half() * 16 + s;
-            if (col >= a.N) continue;
-            float v[8];
-            const float *ws = a.w_scale + (int64_t)at.e * (kGated ? 2 : 1) * a.N + col;
+        for (int e = 0; e < 8; e += 4) {
+            const f32x4 w = *(const f32x4_any *)(ws + e), wu = kGated ? *(const f32x4_any *)(ws + a.N + e) : w;
 #pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                const f32x4 w = *(const f32x4_any *)(ws + e), wu = kGated ? *(const f32x4_any *)(ws + a.N + e) : w;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float value = (float)t[s + e + q] * scale * w[q];
-                    if constexpr (kGated) v[e + q] = value * tile_sigmoid(value) * ((float)u[s + e + q] * scale * wu[q]);
-                    else v[e + q] = a.row_weights ? weight * value : value;
-                }
+            for (int q = 0; q < 4; ++q) {
+                const float value = (float)t[e + q] * scale * w[q];
+                if constexpr (kGated) v[e + q] = value * tile_sigmoid(value) * ((float)u[e + q] * scale * wu[q]);
+                else v[e + q] = a.row_weights ? weight * value : value;
             }
-            if constexpr (kF32) {
-                float *y = (float *)a.y + (at.first + row) * a.y_stride + col;
-                *(f32x4 *)y = f32x4{v[0], v[1], v[2], v[3]};
-                *(f32x4 *)(y + 4) = f32x4{v[4], v[5], v[6], v[7]};
-            } else {
-                store_bf16<8>((uint16_t *)a.y + (at.first + row) * a.y_stride + col, v);
-            }
+        }
+        if constexpr (kF32) {
+            float *y = (float *)a.y + (at.first + row) * a.y_stride + col;
+            *(f32x4 *)y = f32x4{v[0], v[1], v[2], v[3]};
+            *(f32x4 *)(y + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        } else {
+            store_bf16((uint16_t *)a.y + (at.first + row) * a.y_stride + col, v);
         }
     }
     static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * (kGated ? 2 : 1) * a.N * a.K; }

@@ -14,7 +14,7 @@
 #ifndef MW_TILE_H_
 #define MW_TILE_H_
 
-#include "mw_math.h"
+#include "mw_stream.h"
 
 namespace {
 
@@ -259,6 +259,7 @@ struct tile_product {
             }
         }
         tile_wait<0>();
+        tile_reads_done();                              // (the results go through LDS)
         stay();
     }
     // The accumulators stay where the matrix instructions left them until a piece is used: brought to ordinary registers together, they are spilled.
@@ -369,51 +370,88 @@ struct tile_runs {
     }
 };
 
-// A product's kernels.  Op has: args (with g, p_tiles, K and parts, memory for kRound tiles' sums or null); kP, kQ, kTrP, kInt8; kPair: pieces i and i + half of a wave's
-// columns are used together; feeds(): what is loaded; emit(): what becomes of a piece of 32 columns and 32 rows, a lane's sixteen sums.
+// How results leave: a wave's quarter of a tile goes through LDS, 64 (small tiles: 32) rows at a time, and comes back eight neighbouring columns a lane, whole rows of it to
+// neighbouring lanes: memory is written (and what belongs to the results is read) in whole lines.  From the accumulators a lane would write sixteen bytes here and there.
+// kPair: the wave's columns are two halves that belong together, a lane gets eight of each.
+template <int kP, int kQ, bool kPair>
+struct tile_out {
+    static constexpr int kCols = kP / 2, kRows = kQ / 2 < 64 ? kQ / 2 : 64, kPitch = kCols * 4 + 16, kBytes = kRows * kPitch;          // (rows begin on different banks)
+    static constexpr int kLanes = kCols / (kPair ? 16 : 8), kAtOnce = 64 / kLanes;                                                      // lanes of a row, rows at once
+    template <class Acc>
+    static __device__ __forceinline__ void put(lds_char *lds, int i, int j, const Acc &v)                                              // piece i, j (of kRows / 32) of the accumulators
+    {
+        const int lane = threadIdx.x & 63;
+        typedef decltype(__builtin_shufflevector(v, v, 0, 1, 2, 3)) quarter;
+        typedef __attribute__((address_space(3))) quarter lds_quarter;
+        lds_quarter *to = (lds_quarter *)(lds + (j * 32 + (lane & 31)) * kPitch + (i * 32 + (lane >> 5) * 4) * 4);
+        to[0] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+        to[2] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+        to[4] = __builtin_shufflevector(v, v, 8, 9, 10, 11);
+        to[6] = __builtin_shufflevector(v, v, 12, 13, 14, 15);
+    }
+    template <class Value>
+    static __device__ __forceinline__ void take(const lds_char *lds, int row, int half, Value (&v)[8])
+    {
+        typedef Value quarter __attribute__((ext_vector_type(4)));
+        const __attribute__((address_space(3))) quarter *from =
+            (const __attribute__((address_space(3))) quarter *)(lds + row * kPitch + (((int)threadIdx.x & (kLanes - 1)) * 8 + half * (kCols / 2)) * 4);
+        const quarter a = from[0], b = from[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+    }
+};
+// Every row of the tile, a wave's quarter: use(row, column, v, u), column of the tile's (kPair: of its half).
+template <int kP, int kQ, bool kPair, class Product, class Use>
+__device__ __forceinline__ void tile_results(const Product &t, lds_char *lds, Use use)
+{
+    typedef tile_out<kP, kQ, kPair> out;
+    typedef decltype(t.acc[0][0][0] + t.acc[0][0][0]) value;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    lds_char *mine = lds + wave * out::kBytes;
+    constexpr int kJ = out::kRows / 32;
+#pragma unroll
+    for (int j = 0; j < Product::kNQ; j += kJ) {
+#pragma unroll
+        for (int i = 0; i < Product::kNP; ++i)
+#pragma unroll
+            for (int n = 0; n < kJ; ++n) out::put(mine, i, n, t.acc[i][j + n]);
+        wave_order();
+#pragma unroll 4
+        for (int r = 0; r < out::kRows; r += out::kAtOnce) {
+            const int row = r + lane / out::kLanes;
+            value v[8], u[8];
+            out::take(mine, row, 0, v);
+            if constexpr (kPair) out::take(mine, row, 1, u);
+            use((wave >> 1) * (kQ / 2) + j * 32 + row, (wave & 1) * (kPair ? kP / 4 : kP / 2) + (lane & (out::kLanes - 1)) * 8, v, kPair ? u : v);
+        }
+        wave_order();
+    }
+}
+
+// A product's kernels.  Op has: args (with g, p_tiles, K and parts, memory for kRound tiles' sums or null); kP, kQ, kTrP, kInt8; kPair: half of a wave's columns belong to
+// the other half; feeds(): what is loaded; emit(): what becomes of eight columns of a row.
 template <class Op>
 struct tile_op : Op {
     typedef tile_product<Op::kP, Op::kQ, Op::kTrP, false, Op::kInt8> product;
-    typedef typename product::kind::acc acc;
+    typedef tile_out<Op::kP, Op::kQ, Op::kPair> out;
+    typedef decltype(typename product::kind::acc{}[0] + 0) value;
     // Workgroups that run at a time: LDS holds one of the large tiles a CU, two of 128 x 128, three of 128 x 64.
     static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : Op::kP * Op::kQ == 128 * 128 ? 512 : 768, kLeastSteps = 8;
-    static constexpr int kNP = product::kNP, kNQ = product::kNQ, kPieces = kNP * kNQ, kEmits = Op::kPair ? kPieces / 2 : kPieces;
-    static constexpr int64_t kTileBytes = (int64_t)Op::kP * Op::kQ * 4;
+    static constexpr int kLds = product::kLds > kTileWaves * out::kBytes ? product::kLds : kTileWaves * out::kBytes;
+    static constexpr int kColumns = Op::kPair ? Op::kP / 2 : Op::kP, kJoinRows = kTileThreads * 8 / kColumns;         // rows that a workgroup of k_join takes
     static __device__ __forceinline__ int steps(const typename Op::args &a) { return (a.K + (Op::kInt8 ? 127 : 63)) / (Op::kInt8 ? 128 : 64); }
-    // A piece's sums in memory: sixteen bytes a lane, four times.
-    typedef decltype(__builtin_shufflevector(acc{}, acc{}, 0, 1, 2, 3)) quarter;
-    static __device__ __forceinline__ quarter *place(const typename Op::args &a, uint32_t slot, int piece)
-    {
-        return (quarter *)((char *)a.parts + slot * kTileBytes) + piece * 4 * kTileThreads + threadIdx.x;
-    }
-    static __device__ __forceinline__ void put(const typename Op::args &a, uint32_t slot, int piece, const acc &v)
-    {
-        quarter *to = place(a, slot, piece);
-        to[0] = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-        to[kTileThreads] = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-        to[2 * kTileThreads] = __builtin_shufflevector(v, v, 8, 9, 10, 11);
-        to[3 * kTileThreads] = __builtin_shufflevector(v, v, 12, 13, 14, 15);
-    }
-    // The parts' sums of a piece, in their order.
-    static __device__ __forceinline__ acc sum(const typename Op::args &a, const tile_split &split, uint32_t tile, int piece)
-    {
-        quarter v[4] = {};
-#pragma unroll 4
-        for (uint32_t n = 0; n < split.parts; ++n) {
-            const quarter *from = place(a, n * split.rest + tile, piece);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += from[i * kTileThreads];
-        }
-        const auto low = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7), high = __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3, 4, 5, 6, 7);
-        return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 14, 15);
-    }
+    // Eight sums of a part, at a row and a column of a tile of kP columns.
+    typedef value eight __attribute__((ext_vector_type(8)));
+    static __device__ __forceinline__ eight *place(const typename Op::args &a, uint32_t slot, int row, int column) { return (eight *)((value *)a.parts + ((int64_t)slot * Op::kQ + row) * Op::kP + column); }
+    // Column of a tile in a part, from a column that emit() has: waves' columns are kP / 2 each, the two halves of a pair behind one another.
+    static __device__ __forceinline__ int column_of(int column, int half) { return Op::kPair ? column / (Op::kP / 4) * (Op::kP / 2) + column % (Op::kP / 4) + half * (Op::kP / 4) : column; }
 };
 template <class Op>
 __global__ __launch_bounds__(kTileThreads, Op::kP * Op::kQ > 128 * 128 ? 1 : 2) void k_tiles(typename Op::args a)
 {
     typedef tile_op<Op> op;
     typedef typename op::product product;
-    __shared__ __attribute__((aligned(1024))) char lds[product::kLds];
+    __shared__ __attribute__((aligned(1024))) char lds[op::kLds];
     tile_runs<Op::kQ> runs;
     runs.count(a.g);
     const int steps = op::steps(a);
@@ -433,22 +471,17 @@ __global__ __launch_bounds__(kTileThreads, Op::kP * Op::kQ > 128 * 128 ? 1 : 2) 
     product t;
     t.run(fp, fq, n, (lds_char *)lds);
     const uint32_t slot = u.part * split.rest + u.tile - split.whole;
-    constexpr int kHalf = Op::kPair ? op::kNP / 2 : op::kNP;
-#pragma unroll
-    for (int j = 0; j < op::kNQ; ++j)
-#pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-            const int second = Op::kPair ? i + kHalf : i;
-            if (part) {
-                op::put(a, slot, i * op::kNQ + j, t.acc[i][j]);
-                if constexpr (Op::kPair) op::put(a, slot, second * op::kNQ + j, t.acc[second][j]);
-            } else {
-                Op::emit(a, at, i, j, t.acc[i][j], t.acc[second][j]);
-            }
-            __builtin_amdgcn_sched_barrier(0);          // (a piece at a time: all of them at once take more registers than there are)
+    typedef typename op::value value;
+    tile_results<Op::kP, Op::kQ, Op::kPair>(t, (lds_char *)lds, [&](int row, int column, const value (&v)[8], const value (&w)[8]) {
+        if (part) {
+            *op::place(a, slot, row, op::column_of(column, 0)) = typename op::eight{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+            if constexpr (Op::kPair) *op::place(a, slot, row, op::column_of(column, 1)) = typename op::eight{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
+        } else {
+            Op::emit(a, at, row, column, v, w);
         }
+    });
 }
-// grid: (pieces of a tile, tiles in parts at most)
+// The parts' sums in their order.  grid: (kJoinRows rows of a tile, tiles in parts at most)
 template <class Op>
 __global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
 {
@@ -458,10 +491,18 @@ __global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
     const tile_split split = split_tiles(runs.total * (uint32_t)a.p_tiles, op::kRound, (uint32_t)op::steps(a), op::kLeastSteps, true);
     tile_at at;
     if (split.parts == 1 || blockIdx.y >= split.rest || !runs.find(a.g, (uint32_t)a.p_tiles, split.whole + blockIdx.y, at)) return;
-    constexpr int kHalf = Op::kPair ? op::kNP / 2 : op::kNP;
-    const int i = (int)blockIdx.x / op::kNQ, j = (int)blockIdx.x % op::kNQ, second = Op::kPair ? i + kHalf : i;
-    const typename op::acc v = op::sum(a, split, blockIdx.y, i * op::kNQ + j), w = Op::kPair ? op::sum(a, split, blockIdx.y, second * op::kNQ + j) : v;
-    Op::emit(a, at, i, j, v, w);
+    const int row = (int)blockIdx.x * op::kJoinRows + (int)threadIdx.x / (op::kColumns / 8), column = (int)threadIdx.x % (op::kColumns / 8) * 8;
+    if ((int)blockIdx.x * op::kJoinRows >= at.rows) return;
+    typename op::eight v = {}, w = {};
+#pragma unroll 4
+    for (uint32_t n = 0; n < split.parts; ++n) {
+        v += *op::place(a, n * split.rest + blockIdx.y, row, op::column_of(column, 0));
+        if constexpr (Op::kPair) w += *op::place(a, n * split.rest + blockIdx.y, row, op::column_of(column, 1));
+    }
+    typename op::value x[8], y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { x[e] = v[e]; y[e] = w[e]; }
+    Op::emit(a, at, row, column, x, y);
 }
 static inline int64_t most_tiles(int64_t n_rows, int64_t n, int rows_a_tile) { return n_rows / rows_a_tile + (n < n_rows ? n : n_rows); }
 // The most tiles in parts there are: two parts each at least.
@@ -476,31 +517,19 @@ int32_t launch_tiles(typename Op::args a, int columns, hipStream_t s)
     hipLaunchKernelGGL((k_tiles<Op>), dim3((uint32_t)((tiles + round + 15) / 8 * 8)), dim3(kTileThreads), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     if (a.parts) {
-        hipLaunchKernelGGL((k_join<Op>), dim3(op::kEmits, (uint32_t)(tiles < round / 2 ? tiles : round / 2)), dim3(kTileThreads), 0, s, a);
+        hipLaunchKernelGGL((k_join<Op>), dim3(Op::kQ / op::kJoinRows, (uint32_t)(tiles < round / 2 ? tiles : round / 2)), dim3(kTileThreads), 0, s, a);
         MW_HIP_CHECK(hipGetLastError());
     }
     return MW_OK;
 }
 
-// Row r of a tile of columns in LDS -> column of the tile: lanes then hold sixteen columns in a row of each 32 (the matrix instruction's result
-// has eights of rows, the lower four of each in the lower half of the wave).
-__device__ __forceinline__ int tile_column(int r) { return (r & ~31) | ((r >> 2) & 1) << 4 | ((r >> 3) & 3) << 2 | (r & 3); }
-
-// A lane's place in a piece: the row of the tile, and the column (of the tile's) that its first sum belongs to.
-template <int kQ> __device__ __forceinline__ int piece_row(int j) { return ((int)threadIdx.x >> 7) * (kQ / 2) + j * 32 + ((int)threadIdx.x & 31); }
-template <int kColumns> __device__ __forceinline__ int piece_column(int i) { return ((int)threadIdx.x >> 6 & 1) * (kColumns / 2) + i * 32; }
-__device__ __forceinline__ int lane_half() { return (int)threadIdx.x >> 5 & 1; }
-
 __device__ __forceinline__ float tile_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
-template <int kN>
-__device__ __forceinline__ void store_bf16(uint16_t *to, const float *v)
+__device__ __forceinline__ void store_bf16(uint16_t *to, const float (&v)[8])
 {
-    static_assert(kN == 4 || kN == 8, "");
-    typedef __bf16 vec __attribute__((ext_vector_type(kN)));
-    vec o;
+    bf16x8 o;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) o[i] = (__bf16)v[i];
-    *(vec *)to = o;
+    for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
+    *(bf16x8 *)to = o;
 }
 
 }  // namespace
