@@ -9,7 +9,7 @@ namespace {
 template <int kCols, int kRows>
 struct up_op {
     static constexpr int kP = kCols, kQ = kRows;
-    static constexpr bool kTrP = false, kInt8 = false, kPair = true;
+    static constexpr bool kTrP = false, kInt8 = false, kPair = true, kRowValues = false;
     struct args {
         row_groups g;
         const uint16_t *x; int64_t x_stride;
@@ -27,7 +27,9 @@ struct up_op {
         });
         fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&gate)[8], const float (&up)[8])
+    static __device__ __forceinline__ tile_nothing columns(const args &, const tile_at &, int) { return {}; }
+    static __device__ __forceinline__ tile_nothing fetch(const args &, const tile_at &, int, int) { return {}; }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&gate)[8], const float (&up)[8], tile_nothing, f32x2, tile_nothing)
     {
         const int col = at.p * (kP / 2) + column;
         if (row >= at.rows || col >= a.I) return;               // (I is a multiple of eight)
@@ -74,7 +76,7 @@ __device__ __forceinline__ void columns_from(tile_feed<kP, false, false> &fp, co
 template <int kCols, int kRows, bool kTr>
 struct rows_op {
     static constexpr int kP = kCols, kQ = kRows;
-    static constexpr bool kTrP = kTr, kInt8 = false, kPair = false;
+    static constexpr bool kTrP = kTr, kInt8 = false, kPair = false, kRowValues = !kTr;          // (gradients of rows have no weights)
     struct args {
         row_groups g;
         const uint16_t *x; int64_t x_stride;    // [rows][K]
@@ -89,14 +91,16 @@ struct rows_op {
         columns_from(fp, a.w + (int64_t)at.e * a.N * a.K, at.p * kP, a.K, a.N);
         fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride * 2 : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&t)[8], const float (&)[8])
+    static __device__ __forceinline__ f32x2 rows(const args &a, int64_t row) { return {a.row_weights ? a.row_weights[row] : 1.0f, 0.0f}; }
+    static __device__ __forceinline__ tile_nothing columns(const args &, const tile_at &, int) { return {}; }
+    static __device__ __forceinline__ tile_nothing fetch(const args &, const tile_at &, int, int) { return {}; }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&t)[8], const float (&)[8], tile_nothing, f32x2 weight, tile_nothing)
     {
         const int col = at.p * kP + column;
         if (row >= at.rows || col >= a.N) return;
-        const float weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = a.row_weights ? weight * t[e] : t[e];
+        for (int e = 0; e < 8; ++e) v[e] = kRowValues ? weight[0] * t[e] : t[e];
         store_bf16(a.y + (at.first + row) * a.y_stride + col, v);
     }
     static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * a.N * a.K; }
@@ -116,7 +120,7 @@ constexpr int kSum = 64;
 template <int kCols, int kRows>
 struct act_op {
     static constexpr int kP = kCols, kQ = kRows;
-    static constexpr bool kTrP = true, kInt8 = false, kPair = false;
+    static constexpr bool kTrP = true, kInt8 = false, kPair = false, kRowValues = true;
     struct args {
         row_groups g;
         const uint16_t *dy; int64_t dy_stride;
@@ -133,22 +137,29 @@ struct act_op {
         fp.lines((const char *)(a.down + (int64_t)at.e * a.K * a.I + at.p * kP), a.K, (int64_t)a.I * 2, a.I - at.p * kP);
         fq.rows((const char *)(a.dy + at.first * a.dy_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.dy_stride * 2 : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&da)[8], const float (&)[8])
+    static __device__ __forceinline__ f32x2 rows(const args &a, int64_t row) { return {a.row_weights ? a.row_weights[row] : 1.0f, 0.0f}; }
+    struct values { bf16x8 gate, up; };
+    static __device__ __forceinline__ tile_nothing columns(const args &, const tile_at &, int) { return {}; }
+    static __device__ __forceinline__ values fetch(const args &a, const tile_at &at, int row, int column)
+    {
+        const int col = at.p * kP + column;
+        if (row >= at.rows || col >= a.I) return values{};
+        const uint16_t *kept = a.kept + (at.first + row) * 2 * a.I + col;
+        return values{*(const bf16x8 *)kept, *(const bf16x8 *)(kept + a.I)};
+    }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const float (&da)[8], const float (&)[8], tile_nothing, f32x2 weight, const values &kept)
     {
         const int col = at.p * kP + column;
         const bool mine = row < at.rows && col < a.I;
         float sum = 0.0f;
         if (mine) {
-            const float weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
-            const uint16_t *kept = a.kept + (at.first + row) * 2 * a.I + col;
             uint16_t *act = a.act + (at.first + row) * a.I + col, *d = a.d_gate_up + (at.first + row) * 2 * a.I + col;
-            const bf16x8 gate = *(const bf16x8 *)kept, up = *(const bf16x8 *)(kept + a.I);
             float h[8], dg[8], du[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float g = (float)gate[e], u = (float)up[e], sig = tile_sigmoid(g), silu = g * sig, dh = weight * da[e];
+                const float g = (float)kept.gate[e], u = (float)kept.up[e], sig = tile_sigmoid(g), silu = g * sig, dh = weight[0] * da[e];
                 sum += da[e] * silu * u;
-                h[e] = weight * silu * u;
+                h[e] = weight[0] * silu * u;
                 dg[e] = dh * u * (sig + silu * (1.0f - sig));
                 du[e] = dh * silu;
             }
@@ -225,7 +236,7 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_f
     product t;
     t.run(fp, fq, (rows + 63) / 64, (lds_char *)lds);
     uint16_t *out = a.out + (int64_t)e * a.M * a.N;
-    tile_results<kP, kQ, false>(t, (lds_char *)lds, [&](int row, int column, const float (&v)[8], const float (&)[8]) {
+    tile_results<kP, kQ, false>(t, (lds_char *)lds, [](int, int) { return 0; }, [&](int row, int column, const float (&v)[8], const float (&)[8], int) {
         if (q0 + row < a.M && p0 + column < a.N) store_bf16(out + (int64_t)(q0 + row) * a.N + p0 + column, v);
     });
 }

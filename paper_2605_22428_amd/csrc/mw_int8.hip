@@ -62,7 +62,7 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 template <int kCols, int kRows, bool kGated, bool kF32>
 struct int8_op {
     static constexpr int kP = kCols, kQ = kRows;
-    static constexpr bool kTrP = false, kInt8 = true, kPair = kGated;
+    static constexpr bool kTrP = false, kInt8 = true, kPair = kGated, kRowValues = true;
     struct args {
         row_groups g;
         const int8_t *x; int64_t x_stride;
@@ -84,22 +84,33 @@ struct int8_op {
         });
         fq.rows((const char *)(a.x + at.first * a.x_stride), a.K, [&](int r) { return r < at.rows ? (uint32_t)r * (uint32_t)a.x_stride : kNowhereAt; });
     }
-    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const int (&t)[8], const int (&u)[8])
+    static __device__ __forceinline__ f32x2 rows(const args &a, int64_t row) { return {a.x_scale[row], a.row_weights ? a.row_weights[row] : 1.0f}; }
+    struct scales { f32x4 w[2], up[kGated ? 2 : 1]; };
+    static __device__ __forceinline__ scales columns(const args &a, const tile_at &at, int column)
     {
         const int col = at.p * 2 * kHalf + column;
-        if (row >= at.rows || col >= a.N) return;               // (N is a multiple of sixteen)
-        const float scale = a.x_scale[at.first + row], weight = a.row_weights ? a.row_weights[at.first + row] : 1.0f;
-        const float *ws = a.w_scale + (int64_t)at.e * (kGated ? 2 : 1) * a.N + col;
+        scales s = {};
+        if (col < a.N) {                                        // (N is a multiple of sixteen)
+            const float *w = a.w_scale + (int64_t)at.e * (kGated ? 2 : 1) * a.N + col;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s.w[i] = *(const f32x4_any *)(w + i * 4);
+                if constexpr (kGated) s.up[i] = *(const f32x4_any *)(w + a.N + i * 4);
+            }
+        }
+        return s;
+    }
+    static __device__ __forceinline__ tile_nothing fetch(const args &, const tile_at &, int, int) { return {}; }
+    static __device__ __forceinline__ void emit(const args &a, const tile_at &at, int row, int column, const int (&t)[8], const int (&u)[8], const scales &s, f32x2 of_row, tile_nothing)
+    {
+        const int col = at.p * 2 * kHalf + column;
+        if (row >= at.rows || col >= a.N) return;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-            const f32x4 w = *(const f32x4_any *)(ws + e), wu = kGated ? *(const f32x4_any *)(ws + a.N + e) : w;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float value = (float)t[e + q] * scale * w[q];
-                if constexpr (kGated) v[e + q] = value * tile_sigmoid(value) * ((float)u[e + q] * scale * wu[q]);
-                else v[e + q] = a.row_weights ? weight * value : value;
-            }
+        for (int e = 0; e < 8; ++e) {
+            const float value = (float)t[e] * of_row[0] * s.w[e / 4][e % 4];
+            if constexpr (kGated) v[e] = value * tile_sigmoid(value) * ((float)u[e] * of_row[0] * s.up[e / 4][e % 4]);
+            else v[e] = of_row[1] * value;
         }
         if constexpr (kF32) {
             float *y = (float *)a.y + (at.first + row) * a.y_stride + col;

@@ -22,6 +22,8 @@ typedef u32x4 tile_array;
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+struct tile_nothing {};
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 constexpr uint32_t kNowhereAt = 0x80000000u;
@@ -400,15 +402,17 @@ struct tile_out {
         for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
     }
 };
-// Every row of the tile, a wave's quarter: use(row, column, v, u), column of the tile's (kPair: of its half).
-template <int kP, int kQ, bool kPair, class Product, class Use>
-__device__ __forceinline__ void tile_results(const Product &t, lds_char *lds, Use use)
+// Every row of the tile, a wave's quarter: column c of the tile's (kPair: of its half) and seven more of every row are a lane's.  fetch(row, c) asks for what else a row needs, kAhead
+// rows at once before any of them is stored (loads are not moved over stores, and one at a time each waits for memory); use(row, c, v, u, fetched).
+template <int kP, int kQ, bool kPair, class Product, class Fetch, class Use>
+__device__ __forceinline__ void tile_results(const Product &t, lds_char *lds, Fetch fetch, Use use)
 {
     typedef tile_out<kP, kQ, kPair> out;
     typedef decltype(t.acc[0][0][0] + t.acc[0][0][0]) value;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     lds_char *mine = lds + wave * out::kBytes;
-    constexpr int kJ = out::kRows / 32;
+    const int c = (wave & 1) * (kPair ? kP / 4 : kP / 2) + (lane & (out::kLanes - 1)) * 8;
+    constexpr int kJ = out::kRows / 32, kTimes = out::kRows / out::kAtOnce, kAhead = kTimes < 8 ? kTimes : 8;
 #pragma unroll
     for (int j = 0; j < Product::kNQ; j += kJ) {
 #pragma unroll
@@ -416,20 +420,28 @@ __device__ __forceinline__ void tile_results(const Product &t, lds_char *lds, Us
 #pragma unroll
             for (int n = 0; n < kJ; ++n) out::put(mine, i, n, t.acc[i][j + n]);
         wave_order();
-#pragma unroll 4
-        for (int r = 0; r < out::kRows; r += out::kAtOnce) {
-            const int row = r + lane / out::kLanes;
-            value v[8], u[8];
-            out::take(mine, row, 0, v);
-            if constexpr (kPair) out::take(mine, row, 1, u);
-            use((wave >> 1) * (kQ / 2) + j * 32 + row, (wave & 1) * (kPair ? kP / 4 : kP / 2) + (lane & (out::kLanes - 1)) * 8, v, kPair ? u : v);
+        const int row0 = (wave >> 1) * (kQ / 2) + j * 32;
+#pragma unroll 1
+        for (int n = 0; n < kTimes; n += kAhead) {
+            decltype(fetch(0, 0)) more[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) more[i] = fetch(row0 + (n + i) * out::kAtOnce + lane / out::kLanes, c);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int row = (n + i) * out::kAtOnce + lane / out::kLanes;
+                value v[8], u[8];
+                out::take(mine, row, 0, v);
+                if constexpr (kPair) out::take(mine, row, 1, u);
+                use(row0 + row, c, v, kPair ? u : v, more[i]);
+            }
         }
         wave_order();
     }
 }
 
 // A product's kernels.  Op has: args (with g, p_tiles, K and parts, memory for kRound tiles' sums or null); kP, kQ, kTrP, kInt8; kPair: half of a wave's columns belong to
-// the other half; feeds(): what is loaded; emit(): what becomes of eight columns of a row.
+// the other half; feeds(): what is loaded; emit(): what becomes of eight columns of a row, with what columns() gives for the columns, rows() for the row (kRowValues: two
+// values at most, which wait in LDS) and fetch() for both.
 template <class Op>
 struct tile_op : Op {
     typedef tile_product<Op::kP, Op::kQ, Op::kTrP, false, Op::kInt8> product;
@@ -438,6 +450,7 @@ struct tile_op : Op {
     // Workgroups that run at a time: LDS holds one of the large tiles a CU, two of 128 x 128, three of 128 x 64.
     static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : Op::kP * Op::kQ == 128 * 128 ? 512 : 768, kLeastSteps = 8;
     static constexpr int kLds = product::kLds > kTileWaves * out::kBytes ? product::kLds : kTileWaves * out::kBytes;
+    static constexpr int kRowsAt = kLds, kAllLds = kLds + (Op::kRowValues ? 8 * Op::kQ : 0);           // a row's values behind the stages
     static constexpr int kColumns = Op::kPair ? Op::kP / 2 : Op::kP, kJoinRows = kTileThreads * 8 / kColumns;         // rows that a workgroup of k_join takes
     static __device__ __forceinline__ int steps(const typename Op::args &a) { return (a.K + (Op::kInt8 ? 127 : 63)) / (Op::kInt8 ? 128 : 64); }
     // Eight sums of a part, at a row and a column of a tile of kP columns.
@@ -451,7 +464,7 @@ __global__ __launch_bounds__(kTileThreads, Op::kP * Op::kQ > 128 * 128 ? 1 : 2) 
 {
     typedef tile_op<Op> op;
     typedef typename op::product product;
-    __shared__ __attribute__((aligned(1024))) char lds[op::kLds];
+    __shared__ __attribute__((aligned(1024))) char lds[op::kAllLds];
     tile_runs<Op::kQ> runs;
     runs.count(a.g);
     const int steps = op::steps(a);
@@ -468,18 +481,30 @@ __global__ __launch_bounds__(kTileThreads, Op::kP * Op::kQ > 128 * 128 ? 1 : 2) 
         fp.part(k0, n);
         fq.part(k0, n);
     }
+    f32x2 of_row = {};                               // (asked for before the stages' loads, kept until they are through)
+    if constexpr (Op::kRowValues) if ((int)threadIdx.x < min(Op::kQ, at.rows) && !part) of_row = Op::rows(a, at.first + (int)threadIdx.x);
     product t;
     t.run(fp, fq, n, (lds_char *)lds);
     const uint32_t slot = u.part * split.rest + u.tile - split.whole;
     typedef typename op::value value;
-    tile_results<Op::kP, Op::kQ, Op::kPair>(t, (lds_char *)lds, [&](int row, int column, const value (&v)[8], const value (&w)[8]) {
-        if (part) {
+    if (part) {
+        tile_results<Op::kP, Op::kQ, Op::kPair>(t, (lds_char *)lds, [](int, int) { return 0; }, [&](int row, int column, const value (&v)[8], const value (&w)[8], int) {
             *op::place(a, slot, row, op::column_of(column, 0)) = typename op::eight{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
             if constexpr (Op::kPair) *op::place(a, slot, row, op::column_of(column, 1)) = typename op::eight{w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]};
-        } else {
-            Op::emit(a, at, row, column, v, w);
-        }
-    });
+        });
+        return;
+    }
+    f32x2 *rows = (f32x2 *)(lds + op::kRowsAt);
+    if constexpr (Op::kRowValues) {
+        if ((int)threadIdx.x < Op::kQ) rows[threadIdx.x] = of_row;
+        mw_lds_barrier();
+    }
+    const auto columns = Op::columns(a, at, (int)(threadIdx.x >> 6 & 1) * (op::kColumns / 2) + (int)(threadIdx.x & (op::out::kLanes - 1)) * 8);
+    tile_results<Op::kP, Op::kQ, Op::kPair>(
+        t, (lds_char *)lds, [&](int row, int column) { return Op::fetch(a, at, row, column); },
+        [&](int row, int column, const value (&v)[8], const value (&w)[8], const decltype(Op::fetch(a, at, 0, 0)) &more) {
+            Op::emit(a, at, row, column, v, w, columns, Op::kRowValues ? rows[row] : f32x2{}, more);
+        });
 }
 // The parts' sums in their order.  grid: (kJoinRows rows of a tile, tiles in parts at most)
 template <class Op>
@@ -502,7 +527,9 @@ __global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
     typename op::value x[8], y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) { x[e] = v[e]; y[e] = w[e]; }
-    Op::emit(a, at, row, column, x, y);
+    f32x2 of_row = {};
+    if constexpr (Op::kRowValues) if (row < at.rows) of_row = Op::rows(a, at.first + row);
+    Op::emit(a, at, row, column, x, y, Op::columns(a, at, column), of_row, Op::fetch(a, at, row, column));
 }
 static inline int64_t most_tiles(int64_t n_rows, int64_t n, int rows_a_tile) { return n_rows / rows_a_tile + (n < n_rows ? n : n_rows); }
 // The most tiles in parts there are: two parts each at least.
