@@ -39,8 +39,8 @@ struct up_op {
         store_bf16(a.h + (at.first + row) * a.I + col, v);
         if (a.kept) {
             uint16_t *kept = a.kept + (at.first + row) * 2 * a.I + col;
-            store_bf16(kept, gate);
-            store_bf16(kept + a.I, up);
+            store_bf16<true>(kept, gate);
+            store_bf16<true>(kept + a.I, up);
         }
     }
     // A few rows: eight gate rows and the eight up rows beside them.
@@ -101,7 +101,7 @@ struct rows_op {
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = kRowValues ? weight[0] * t[e] : t[e];
-        store_bf16(a.y + (at.first + row) * a.y_stride + col, v);
+        store_bf16<true>(a.y + (at.first + row) * a.y_stride + col, v);
     }
     static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * a.N * a.K; }
     static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
@@ -195,12 +195,12 @@ __global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, const float *
 }
 
 // ---- gradients of matrices: out[q][p] = sum over a run's rows of q's value times p's ---------------------------------
-struct grads_args {
-    row_groups g;
+struct grads_matrix {
     const uint16_t *q, *p; int64_t q_stride, p_stride;
-    uint16_t *out;                          // [n][M][N]
+    uint16_t *out;                          // [n][M][N], or null
     int32_t M, N, p_tiles, q_tiles;
 };
+struct grads_args { row_groups g; grads_matrix m[2]; uint32_t first; };         // first: workgroups of m[0]
 // Tiles of a matrix take as long as its run is: the XCDs get an eighth of every matrix's tiles each, and those of the longest run first.
 template <int kP, int kQ>
 __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_ffn_grads(grads_args a)
@@ -208,8 +208,10 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_f
     typedef tile_product<kP, kQ, true, true, false> product;
     typedef tile_out<kP, kQ, false> out_form;
     __shared__ __attribute__((aligned(1024))) char lds[product::kLds > kTileWaves * out_form::kBytes ? product::kLds : kTileWaves * out_form::kBytes];
-    const uint32_t each = (uint32_t)a.p_tiles * (uint32_t)a.q_tiles, per = (each + 7) / 8, at = blockIdx.x >> 3;
-    const uint32_t tile = (blockIdx.x & 7) * per + at % per;
+    const bool second = blockIdx.x >= a.first;
+    const grads_matrix m = second ? a.m[1] : a.m[0];
+    const uint32_t id = blockIdx.x - (second ? a.first : 0), each = (uint32_t)m.p_tiles * (uint32_t)m.q_tiles, per = (each + 7) / 8, at = id >> 3;
+    const uint32_t tile = (id & 7) * per + at % per;
     int e = (int)(at / per);
     if (tile >= each || e >= a.g.n) return;
     int64_t first, end;
@@ -227,17 +229,17 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_f
     }
     group_bounds(a.g, e, first, end);
     uint32_t pt, qt;
-    tile_in_block(tile, a.p_tiles, a.q_tiles, pt, qt);
+    tile_in_block(tile, m.p_tiles, m.q_tiles, pt, qt);
     const int q0 = (int)qt * kQ, p0 = (int)pt * kP, rows = (int)(end - first);
     tile_feed<kP, true, false> fp;
     tile_feed<kQ, true, false> fq;
-    fp.lines((const char *)(a.p + first * a.p_stride + p0), rows, a.p_stride * 2, a.N - p0);
-    fq.lines((const char *)(a.q + first * a.q_stride + q0), rows, a.q_stride * 2, a.M - q0);
+    fp.lines((const char *)(m.p + first * m.p_stride + p0), rows, m.p_stride * 2, m.N - p0);
+    fq.lines((const char *)(m.q + first * m.q_stride + q0), rows, m.q_stride * 2, m.M - q0);
     product t;
     t.run(fp, fq, (rows + 63) / 64, (lds_char *)lds);
-    uint16_t *out = a.out + (int64_t)e * a.M * a.N;
+    uint16_t *out = m.out + (int64_t)e * m.M * m.N;
     tile_results<kP, kQ, false>(t, (lds_char *)lds, [](int, int) { return 0; }, [&](int row, int column, const float (&v)[8], const float (&)[8], int) {
-        if (q0 + row < a.M && p0 + column < a.N) store_bf16(out + (int64_t)(q0 + row) * a.N + p0 + column, v);
+        if (q0 + row < m.M && p0 + column < m.N) store_bf16<true>(out + (int64_t)(q0 + row) * m.N + p0 + column, v);
     });
 }
 
@@ -284,14 +286,20 @@ int32_t ffn_ready(const mw_ctx *ctx, const mw_experts *e, bool backward)
 }
 // A matrix of bf16 rows of the caller's.
 bool rows_fit(const void *p, int64_t stride, int64_t width) { return p && !((uintptr_t)p & 15u) && stride >= width && stride % 8 == 0; }
+static inline bool grads_large(int64_t n_rows, int64_t n) { return n_rows >= 384 * n; }
 template <int kP, int kQ>
 int32_t launch_grads(grads_args a, hipStream_t s)
 {
-    a.p_tiles = (int32_t)pieces(a.N, kP);
-    a.q_tiles = (int32_t)pieces(a.M, kQ);
-    const int64_t grid = pieces((int64_t)a.p_tiles * a.q_tiles, 8) * 8 * a.g.n;
-    if (grid > 0x7ffffff0LL) return MW_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), dim3((uint32_t)grid), dim3(kTileThreads), 0, s, a);
+    int64_t grid[2];
+    for (int i = 0; i < 2; ++i) {
+        grads_matrix &m = a.m[i];
+        m.p_tiles = (int32_t)pieces(m.N, kP);
+        m.q_tiles = (int32_t)pieces(m.M, kQ);
+        grid[i] = m.out ? pieces((int64_t)m.p_tiles * m.q_tiles, 8) * 8 * a.g.n : 0;
+    }
+    if (grid[0] + grid[1] > 0x7ffffff0LL) return MW_ERR_UNSUPPORTED;
+    a.first = (uint32_t)grid[0];
+    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), dim3((uint32_t)(grid[0] + grid[1])), dim3(kTileThreads), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }
@@ -376,14 +384,10 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
             if (rc != MW_OK) return rc;
         }
     }
-    if (d_gate_up_dev) {
-        grads_args a = {g, d_act, (const uint16_t *)x_dev, 2 * (int64_t)I, x_stride, (uint16_t *)d_gate_up_dev, 2 * I, H, 0, 0};
-        rc = launch_grads<256, 256>(a, s);
-        if (rc != MW_OK) return rc;
-    }
-    if (d_down_dev) {
-        grads_args a = {g, (const uint16_t *)dy_dev, act, dy_stride, I, (uint16_t *)d_down_dev, H, I, 0, 0};
-        rc = launch_grads<256, 256>(a, s);
+    if (d_gate_up_dev || d_down_dev) {
+        const grads_args a = {g, {{d_act, (const uint16_t *)x_dev, 2 * (int64_t)I, x_stride, (uint16_t *)d_gate_up_dev, 2 * I, H, 0, 0},
+                                  {(const uint16_t *)dy_dev, act, dy_stride, I, (uint16_t *)d_down_dev, H, I, 0, 0}}, 0};
+        rc = grads_large(n_rows, g.n) ? launch_grads<256, 256>(a, s) : launch_grads<128, 128>(a, s);
     }
     return rc;
 }

@@ -551,12 +551,15 @@ int32_t launch_tiles(typename Op::args a, int columns, hipStream_t s)
 }
 
 __device__ __forceinline__ float tile_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+// kStreaming: nobody reads it soon.
+template <bool kStreaming = false>
 __device__ __forceinline__ void store_bf16(uint16_t *to, const float (&v)[8])
 {
     bf16x8 o;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-    *(bf16x8 *)to = o;
+    if constexpr (kStreaming) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, o), (u32x4 *)to);
+    else *(bf16x8 *)to = o;
 }
 
 }  // namespace
