@@ -18,7 +18,7 @@ template <> struct few_kind<true> {
     typedef i32x4 acc;
     static __device__ __forceinline__ acc mma(u32x4 a, u32x4 b, acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0); }
 };
-constexpr int kFewWaves = 8, kFewThreads = 64 * kFewWaves, kSpanBytes = 128;
+constexpr int kSpanBytes = 128;
 
 template <int kCols> struct few_operands {
     array w, x;
@@ -60,7 +60,7 @@ struct few_stage {
 };
 
 // Sixteen matrix rows of tile `tile` times rows first .. of run e (count of them left).
-template <class Op, int kCols, int kDepth>
+template <class Op, int kFewWaves, int kCols, int kDepth>
 __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, int tile, int64_t first, int count, char *lds)
 {
     typedef few_kind<Op::kInt8> kind;
@@ -100,8 +100,9 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
         *(typename kind::acc *)&part[(wave * 16 + (lane & 15)) * 16 + (lane >> 4) * 4] = acc[c];
         __syncthreads();
         constexpr int kEach = Op::kPair ? 8 : 16;
-        const int col = (int)threadIdx.x / kEach, r = (int)threadIdx.x % kEach;
-        if (col < 16 && c * 16 + col < count) {
+        for (int t = threadIdx.x; t < 16 * kEach; t += 64 * kFewWaves) {
+            const int col = t / kEach, r = t % kEach;
+            if (c * 16 + col >= count) continue;
             value v = 0, w = 0;
 #pragma unroll
             for (int n = 0; n < kFewWaves; ++n) {
@@ -114,8 +115,8 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
     __syncthreads();
 }
 // grid: (tiles of sixteen matrix rows, runs)
-template <class Op>
-__global__ __launch_bounds__(kFewThreads) void k_few(typename Op::args a)
+template <class Op, int kFewWaves>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few(typename Op::args a)
 {
     __shared__ __align__(16) char lds[kFewWaves * 3 * kTileBytes];
     const int e = blockIdx.y, tile = blockIdx.x;
@@ -123,15 +124,20 @@ __global__ __launch_bounds__(kFewThreads) void k_few(typename Op::args a)
     group_bounds(a.g, e, first, end);
     while (first < end) {
         const int left = (int)(end - first);
-        if (left <= 16) few_columns<Op, 1, 4>(a, e, tile, first, left, lds);
-        else few_columns<Op, 2, 3>(a, e, tile, first, left, lds);
+        if (left <= 16) few_columns<Op, kFewWaves, 1, 4>(a, e, tile, first, left, lds);
+        else few_columns<Op, kFewWaves, 2, 3>(a, e, tile, first, left, lds);
         first += left <= 16 ? 16 : 32;
     }
 }
+// Eight waves to a workgroup where there is hardly one a CU and rows are long, else four.  us, 4 / 8: 1 row of four experts 7168 x 2048 24.3 / 20.7, 1 row of codes 7168 -> 4096
+// 12.5 / 11.1; 64 rows of four experts 70.7 / 73.6, of eight 4096 x 1024 41.0 / 49.4, of sixteen 2048 x 768 31.4 / 44.1, codes 28.9 / 41.5.
+static inline int few_waves(int64_t workgroups, int64_t row_bytes) { return workgroups <= 256 && row_bytes >= 4096 ? 8 : 4; }
 template <class Op>
 int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_few<Op>), dim3((uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), (uint32_t)a.g.n), dim3(kFewThreads), 0, s, a);
+    const dim3 grid((uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), (uint32_t)a.g.n);
+    if (few_waves((int64_t)grid.x * (a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows), (int64_t)a.K * (Op::kInt8 ? 1 : 2)) == 8) hipLaunchKernelGGL((k_few<Op, 8>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_few<Op, 4>), grid, dim3(256), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }
@@ -142,7 +148,7 @@ static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t 
 {
     if (n_rows <= 16 * n) return kFew;
     const double size = (double)n_rows * (double)columns * (double)bytes;
-    return n_rows >= 192 * n && size >= 7e10 ? kLarge : n_rows >= 96 * n && size >= 2.4e10 ? kMiddle : kSmall;
+    return n_rows >= 192 * n && size >= 1.1e11 ? kLarge : n_rows >= 64 * n && size >= 2.3e10 ? kMiddle : kSmall;
 }
 // The tile sizes' arguments are alike.
 template <class To, class From> To as(const From &f)
@@ -150,7 +156,7 @@ template <class To, class From> To as(const From &f)
     static_assert(sizeof(To) == sizeof(From), "");
     return __builtin_bit_cast(To, f);
 }
-// Large, Middle, Small: one product with tiles of 256 x 256, 128 x 128 and 128 x 64.  kHasFew: the product has few_emit().
+// Large, Middle, Small: one product with tiles of 256 x 256, 256 x 128 and 128 x 64.  kHasFew: the product has few_emit().
 template <class Large, class Middle, class Small, bool kHasFew>
 int32_t launch_product(int form, const typename Large::args &a, int columns, hipStream_t s)
 {

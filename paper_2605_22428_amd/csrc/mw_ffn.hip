@@ -244,7 +244,7 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_f
 }
 
 // ---- entry points -----------------------------------------------------------------------------------------------------
-constexpr int64_t kPartsBytes = 256LL * 256 * 256 * 4;          // sums of a round of the large tiles; of the small ones less
+constexpr int64_t kPartsBytes = 256LL * 256 * 256 * 4;          // sums of a round of the large tiles; the others take less
 int64_t pieces(int64_t n, int64_t each) { return (n + each - 1) / each; }
 
 struct ffn_ws { int64_t act, d_gate_up, sums, parts, codes, scales, total; };
@@ -341,8 +341,8 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, 2 * (int64_t)H);
     const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
     const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
-    rc = launch_product<up_op<256, 256>, up_op<128, 128>, up_op<128, 64>, true>(form, u, I, s);
-    if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<128, 128, false>, rows_op<128, 64, false>, true>(form, d, H, s);
+    rc = launch_product<up_op<256, 256>, up_op<256, 128>, up_op<128, 64>, true>(form, u, I, s);
+    if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<256, 128, false>, rows_op<128, 64, false>, true>(form, d, H, s);
     return rc;
 }
 
@@ -372,7 +372,7 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
     const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, 2 * (int64_t)H);
     if (n_rows > 0) {
         const act_op<256, 256>::args a = {g, (const uint16_t *)dy_dev, dy_stride, (const uint16_t *)experts->down_dev, row_weights_dev, (const uint16_t *)kept_dev, act, d_act, sums, parts, H, I, 0};
-        rc = launch_product<act_op<256, 256>, act_op<128, 128>, act_op<128, 64>, false>(form, a, I, s);
+        rc = launch_product<act_op<256, 256>, act_op<256, 128>, act_op<128, 64>, false>(form, a, I, s);
         if (rc != MW_OK) return rc;
         if (sums) {
             hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 16)), dim3(256), 0, s, g, sums, (int)pieces(I, kSum), d_row_weights_dev);
@@ -380,7 +380,7 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
         }
         if (dx_dev) {
             const rows_op<256, 256, true>::args d = {g, d_act, 2 * (int64_t)I, (const uint16_t *)experts->gate_up_dev, nullptr, (uint16_t *)dx_dev, dx_stride, parts, 2 * I, H, 0};
-            rc = launch_product<rows_op<256, 256, true>, rows_op<128, 128, true>, rows_op<128, 64, true>, false>(form, d, H, s);
+            rc = launch_product<rows_op<256, 256, true>, rows_op<256, 128, true>, rows_op<128, 64, true>, false>(form, d, H, s);
             if (rc != MW_OK) return rc;
         }
     }
