@@ -142,13 +142,19 @@ int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
     return MW_OK;
 }
 
-// How a product of rows with n matrices of `columns` rows of `bytes` is cut.
+// How rows' products with n matrices of `columns` rows of `width` values are cut; parts: a broken round's tiles are cut along the sum.  us of the whole call, rows of uneven runs, weights
+// from memory, few / small / middle / large:
+//   mw_ffn, four experts 7168 x 2048, 64 rows 74 / 95 / 96 / 122, 128 rows 120 / 96 / 98 / 124, 256 210 / 102 / 102 / 126, 512 - / 136 / 116 / 132, 1024 - / 205 / 162 / 157, 4096 - / 528 / 385 / 348
+//   eight 4096 x 1024, 128 rows 53 / 66 / 70 / 96, 256 80 / 69 / 72 / 96, 1024 - / 89 / 82 / 94, 4096 - / 187 / 149 / 162, 8192 - / 314 / 247 / 239; codes, 1024 rows - / 67 / 62 / 80
+//   one 4096 x 2048, 512 rows - / 59 / 60 / 78, 1024 - / 72 / 81 / 99, 2048 - / 164 / 100 / 135, 4096 - / 262 / 193 / 184
+//   mw_matmul_int8 with its rows' codes, four matrices 7168 -> 2048, 64 rows 20 / 27 / 44 / 66, 1024 - / 44 / 50 / 73, 2048 - / 81 / 67 / 95, 4096 - / 124 / 121 / 108
+//   mw_ffn_backward, four experts 7168 x 2048, 512 rows - / 292 / 267 / 284, 2048 - / 579 / 515 / 493
 enum { kFew, kSmall, kMiddle, kLarge };
-static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t bytes)
+static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t width, bool parts)
 {
     if (n_rows <= 16 * n) return kFew;
-    const double size = (double)n_rows * (double)columns * (double)bytes;
-    return n_rows >= 192 * n && size >= 1.1e11 ? kLarge : n_rows >= 64 * n && size >= 2.3e10 ? kMiddle : kSmall;
+    const double size = (double)n_rows * (double)columns * (double)width;
+    return n_rows >= 192 * n && size >= (parts ? 6.5e10 : 5e10) ? kLarge : n_rows >= 64 * n && size >= (parts ? 7.5e9 : 1.6e10) ? kMiddle : kSmall;
 }
 // The tile sizes' arguments are alike.
 template <class To, class From> To as(const From &f)

@@ -338,7 +338,7 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     const row_groups g = {expert_offsets_dev, n_rows, ctx->n_local};
     const hipStream_t s = (hipStream_t)stream;
     if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), (float *)(b + w.parts), s);
-    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, 2 * (int64_t)H);
+    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, H, true);
     const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
     const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
     rc = launch_product<up_op<256, 256>, up_op<256, 128>, up_op<128, 64>, true>(form, u, I, s);
@@ -369,7 +369,7 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
     const hipStream_t s = (hipStream_t)stream;
     uint16_t *act = (uint16_t *)(b + w.act), *d_act = (uint16_t *)(b + w.d_gate_up);
     float *sums = d_row_weights_dev ? (float *)(b + w.sums) : nullptr, *parts = (float *)(b + w.parts);
-    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, 2 * (int64_t)H);
+    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, H, true);
     if (n_rows > 0) {
         const act_op<256, 256>::args a = {g, (const uint16_t *)dy_dev, dy_stride, (const uint16_t *)experts->down_dev, row_weights_dev, (const uint16_t *)kept_dev, act, d_act, sums, parts, H, I, 0};
         rc = launch_product<act_op<256, 256>, act_op<256, 128>, act_op<128, 64>, false>(form, a, I, s);

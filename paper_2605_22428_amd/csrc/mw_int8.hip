@@ -5,8 +5,11 @@
 namespace {
 
 // ---- rows -> codes and scales ---------------------------------------------------------------------------------------
-// code = round-half-even(127 x / a), a the row's largest |x|.  127 x is exact in fp32, and quotients that are no half are far enough
-// from one (a and x have eight bits each) that a division rounded once cannot cross it; halves themselves are exact.
+// code = round-half-even(127 x / a), a the row's largest |x|, of the exact quotient v.  x and a have eight significant bits, so v is a half of an odd number exactly or at least
+// |v| 2^-17 away from one: |v - (2m + 1) / 2| = |254 X 2^d - (2m + 1) A| / 2A with whole X, A of eight bits and d the difference of their exponents, and a numerator that is not 0
+// is 2^d at least.  y = x (127 / a) is off by |v| 2^-23 at most.  Rounded to 18 bits (off by |v| 2^-18 at most) it is such a half exactly where v is one, and on v's side of it
+// elsewhere; adding 1.5 2^23 then rounds to the even whole number and leaves it in the low bits.  Six instructions a value instead of a division's dozen: 8192 rows of
+// 7168 values, 176 MB, 36 -> 31 us (5.7 TB/s), 16384 rows of 2048, 100 MB, 27 -> 18 us.
 struct quant_args {
     const uint16_t *x; int64_t x_stride;
     int8_t *codes; int64_t codes_stride;
@@ -15,45 +18,66 @@ struct quant_args {
     const int64_t *end;                     // rows from here on are left alone; or null
     int32_t n;
 };
-constexpr int kQuantChunks = 4;             // of 8 values a lane that stay in registers
+__device__ __forceinline__ uint32_t row_most(uint32_t most, u32x4 q)        // |x| as its bits, which order like the values; NaN and infinity are above all
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = max(most, max(q[i] << 16 & 0x7fff0000u, q[i] & 0x7fff0000u));
+    return most;
+}
+struct row_factor { float pre, by; };                                       // pre: a power of two, so that 127 / a does not overflow
+__device__ __forceinline__ row_factor factor_of(uint32_t most)
+{
+    const float a = __uint_as_float(most), pre = a < 0x1p-60f ? 0x1p64f : 1.0f;
+    return most == 0 || most >= 0x7f800000u ? row_factor{0.0f, 0.0f} : row_factor{pre, 127.0f / (a * pre)};
+}
+__device__ __forceinline__ uint32_t code_of(uint32_t bits, row_factor f)    // in the low byte
+{
+    const float y = __uint_as_float(bits) * f.pre * f.by;
+    return __float_as_uint(__uint_as_float((__float_as_uint(y) + 0x20u) & ~0x3fu) + 12582912.0f);
+}
+__device__ __forceinline__ void put_codes(const quant_args &a, int64_t row, int chunk, u32x4 q, row_factor f, bool some)
+{
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    u32x2 o;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t c0 = code_of(q[i * 2] << 16, f), c1 = code_of(q[i * 2] & 0xffff0000u, f), c2 = code_of(q[i * 2 + 1] << 16, f), c3 = code_of(q[i * 2 + 1] & 0xffff0000u, f);
+        const uint32_t low = __builtin_amdgcn_perm(c1, c0, 0x0c0c0400u), high = __builtin_amdgcn_perm(c3, c2, 0x04000c0cu);
+        o[i] = some ? low | high : 0u;
+    }
+    *(u32x2 *)(a.codes + row * a.codes_stride + chunk * 8) = o;
+}
+__device__ __forceinline__ float scale_of(uint32_t most) { return most < 0x7f800000u ? __uint_as_float(most) / 127.0f : __uint_as_float(0x7fc00000u); }
+
+// kWaves waves a row; up to kChunks pieces of eight values a lane stay in registers, of longer rows the rest is read twice.
+template <int kWaves, int kChunks>
 __global__ __launch_bounds__(256) void k_quantize(quant_args a)
 {
     __shared__ uint32_t waves[4];
-    const int tid = threadIdx.x, chunks = a.n / 8;
-    const int64_t row = blockIdx.x;
-    if (a.end && row >= *a.end) return;
+    constexpr int kLanes = kWaves * 64;
+    const int tid = (int)threadIdx.x % kLanes, chunks = a.n / 8;
+    const int64_t row = (int64_t)blockIdx.x * (4 / kWaves) + (int)threadIdx.x / kLanes;
+    if (row >= a.n_rows || (a.end && row >= *a.end)) return;                // (a wave's or the workgroup's)
     const uint16_t *x = a.x + row * a.x_stride;
-    u32x4 v[kQuantChunks];
-    uint32_t most = 0;                      // |x| as its bits, which order like the values; NaN and infinity are above all
-    auto look = [&](u32x4 q) {
+    u32x4 v[kChunks];
+    uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = max(most, max(q[i] << 16 & 0x7fff0000u, q[i] & 0x7fff0000u));
-    };
+    for (int c = 0; c < kChunks; ++c) v[c] = tid + c * kLanes < chunks ? *(const u32x4 *)(x + (tid + c * kLanes) * 8) : u32x4{};
 #pragma unroll
-    for (int c = 0; c < kQuantChunks; ++c) v[c] = tid + c * 256 < chunks ? *(const u32x4 *)(x + (tid + c * 256) * 8) : u32x4{};
-#pragma unroll
-    for (int c = 0; c < kQuantChunks; ++c) look(v[c]);
-    for (int c = tid + kQuantChunks * 256; c < chunks; c += 256) look(*(const u32x4 *)(x + c * 8));
+    for (int c = 0; c < kChunks; ++c) most = row_most(most, v[c]);
+    for (int c = tid + kChunks * kLanes; c < chunks; c += kLanes) most = row_most(most, *(const u32x4 *)(x + c * 8));
     most = mw_wave_max(most);
-    if ((tid & 63) == 0) waves[tid >> 6] = most;
-    mw_lds_barrier();
-    most = max(max(waves[0], waves[1]), max(waves[2], waves[3]));
-    const bool finite = most < 0x7f800000u;
-    const float a_max = __uint_as_float(most);
-    if (tid == 0) a.scales[row] = finite ? a_max / 127.0f : __uint_as_float(0x7fc00000u);
-    const bool some = finite && most != 0;
-    auto code = [&](uint32_t bits) { return some ? (uint32_t)(int)__builtin_rintf(127.0f * __uint_as_float(bits) / a_max) & 0xffu : 0u; };
-    auto put = [&](int c, u32x4 q) {
-        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        u32x2 o;
+    if constexpr (kWaves > 1) {
+        if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
+        mw_lds_barrier();
+        most = max(max(waves[0], waves[1]), max(waves[2], waves[3]));
+    }
+    if (tid == 0) a.scales[row] = scale_of(most);
+    const row_factor f = factor_of(most);
+    const bool some = f.by != 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            o[i] = code(q[i * 2] << 16) | code(q[i * 2] & 0xffff0000u) << 8 | code(q[i * 2 + 1] << 16) << 16 | code(q[i * 2 + 1] & 0xffff0000u) << 24;
-        *(u32x2 *)(a.codes + row * a.codes_stride + c * 8) = o;
-    };
-#pragma unroll
-    for (int c = 0; c < kQuantChunks; ++c) if (tid + c * 256 < chunks) put(tid + c * 256, v[c]);
-    for (int c = tid + kQuantChunks * 256; c < chunks; c += 256) put(c, *(const u32x4 *)(x + c * 8));
+    for (int c = 0; c < kChunks; ++c) if (tid + c * kLanes < chunks) put_codes(a, row, tid + c * kLanes, v[c], f, some);
+    for (int c = tid + kChunks * kLanes; c < chunks; c += kLanes) put_codes(a, row, c, *(const u32x4 *)(x + c * 8), f, some);
 }
 
 // ---- rows of codes times matrices of codes ------------------------------------------------------------------------
@@ -140,11 +164,15 @@ struct int8_op {
 template <bool kGated, bool kF32>
 int32_t launch_int8(const typename int8_op<256, 256, kGated, kF32>::args &a, hipStream_t s)
 {
-    return launch_product<int8_op<256, 256, kGated, kF32>, int8_op<256, 128, kGated, kF32>, int8_op<128, 64, kGated, kF32>, true>(rows_form(a.g.n_rows, a.g.n, kGated ? 2 * (int64_t)a.N : a.N, a.K), a, a.N, s);
+    return launch_product<int8_op<256, 256, kGated, kF32>, int8_op<256, 128, kGated, kF32>, int8_op<128, 64, kGated, kF32>, true>(rows_form(a.g.n_rows, a.g.n, kGated ? 2 * (int64_t)a.N : a.N, a.K, a.parts != nullptr), a, a.N, s);
 }
+// Many rows take a wave each, few or long ones a workgroup each.  us: 16384 rows of 2048 values a workgroup / a wave 22 / 18; of 7168 values 62 / 67.
 int32_t launch_quantize(const quant_args &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_quantize, dim3((uint32_t)a.n_rows), dim3(256), 0, s, a);
+    const dim3 four((uint32_t)((a.n_rows + 3) / 4));
+    if (a.n_rows < 2048 || a.n > 4096) hipLaunchKernelGGL((k_quantize<4, 4>), dim3((uint32_t)a.n_rows), dim3(256), 0, s, a);
+    else if (a.n <= 2048) hipLaunchKernelGGL((k_quantize<1, 4>), four, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_quantize<1, 8>), four, dim3(256), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }

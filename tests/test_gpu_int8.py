@@ -24,7 +24,7 @@ def quantized(x, pad=0):
     return codes[:-1, :x.shape[1]], scales[:-1]
 
 
-@pytest.mark.parametrize("rows,cols", [(1, 16), (3, 48), (64, 272), (5, 2048), (2, 7168), (3, 8192), (2, 8208), (1, 65536), (1000, 64)])
+@pytest.mark.parametrize("rows,cols", [(1, 16), (3, 48), (64, 272), (5, 2048), (2, 7168), (3, 8192), (2, 8208), (1, 65536), (1000, 64), (2048, 16), (2051, 2048), (2049, 2064), (2050, 4112), (2048, 8192)])
 @pytest.mark.parametrize("pad", [0, 16])
 def test_codes(rows, cols, pad):
     x = normal(rows + cols, rows, cols).bfloat16()
