@@ -953,7 +953,8 @@ MW_API int32_t mw_ffn_workspace_bytes(mw_ctx *ctx, const mw_experts *experts, in
  * mw_ffn: the experts' gated feed-forward blocks over the rows that a dispatch brought, between mw_unpack and mw_combine_gather.  For a row r of
  * local expert e, with silu(v) = v / (1 + exp(-v)):
  *   g = gate_e x_r,   u = up_e x_r,   h = silu(g) u,   y_r = w_r (down_e h)
- * in fp32 sums; h is rounded to bf16 between the two products, y once.
+ * in fp32 sums; between the two products h is rounded to bf16, or with few rows held as the sum of two bf16 values (an infinite value of down_e can then give a NaN
+ * where one product would be infinite); y is rounded once.
  *   experts: bf16 or MW_WEIGHT_INT8_CHANNEL (fp8: MW_ERR_UNSUPPORTED).  With 8-bit experts x, and h after its rounding to bf16, are held in codes as
  *     mw_quantize_rows makes them, and products are mw_matmul_int8's.
  *   x_dev, y_dev: bf16 rows of `hidden` values in the order of their experts (mw_unpack's out_rows), x_stride and y_stride elements apart (multiples of 8;

@@ -59,25 +59,27 @@ struct few_stage {
     }
 };
 
-// Sixteen matrix rows of tile `tile` times rows first .. of run e (count of them left).
+// Sixteen matrix rows of tile `tile` times rows first .. of run e (count of them left).  Op::kTerms 2: rows are sums of two, the second K values behind the first; both are
+// columns of the matrix instruction, which has sixteen whether they are used or not.
 template <class Op, int kFewWaves, int kCols, int kDepth>
 __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, int tile, int64_t first, int count, char *lds)
 {
     typedef few_kind<Op::kInt8> kind;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l8 = lane >> 3;
     const uint32_t piece = (uint32_t)(lane & 7) * 16;
+    constexpr int kUnit = Op::kInt8 ? 1 : 2, kTerms = Op::kTerms, kPass = kCols * 16 / kTerms;
     few_operands<kCols> o;
     o.w = array_at(Op::few_matrix(a, e));
     o.x = array_at(Op::few_x(a, first));
-    o.limit = (uint32_t)a.K * (Op::kInt8 ? 1 : 2);
+    o.limit = (uint32_t)a.K * kUnit;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint32_t at = Op::few_row(a, tile, i * 8 + l8);
         o.row[i] = at == kNowhere ? at : at + piece;
 #pragma unroll
         for (int c = 0; c < kCols; ++c) {
-            const int r = c * 16 + i * 8 + l8;
-            o.col[c][i] = r < count ? (uint32_t)r * (uint32_t)a.x_stride * (Op::kInt8 ? 1 : 2) + piece : kNowhere;
+            const int column = c * 16 + i * 8 + l8, r = column % kPass, term = column / kPass;
+            o.col[c][i] = r < count ? ((uint32_t)r * (uint32_t)a.x_stride + (uint32_t)(term * a.K)) * kUnit + piece : kNowhere;
         }
     }
     typename kind::acc acc[kCols] = {};
@@ -94,19 +96,22 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
     }
     typedef decltype(acc[0][0] + acc[0][0]) value;
     value *part = (value *)lds;                  // [wave][column][16 rows]
+    if constexpr (kTerms == 2 && kCols == 2) acc[0] += acc[1];
+    constexpr int kSums = kTerms == 2 ? 1 : kCols, kHere = kPass < 16 ? kPass : 16;
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {
+    for (int c = 0; c < kSums; ++c) {
         __syncthreads();                         // (the sums take the place of the waves' pieces)
         *(typename kind::acc *)&part[(wave * 16 + (lane & 15)) * 16 + (lane >> 4) * 4] = acc[c];
         __syncthreads();
         constexpr int kEach = Op::kPair ? 8 : 16;
-        for (int t = threadIdx.x; t < 16 * kEach; t += 64 * kFewWaves) {
+        for (int t = threadIdx.x; t < kHere * kEach; t += 64 * kFewWaves) {
             const int col = t / kEach, r = t % kEach;
             if (c * 16 + col >= count) continue;
             value v = 0, w = 0;
 #pragma unroll
             for (int n = 0; n < kFewWaves; ++n) {
                 v += part[(n * 16 + col) * 16 + r];
+                if constexpr (kTerms == 2 && kCols == 1) v += part[(n * 16 + 8 + col) * 16 + r];
                 if constexpr (Op::kPair) w += part[(n * 16 + col) * 16 + 8 + r];
             }
             Op::few_emit(a, e, first + c * 16 + col, tile * kEach + r, v, w);
@@ -122,11 +127,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(typename Op::args a)
     const int e = blockIdx.y, tile = blockIdx.x;
     int64_t first, end;
     group_bounds(a.g, e, first, end);
+    constexpr int kPass = 16 / Op::kTerms;
     while (first < end) {
         const int left = (int)(end - first);
-        if (left <= 16) few_columns<Op, kFewWaves, 1, 4>(a, e, tile, first, left, lds);
+        if (left <= kPass) few_columns<Op, kFewWaves, 1, 4>(a, e, tile, first, left, lds);
         else few_columns<Op, kFewWaves, 2, 3>(a, e, tile, first, left, lds);
-        first += left <= 16 ? 16 : 32;
+        first += left <= kPass ? kPass : 2 * kPass;
     }
 }
 // Eight waves to a workgroup where there is hardly one a CU and rows are long, else four.  us, 4 / 8: 1 row of four experts 7168 x 2048 24.3 / 20.7, 1 row of codes 7168 -> 4096

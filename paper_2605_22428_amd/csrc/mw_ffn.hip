@@ -10,11 +10,12 @@ template <int kCols, int kRows>
 struct up_op {
     static constexpr int kP = kCols, kQ = kRows;
     static constexpr bool kTrP = false, kInt8 = false, kPair = true, kRowValues = false;
+    static constexpr int kTerms = 1;
     struct args {
         row_groups g;
         const uint16_t *x; int64_t x_stride;
         const uint16_t *w;                      // [n][2][I][H]
-        uint16_t *h, *kept;                     // [rows][I], [rows][2][I] or null
+        uint16_t *h, *kept;                     // [rows][I], a few rows: [rows][2][I] with what its rounding left; [rows][2][I] or null
         float *parts;
         int32_t K, I, p_tiles;
     };
@@ -52,7 +53,12 @@ struct up_op {
     }
     static __device__ __forceinline__ void few_emit(const args &a, int, int64_t row, int col, float gate, float up)
     {
-        a.h[row * a.I + col] = mw_f32_to_bf16(gate * tile_sigmoid(gate) * up);
+        // Matrices bound these products, so h can be held as two bf16 values, 16 bits of mantissa: one alone adds as much error as the output's own rounding.
+        const float v = gate * tile_sigmoid(gate) * up;
+        const uint16_t high = mw_f32_to_bf16(v);
+        const float rest = v - mw_bf16_to_f32(high);
+        a.h[row * 2 * a.I + col] = high;
+        a.h[row * 2 * a.I + a.I + col] = rest - rest == 0.0f ? mw_f32_to_bf16(rest) : 0;
         if (a.kept) {
             a.kept[row * 2 * a.I + col] = mw_f32_to_bf16(gate);
             a.kept[row * 2 * a.I + a.I + col] = mw_f32_to_bf16(up);
@@ -76,6 +82,7 @@ __device__ __forceinline__ void columns_from(tile_feed<kP, false, false> &fp, co
 template <int kCols, int kRows, bool kTr>
 struct rows_op {
     static constexpr int kP = kCols, kQ = kRows;
+    static constexpr int kTerms = 2;
     static constexpr bool kTrP = kTr, kInt8 = false, kPair = false, kRowValues = !kTr;          // (gradients of rows have no weights)
     struct args {
         row_groups g;
@@ -253,7 +260,7 @@ ffn_ws ffn_layout(const mw_experts *e, int32_t hidden, int64_t rows, bool backwa
     ffn_ws w = {};
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += mw_align_up(bytes, 256); return at; };
-    w.act = take(2 * rows * e->inter);
+    w.act = take((backward || e->format != MW_ROW_BF16 ? 2 : 4) * rows * e->inter);         // (a few rows' are held as two values each)
     if (backward) {
         w.d_gate_up = take(4 * rows * e->inter);
         w.sums = take(4 * rows * pieces(e->inter, kSum));
@@ -340,7 +347,7 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), (float *)(b + w.parts), s);
     const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, H, true);
     const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
-    const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
+    const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), form == kFew ? 2 * (int64_t)I : I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
     rc = launch_product<up_op<256, 256>, up_op<256, 128>, up_op<128, 64>, true>(form, u, I, s);
     if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<256, 128, false>, rows_op<128, 64, false>, true>(form, d, H, s);
     return rc;

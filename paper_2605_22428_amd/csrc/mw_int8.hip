@@ -87,6 +87,7 @@ template <int kCols, int kRows, bool kGated, bool kF32>
 struct int8_op {
     static constexpr int kP = kCols, kQ = kRows;
     static constexpr bool kTrP = false, kInt8 = true, kPair = kGated, kRowValues = true;
+    static constexpr int kTerms = 1;
     struct args {
         row_groups g;
         const int8_t *x; int64_t x_stride;
