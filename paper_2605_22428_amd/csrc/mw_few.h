@@ -7,7 +7,7 @@
 
 namespace {
 
-// Sixteen matrix rows are one side of the matrix instruction, up to sixteen rows the other.  A workgroup's waves take every kFewWaves-th 128 bytes along the sum, kDepth of
+// Sixteen matrix rows are one side of the matrix instruction, up to sixteen rows the other.  Waves that share a tile take every kAlong-th 128 bytes along the sum, kDepth of
 // them on the way at a time, as mw_stream.h does and for its reasons; bf16 values and codes differ in the instruction only.
 template <bool kInt8> struct few_kind;
 template <> struct few_kind<false> {
@@ -61,11 +61,11 @@ struct few_stage {
 
 // Sixteen matrix rows of tile `tile` times rows first .. of run e (count of them left).  Op::kTerms 2: rows are sums of two, the second K values behind the first; both are
 // columns of the matrix instruction, which has sixteen whether they are used or not.
-template <class Op, int kFewWaves, int kCols, int kDepth>
+template <class Op, int kAlong, int kCols, int kDepth>
 __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, int tile, int64_t first, int count, char *lds)
 {
     typedef few_kind<Op::kInt8> kind;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l8 = lane >> 3;
+    const int lane = threadIdx.x & 63, wave = kAlong > 1 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : 0, l8 = lane >> 3;
     const uint32_t piece = (uint32_t)(lane & 7) * 16;
     constexpr int kUnit = Op::kInt8 ? 1 : 2, kTerms = Op::kTerms, kPass = kCols * 16 / kTerms;
     few_operands<kCols> o;
@@ -86,30 +86,31 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
     few_stage<Op::kInt8, kCols> st[kDepth];
     char *mine = lds + wave * (kCols + 1) * kTileBytes;
 #pragma unroll
-    for (int d = 0; d < kDepth - 1; ++d) st[d].load(o, (uint32_t)(wave + d * kFewWaves) * kSpanBytes, lane);
-    for (uint32_t byte = (uint32_t)wave * kSpanBytes; byte < o.limit; byte += kFewWaves * kDepth * kSpanBytes) {
+    for (int d = 0; d < kDepth - 1; ++d) st[d].load(o, (uint32_t)(wave + d * kAlong) * kSpanBytes, lane);
+    for (uint32_t byte = (uint32_t)wave * kSpanBytes; byte < o.limit; byte += kAlong * kDepth * kSpanBytes) {
 #pragma unroll
         for (int d = 0; d < kDepth; ++d) {
-            st[(d + kDepth - 1) % kDepth].load(o, byte + (uint32_t)(d + kDepth - 1) * kFewWaves * kSpanBytes, lane);
-            if (byte + (uint32_t)d * kFewWaves * kSpanBytes < o.limit) st[d].add_to(acc, mine, lane);
+            st[(d + kDepth - 1) % kDepth].load(o, byte + (uint32_t)(d + kDepth - 1) * kAlong * kSpanBytes, lane);
+            if (byte + (uint32_t)d * kAlong * kSpanBytes < o.limit) st[d].add_to(acc, mine, lane);
         }
     }
     typedef decltype(acc[0][0] + acc[0][0]) value;
     value *part = (value *)lds;                  // [wave][column][16 rows]
     if constexpr (kTerms == 2 && kCols == 2) acc[0] += acc[1];
+    auto order = [] { if constexpr (kAlong > 1) __syncthreads(); else wave_order(); };
     constexpr int kSums = kTerms == 2 ? 1 : kCols, kHere = kPass < 16 ? kPass : 16;
 #pragma unroll
     for (int c = 0; c < kSums; ++c) {
-        __syncthreads();                         // (the sums take the place of the waves' pieces)
+        order();                                 // (the sums take the place of the waves' pieces)
         *(typename kind::acc *)&part[(wave * 16 + (lane & 15)) * 16 + (lane >> 4) * 4] = acc[c];
-        __syncthreads();
+        order();
         constexpr int kEach = Op::kPair ? 8 : 16;
-        for (int t = threadIdx.x; t < kHere * kEach; t += 64 * kFewWaves) {
+        for (int t = (int)threadIdx.x % (64 * kAlong); t < kHere * kEach; t += 64 * kAlong) {
             const int col = t / kEach, r = t % kEach;
             if (c * 16 + col >= count) continue;
             value v = 0, w = 0;
 #pragma unroll
-            for (int n = 0; n < kFewWaves; ++n) {
+            for (int n = 0; n < kAlong; ++n) {
                 v += part[(n * 16 + col) * 16 + r];
                 if constexpr (kTerms == 2 && kCols == 1) v += part[(n * 16 + 8 + col) * 16 + r];
                 if constexpr (Op::kPair) w += part[(n * 16 + col) * 16 + 8 + r];
@@ -117,33 +118,44 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
             Op::few_emit(a, e, first + c * 16 + col, tile * kEach + r, v, w);
         }
     }
-    __syncthreads();
+    order();
 }
-// grid: (tiles of sixteen matrix rows, runs)
-template <class Op, int kFewWaves>
-__global__ __launch_bounds__(64 * kFewWaves) void k_few(typename Op::args a)
+// A workgroup's kAlong waves share a tile of sixteen matrix rows, or (kAlong 1) each of four has its own.  grid: (tiles, four of them at kAlong 1; runs)
+template <class Op, int kAlong>
+__global__ __launch_bounds__(kAlong == 8 ? 512 : 256) void k_few(typename Op::args a)
 {
-    __shared__ __align__(16) char lds[kFewWaves * 3 * kTileBytes];
-    const int e = blockIdx.y, tile = blockIdx.x;
+    __shared__ __align__(16) char all[(kAlong == 8 ? 8 : 4) * 3 * kTileBytes];
+    const int e = blockIdx.y, own = kAlong > 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), tile = kAlong > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + own;
+    char *lds = all + own * 3 * kTileBytes;
     int64_t first, end;
     group_bounds(a.g, e, first, end);
     constexpr int kPass = 16 / Op::kTerms;
     while (first < end) {
         const int left = (int)(end - first);
-        if (left <= kPass) few_columns<Op, kFewWaves, 1, 4>(a, e, tile, first, left, lds);
-        else few_columns<Op, kFewWaves, 2, 3>(a, e, tile, first, left, lds);
+        if (left <= kPass) few_columns<Op, kAlong, 1, 4>(a, e, tile, first, left, lds);
+        else few_columns<Op, kAlong, 2, 3>(a, e, tile, first, left, lds);
         first += left <= kPass ? kPass : 2 * kPass;
     }
 }
-// Eight waves to a workgroup where there is hardly one a CU and rows are long, else four.  us, 4 / 8: 1 row of four experts 7168 x 2048 24.3 / 20.7, 1 row of codes 7168 -> 4096
-// 12.5 / 11.1; 64 rows of four experts 70.7 / 73.6, of eight 4096 x 1024 41.0 / 49.4, of sixteen 2048 x 768 31.4 / 44.1, codes 28.9 / 41.5.
-static inline int few_waves(int64_t workgroups, int64_t row_bytes) { return workgroups <= 256 && row_bytes >= 4096 ? 8 : 4; }
+// Waves that share sixteen matrix rows, by the tiles of all runs and the rows' bytes: eight where there is hardly a tile a CU and rows are long, one where there are many tiles of
+// short rows, else four.  us of the call, one / four / eight:
+//   1 row of four experts 7168 x 2048 23.7 / 24.3 / 20.7, of codes 7168 -> 4096 12.4 / 12.5 / 11.1 (256 tiles of 14336 and 7168 bytes)
+//   second product, 64 rows of eight experts 4096 x 1024 (2048 tiles, 2048 bytes) 40.8 / 42.2 / 49.4, codes (1024 bytes) 27.8 / 32.3 / 41.5; 32 rows of four 7168 x 2048 (1792, 4096 bytes)
+//   61.6 / 64.6 / 67.0; 32 rows of 32 experts 256 x 512 (512, 1024 bytes) 10.2 / 13.8 / 22.6; but 1 row of eight 4096 x 1024 (256, 2048 bytes) 14.4 / 11.9 / 14.0
+//   64 rows of codes, eight matrices 4096 -> 1024 (512, 4096 bytes) 11.7 / 7.1 / 7.9, sixteen 2048 -> 768 (768, 2048 bytes) 7.2 / 5.5 / 10.3
+static inline int few_waves(int64_t tiles, int64_t row_bytes)
+{
+    if (tiles <= 256 && row_bytes >= 4096) return 8;
+    return (row_bytes <= 1024 && tiles >= 512) || (row_bytes <= 4096 && tiles >= 1792) ? 1 : 4;
+}
 template <class Op>
 int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
 {
-    const dim3 grid((uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), (uint32_t)a.g.n);
-    if (few_waves((int64_t)grid.x * (a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows), (int64_t)a.K * (Op::kInt8 ? 1 : 2)) == 8) hipLaunchKernelGGL((k_few<Op, 8>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_few<Op, 4>), grid, dim3(256), 0, s, a);
+    const uint32_t tiles = (uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), n = (uint32_t)a.g.n;
+    const int waves = few_waves((int64_t)tiles * (a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows), (int64_t)a.K * (Op::kInt8 ? 1 : 2));
+    if (waves == 8) hipLaunchKernelGGL((k_few<Op, 8>), dim3(tiles, n), dim3(512), 0, s, a);
+    else if (waves == 4) hipLaunchKernelGGL((k_few<Op, 4>), dim3(tiles, n), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_few<Op, 1>), dim3((tiles + 3) / 4, n), dim3(256), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }

@@ -49,10 +49,12 @@ struct up_op {
     static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
     static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)          // (I is a multiple of eight)
     {
+        if (tile * 8 >= a.I) return kNowhere;
         return (uint32_t)((r >> 3) * a.I + tile * 8 + (r & 7)) * (uint32_t)a.K * 2;
     }
     static __device__ __forceinline__ void few_emit(const args &a, int, int64_t row, int col, float gate, float up)
     {
+        if (col >= a.I) return;
         // Matrices bound these products, so h can be held as two bf16 values, 16 bits of mantissa: one alone adds as much error as the output's own rounding.
         const float v = gate * tile_sigmoid(gate) * up;
         const uint16_t high = mw_f32_to_bf16(v);

@@ -149,10 +149,12 @@ struct int8_op {
     static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
     static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)          // (N is a multiple of sixteen)
     {
+        if (tile * (kGated ? 8 : 16) >= a.N) return kNowhere;
         return (uint32_t)(kGated ? (r >> 3) * a.N + tile * 8 + (r & 7) : tile * 16 + r) * (uint32_t)a.K;
     }
     static __device__ __forceinline__ void few_emit(const args &a, int e, int64_t row, int col, int t, int u)
     {
+        if (col >= a.N) return;
         const float scale = a.x_scale[row], *w = a.w_scale + (int64_t)e * (kGated ? 2 : 1) * a.N + col, value = (float)t * scale * w[0];
         float v;
         if constexpr (kGated) v = value * tile_sigmoid(value) * ((float)u * scale * w[a.N]);

@@ -100,6 +100,13 @@ def test_products(counts, n_in, n_out):
 
 def test_products_of_many_matrices():
     Matrices(100, 64, 48).check([(5 * m) % 4 for m in range(100)], spare=2)
+    Matrices(100, 144, 144).check([(7 * m) % 40 if m % 10 == 0 else m % 3 for m in range(100)], spare=2, dtype=torch.float32)
+
+
+@pytest.mark.parametrize("rows", [1, 16, 17])
+def test_long_rows(rows):
+    Matrices(1, 4112, 272).check([rows], spare=1, pad=16)
+    Matrices(3, 8208, 48).check([rows, 0, 16], dtype=torch.float32)
 
 
 @pytest.mark.parametrize("rows", [1, 40, 256])
