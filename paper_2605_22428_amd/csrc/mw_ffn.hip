@@ -188,15 +188,16 @@ __global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, const float *
 {
     __shared__ float part[16][17];
     const int r = threadIdx.x & 15, n = threadIdx.x >> 4;
-    const int64_t row = (int64_t)blockIdx.x * 16 + r, end = min(max(g.offsets[g.n], (int64_t)0), g.n_rows);
+    const int64_t row = (int64_t)blockIdx.x * 16 + r;
+    const bool mine = row >= max(g.offsets[0], (int64_t)0) && row < min(g.offsets[g.n], g.n_rows);          // (no expert's rows are left alone)
     float v = 0.0f;
-    if (row < end) {
+    if (mine) {
 #pragma unroll 4
         for (int i = n; i < n_sums; i += 16) v += sums[(int64_t)i * g.n_rows + row];
     }
     part[n][r] = v;
     __syncthreads();
-    if (n > 0 || row >= end) return;
+    if (n > 0 || !mine) return;
     v = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) v += part[i][r];

@@ -202,6 +202,32 @@ def test_offsets_outside_the_rows_count_as_the_nearest_inside():
     assert all(torch.equal(a, b) for a, b in zip(first, s.backward()))
 
 
+@pytest.mark.parametrize("before,counts", [(3, [4, 5]), (40, [70, 0, 30]), (300, [300, 200])])
+def test_rows_before_the_first_expert_are_left_as_they_were(before, counts):
+    """The same rows behind `before` rows of no expert give the same values, and those rows are neither read nor written.  (Experts with as many rows: the
+    room's size may choose other tiles, so values are held against the plain form.)"""
+    s = Set([before] + counts, 136, 72, spare=2)
+    s.offsets[0] = before                                                 # the first expert's rows are no expert's now
+    s.counts[0] = 0
+    s.offsets[1] = before
+    for t in (s.x, s.dy, s.kept, s.w):
+        t[:before] = float("nan")
+    s.dev_x[:before], s.dev_dy[:before], s.dev_kept[:before], s.dev_w[:before] = (float("nan"),) * 4
+    y, kept = s.forward()
+    dx, dgu, dd, dw = s.backward()
+    assert all((t[:before] == 7).all() for t in (y, kept, dx, dw)) and (dgu[0] == 0).all() and (dd[0] == 0).all()
+    first = before
+    for e, c in list(enumerate(counts, 1)):
+        if c:
+            at, w = slice(first, first + c), host(s.w[first:first + c])
+            (want, off), _ = P.block(host(s.x[at]), host(s.gate_up[e]), host(s.down[e]), w)
+            near(y[at], want, off)
+            want = P.block_backward(host(s.x[at]), host(s.gate_up[e]), host(s.down[e]), w, host(s.kept[at]), host(s.dy[at]))
+            for got, (v, off), rounding in ((dx[at], want[0], P.BF16), (dgu[e], want[1], P.BF16), (dd[e], want[2], P.BF16), (dw[at], want[3], P.U)):
+                near(got, v, off, rounding)
+        first += c
+
+
 def test_gradients_against_differences():
     """L = sum of dy y; central differences of a 64-bit forward pass in random directions of x, weights and gate weights.  The step is 2^-12 of a
     direction of the values' own size: the difference is off by 2^-24 times L's cubic term along it, which is below 100 sizes of the gradient's product here; the gradient by its
