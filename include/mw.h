@@ -919,6 +919,7 @@ MW_API int32_t mw_adapt_backward(const mw_adapters *adapters, const void *x_dev,
  * NaN and codes 0, so whatever is made of it is NaN and other rows are not touched.
  *   x_dev: n_rows rows of n_cols values, x_stride elements apart (a multiple of 8; 16-byte aligned).  codes_dev: rows of n_cols bytes, codes_stride
  *   apart (a multiple of 16; 16-byte aligned).  scales_dev [n_rows].  n_cols is a multiple of 16, at most MW_INT8_MAX_IN.
+ *   Outputs must not overlap x or one another.
  * Runs on the current device; needs no context.  n_rows > MW_FFN_MAX_ROWS: MW_ERR_CAPACITY.
  */
 MW_API int32_t mw_quantize_rows(const void *x_dev, int64_t x_stride, int64_t n_rows, int32_t n_cols, int8_t *codes_dev, int64_t codes_stride,

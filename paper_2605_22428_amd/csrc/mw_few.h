@@ -69,7 +69,7 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
     const uint32_t piece = (uint32_t)(lane & 7) * 16;
     constexpr int kUnit = Op::kInt8 ? 1 : 2, kTerms = Op::kTerms, kPass = kCols * 16 / kTerms;
     few_operands<kCols> o;
-    o.w = array_at(Op::few_matrix(a, e));
+    o.w = array_at(Op::few_matrix(a, e, tile));          // (of the tile on: a matrix may be larger than an array's 2 GiB)
     o.x = array_at(Op::few_x(a, first));
     o.limit = (uint32_t)a.K * kUnit;
 #pragma unroll
@@ -120,21 +120,23 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
     }
     order();
 }
-// A workgroup's kAlong waves share a tile of sixteen matrix rows, or (kAlong 1) each of four has its own.  grid: (tiles, four of them at kAlong 1; runs)
+// A workgroup's kAlong waves share a tile of sixteen matrix rows, or (kAlong 1) each of four has its own.  grid: (tiles, four of them at kAlong 1; runs, 65535 at most)
 template <class Op, int kAlong>
 __global__ __launch_bounds__(kAlong == 8 ? 512 : 256) void k_few(typename Op::args a)
 {
     __shared__ __align__(16) char all[(kAlong == 8 ? 8 : 4) * 3 * kTileBytes];
-    const int e = blockIdx.y, own = kAlong > 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), tile = kAlong > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + own;
+    const int own = kAlong > 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), tile = kAlong > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + own;
     char *lds = all + own * 3 * kTileBytes;
-    int64_t first, end;
-    group_bounds(a.g, e, first, end);
     constexpr int kPass = 16 / Op::kTerms;
-    while (first < end) {
-        const int left = (int)(end - first);
-        if (left <= kPass) few_columns<Op, kAlong, 1, 4>(a, e, tile, first, left, lds);
-        else few_columns<Op, kAlong, 2, 3>(a, e, tile, first, left, lds);
-        first += left <= kPass ? kPass : 2 * kPass;
+    for (int e = blockIdx.y; e < a.g.n; e += gridDim.y) {
+        int64_t first, end;
+        group_bounds(a.g, e, first, end);
+        while (first < end) {
+            const int left = (int)(end - first);
+            if (left <= kPass) few_columns<Op, kAlong, 1, 4>(a, e, tile, first, left, lds);
+            else few_columns<Op, kAlong, 2, 3>(a, e, tile, first, left, lds);
+            first += left <= kPass ? kPass : 2 * kPass;
+        }
     }
 }
 // Waves that share sixteen matrix rows, by the tiles of all runs and the rows' bytes: eight where there is hardly a tile a CU and rows are long, one where there are many tiles of
@@ -151,7 +153,7 @@ static inline int few_waves(int64_t tiles, int64_t row_bytes)
 template <class Op>
 int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
 {
-    const uint32_t tiles = (uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), n = (uint32_t)a.g.n;
+    const uint32_t tiles = (uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), n = (uint32_t)(a.g.n < 65535 ? a.g.n : 65535);
     const int waves = few_waves((int64_t)tiles * (a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows), (int64_t)a.K * (Op::kInt8 ? 1 : 2));
     if (waves == 8) hipLaunchKernelGGL((k_few<Op, 8>), dim3(tiles, n), dim3(512), 0, s, a);
     else if (waves == 4) hipLaunchKernelGGL((k_few<Op, 4>), dim3(tiles, n), dim3(256), 0, s, a);

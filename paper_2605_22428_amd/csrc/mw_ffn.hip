@@ -45,12 +45,12 @@ struct up_op {
         }
     }
     // A few rows: eight gate rows and the eight up rows beside them.
-    static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * 2 * a.I * a.K; }
+    static __device__ __forceinline__ const void *few_matrix(const args &a, int e, int tile) { return a.w + ((int64_t)e * 2 * a.I + tile * 8) * a.K; }
     static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
     static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)          // (I is a multiple of eight)
     {
         if (tile * 8 >= a.I) return kNowhere;
-        return (uint32_t)((r >> 3) * a.I + tile * 8 + (r & 7)) * (uint32_t)a.K * 2;
+        return (uint32_t)((r >> 3) * a.I + (r & 7)) * (uint32_t)a.K * 2;
     }
     static __device__ __forceinline__ void few_emit(const args &a, int, int64_t row, int col, float gate, float up)
     {
@@ -112,11 +112,11 @@ struct rows_op {
         for (int e = 0; e < 8; ++e) v[e] = kRowValues ? weight[0] * t[e] : t[e];
         store_bf16<true>(a.y + (at.first + row) * a.y_stride + col, v);
     }
-    static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * a.N * a.K; }
+    static __device__ __forceinline__ const void *few_matrix(const args &a, int e, int tile) { return a.w + ((int64_t)e * a.N + tile * 16) * a.K; }
     static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
     static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)
     {
-        return tile * 16 + r < a.N ? (uint32_t)(tile * 16 + r) * (uint32_t)a.K * 2 : kNowhere;
+        return tile * 16 + r < a.N ? (uint32_t)r * (uint32_t)a.K * 2 : kNowhere;
     }
     static __device__ __forceinline__ void few_emit(const args &a, int, int64_t row, int col, float v, float)
     {

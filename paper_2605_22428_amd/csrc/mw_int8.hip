@@ -145,12 +145,12 @@ struct int8_op {
             store_bf16((uint16_t *)a.y + (at.first + row) * a.y_stride + col, v);
         }
     }
-    static __device__ __forceinline__ const void *few_matrix(const args &a, int e) { return a.w + (int64_t)e * (kGated ? 2 : 1) * a.N * a.K; }
+    static __device__ __forceinline__ const void *few_matrix(const args &a, int e, int tile) { return a.w + ((int64_t)e * (kGated ? 2 : 1) * a.N + tile * (kGated ? 8 : 16)) * a.K; }
     static __device__ __forceinline__ const void *few_x(const args &a, int64_t row) { return a.x + row * a.x_stride; }
     static __device__ __forceinline__ uint32_t few_row(const args &a, int tile, int r)          // (N is a multiple of sixteen)
     {
         if (tile * (kGated ? 8 : 16) >= a.N) return kNowhere;
-        return (uint32_t)(kGated ? (r >> 3) * a.N + tile * 8 + (r & 7) : tile * 16 + r) * (uint32_t)a.K;
+        return (uint32_t)(kGated ? (r >> 3) * a.N + (r & 7) : r) * (uint32_t)a.K;
     }
     static __device__ __forceinline__ void few_emit(const args &a, int e, int64_t row, int col, int t, int u)
     {

@@ -103,6 +103,42 @@ def test_products_of_many_matrices():
     Matrices(100, 144, 144).check([(7 * m) % 40 if m % 10 == 0 else m % 3 for m in range(100)], spare=2, dtype=torch.float32)
 
 
+@pytest.mark.parametrize("many", [2, 17 * 66000])
+def test_more_matrices_than_a_grid_is_high(many):
+    """A few rows of a few of 66000 matrices, and (tiles of many rows) one of them with most."""
+    n, counts = 66000, [0] * 66000
+    for m in (0, 1, 65534, 65535, 65536, 65999):
+        counts[m] = 1 + m % 3
+    counts[65700] = many
+    s, rows, g = Matrices(n, 16, 16), sum(counts), torch.Generator().manual_seed(4)
+    codes = torch.randint(-127, 128, (rows + 3, 16), generator=g).to(torch.int8)
+    out = torch.full((rows + 3, 16), 7.0, device=DEV)
+    s.dev.mw_matmul_int8(codes.to(DEV), torch.ones(rows + 3, device=DEV), torch.tensor([0] + list(itertools.accumulate(counts)), device=DEV), out)
+    torch.cuda.synchronize()
+    first = 0
+    for m, c in enumerate(counts):
+        if c:
+            want = host(codes[first:first + c]) @ host(s.w[m]).T * host(s.scale[m])
+            near(out[first:first + c], want, 4 * P.U * np.abs(want), 0.0)
+            first += c
+    assert (out[rows:] == 7).all()
+
+
+@pytest.mark.parametrize("rows", [1, 20, 130])
+def test_a_matrix_larger_than_2_gib(rows):
+    """Columns below, around and above the 2 GiB border, whose places in bytes need more than 31 bits."""
+    n_in, n_out = 16384, 131072 + 4096
+    w = torch.randint(-127, 128, (1, n_out, n_in), dtype=torch.int8, device=DEV, generator=torch.Generator(DEV).manual_seed(1))
+    scale = torch.rand((1, n_out), device=DEV, generator=torch.Generator(DEV).manual_seed(2))
+    codes = torch.randint(-127, 128, (rows, n_in), generator=torch.Generator().manual_seed(3)).to(torch.int8)
+    out = torch.full((rows, n_out), 7.0, device=DEV)
+    B.MatricesInt8(w, scale).mw_matmul_int8(codes.to(DEV), torch.ones(rows, device=DEV), None, out)
+    torch.cuda.synchronize()
+    for at in (slice(0, 40), slice(131072 - 300, 131072 + 300), slice(n_out - 40, n_out)):
+        want = host(codes) @ host(w[0, at]).T * host(scale[0, at])
+        near(out[:, at], want, 4 * P.U * np.abs(want), 0.0)
+
+
 @pytest.mark.parametrize("rows", [1, 16, 17])
 def test_long_rows(rows):
     Matrices(1, 4112, 272).check([rows], spare=1, pad=16)
