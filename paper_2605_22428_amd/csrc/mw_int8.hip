@@ -49,6 +49,7 @@ __device__ __forceinline__ void put_codes(const quant_args &a, int64_t row, int 
 }
 __device__ __forceinline__ float scale_of(uint32_t most) { return most < 0x7f800000u ? __uint_as_float(most) / 127.0f : __uint_as_float(0x7fc00000u); }
 
+constexpr uint32_t kQuantizeRun = 1u << 20;        // workgroups along x: a grid has fewer than 2^32 threads along one axis
 // kWaves waves a row; up to kChunks pieces of eight values a lane stay in registers, of longer rows the rest is read twice.
 template <int kWaves, int kChunks>
 __global__ __launch_bounds__(256) void k_quantize(quant_args a)
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(256) void k_quantize(quant_args a)
     __shared__ uint32_t waves[4];
     constexpr int kLanes = kWaves * 64;
     const int tid = (int)threadIdx.x % kLanes, chunks = a.n / 8;
-    const int64_t row = (int64_t)blockIdx.x * (4 / kWaves) + (int)threadIdx.x / kLanes;
+    const int64_t row = ((int64_t)blockIdx.y * kQuantizeRun + blockIdx.x) * (4 / kWaves) + (int)threadIdx.x / kLanes;
     if (row >= a.n_rows || (a.end && row >= *a.end)) return;                // (a wave's or the workgroup's)
     const uint16_t *x = a.x + row * a.x_stride;
     u32x4 v[kChunks];
@@ -172,8 +173,9 @@ int32_t launch_int8(const typename int8_op<256, 256, kGated, kF32>::args &a, hip
 // Many rows take a wave each, few or long ones a workgroup each.  us: 16384 rows of 2048 values a workgroup / a wave 22 / 18; of 7168 values 62 / 67.
 int32_t launch_quantize(const quant_args &a, hipStream_t s)
 {
-    const dim3 four((uint32_t)((a.n_rows + 3) / 4));
-    if (a.n_rows < 2048 || a.n > 4096) hipLaunchKernelGGL((k_quantize<4, 4>), dim3((uint32_t)a.n_rows), dim3(256), 0, s, a);
+    auto grid = [](int64_t groups) { return dim3((uint32_t)(groups < kQuantizeRun ? groups : kQuantizeRun), (uint32_t)((groups + kQuantizeRun - 1) / kQuantizeRun)); };
+    const dim3 four = grid((a.n_rows + 3) / 4);
+    if (a.n_rows < 2048 || a.n > 4096) hipLaunchKernelGGL((k_quantize<4, 4>), grid(a.n_rows), dim3(256), 0, s, a);
     else if (a.n <= 2048) hipLaunchKernelGGL((k_quantize<1, 4>), four, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((k_quantize<1, 8>), four, dim3(256), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
