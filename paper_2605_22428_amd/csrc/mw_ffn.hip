@@ -1,4 +1,6 @@
 // mw_ffn, mw_ffn_backward: the experts of the rows that a dispatch brought.
+#include <type_traits>
+
 #include "mw_few.h"
 #include "mw_ffn.h"
 
@@ -213,9 +215,9 @@ struct grads_matrix {
 struct grads_args { row_groups g; grads_matrix m[2]; uint32_t first; };         // first: workgroups of m[0]
 // Tiles of a matrix take as long as its run is: the XCDs get an eighth of every matrix's tiles each, and those of the longest run first.
 template <int kP, int kQ>
-__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 2) void k_ffn_grads(grads_args a)
+__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 4) void k_ffn_grads(grads_args a)
 {
-    typedef tile_product<kP, kQ, true, true, false> product;
+    typedef std::conditional_t<(kP * kQ > 128 * 128), tile_product<kP, kQ, true, true, false>, tile_product_short<kP, kQ, true, true, false>> product;
     typedef tile_out<kP, kQ, false> out_form;
     __shared__ __attribute__((aligned(1024))) char lds[product::kLds > kTileWaves * out_form::kBytes ? product::kLds : kTileWaves * out_form::kBytes];
     const bool second = blockIdx.x >= a.first;

@@ -276,6 +276,43 @@ struct tile_product {
     }
 };
 
+// The same with room for one step: for sums of a few steps, whose time is waiting for the first loads and writing results, four workgroups a CU that wait for themselves hide
+// more than two that load ahead.
+template <int kP, int kQ, bool kTrP, bool kTrQ, bool kInt8>
+struct tile_product_short {
+    typedef tile_kind<kInt8> kind;
+    typedef typename kind::frag frag;
+    static constexpr int kNP = kP / 64, kNQ = kQ / 64, kStage = (kP + kQ) * kStep, kLds = kStage;
+    typename kind::acc acc[kNP][kNQ];
+    __device__ __forceinline__ void run(const tile_feed<kP, kTrP, kInt8> &p, const tile_feed<kQ, kTrQ, kInt8> &q, int steps, lds_char *lds)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+        tile_frags<kP, kTrP, kInt8> fp;
+        tile_frags<kQ, kTrQ, kInt8> fq;
+        fp.begin(wave & 1);
+        fq.begin(wave >> 1);
+#pragma unroll
+        for (int n = 0; n < kNP * kNQ; ++n) acc[n / kNQ][n % kNQ] = typename kind::acc{};
+        for (int k = 0; k < steps; ++k) {
+            p.issue_all(k, lds);
+            q.issue_all(k, lds + kP * kStep);
+            tile_wait<0>();
+            tile_barrier();
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                frag a[kNP], b[kNQ];
+#pragma unroll
+                for (int i = 0; i < kNP; ++i) a[i] = fp.read(lds, kk, i);
+#pragma unroll
+                for (int j = 0; j < kNQ; ++j) b[j] = fq.read(lds + kP * kStep, kk, j);
+#pragma unroll
+                for (int n = 0; n < kNP * kNQ; ++n) acc[n / kNQ][n % kNQ] = kind::mma(a[n / kNQ], b[n % kNQ], acc[n / kNQ][n % kNQ]);
+            }
+            tile_reads_done();
+        }
+    }
+};
+
 // ---- rows in runs, one run a matrix ---------------------------------------------------------------------------
 struct row_groups {
     const int64_t *offsets;     // [n + 1], or null: one run of all rows
@@ -377,7 +414,7 @@ struct tile_runs {
 // kPair: the wave's columns are two halves that belong together, a lane gets eight of each.
 template <int kP, int kQ, bool kPair>
 struct tile_out {
-    static constexpr int kCols = kP / 2, kRows = kQ / 2 < 64 ? kQ / 2 : 64, kPitch = kCols * 4 + 16, kBytes = kRows * kPitch;          // (rows begin on different banks)
+    static constexpr int kCols = kP / 2, kRows = kP * kQ <= 128 * 128 ? 32 : 64, kPitch = kCols * 4 + 16, kBytes = kRows * kPitch;          // (rows begin on different banks)
     static constexpr int kLanes = kCols / (kPair ? 16 : 8), kAtOnce = 64 / kLanes;                                                      // lanes of a row, rows at once
     template <class Acc>
     static __device__ __forceinline__ void put(lds_char *lds, int i, int j, const Acc &v)                                              // piece i, j (of kRows / 32) of the accumulators
