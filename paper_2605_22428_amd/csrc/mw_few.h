@@ -162,19 +162,28 @@ int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
     return MW_OK;
 }
 
-// How rows' products with n matrices of `columns` rows of `width` values are cut; parts: a broken round's tiles are cut along the sum.  us of the whole call, rows of uneven runs, weights
-// from memory, few / small / middle / large:
-//   mw_ffn, four experts 7168 x 2048, 64 rows 74 / 95 / 96 / 122, 128 rows 120 / 96 / 98 / 124, 256 210 / 102 / 102 / 126, 512 - / 136 / 116 / 132, 1024 - / 205 / 162 / 157, 4096 - / 528 / 385 / 348
-//   eight 4096 x 1024, 128 rows 53 / 66 / 70 / 96, 256 80 / 69 / 72 / 96, 1024 - / 89 / 82 / 94, 4096 - / 187 / 149 / 162, 8192 - / 314 / 247 / 239; codes, 1024 rows - / 67 / 62 / 80
-//   one 4096 x 2048, 512 rows - / 59 / 60 / 78, 1024 - / 72 / 81 / 99, 2048 - / 164 / 100 / 135, 4096 - / 262 / 193 / 184
-//   mw_matmul_int8 with its rows' codes, four matrices 7168 -> 2048, 64 rows 20 / 27 / 44 / 66, 1024 - / 44 / 50 / 73, 2048 - / 81 / 67 / 95, 4096 - / 124 / 121 / 108
-//   mw_ffn_backward, four experts 7168 x 2048, 512 rows - / 292 / 267 / 284, 2048 - / 579 / 515 / 493
+// How a product of rows with n matrices, `columns` values of a row from each, is cut: few rows a run to a form of their own, others to the tile size that is through first, counted
+// in rounds of the CUs times what a step takes with a tile on every CU, 128 x 64, 256 x 128, 256 x 256 as 0.49 : 1 : 1.5 (fitted to 95
+// calls of random sizes, each timed with all nine pairs of sizes for its two products: the sizes taken are 0.5 % from the best of them on average, 10 % at most).  parts: a last round's tiles
+// may be cut along the sum.  us, weights from memory, runs of uneven lengths, both products with 128 x 64 / 256 x 128 / 256 x 256 tiles, and the ones taken:
+//   mw_ffn, four experts 7168 x 2048, 512 rows 150 / 116 / 134, 123; 16384 rows - / - / 1242, the same; mw_ffn of codes, 512 rows 90 / 87 / 97, 90; 16384 rows 1062 / 854 / 804, 804
+//   mw_ffn_backward, 333 rows of five 2880 x 1000 77 / 98 / 130, 77; 2048 rows of eight 4096 x 1024 209 / 203 / 195, 195
+//   mw_matmul_int8, 8192 rows 7168 -> 7168 568 / 427 / 396, 396; four matrices 7168 -> 2048, 2048 rows 40 / 42 / 66, 40
+// A few rows: mw_ffn, four experts 7168 x 2048, few / 128 x 64: 64 rows 74 / 88, 96 rows 104 / 88; 32 of 2048 x 768, 512 rows 65 / 67; codes, eight of 4096 x 1024, 128 rows 31 / 39.
 enum { kFew, kSmall, kMiddle, kLarge };
-static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t width, bool parts)
+static inline double tile_rounds(int64_t n_rows, int64_t n, int rows_a_tile, int64_t column_tiles, int64_t at_once, int64_t steps, bool parts)
+{
+    const int64_t rows_tiles = (n_rows + rows_a_tile - 1) / rows_a_tile + (n - 1) / 2, runs = n < n_rows ? n : n_rows;         // (half of a run's last tile is empty)
+    const int64_t tiles = (rows_tiles > runs ? rows_tiles : runs) * column_tiles, left = tiles % at_once, whole = (tiles - left) / kUnits;
+    if (parts && left > 0 && parts_pay((uint32_t)left, (uint32_t)steps)) return (double)whole + (double)left / kUnits + (double)join_steps((uint32_t)left) / (double)steps;
+    return (double)(whole + (left + kUnits - 1) / kUnits);
+}
+static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t steps, bool parts)
 {
     if (n_rows <= 16 * n) return kFew;
-    const double size = (double)n_rows * (double)columns * (double)width;
-    return n_rows >= 192 * n && size >= (parts ? 6.5e10 : 5e10) ? kLarge : n_rows >= 64 * n && size >= (parts ? 7.5e9 : 1.6e10) ? kMiddle : kSmall;
+    const double small = 0.49 * tile_rounds(n_rows, n, 64, (columns + 127) / 128, 768, steps, parts), middle = tile_rounds(n_rows, n, 128, (columns + 255) / 256, kUnits, steps, parts),
+                 large = 1.5 * tile_rounds(n_rows, n, 256, (columns + 255) / 256, kUnits, steps, parts);
+    return small < middle && small < large ? kSmall : middle < large ? kMiddle : kLarge;
 }
 // The tile sizes' arguments are alike.
 template <class To, class From> To as(const From &f)

@@ -186,16 +186,16 @@ struct act_op {
     }
 };
 // d_row_weights: a row's sums, sixteen rows a workgroup; sixteen lanes' sums of every sixteenth each, then of these, in a fixed order.
-__global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, const float *sums, int n_sums, float *out)
+struct weights_args { const float *sums; float *out; int32_t n; };
+__device__ __forceinline__ void row_weights_of(const row_groups &g, const weights_args &a, uint32_t block, float (*part)[17])
 {
-    __shared__ float part[16][17];
     const int r = threadIdx.x & 15, n = threadIdx.x >> 4;
-    const int64_t row = (int64_t)blockIdx.x * 16 + r;
+    const int64_t row = (int64_t)block * 16 + r;
     const bool mine = row >= max(g.offsets[0], (int64_t)0) && row < min(g.offsets[g.n], g.n_rows);          // (no expert's rows are left alone)
     float v = 0.0f;
     if (mine) {
 #pragma unroll 4
-        for (int i = n; i < n_sums; i += 16) v += sums[(int64_t)i * g.n_rows + row];
+        for (int i = n; i < a.n; i += 16) v += a.sums[(int64_t)i * g.n_rows + row];
     }
     part[n][r] = v;
     __syncthreads();
@@ -203,7 +203,12 @@ __global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, const float *
     v = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) v += part[i][r];
-    out[row] = v;
+    a.out[row] = v;
+}
+__global__ __launch_bounds__(256) void k_ffn_weights(row_groups g, weights_args a)
+{
+    __shared__ float part[16][17];
+    row_weights_of(g, a, blockIdx.x, part);
 }
 
 // ---- gradients of matrices: out[q][p] = sum over a run's rows of q's value times p's ---------------------------------
@@ -212,7 +217,7 @@ struct grads_matrix {
     uint16_t *out;                          // [n][M][N], or null
     int32_t M, N, p_tiles, q_tiles;
 };
-struct grads_args { row_groups g; grads_matrix m[2]; uint32_t first; };         // first: workgroups of m[0]
+struct grads_args { row_groups g; grads_matrix m[2]; uint32_t first, weights; weights_args w; };          // workgroups of m[0]; of the rows' weights, before all others
 // Tiles of a matrix take as long as its run is: the XCDs get an eighth of every matrix's tiles each, and those of the longest run first.
 template <int kP, int kQ>
 __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 4) void k_ffn_grads(grads_args a)
@@ -220,9 +225,13 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 4) void k_f
     typedef std::conditional_t<(kP * kQ > 128 * 128), tile_product<kP, kQ, true, true, false>, tile_product_short<kP, kQ, true, true, false>> product;
     typedef tile_out<kP, kQ, false> out_form;
     __shared__ __attribute__((aligned(1024))) char lds[product::kLds > kTileWaves * out_form::kBytes ? product::kLds : kTileWaves * out_form::kBytes];
-    const bool second = blockIdx.x >= a.first;
+    if (blockIdx.x < a.weights) {
+        row_weights_of(a.g, a.w, blockIdx.x, (float (*)[17])lds);
+        return;
+    }
+    const bool second = blockIdx.x - a.weights >= a.first;
     const grads_matrix m = second ? a.m[1] : a.m[0];
-    const uint32_t id = blockIdx.x - (second ? a.first : 0), each = (uint32_t)m.p_tiles * (uint32_t)m.q_tiles, per = (each + 7) / 8, at = id >> 3;
+    const uint32_t id = blockIdx.x - a.weights - (second ? a.first : 0), each = (uint32_t)m.p_tiles * (uint32_t)m.q_tiles, per = (each + 7) / 8, at = id >> 3;
     const uint32_t tile = (id & 7) * per + at % per;
     int e = (int)(at / per);
     if (tile >= each || e >= a.g.n) return;
@@ -309,9 +318,11 @@ int32_t launch_grads(grads_args a, hipStream_t s)
         m.q_tiles = (int32_t)pieces(m.M, kQ);
         grid[i] = m.out ? pieces((int64_t)m.p_tiles * m.q_tiles, 8) * 8 * a.g.n : 0;
     }
-    if (grid[0] + grid[1] > 0x7ffffff0LL) return MW_ERR_UNSUPPORTED;
+    const int64_t weights = a.w.out ? pieces(a.g.n_rows, 16 * 8) * 8 : 0;          // (eights, as the others are dealt out)
+    if (weights + grid[0] + grid[1] > 0x7ffffff0LL) return MW_ERR_UNSUPPORTED;
     a.first = (uint32_t)grid[0];
-    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), dim3((uint32_t)(grid[0] + grid[1])), dim3(kTileThreads), 0, s, a);
+    a.weights = (uint32_t)weights;
+    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), dim3((uint32_t)(weights + grid[0] + grid[1])), dim3(kTileThreads), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }
@@ -350,11 +361,11 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     const row_groups g = {expert_offsets_dev, n_rows, ctx->n_local};
     const hipStream_t s = (hipStream_t)stream;
     if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), (float *)(b + w.parts), s);
-    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, H, true);
+    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, pieces(H, 64), true), down_form = rows_form(n_rows, g.n, H, pieces(I, 64), true);
     const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
     const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), form == kFew ? 2 * (int64_t)I : I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
     rc = launch_product<up_op<256, 256>, up_op<256, 128>, up_op<128, 64>, true>(form, u, I, s);
-    if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<256, 128, false>, rows_op<128, 64, false>, true>(form, d, H, s);
+    if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<256, 128, false>, rows_op<128, 64, false>, true>(down_form, d, H, s);
     return rc;
 }
 
@@ -381,24 +392,25 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
     const hipStream_t s = (hipStream_t)stream;
     uint16_t *act = (uint16_t *)(b + w.act), *d_act = (uint16_t *)(b + w.d_gate_up);
     float *sums = d_row_weights_dev ? (float *)(b + w.sums) : nullptr, *parts = (float *)(b + w.parts);
-    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, H, true);
+    const bool matrices = d_gate_up_dev || d_down_dev;
+    const weights_args of_rows = {sums, d_row_weights_dev, (int32_t)pieces(I, kSum)};
     if (n_rows > 0) {
         const act_op<256, 256>::args a = {g, (const uint16_t *)dy_dev, dy_stride, (const uint16_t *)experts->down_dev, row_weights_dev, (const uint16_t *)kept_dev, act, d_act, sums, parts, H, I, 0};
-        rc = launch_product<act_op<256, 256>, act_op<256, 128>, act_op<128, 64>, false>(form, a, I, s);
+        rc = launch_product<act_op<256, 256>, act_op<256, 128>, act_op<128, 64>, false>(rows_form(n_rows, g.n, I, pieces(H, 64), true), a, I, s);
         if (rc != MW_OK) return rc;
-        if (sums) {
-            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 16)), dim3(256), 0, s, g, sums, (int)pieces(I, kSum), d_row_weights_dev);
+        if (sums && !matrices) {
+            hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 16)), dim3(256), 0, s, g, of_rows);
             MW_HIP_CHECK(hipGetLastError());
         }
         if (dx_dev) {
             const rows_op<256, 256, true>::args d = {g, d_act, 2 * (int64_t)I, (const uint16_t *)experts->gate_up_dev, nullptr, (uint16_t *)dx_dev, dx_stride, parts, 2 * I, H, 0};
-            rc = launch_product<rows_op<256, 256, true>, rows_op<256, 128, true>, rows_op<128, 64, true>, false>(form, d, H, s);
+            rc = launch_product<rows_op<256, 256, true>, rows_op<256, 128, true>, rows_op<128, 64, true>, false>(rows_form(n_rows, g.n, H, pieces(2 * (int64_t)I, 64), true), d, H, s);
             if (rc != MW_OK) return rc;
         }
     }
-    if (d_gate_up_dev || d_down_dev) {
+    if (matrices) {
         const grads_args a = {g, {{d_act, (const uint16_t *)x_dev, 2 * (int64_t)I, x_stride, (uint16_t *)d_gate_up_dev, 2 * I, H, 0, 0},
-                                  {(const uint16_t *)dy_dev, act, dy_stride, I, (uint16_t *)d_down_dev, H, I, 0, 0}}, 0};
+                                  {(const uint16_t *)dy_dev, act, dy_stride, I, (uint16_t *)d_down_dev, H, I, 0, 0}}, 0, 0, of_rows};
         rc = grads_large(n_rows, g.n) ? launch_grads<256, 256>(a, s) : launch_grads<128, 128>(a, s);
     }
     return rc;

@@ -332,13 +332,22 @@ struct tile_at {
     int p;                      // tile of columns
 };
 // Work is cut into units: a whole tile, or a part of a tile's sum.  kRound workgroups run at a time, so T tiles of one duration take ceil(T / kRound) rounds; the tiles of
-// a last round that is at most half full are cut into as many parts as fill it.  The parts' sums go to memory, and k_join adds them up in their order.
+// a last round may be cut into as many parts as fill it.  The parts' sums go to memory, and k_join adds them up in their order.
+//
+// That pays if it saves more steps than writing, reading and a launch cost, which is as many for all three tile sizes (a step of 128 x 64, 256 x 128 and 256 x 256 takes 0.33, 0.63 and
+// 1.3 us, a join with its traffic 10, 20 and 41 us).  R tiles on 256 CUs leave 1 - R / 256 of them idle.  us of a call whole / in parts, its products' steps and tiles:
+//   128 x 64: 128 rows of one expert 4096 x 2048 (64 steps of 64 tiles, 32 of 64) 40 / 33, 512 rows (256 tiles both) 43 / 58; 512 rows of four 7168 x 2048, backward without the
+//   matrices' gradients (112 of 128, 64 of 448) 138 / 126, forward (112 of 256, 32 of 448) 104 / 113; 333 rows of five 2880 x 1000, backward (45 of 80, 32 of 230) 36 / 42
+//   256 x 128: 512 rows of four 7168 x 2048 (112 of 64, 32 of 112) 149 / 99; 1024 rows of one 4096 x 2048 (64 of 128, 32 of 128) 70 / 80
+//   256 x 256: 2048 rows of four 7168 x 2048 (112 of 128, 32 of 224) 221 / 188; 2048 rows of one 4096 x 2048 (64 of 128, 32 of 128) 115 / 134
+constexpr uint32_t kMostParts = 16, kLeastSteps = 8, kUnits = 256;
+__host__ __device__ __forceinline__ uint32_t join_steps(uint32_t tiles) { return 20 + tiles / 8; }
+__host__ __device__ __forceinline__ bool parts_pay(uint32_t tiles, uint32_t steps) { return tiles < kUnits && (uint64_t)steps * (kUnits - tiles) >= (uint64_t)join_steps(tiles) * kUnits; }
 struct tile_split { uint32_t whole, rest, parts; };             // tiles in one piece, tiles in parts, parts of each (1: rest are in one piece too)
-constexpr uint32_t kMostParts = 16;
-__device__ __forceinline__ tile_split split_tiles(uint32_t total, uint32_t round, uint32_t steps, uint32_t least_steps, bool may)
+__device__ __forceinline__ tile_split split_tiles(uint32_t total, uint32_t round, uint32_t steps, bool may)
 {
     tile_split s = {total - total % round, total % round, 1};
-    if (may && s.rest > 0) s.parts = max(1u, min(min(round / s.rest, kMostParts), steps / least_steps));
+    if (may && s.rest > 0 && parts_pay(s.rest, steps)) s.parts = max(1u, min(min(round / s.rest, kMostParts), steps / kLeastSteps));
     return s;
 }
 struct tile_unit { uint32_t tile, part; };
@@ -484,12 +493,12 @@ struct tile_op : Op {
     typedef tile_product<Op::kP, Op::kQ, Op::kTrP, false, Op::kInt8> product;
     typedef tile_out<Op::kP, Op::kQ, Op::kPair> out;
     typedef decltype(typename product::kind::acc{}[0] + 0) value;
-    // Workgroups that run at a time: LDS holds one of the large tiles a CU, two of 128 x 128, three of 128 x 64.
-    static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : Op::kP * Op::kQ == 128 * 128 ? 512 : 768, kLeastSteps = 8;
+    // Workgroups that run at a time: LDS holds one of the two larger tiles a CU, three of 128 x 64.
+    static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : 768;
     static constexpr int kLds = product::kLds > kTileWaves * out::kBytes ? product::kLds : kTileWaves * out::kBytes;
     static constexpr int kRowsAt = kLds, kAllLds = kLds + (Op::kRowValues ? 8 * Op::kQ : 0);           // a row's values behind the stages
     static constexpr int kColumns = Op::kPair ? Op::kP / 2 : Op::kP, kJoinRows = kTileThreads * 8 / kColumns;         // rows that a workgroup of k_join takes
-    static __device__ __forceinline__ int steps(const typename Op::args &a) { return (a.K + (Op::kInt8 ? 127 : 63)) / (Op::kInt8 ? 128 : 64); }
+    static __host__ __device__ __forceinline__ int steps(const typename Op::args &a) { return (a.K + (Op::kInt8 ? 127 : 63)) / (Op::kInt8 ? 128 : 64); }
     // Eight sums of a part, at a row and a column of a tile of kP columns.
     typedef value eight __attribute__((ext_vector_type(8)));
     static __device__ __forceinline__ eight *place(const typename Op::args &a, uint32_t slot, int row, int column) { return (eight *)((value *)a.parts + ((int64_t)slot * Op::kQ + row) * Op::kP + column); }
@@ -505,7 +514,7 @@ __global__ __launch_bounds__(kTileThreads, Op::kP * Op::kQ > 128 * 128 ? 1 : 2) 
     tile_runs<Op::kQ> runs;
     runs.count(a.g);
     const int steps = op::steps(a);
-    const tile_split split = split_tiles(runs.total * (uint32_t)a.p_tiles, op::kRound, (uint32_t)steps, op::kLeastSteps, a.parts != nullptr);
+    const tile_split split = split_tiles(runs.total * (uint32_t)a.p_tiles, op::kRound, (uint32_t)steps, a.parts != nullptr);
     tile_unit u;
     tile_at at;
     if (!unit_of_workgroup(split, u) || !runs.find(a.g, (uint32_t)a.p_tiles, u.tile, at)) return;
@@ -550,7 +559,7 @@ __global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
     typedef tile_op<Op> op;
     tile_runs<Op::kQ> runs;
     runs.count(a.g);
-    const tile_split split = split_tiles(runs.total * (uint32_t)a.p_tiles, op::kRound, (uint32_t)op::steps(a), op::kLeastSteps, true);
+    const tile_split split = split_tiles(runs.total * (uint32_t)a.p_tiles, op::kRound, (uint32_t)op::steps(a), true);
     tile_at at;
     if (split.parts == 1 || blockIdx.y >= split.rest || !runs.find(a.g, (uint32_t)a.p_tiles, split.whole + blockIdx.y, at)) return;
     const int row = (int)blockIdx.x * op::kJoinRows + (int)threadIdx.x / (op::kColumns / 8), column = (int)threadIdx.x % (op::kColumns / 8) * 8;
@@ -569,19 +578,21 @@ __global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
     Op::emit(a, at, row, column, x, y, Op::columns(a, at, column), of_row, Op::fetch(a, at, row, column));
 }
 static inline int64_t most_tiles(int64_t n_rows, int64_t n, int rows_a_tile) { return n_rows / rows_a_tile + (n < n_rows ? n : n_rows); }
-// The most tiles in parts there are: two parts each at least.
 template <class Op>
 int32_t launch_tiles(typename Op::args a, int columns, hipStream_t s)
 {
     typedef tile_op<Op> op;
     a.p_tiles = (columns + (Op::kPair ? Op::kP / 2 : Op::kP) - 1) / (Op::kPair ? Op::kP / 2 : Op::kP);
+    // Whether there may be parts is settled here, from the fewest tiles that so many rows are (after whole rounds the rest can be any number); which, by the runs' lengths.
+    const int64_t rows_tiles = (a.g.n_rows + Op::kQ - 1) / Op::kQ, runs = a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows, fewest = (rows_tiles > runs ? rows_tiles : runs) * a.p_tiles;
+    if (!parts_pay((uint32_t)(fewest < kUnits ? fewest : kUnits / 2), (uint32_t)op::steps(a))) a.parts = nullptr;
     const int64_t tiles = most_tiles(a.g.n_rows, a.g.n, Op::kQ) * a.p_tiles, round = a.parts ? op::kRound : 0;
     if (tiles > 0x7ff00000LL) return MW_ERR_UNSUPPORTED;
     // T tiles are at most T - rest + kRound units, eights of them
     hipLaunchKernelGGL((k_tiles<Op>), dim3((uint32_t)((tiles + round + 15) / 8 * 8)), dim3(kTileThreads), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     if (a.parts) {
-        hipLaunchKernelGGL((k_join<Op>), dim3(Op::kQ / op::kJoinRows, (uint32_t)(tiles < round / 2 ? tiles : round / 2)), dim3(kTileThreads), 0, s, a);
+        hipLaunchKernelGGL((k_join<Op>), dim3(Op::kQ / op::kJoinRows, (uint32_t)(tiles < kUnits ? tiles : kUnits)), dim3(kTileThreads), 0, s, a);
         MW_HIP_CHECK(hipGetLastError());
     }
     return MW_OK;
