@@ -307,7 +307,13 @@ int32_t ffn_ready(const mw_ctx *ctx, const mw_experts *e, bool backward)
 }
 // A matrix of bf16 rows of the caller's.
 bool rows_fit(const void *p, int64_t stride, int64_t width) { return p && !((uintptr_t)p & 15u) && stride >= width && stride % 8 == 0; }
-static inline bool grads_large(int64_t n_rows, int64_t n) { return n_rows >= 384 * n; }
+// Gradients of matrices by the runs' length and the tiles: sums of a few steps take 128 x 128 with room for one step, long ones over enough tiles 256 x 256.  us of the gradients alone, 128 x 128 /
+// 256 x 256: four experts 7168 x 2048, 512 rows 90 / 117, 2048 200 / 201, 4096 365 / 334, 8192 675 / 596; eight 4096 x 1024, 2048 rows 77 / 82, 4096 115 / 115, 8192 204 / 189;
+// 32 of 2048 x 768, 4096 rows 84 / 109; five 2880 x 1000, 2000 rows 52 / 49; two 1024 x 512 (48 of the larger tiles), 4000 rows 45 / 54.
+static inline bool grads_large(int64_t n_rows, int64_t n, int64_t hidden, int64_t inter)
+{
+    return n_rows >= 512 * n && (pieces(2 * inter, 256) + pieces(inter, 256)) * pieces(hidden, 256) * n >= kUnits;
+}
 template <int kP, int kQ>
 int32_t launch_grads(grads_args a, hipStream_t s)
 {
@@ -411,7 +417,7 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
     if (matrices) {
         const grads_args a = {g, {{d_act, (const uint16_t *)x_dev, 2 * (int64_t)I, x_stride, (uint16_t *)d_gate_up_dev, 2 * I, H, 0, 0},
                                   {(const uint16_t *)dy_dev, act, dy_stride, I, (uint16_t *)d_down_dev, H, I, 0, 0}}, 0, 0, of_rows};
-        rc = grads_large(n_rows, g.n) ? launch_grads<256, 256>(a, s) : launch_grads<128, 128>(a, s);
+        rc = grads_large(n_rows, g.n, H, I) ? launch_grads<256, 256>(a, s) : launch_grads<128, 128>(a, s);
     }
     return rc;
 }
