@@ -11,6 +11,11 @@
 // operand's rows, a row is 128 bytes and its 16-byte chunks are exchanged by the row's number: a read of 32 rows uses all banks evenly.  Where it runs
 // across them (kTr), 64 lines of kR values are there, a line's 32-byte chunks exchanged by the line's number, and a read that transposes four lines of sixteen values makes
 // the operand.  Neither has a bank conflict (counted).
+//
+// What bounds it: with all CUs busy the matrix instructions and, behind them, the clock that the card holds while they run (a large product's first calls after a pause take a tenth less than
+// those that follow).  16384 rows of codes times 7168 x 7168, 682 us, 2470 TOP/s; bf16 sums of 7168, 16384 x 4096, 740 us, 1300 TFLOP/s; 10 to 18 us a round of tiles go to first loads and to results.
+// Workgroups that stay, and load their next tile's first step before the results of the one before leave, were not faster (sums of 7168 and 2048, 16384 rows, 1240 -> 1246 us; gradients
+// of uneven runs 2429 -> 2526): the hardware hands the next tile to whichever CU is free.
 #ifndef MW_TILE_H_
 #define MW_TILE_H_
 
@@ -33,11 +38,11 @@ constexpr int kStep = 128;               // bytes along the sum of a step
 
 template <bool kInt8> struct tile_kind;
 template <> struct tile_kind<false> {
-    typedef bf16x8 frag; typedef f32x16 acc; static constexpr int bytes = 2;
+    typedef bf16x8 frag; typedef f32x16 acc;
     static __device__ __forceinline__ acc mma(frag a, frag b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct tile_kind<true> {
-    typedef i32x4 frag; typedef i32x16 acc; static constexpr int bytes = 1;
+    typedef i32x4 frag; typedef i32x16 acc;
     static __device__ __forceinline__ acc mma(frag a, frag b, acc c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
 };
 
