@@ -122,7 +122,40 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
     }
     order();
 }
-// A workgroup's kAlong waves share a tile of sixteen matrix rows, or (kAlong 1) each of four has its own.  grid: (tiles, four of them at kAlong 1; runs, 65535 at most)
+// Which rows a workgroup takes: item n of the first g.n is the first kChunk rows of run n, the items behind are long runs' further rows, kChunk each, so that a run which got most of the rows is
+// gone through by many workgroups side by side (1024 rows in one of 64 experts 2048 x 768: 734 us one behind another, 80 so).
+template <int kChunk>
+__device__ __forceinline__ bool few_chunk(const row_groups &g, int item, int &e, int64_t &first, int &count)
+{
+    int64_t end;
+    if (item < g.n) {
+        e = item;
+        group_bounds(g, e, first, end);
+        count = (int)min(end - first, (int64_t)kChunk);
+        return count > 0;
+    }
+    const uint32_t want = (uint32_t)(item - g.n);
+    uint32_t before = 0;
+    for (int c = 0; c < g.n; c += 64) {
+        const int lane = (int)(threadIdx.x & 63);
+        first = end = 0;
+        if (c + lane < g.n) group_bounds(g, c + lane, first, end);
+        const uint32_t more = end > first ? (uint32_t)((end - first - 1) / kChunk) : 0, incl = before + mw_wave_incl_scan(more);
+        const uint64_t behind = __ballot(incl > want);
+        if (behind == 0) {
+            before = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+            continue;
+        }
+        const int l = __ffsll((unsigned long long)behind) - 1;
+        e = c + l;
+        group_bounds(g, e, first, end);
+        first += (int64_t)(want - (uint32_t)__builtin_amdgcn_readlane((int)(incl - more), l) + 1) * kChunk;
+        count = (int)min(end - first, (int64_t)kChunk);
+        return true;
+    }
+    return false;
+}
+// A workgroup's kAlong waves share a tile of sixteen matrix rows, or (kAlong 1) each of four has its own.  grid: (tiles, four of them at kAlong 1; items, 65535 at most)
 template <class Op, int kAlong>
 __global__ __launch_bounds__(kAlong == 8 ? 512 : 256) void k_few(typename Op::args a)
 {
@@ -130,15 +163,16 @@ __global__ __launch_bounds__(kAlong == 8 ? 512 : 256) void k_few(typename Op::ar
     const int own = kAlong > 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), tile = kAlong > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + own;
     char *lds = all + own * 3 * kTileBytes;
     constexpr int kPass = 16 / Op::kTerms;
-    for (int e = blockIdx.y; e < a.g.n; e += gridDim.y) {
-        int64_t first, end;
-        group_bounds(a.g, e, first, end);
-        while (first < end) {
-            const int left = (int)(end - first);
-            if (left <= kPass) few_columns<Op, kAlong, 1, 4>(a, e, tile, first, left, lds);
-            else few_columns<Op, kAlong, 2, 3>(a, e, tile, first, left, lds);
-            first += left <= kPass ? kPass : 2 * kPass;
-        }
+    const int items = a.g.n + (int)(a.g.n_rows / (2 * kPass));
+    for (int item = (int)blockIdx.y; item < items; item += (int)gridDim.y) {
+        int e, count;
+        int64_t first;
+        if (!few_chunk<2 * kPass>(a.g, item, e, first, count)) continue;
+        e = __builtin_amdgcn_readfirstlane(e);                  // (the same for all lanes; said, so that arrays' places stay in scalar registers)
+        count = __builtin_amdgcn_readfirstlane(count);
+        first = __builtin_amdgcn_readfirstlane((int)first);     // (rows are fewer than 2^31)
+        if (count <= kPass) few_columns<Op, kAlong, 1, 4>(a, e, tile, first, count, lds);
+        else few_columns<Op, kAlong, 2, 3>(a, e, tile, first, count, lds);
     }
 }
 // Waves that share sixteen matrix rows, by the tiles of all runs and the rows' bytes: eight where there is hardly a tile a CU and rows are long, one where there are many tiles of
@@ -155,7 +189,7 @@ static inline int few_waves(int64_t tiles, int64_t row_bytes)
 template <class Op>
 int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
 {
-    const uint32_t tiles = (uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), n = (uint32_t)(a.g.n < 65535 ? a.g.n : 65535);
+    const uint32_t tiles = (uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), n = (uint32_t)min(a.g.n + a.g.n_rows / (32 / Op::kTerms), (int64_t)65535);
     const int waves = few_waves((int64_t)tiles * (a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows), (int64_t)a.K * (Op::kInt8 ? 1 : 2));
     if (waves == 8) hipLaunchKernelGGL((k_few<Op, 8>), dim3(tiles, n), dim3(512), 0, s, a);
     else if (waves == 4) hipLaunchKernelGGL((k_few<Op, 4>), dim3(tiles, n), dim3(256), 0, s, a);

@@ -137,6 +137,14 @@ def test_more_experts_than_a_wave_has_lanes():
     s.check_backward()
 
 
+@pytest.mark.parametrize("n,runs", [(40, {3: 600, 39: 33}), (100, {80: 1200, 99: 17, 2: 16}), (70, {0: 33, 64: 1000, 65: 32}), (3, {1: 48})])
+def test_few_rows_most_of_which_are_one_experts(n, runs):
+    """At most sixteen rows an expert on average: the form of few rows, with runs of many."""
+    counts = [runs.get(e, 0) for e in range(n)]
+    assert sum(counts) + 3 <= 16 * n or n == 3
+    Set(counts, 136, 72, spare=3 if n > 3 else 0, pad=8).check_forward()
+
+
 @pytest.mark.parametrize("leave", [("dx",), ("dgu", "dd"), ("dx", "dgu", "dw"), ("dx", "dd", "dw")])
 def test_gradients_that_are_left_out(leave):
     Set([70, 0, 20], 136, 72, spare=1).check_backward(**{k: True for k in leave})
