@@ -205,7 +205,9 @@ int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
 //   mw_ffn, four experts 7168 x 2048, 512 rows 150 / 116 / 134, 123; 16384 rows - / - / 1242, the same; mw_ffn of codes, 512 rows 90 / 87 / 97, 90; 16384 rows 1062 / 854 / 804, 804
 //   mw_ffn_backward, 333 rows of five 2880 x 1000 77 / 98 / 130, 77; 2048 rows of eight 4096 x 1024 209 / 203 / 195, 195
 //   mw_matmul_int8, 8192 rows 7168 -> 7168 568 / 427 / 396, 396; four matrices 7168 -> 2048, 2048 rows 40 / 42 / 66, 40
-// A few rows: mw_ffn, four experts 7168 x 2048, few / 128 x 64: 64 rows 74 / 88, 96 rows 104 / 88; 32 of 2048 x 768, 512 rows 65 / 67; codes, eight of 4096 x 1024, 128 rows 31 / 39.
+// A few rows a run, 16 at most, with two terms a row (bf16 rows of h) 10 where the matrices make more tiles of 128 x 64 than there are CUs: mw_ffn, uneven runs, few / 128 x 64: four experts 7168 x 2048,
+// 32 rows 67 / 87, 64 rows 84 / 88, 96 rows (even) 104 / 88; 32 of 4096 x 1024, 128 rows 128 / 153, 256 rows 140 / 154, 384 rows 157 / 153, 512 rows 181 / 154; codes, 512 rows 96 / 98;
+// mw_matmul_int8, 64 matrices 4096 -> 1024, 1024 rows 58 / 62.
 enum { kFew, kSmall, kMiddle, kLarge };
 static inline double tile_rounds(int64_t n_rows, int64_t n, int rows_a_tile, int64_t column_tiles, int64_t at_once, int64_t steps, bool parts)
 {
@@ -214,9 +216,9 @@ static inline double tile_rounds(int64_t n_rows, int64_t n, int rows_a_tile, int
     if (parts && left > 0 && parts_pay((uint32_t)left, (uint32_t)steps)) return (double)whole + (double)left / kUnits + (double)join_steps((uint32_t)left) / (double)steps;
     return (double)(whole + (left + kUnits - 1) / kUnits);
 }
-static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t steps, bool parts)
+static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t steps, bool parts, int few = 16)
 {
-    if (n_rows <= 16 * n) return kFew;
+    if (n_rows <= few * n) return kFew;
     const double small = 0.49 * tile_rounds(n_rows, n, 64, (columns + 127) / 128, 768, steps, parts), middle = tile_rounds(n_rows, n, 128, (columns + 255) / 256, kUnits, steps, parts),
                  large = 1.5 * tile_rounds(n_rows, n, 256, (columns + 255) / 256, kUnits, steps, parts);
     return small < middle && small < large ? kSmall : middle < large ? kMiddle : kLarge;

@@ -376,7 +376,8 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     const row_groups g = {expert_offsets_dev, n_rows, ctx->n_local};
     const hipStream_t s = (hipStream_t)stream;
     if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), (float *)(b + w.parts), s);
-    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, pieces(H, 64), true), down_form = rows_form(n_rows, g.n, H, pieces(I, 64), true);
+    const int few = pieces(2 * (int64_t)I, 128) * g.n > kUnits ? 10 : 16;          // (both products' rows are few, or neither's)
+    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, pieces(H, 64), true, few), down_form = rows_form(n_rows, g.n, H, pieces(I, 64), true, few);
     const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
     const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), form == kFew ? 2 * (int64_t)I : I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
     rc = launch_product<up_op<256, 256>, up_op<256, 128>, up_op<128, 64>, true>(form, u, I, s);
