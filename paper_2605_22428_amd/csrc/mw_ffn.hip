@@ -229,10 +229,10 @@ struct grads_args { row_groups g; grads_matrix m[2]; uint32_t first, weights; we
 // sums, which wait for the same kernel, its first workgroups.  Results are written past the caches: no one reads them soon.  16384 rows of four experts 7168 x 2048: 1165 us, 1240 TFLOP/s; 2048
 // rows of eight 4096 x 1024: 79 us for 52 GFLOP and 201 MB written (writing zeros takes 28).
 template <int kP, int kQ>
-__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 4) void k_ffn_grads(grads_args a)
+__global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 5) void k_ffn_grads(grads_args a)
 {
     typedef std::conditional_t<(kP * kQ > 128 * 128), tile_product<kP, kQ, true, true, false>, tile_product_short<kP, kQ, true, true, false>> product;
-    typedef tile_out<kP, kQ, false> out_form;
+    typedef tile_out_bf16<kP, kQ> out_form;
     __shared__ __attribute__((aligned(1024))) char lds[product::kLds > kTileWaves * out_form::kBytes ? product::kLds : kTileWaves * out_form::kBytes];
     if (blockIdx.x < a.weights) {
         row_weights_of(a.g, a.w, blockIdx.x, (float (*)[17])lds);
@@ -268,8 +268,8 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 4) void k_f
     product t;
     t.run(fp, fq, (rows + 63) / 64, (lds_char *)lds);
     uint16_t *out = m.out + (int64_t)e * m.M * m.N;
-    tile_results<kP, kQ, false>(t, (lds_char *)lds, [](int, int) { return 0; }, [&](int row, int column, const float (&v)[8], const float (&)[8], int) {
-        if (q0 + row < m.M && p0 + column < m.N) store_bf16<true>(out + (int64_t)(q0 + row) * m.N + p0 + column, v);
+    tile_results_bf16<kP, kQ>(t, (lds_char *)lds, [&](int row, int column, u32x4 v) {
+        if (q0 + row < m.M && p0 + column < m.N) __builtin_nontemporal_store(v, (u32x4 *)(out + (int64_t)(q0 + row) * m.N + p0 + column));
     });
 }
 

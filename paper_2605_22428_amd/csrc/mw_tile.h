@@ -490,6 +490,43 @@ __device__ __forceinline__ void tile_results(const Product &t, lds_char *lds, Fe
     }
 }
 
+// The same where results are only rounded to bf16: rounded before they go through LDS, half the bytes both ways.  use(row, c, eight values).
+template <int kP, int kQ>
+struct tile_out_bf16 {
+    static constexpr int kCols = kP / 2, kPitch = kCols * 2 + 16, kBytes = 32 * kPitch, kLanes = kCols / 8, kAtOnce = 64 / kLanes;
+};
+template <int kP, int kQ, class Product, class Use>
+__device__ __forceinline__ void tile_results_bf16(const Product &t, lds_char *lds, Use use)
+{
+    typedef tile_out_bf16<kP, kQ> out;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) bf16x4 lds_four;
+    typedef const __attribute__((address_space(3))) u32x4 lds_eight;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    lds_char *mine = lds + wave * out::kBytes;
+#pragma unroll
+    for (int j = 0; j < Product::kNQ; ++j) {
+#pragma unroll
+        for (int i = 0; i < Product::kNP; ++i) {
+            lds_char *to = mine + (lane & 31) * out::kPitch + (i * 32 + (lane >> 5) * 4) * 2;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                bf16x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (__bf16)t.acc[i][j][q * 4 + e];
+                *(lds_four *)(to + q * 16) = v;
+            }
+        }
+        wave_order();
+#pragma unroll
+        for (int n = 0; n < 32 / out::kAtOnce; ++n) {
+            const int row = n * out::kAtOnce + lane / out::kLanes, c = (lane & (out::kLanes - 1)) * 8;
+            use((wave >> 1) * (kQ / 2) + j * 32 + row, (wave & 1) * (kP / 2) + c, *(lds_eight *)(mine + row * out::kPitch + c * 2));
+        }
+        wave_order();
+    }
+}
+
 // A product's kernels.  Op has: args (with g, p_tiles, K and parts, memory for kRound tiles' sums or null); kP, kQ, kTrP, kInt8; kPair: half of a wave's columns belong to
 // the other half; feeds(): what is loaded; emit(): what becomes of eight columns of a row, with what columns() gives for the columns, rows() for the row (kRowValues: two
 // values at most, which wait in LDS) and fetch() for both.
