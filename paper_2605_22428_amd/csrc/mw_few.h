@@ -123,34 +123,37 @@ __device__ __forceinline__ void few_columns(const typename Op::args &a, int e, i
     order();
 }
 // Which rows a workgroup takes: item n of the first g.n is the first kChunk rows of run n, the items behind are long runs' further rows, kChunk each, so that a run which got most of the rows is
-// gone through by many workgroups side by side (1024 rows in one of 64 experts 2048 x 768: 734 us one behind another, 80 so).
+// gone through by many workgroups side by side (1024 rows in one of 64 experts 2048 x 768: 734 us one behind another, 80 so).  Where that makes many workgroups without rows, items are
+// the chunks of all runs in order (listed): 2 rows among 32 experts 2880 x 2048 in codes 26.6 -> 18.6 us; the scan takes half a microsecond, 16 rows of eight 4096 x 1024 24.2 -> 25.2.
+static __host__ __device__ __forceinline__ bool few_listed(int64_t n, int64_t n_rows, int64_t tiles) { return (n - n_rows) * tiles > 2048; }
 template <int kChunk>
-__device__ __forceinline__ bool few_chunk(const row_groups &g, int item, int &e, int64_t &first, int &count)
+__device__ __forceinline__ bool few_chunk(const row_groups &g, int item, bool listed, int &e, int64_t &first, int &count)
 {
-    int64_t end;
-    if (item < g.n) {
+    if (!listed && item < g.n) {
+        int64_t end;
         e = item;
         group_bounds(g, e, first, end);
         count = (int)min(end - first, (int64_t)kChunk);
         return count > 0;
     }
-    const uint32_t want = (uint32_t)(item - g.n);
+    const uint32_t want = (uint32_t)(listed ? item : item - g.n);
     uint32_t before = 0;
     for (int c = 0; c < g.n; c += 64) {
         const int lane = (int)(threadIdx.x & 63);
-        first = end = 0;
-        if (c + lane < g.n) group_bounds(g, c + lane, first, end);
-        const uint32_t more = end > first ? (uint32_t)((end - first - 1) / kChunk) : 0, incl = before + mw_wave_incl_scan(more);
+        int64_t f = 0, end = 0;
+        if (c + lane < g.n) group_bounds(g, c + lane, f, end);
+        const int rows = (int)(end - f);
+        const uint32_t chunks = (uint32_t)((rows + kChunk - 1) / kChunk) - (!listed && rows > 0), incl = before + mw_wave_incl_scan(chunks);
         const uint64_t behind = __ballot(incl > want);
         if (behind == 0) {
             before = (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
             continue;
         }
         const int l = __ffsll((unsigned long long)behind) - 1;
+        const int skip = (int)(want - (uint32_t)__builtin_amdgcn_readlane((int)(incl - chunks), l) + (listed ? 0 : 1)) * kChunk;
         e = c + l;
-        group_bounds(g, e, first, end);
-        first += (int64_t)(want - (uint32_t)__builtin_amdgcn_readlane((int)(incl - more), l) + 1) * kChunk;
-        count = (int)min(end - first, (int64_t)kChunk);
+        first = __builtin_amdgcn_readlane((int)f, l) + skip;    // (rows are fewer than 2^31)
+        count = min(__builtin_amdgcn_readlane(rows, l) - skip, kChunk);
         return true;
     }
     return false;
@@ -163,14 +166,15 @@ __global__ __launch_bounds__(kAlong == 8 ? 512 : 256) void k_few(typename Op::ar
     const int own = kAlong > 1 ? 0 : __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), tile = kAlong > 1 ? (int)blockIdx.x : (int)blockIdx.x * 4 + own;
     char *lds = all + own * 3 * kTileBytes;
     constexpr int kPass = 16 / Op::kTerms;
-    const int items = a.g.n + (int)(a.g.n_rows / (2 * kPass));
+    const bool listed = few_listed(a.g.n, a.g.n_rows, (int64_t)gridDim.x * (kAlong > 1 ? 1 : 4));
+    const int items = (int)(listed ? a.g.n_rows : a.g.n) + (int)(a.g.n_rows / (2 * kPass));
     for (int item = (int)blockIdx.y; item < items; item += (int)gridDim.y) {
         int e, count;
         int64_t first;
-        if (!few_chunk<2 * kPass>(a.g, item, e, first, count)) continue;
+        if (!few_chunk<2 * kPass>(a.g, item, listed, e, first, count)) continue;
         e = __builtin_amdgcn_readfirstlane(e);                  // (the same for all lanes; said, so that arrays' places stay in scalar registers)
         count = __builtin_amdgcn_readfirstlane(count);
-        first = __builtin_amdgcn_readfirstlane((int)first);     // (rows are fewer than 2^31)
+        first = __builtin_amdgcn_readfirstlane((int)first);
         if (count <= kPass) few_columns<Op, kAlong, 1, 4>(a, e, tile, first, count, lds);
         else few_columns<Op, kAlong, 2, 3>(a, e, tile, first, count, lds);
     }
@@ -189,8 +193,10 @@ static inline int few_waves(int64_t tiles, int64_t row_bytes)
 template <class Op>
 int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
 {
-    const uint32_t tiles = (uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16)), n = (uint32_t)min(a.g.n + a.g.n_rows / (32 / Op::kTerms), (int64_t)65535);
+    const uint32_t tiles = (uint32_t)((columns + (Op::kPair ? 7 : 15)) / (Op::kPair ? 8 : 16));
     const int waves = few_waves((int64_t)tiles * (a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows), (int64_t)a.K * (Op::kInt8 ? 1 : 2));
+    const int64_t items = (few_listed(a.g.n, a.g.n_rows, waves > 1 ? tiles : (tiles + 3) / 4 * 4) ? a.g.n_rows : a.g.n) + a.g.n_rows / (32 / Op::kTerms);
+    const uint32_t n = (uint32_t)(items < 65535 ? items : 65535);
     if (waves == 8) hipLaunchKernelGGL((k_few<Op, 8>), dim3(tiles, n), dim3(512), 0, s, a);
     else if (waves == 4) hipLaunchKernelGGL((k_few<Op, 4>), dim3(tiles, n), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((k_few<Op, 1>), dim3((tiles + 3) / 4, n), dim3(256), 0, s, a);

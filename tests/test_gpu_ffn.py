@@ -137,7 +137,7 @@ def test_more_experts_than_a_wave_has_lanes():
     s.check_backward()
 
 
-@pytest.mark.parametrize("n,runs", [(40, {3: 600, 39: 33}), (100, {80: 1200, 99: 17, 2: 16}), (70, {0: 33, 64: 1000, 65: 32}), (3, {1: 48})])
+@pytest.mark.parametrize("n,runs", [(40, {3: 600, 39: 33}), (100, {80: 1200, 99: 17, 2: 16}), (70, {0: 33, 64: 1000, 65: 32}), (3, {1: 48}), (300, {5: 70, 250: 17, 299: 1}), (300, {299: 33})])
 def test_few_rows_most_of_which_are_one_experts(n, runs):
     """At most sixteen rows an expert on average: the form of few rows, with runs of many."""
     counts = [runs.get(e, 0) for e in range(n)]

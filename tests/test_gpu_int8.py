@@ -103,7 +103,7 @@ def test_products_of_many_matrices():
     Matrices(100, 144, 144).check([(7 * m) % 40 if m % 10 == 0 else m % 3 for m in range(100)], spare=2, dtype=torch.float32)
 
 
-@pytest.mark.parametrize("n,runs", [(40, {3: 600, 39: 33}), (100, {80: 1200, 99: 17, 2: 16}), (70, {0: 33, 64: 1000, 65: 32}), (1, {0: 16})])
+@pytest.mark.parametrize("n,runs", [(40, {3: 600, 39: 33}), (100, {80: 1200, 99: 17, 2: 16}), (70, {0: 33, 64: 1000, 65: 32}), (1, {0: 16}), (700, {5: 70, 250: 17, 699: 1}), (700, {64: 33})])
 def test_few_rows_most_of_which_are_one_matrix(n, runs):
     counts = [runs.get(m, 0) for m in range(n)]
     Matrices(n, 144, 80).check(counts, spare=3 if n > 1 else 0, pad=16)
