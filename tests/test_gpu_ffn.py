@@ -314,6 +314,64 @@ def test_replayed_from_a_graph_on_another_stream(counts):
             assert torch.equal(a[:n] if a.shape[0] == s.room else a, b[:n] if b.shape[0] == s.room else b)
 
 
+def _step(s, out, ws):
+    y, kept, dx, dgu, dd, dw = out
+    s.ctx.mw_ffn(s.dev, s.dev_x, s.offsets, y, ws, s.dev_w, kept)
+    s.ctx.mw_ffn_backward(s.dev, s.dev_x, s.offsets, kept, s.dev_dy, dx, dgu, dd, ws, s.dev_w, dw)
+
+
+def _outputs(s):
+    return ([torch.zeros((s.room, s.hidden), dtype=torch.bfloat16, device=DEV), torch.zeros((s.room, 2, s.inter), dtype=torch.bfloat16, device=DEV), torch.zeros((s.room, s.hidden), dtype=torch.bfloat16, device=DEV)] +
+            [torch.zeros_like(t) for t in s.dev._held[:2]] + [torch.zeros(s.room, device=DEV)])
+
+
+@pytest.mark.parametrize("counts", [[9, 3], [200, 130], [700, 300]])
+def test_calls_on_two_streams_at_once(counts):
+    """Two contexts' steps side by side, each with its own workspace and stream, give what they give alone."""
+    sets = [Set(counts, 264, 328, seed=1), Set(counts[::-1], 264, 328, seed=50)]
+    want = [_outputs(s) for s in sets]
+    for s, o in zip(sets, want):
+        _step(s, o, s.workspace(True))
+        torch.cuda.synchronize()
+    got, spaces, streams = [_outputs(s) for s in sets], [s.workspace(True) for s in sets], [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(6):
+        for s, o, ws, st in zip(sets, got, spaces, streams):
+            with torch.cuda.stream(st):
+                _step(s, o, ws)
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("counts", [[9, 3], [200, 130]])
+def test_two_graphs_that_share_a_workspace(counts):
+    """Replayed in turn, with the eager step between them, each finds nothing in the workspace that it needs and leaves nothing that the other minds."""
+    sets = [Set(counts, 264, 328, seed=1), Set([c + 40 for c in counts], 264, 328, seed=50)]
+    want, got, graphs = [_outputs(s) for s in sets], [_outputs(s) for s in sets], []
+    ws = sets[1].workspace(True)                                          # (the larger one)
+    for s, o in zip(sets, want):
+        _step(s, o, ws)
+        torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for s, o in zip(sets, got):
+        with torch.cuda.stream(st):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=st):
+                _step(s, o, ws)
+        graphs.append(graph)
+    for turn in (0, 1, 0, 0, 1, 1, 0):
+        for t in got[turn]:
+            t.zero_()
+        ws.fill_(turn * 77)
+        torch.cuda.synchronize()
+        graphs[turn].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want[turn], got[turn]))
+        _step(sets[1 - turn], _outputs(sets[1 - turn]), ws)
+
+
 def test_refusals():
     s = Set([3, 2], 64, 32)
     I, CAP, WS, UN = B.MW_ERR_INVALID_ARG, B.MW_ERR_CAPACITY, B.MW_ERR_WORKSPACE, B.MW_ERR_UNSUPPORTED
