@@ -225,7 +225,7 @@ static inline double tile_rounds(int64_t n_rows, int64_t n, int rows_a_tile, int
 static inline int rows_form(int64_t n_rows, int64_t n, int64_t columns, int64_t steps, bool parts, int few = 16)
 {
     if (n_rows <= few * n) return kFew;
-    const double small = 0.49 * tile_rounds(n_rows, n, 64, (columns + 127) / 128, 768, steps, parts), middle = tile_rounds(n_rows, n, 128, (columns + 255) / 256, kUnits, steps, parts),
+    const double small = 0.49 * tile_rounds(n_rows, n, 64, (columns + 127) / 128, 512, steps, parts), middle = tile_rounds(n_rows, n, 128, (columns + 255) / 256, kUnits, steps, parts),
                  large = 1.5 * tile_rounds(n_rows, n, 256, (columns + 255) / 256, kUnits, steps, parts);
     return small < middle && small < large ? kSmall : middle < large ? kMiddle : kLarge;
 }

@@ -1,7 +1,7 @@
 // Products of tiles that stay in registers: the experts' products over many rows.
 //
 // A workgroup of four waves makes a tile of kP columns times kQ rows of an output, one wave a quarter of it, kP / 2 by kQ / 2, in the accumulators
-// of 32 x 32 matrix instructions.  Steps of 128 bytes along the sum (64 bf16 values, 128 codes) come from memory straight into LDS, two steps' room.  A step's
+// of 32 x 32 matrix instructions.  Steps of 128 bytes along the sum (64 bf16 values, 128 codes) come from memory straight into LDS, two steps' room (tiles of 128 x 64 three).  A step's
 // first quarter is in registers when the step begins; beside its products the other three come from LDS, then the stage is free and the step after the next is loaded into
 // it while two more quarters are multiplied, and beside the last one the next step's first quarter comes.  A load has four fifths of two steps
 // to arrive that way; with the stage free only after a step's last quarter had been read it had two fifths: 16384 x 4096, sums of 7168, 795 us instead of 740 (columns by
@@ -202,7 +202,7 @@ template <int kP, int kQ, bool kTrP, bool kTrQ, bool kInt8>
 struct tile_product {
     typedef tile_kind<kInt8> kind;
     typedef typename kind::frag frag;
-    static constexpr int kNP = kP / 64, kNQ = kQ / 64, kStage = (kP + kQ) * kStep, kLds = 2 * kStage, kLoads = (kP + kQ) / 32;
+    static constexpr int kNP = kP / 64, kNQ = kQ / 64, kStages = kP * kQ == 128 * 64 ? 3 : 2, kStage = (kP + kQ) * kStep, kLds = kStages * kStage, kLoads = (kP + kQ) / 32;
     typename kind::acc acc[kNP][kNQ];
     __device__ __forceinline__ void run(const tile_feed<kP, kTrP, kInt8> &p, const tile_feed<kQ, kTrQ, kInt8> &q, int steps, lds_char *lds)
     {
@@ -223,14 +223,15 @@ struct tile_product {
         constexpr int kReads = kNP + kNQ, kMfma = kNP * kNQ;
 #pragma unroll
         for (int n = 0; n < kMfma; ++n) acc[n / kNQ][n % kNQ] = typename kind::acc{};
-        p.issue_all(0, lds); q.issue_all(0, lds + kP * kStep);
-        p.issue_all(1, lds + kStage); q.issue_all(1, lds + kStage + kP * kStep);
-        tile_wait<kLoads>();
+#pragma unroll
+        for (int k = 0; k < kStages; ++k) { p.issue_all(k, lds + k * kStage); q.issue_all(k, lds + k * kStage + kP * kStep); }
+        tile_wait<(kStages - 1) * kLoads>();
         tile_barrier();
 #pragma unroll
         for (int n = 0; n < kReads; ++n) read(lds, 0, n);
+        lds_char *here = lds;
         for (int k = 0; k < steps; ++k) {
-            lds_char *here = lds + (k & 1) * kStage, *next = lds + ((k + 1) & 1) * kStage;
+            lds_char *next = here == lds + (kStages - 1) * kStage ? lds : here + kStage;
             // the step's other three parts come to registers beside the first part's products, in the first three quarters of them
             constexpr int kEarly = (kMfma * 3 + 3) / 4;
 #pragma unroll
@@ -241,9 +242,9 @@ struct tile_product {
                 multiply(0, n);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            tile_reads_done();                          // every wave has read this stage: it is loaded again, for the step after the next
-            const auto sp = p.at_step(k + 2, here);
-            const auto sq = q.at_step(k + 2, here + kP * kStep);
+            tile_reads_done();                          // every wave has read this stage: it is loaded again, for step k + kStages
+            const auto sp = p.at_step(k + kStages, here);
+            const auto sq = q.at_step(k + kStages, here + kP * kStep);
 #pragma unroll
             for (int n = 0; n < 2 * kMfma; ++n) {
 #pragma unroll
@@ -254,7 +255,7 @@ struct tile_product {
                 multiply(1 + n / kMfma, n % kMfma);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            tile_wait<kLoads>();                        // the next step's loads, every wave's
+            tile_wait<(kStages - 1) * kLoads>();        // the next step's loads, every wave's
             tile_barrier();
 #pragma unroll
             for (int n = 0; n < kMfma; ++n) {
@@ -264,6 +265,7 @@ struct tile_product {
                 multiply(3, n);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            here = next;
         }
         tile_wait<0>();
         tile_reads_done();                              // (the results go through LDS)
@@ -535,8 +537,9 @@ struct tile_op : Op {
     typedef tile_product<Op::kP, Op::kQ, Op::kTrP, false, Op::kInt8> product;
     typedef tile_out<Op::kP, Op::kQ, Op::kPair> out;
     typedef decltype(typename product::kind::acc{}[0] + 0) value;
-    // Workgroups that run at a time: LDS holds one of the two larger tiles a CU, three of 128 x 64.
-    static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : 768;
+    // Workgroups that run at a time: LDS holds one of the two larger tiles a CU, two of 128 x 64 (with room for three steps each: with two, three
+    // workgroups a CU, calls of a few tiles take 2 to 12 % longer, those of many up to 2 % less; with four, one a CU, they are 5 % slower than with three; 256 x 128 gains nothing from a third).
+    static constexpr uint32_t kRound = Op::kP * Op::kQ > 128 * 128 ? 256 : 512;
     static constexpr int kLds = product::kLds > kTileWaves * out::kBytes ? product::kLds : kTileWaves * out::kBytes;
     static constexpr int kRowsAt = kLds, kAllLds = kLds + (Op::kRowValues ? 8 * Op::kQ : 0);           // a row's values behind the stages
     static constexpr int kColumns = Op::kPair ? Op::kP / 2 : Op::kP, kJoinRows = kTileThreads * 8 / kColumns;         // rows that a workgroup of k_join takes
