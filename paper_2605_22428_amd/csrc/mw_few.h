@@ -205,8 +205,8 @@ int32_t launch_few(const typename Op::args &a, int columns, hipStream_t s)
 }
 
 // How a product of rows with n matrices, `columns` values of a row from each, is cut: few rows a run to a form of their own, others to the tile size that is through first, counted
-// in rounds of the CUs times what a step takes with a tile on every CU, 128 x 64, 256 x 128, 256 x 256 as 0.49 : 1 : 1.5 (fitted to 95
-// calls of random sizes, each timed with all nine pairs of sizes for its two products: the sizes taken are 0.5 % from the best of them on average, 10 % at most).  parts: a last round's tiles
+// in rounds of the CUs times what a step takes with a tile on every CU, 128 x 64, 256 x 128, 256 x 256 as 0.49 : 1 : 1.5 (fitted to 109
+// calls of random sizes, each timed with all nine pairs of sizes for its two products: the sizes taken are 0.4 % from the best of them on average, 12 % at most).  parts: a last round's tiles
 // may be cut along the sum.  us, weights from memory, runs of uneven lengths, both products with 128 x 64 / 256 x 128 / 256 x 256 tiles, and the ones taken:
 //   mw_ffn, four experts 7168 x 2048, 512 rows 150 / 116 / 134, 123; 16384 rows - / - / 1242, the same; mw_ffn of codes, 512 rows 90 / 87 / 97, 90; 16384 rows 1062 / 854 / 804, 804
 //   mw_ffn_backward, 333 rows of five 2880 x 1000 77 / 98 / 130, 77; 2048 rows of eight 4096 x 1024 209 / 203 / 195, 195
