@@ -85,6 +85,33 @@ def test_experts_of_another_device(monkeypatch):
         ctx.mw_ffn_backward(experts, x, offsets, kept, x, None, None, None, ws)
 
 
+class Elsewhere(torch.Tensor):
+    """An array that says that it is on another device."""
+
+    def get_device(self):
+        return 1
+
+
+def test_arrays_of_another_device(monkeypatch):
+    """Each array of each call, alone on another device than the weights (or rows), is refused before anything is launched."""
+    monkeypatch.setattr(B, "_native", Calls)
+    monkeypatch.setattr(B, "_stream_on", lambda device, where: 0)
+    monkeypatch.setattr(B, "_stream_handle", lambda: 0)
+    ctx = B.Context.__new__(B.Context)
+    ctx._h, ctx.n_local, ctx.hidden, ctx.workspace = None, 1, 16, torch.empty(0)
+    bf, f = dict(dtype=torch.bfloat16), torch.zeros(3)
+    experts = B.Experts(torch.zeros((1, 2, 8, 16), **bf), torch.zeros((1, 16, 8), **bf))
+    m = B.MatricesInt8(torch.zeros((1, 32, 16), dtype=torch.int8), torch.zeros((1, 32)))
+    x, codes, offsets, ws, kept = torch.zeros((3, 16), **bf), torch.zeros((3, 16), dtype=torch.int8), torch.zeros(2, dtype=torch.int64), torch.zeros(1024, dtype=torch.uint8), torch.zeros((3, 2, 8), **bf)
+    calls = ((lambda *a: ctx.mw_ffn(experts, *a), (x, offsets, x.clone(), ws, f, kept)),
+             (lambda *a: ctx.mw_ffn_backward(experts, *a), (x, offsets, kept, x.clone(), x.clone(), torch.zeros((1, 2, 8, 16), **bf), torch.zeros((1, 16, 8), **bf), ws, f, f.clone())),
+             (m.mw_matmul_int8, (codes, f, offsets, torch.zeros((3, 32)))), (B.mw_quantize_rows, (x, codes, f)))
+    for call, args in calls:
+        for at, t in enumerate(args):
+            with pytest.raises(ValueError, match="expected device"):
+                call(*(args[:at] + (t.as_subclass(Elsewhere),) + args[at + 1:]))
+
+
 def test_record_and_constants_match_the_header(tmp_path):
     lines = ['printf("%zu", sizeof(mw_matrices_int8));'] + ['printf(" %%zu", offsetof(mw_matrices_int8, %s));' % f for f, _ in B.MwMatricesInt8._fields_]
     lines += ['printf(" %%lld", (long long)%s);' % n for n in ("MW_WEIGHT_INT8_CHANNEL", "MW_FFN_MAX_ROWS", "MW_MAX_STRIDE", "MW_INT8_MAX_IN")]
