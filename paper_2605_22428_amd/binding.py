@@ -403,7 +403,7 @@ class MatricesInt8:
             raise ValueError("codes int8, out float32 or bfloat16, as many rows each")
         _whole(scales, (n,), torch.float32, "scales")
         _whole(offsets, (self.n + 1,), torch.int64, "offsets")
-        _together(self._held[0].get_device(), "mw_matmul_int8", codes=codes, scales=scales, offsets=offsets, out=out)
+        _together(self._held[0].get_device(), (codes, scales, offsets, out), "mw_matmul_int8 codes scales offsets out")
         _check(_native().mw_matmul_int8(self.address, codes, _rows(codes, self.n_in, "codes"), scales, offsets, n, out, _LOGIT_FORMAT[out.dtype],
                                         _rows(out, self.n_out, "out"), _stream_on(self.device, "mw_matmul_int8")), "mw_matmul_int8")
 
@@ -413,7 +413,7 @@ def mw_quantize_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor)
     if x.dtype != torch.bfloat16 or codes.dtype != torch.int8 or codes.shape != x.shape:
         raise ValueError("x bfloat16, codes int8 of the same shape")
     _whole(scales, (x.shape[0],), torch.float32, "scales")
-    _together(x.get_device(), "mw_quantize_rows", codes=codes, scales=scales)
+    _together(x.get_device(), (codes, scales), "mw_quantize_rows codes scales")
     _check(_native().mw_quantize_rows(x, _rows(x, x.shape[1], "x"), x.shape[0], x.shape[1], codes, _rows(codes, x.shape[1], "codes"), scales,
                                       _stream_on(x.device, "mw_quantize_rows")), "mw_quantize_rows")
 
@@ -434,11 +434,12 @@ def _whole(t: Optional[torch.Tensor], shape: tuple, dtype, what: str):
         raise ValueError("%s: a contiguous tensor of %s and shape %s, got %s and %s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape)))
 
 
-def _together(index: int, where: str, **arrays):
-    """Arrays are on the device of that index (get_device(); -1: none); None is no array."""
-    for name, t in arrays.items():
+def _together(index: int, arrays: tuple, what: str):
+    """Arrays (None: no array) are on the device of that index (get_device(); -1: none); `what` names the call and them."""
+    for t in arrays:
         if t is not None and t.get_device() != index:
-            raise ValueError("%s: %s is on %s, expected device %d" % (where, name, t.device, index))
+            where, *names = what.split()
+            raise ValueError("%s: %s is on %s, expected device %d" % (where, names[[t is o for o in arrays].index(True)], t.device, index))
 
 
 MW_RELAY_BATCH_MAX = 4
@@ -583,7 +584,7 @@ class Context:
                row_weights: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None):
         n = x.shape[0]
         self._ffn_check(experts, n, expert_offsets, row_weights, kept)
-        _together(experts._held[0].get_device(), "mw_ffn", x=x, expert_offsets=expert_offsets, y=y, workspace=workspace, row_weights=row_weights, kept=kept)
+        _together(experts._held[0].get_device(), (x, expert_offsets, y, workspace, row_weights, kept), "mw_ffn x expert_offsets y workspace row_weights kept")
         _check(_native().mw_ffn(self._h, experts.address, x, self._ffn_matrix(x, n, "x"), expert_offsets, n, row_weights, y,
                                 self._ffn_matrix(y, n, "y"), kept, workspace, workspace.numel() * workspace.element_size(),
                                 _stream_handle()), "mw_ffn")
@@ -596,8 +597,7 @@ class Context:
         _whole(d_gate_up, (self.n_local, 2, experts.inter, self.hidden), torch.bfloat16, "d_gate_up")
         _whole(d_down, (self.n_local, self.hidden, experts.inter), torch.bfloat16, "d_down")
         _whole(d_row_weights, (n,), torch.float32, "d_row_weights")
-        _together(experts._held[0].get_device(), "mw_ffn_backward", x=x, expert_offsets=expert_offsets, kept=kept, dy=dy, dx=dx, d_gate_up=d_gate_up, d_down=d_down,
-                  workspace=workspace, row_weights=row_weights, d_row_weights=d_row_weights)
+        _together(experts._held[0].get_device(), (x, expert_offsets, kept, dy, dx, d_gate_up, d_down, workspace, row_weights, d_row_weights), "mw_ffn_backward x expert_offsets kept dy dx d_gate_up d_down workspace row_weights d_row_weights")
         _check(_native().mw_ffn_backward(self._h, experts.address, x, self._ffn_matrix(x, n, "x"), expert_offsets, n, row_weights, kept, dy,
                                          self._ffn_matrix(dy, n, "dy"), dx, self._ffn_matrix(dx, n, "dx"), d_gate_up, d_down, d_row_weights,
                                          workspace, workspace.numel() * workspace.element_size(), _stream_handle()), "mw_ffn_backward")
