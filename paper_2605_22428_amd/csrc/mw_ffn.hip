@@ -234,13 +234,14 @@ __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 5) void k_f
     typedef std::conditional_t<(kP * kQ > 128 * 128), tile_product<kP, kQ, true, true, false>, tile_product_short<kP, kQ, true, true, false>> product;
     typedef tile_out_bf16<kP, kQ> out_form;
     __shared__ __attribute__((aligned(1024))) char lds[product::kLds > kTileWaves * out_form::kBytes ? product::kLds : kTileWaves * out_form::kBytes];
-    if (blockIdx.x < a.weights) {
-        row_weights_of(a.g, a.w, blockIdx.x, (float (*)[17])lds);
+    const uint32_t workgroup = workgroup_id();
+    if (workgroup < a.weights) {
+        row_weights_of(a.g, a.w, workgroup, (float (*)[17])lds);
         return;
     }
-    const bool second = blockIdx.x - a.weights >= a.first;
+    const bool second = workgroup - a.weights >= a.first;
     const grads_matrix m = second ? a.m[1] : a.m[0];
-    const uint32_t id = blockIdx.x - a.weights - (second ? a.first : 0), each = (uint32_t)m.p_tiles * (uint32_t)m.q_tiles, per = (each + 7) / 8, at = id >> 3;
+    const uint32_t id = workgroup - a.weights - (second ? a.first : 0), each = (uint32_t)m.p_tiles * (uint32_t)m.q_tiles, per = (each + 7) / 8, at = id >> 3;
     const uint32_t tile = (id & 7) * per + at % per;
     int e = (int)(at / per);
     if (tile >= each || e >= a.g.n) return;
@@ -337,7 +338,7 @@ int32_t launch_grads(grads_args a, hipStream_t s)
     if (weights + grid[0] + grid[1] > 0x7ffffff0LL) return MW_ERR_UNSUPPORTED;
     a.first = (uint32_t)grid[0];
     a.weights = (uint32_t)weights;
-    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), dim3((uint32_t)(weights + grid[0] + grid[1])), dim3(kTileThreads), 0, s, a);
+    hipLaunchKernelGGL((k_ffn_grads<kP, kQ>), grid_of((uint32_t)(weights + grid[0] + grid[1])), dim3(kTileThreads), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     return MW_OK;
 }

@@ -320,6 +320,12 @@ struct tile_product_short {
     }
 };
 
+// A launch has fewer than 2^32 threads along an axis (2^24 workgroups of kTileThreads): workgroups beyond kAcross go into further rows of the grid, which the hardware deals out like one long row.
+constexpr uint32_t kAcross = 1u << 20;
+__host__ __device__ __forceinline__ uint32_t rows_of_grid(uint32_t workgroups) { return (workgroups + kAcross - 1) / kAcross; }
+static inline dim3 grid_of(uint32_t workgroups) { return dim3(workgroups < kAcross ? workgroups : kAcross, rows_of_grid(workgroups)); }
+__device__ __forceinline__ uint32_t workgroup_id() { return blockIdx.y * kAcross + blockIdx.x; }
+
 // ---- rows in runs, one run a matrix ---------------------------------------------------------------------------
 struct row_groups {
     const int64_t *offsets;     // [n + 1], or null: one run of all rows
@@ -361,7 +367,7 @@ struct tile_unit { uint32_t tile, part; };
 // Runs of consecutive units go to one of the eight XCDs each, whose L2 then holds what they share.  Workgroups are dealt out to XCDs in turn.
 __device__ __forceinline__ bool unit_of_workgroup(const tile_split &s, tile_unit &u)
 {
-    uint32_t id = blockIdx.x;
+    uint32_t id = workgroup_id();
     const bool whole = id < s.whole;
     if (!whole) id -= s.whole;                                  // (a multiple of eight)
     const uint32_t n = whole ? s.whole : s.rest * s.parts, per = (n + 7) / 8, at = id >> 3, t = (id & 7) * per + at;
@@ -634,7 +640,7 @@ int32_t launch_tiles(typename Op::args a, int columns, hipStream_t s)
     const int64_t tiles = most_tiles(a.g.n_rows, a.g.n, Op::kQ) * a.p_tiles, round = a.parts ? op::kRound : 0;
     if (tiles > 0x7ff00000LL) return MW_ERR_UNSUPPORTED;
     // T tiles are at most T - rest + kRound units, eights of them
-    hipLaunchKernelGGL((k_tiles<Op>), dim3((uint32_t)((tiles + round + 15) / 8 * 8)), dim3(kTileThreads), 0, s, a);
+    hipLaunchKernelGGL((k_tiles<Op>), grid_of((uint32_t)((tiles + round + 15) / 8 * 8)), dim3(kTileThreads), 0, s, a);
     MW_HIP_CHECK(hipGetLastError());
     if (a.parts) {
         hipLaunchKernelGGL((k_join<Op>), dim3(Op::kQ / op::kJoinRows, (uint32_t)(tiles < kUnits ? tiles : kUnits)), dim3(kTileThreads), 0, s, a);
