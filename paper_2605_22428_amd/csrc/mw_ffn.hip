@@ -317,13 +317,6 @@ int32_t ffn_ready(const mw_ctx *ctx, const mw_experts *e, bool backward)
 }
 // A matrix of bf16 rows of the caller's.
 bool rows_fit(const void *p, int64_t stride, int64_t width) { return p && !((uintptr_t)p & 15u) && stride >= width && stride % 8 == 0; }
-// Gradients of matrices by the runs' length and the tiles: sums of a few steps take 128 x 128 with room for one step, long ones over enough tiles 256 x 256.  us of the gradients alone, 128 x 128 /
-// 256 x 256: four experts 7168 x 2048, 512 rows 90 / 117, 2048 200 / 201, 4096 365 / 334, 8192 675 / 596; eight 4096 x 1024, 2048 rows 77 / 82, 4096 115 / 115, 8192 204 / 189;
-// 32 of 2048 x 768, 4096 rows 84 / 109; five 2880 x 1000, 2000 rows 52 / 49; two 1024 x 512 (48 of the larger tiles), 4000 rows 45 / 54.
-static inline bool grads_large(int64_t n_rows, int64_t n, int64_t hidden, int64_t inter)
-{
-    return n_rows >= 512 * n && (pieces(2 * inter, 256) + pieces(inter, 256)) * pieces(hidden, 256) * n >= kUnits;
-}
 template <int kP, int kQ>
 int32_t launch_grads(grads_args a, hipStream_t s)
 {
@@ -377,12 +370,11 @@ extern "C" MW_API int32_t mw_ffn(mw_ctx *ctx, const mw_experts *experts, const v
     const row_groups g = {expert_offsets_dev, n_rows, ctx->n_local};
     const hipStream_t s = (hipStream_t)stream;
     if (int8) return mw_ffn_int8(experts, H, x_dev, x_stride, expert_offsets_dev, ctx->n_local, n_rows, row_weights_dev, y_dev, y_stride, b + w.act, (int8_t *)(b + w.codes), (float *)(b + w.scales), (float *)(b + w.parts), s);
-    const int few = pieces(2 * (int64_t)I, 128) * g.n > kUnits ? 10 : 16;          // (both products' rows are few, or neither's)
-    const int form = rows_form(n_rows, g.n, 2 * (int64_t)I, pieces(H, 64), true, few), down_form = rows_form(n_rows, g.n, H, pieces(I, 64), true, few);
+    const two_forms form = forward_forms(n_rows, g.n, H, I);
     const up_op<256, 256>::args u = {g, (const uint16_t *)x_dev, x_stride, (const uint16_t *)experts->gate_up_dev, (uint16_t *)(b + w.act), (uint16_t *)kept_dev, (float *)(b + w.parts), H, I, 0};
-    const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), form == kFew ? 2 * (int64_t)I : I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
-    rc = launch_product<up_op<256, 256>, up_op<256, 128>, up_op<128, 64>, true>(form, u, I, s);
-    if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<256, 128, false>, rows_op<128, 64, false>, true>(down_form, d, H, s);
+    const rows_op<256, 256, false>::args d = {g, (const uint16_t *)(b + w.act), form.second == kFew ? 2 * (int64_t)I : I, (const uint16_t *)experts->down_dev, row_weights_dev, (uint16_t *)y_dev, y_stride, (float *)(b + w.parts), I, H, 0};
+    rc = launch_product<up_op<256, 256>, up_op<256, 128>, up_op<128, 64>, true>(form.first, u, I, s);
+    if (rc == MW_OK) rc = launch_product<rows_op<256, 256, false>, rows_op<256, 128, false>, rows_op<128, 64, false>, true>(form.second, d, H, s);
     return rc;
 }
 
@@ -412,8 +404,9 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
     const bool matrices = d_gate_up_dev || d_down_dev;
     const weights_args of_rows = {sums, d_row_weights_dev, (int32_t)pieces(I, kSum)};
     if (n_rows > 0) {
+        const two_forms form = backward_forms(n_rows, g.n, H, I);
         const act_op<256, 256>::args a = {g, (const uint16_t *)dy_dev, dy_stride, (const uint16_t *)experts->down_dev, row_weights_dev, (const uint16_t *)kept_dev, act, d_act, sums, parts, H, I, 0};
-        rc = launch_product<act_op<256, 256>, act_op<256, 128>, act_op<128, 64>, false>(rows_form(n_rows, g.n, I, pieces(H, 64), true), a, I, s);
+        rc = launch_product<act_op<256, 256>, act_op<256, 128>, act_op<128, 64>, false>(form.first, a, I, s);
         if (rc != MW_OK) return rc;
         if (sums && !matrices) {
             hipLaunchKernelGGL(k_ffn_weights, dim3((uint32_t)pieces(n_rows, 16)), dim3(256), 0, s, g, of_rows);
@@ -421,7 +414,7 @@ extern "C" MW_API int32_t mw_ffn_backward(mw_ctx *ctx, const mw_experts *experts
         }
         if (dx_dev) {
             const rows_op<256, 256, true>::args d = {g, d_act, 2 * (int64_t)I, (const uint16_t *)experts->gate_up_dev, nullptr, (uint16_t *)dx_dev, dx_stride, parts, 2 * I, H, 0};
-            rc = launch_product<rows_op<256, 256, true>, rows_op<256, 128, true>, rows_op<128, 64, true>, false>(rows_form(n_rows, g.n, H, pieces(2 * (int64_t)I, 64), true), d, H, s);
+            rc = launch_product<rows_op<256, 256, true>, rows_op<256, 128, true>, rows_op<128, 64, true>, false>(form.second, d, H, s);
             if (rc != MW_OK) return rc;
         }
     }

@@ -169,7 +169,7 @@ struct int8_op {
 template <bool kGated, bool kF32>
 int32_t launch_int8(const typename int8_op<256, 256, kGated, kF32>::args &a, hipStream_t s)
 {
-    return launch_product<int8_op<256, 256, kGated, kF32>, int8_op<256, 128, kGated, kF32>, int8_op<128, 64, kGated, kF32>, true>(rows_form(a.g.n_rows, a.g.n, kGated ? 2 * (int64_t)a.N : a.N, (a.K + 127) / 128, a.parts != nullptr), a, a.N, s);
+    return launch_product<int8_op<256, 256, kGated, kF32>, int8_op<256, 128, kGated, kF32>, int8_op<128, 64, kGated, kF32>, true>(int8_form(a.g.n_rows, a.g.n, kGated ? 2 * (int64_t)a.N : a.N, a.K, a.parts != nullptr), a, a.N, s);
 }
 // Many rows take a wave each, few or long ones a workgroup each.  us: 16384 rows of 2048 values a workgroup / a wave 22 / 18; of 7168 values 62 / 67.
 int32_t launch_quantize(const quant_args &a, hipStream_t s)

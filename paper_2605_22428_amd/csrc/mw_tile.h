@@ -357,7 +357,7 @@ constexpr uint32_t kMostParts = 16, kLeastSteps = 8, kUnits = 256;
 __host__ __device__ __forceinline__ uint32_t join_steps(uint32_t tiles) { return 20 + tiles / 8; }
 __host__ __device__ __forceinline__ bool parts_pay(uint32_t tiles, uint32_t steps) { return tiles < kUnits && (uint64_t)steps * (kUnits - tiles) >= (uint64_t)join_steps(tiles) * kUnits; }
 struct tile_split { uint32_t whole, rest, parts; };             // tiles in one piece, tiles in parts, parts of each (1: rest are in one piece too)
-__device__ __forceinline__ tile_split split_tiles(uint32_t total, uint32_t round, uint32_t steps, bool may)
+__host__ __device__ __forceinline__ tile_split split_tiles(uint32_t total, uint32_t round, uint32_t steps, bool may)
 {
     tile_split s = {total - total % round, total % round, 1};
     if (may && s.rest > 0 && parts_pay(s.rest, steps)) s.parts = max(1u, min(min(round / s.rest, kMostParts), steps / kLeastSteps));
@@ -629,14 +629,18 @@ __global__ __launch_bounds__(kTileThreads) void k_join(typename Op::args a)
     Op::emit(a, at, row, column, x, y, Op::columns(a, at, column), of_row, Op::fetch(a, at, row, column));
 }
 static inline int64_t most_tiles(int64_t n_rows, int64_t n, int rows_a_tile) { return n_rows / rows_a_tile + (n < n_rows ? n : n_rows); }
+// Whether there may be parts is settled by the host, from the fewest tiles that so many rows are (after whole rounds the rest can be any number); how many there are, on the device by the runs' lengths.
+static inline bool may_have_parts(int64_t n_rows, int64_t n, int rows_a_tile, int64_t column_tiles, int64_t steps)
+{
+    const int64_t rows_tiles = (n_rows + rows_a_tile - 1) / rows_a_tile, runs = n < n_rows ? n : n_rows, fewest = (rows_tiles > runs ? rows_tiles : runs) * column_tiles;
+    return parts_pay((uint32_t)(fewest < kUnits ? fewest : kUnits / 2), (uint32_t)steps);
+}
 template <class Op>
 int32_t launch_tiles(typename Op::args a, int columns, hipStream_t s)
 {
     typedef tile_op<Op> op;
     a.p_tiles = (columns + (Op::kPair ? Op::kP / 2 : Op::kP) - 1) / (Op::kPair ? Op::kP / 2 : Op::kP);
-    // Whether there may be parts is settled here, from the fewest tiles that so many rows are (after whole rounds the rest can be any number); which, by the runs' lengths.
-    const int64_t rows_tiles = (a.g.n_rows + Op::kQ - 1) / Op::kQ, runs = a.g.n < a.g.n_rows ? a.g.n : a.g.n_rows, fewest = (rows_tiles > runs ? rows_tiles : runs) * a.p_tiles;
-    if (!parts_pay((uint32_t)(fewest < kUnits ? fewest : kUnits / 2), (uint32_t)op::steps(a))) a.parts = nullptr;
+    if (!may_have_parts(a.g.n_rows, a.g.n, Op::kQ, a.p_tiles, op::steps(a))) a.parts = nullptr;
     const int64_t tiles = most_tiles(a.g.n_rows, a.g.n, Op::kQ) * a.p_tiles, round = a.parts ? op::kRound : 0;
     if (tiles > 0x7ff00000LL) return MW_ERR_UNSUPPORTED;
     // T tiles are at most T - rest + kRound units, eights of them
