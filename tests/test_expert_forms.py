@@ -40,3 +40,27 @@ def test_the_sizes_of_products_of_codes_reach_every_form():
 def test_both_products_have_few_rows_or_neither(n_rows, n, hidden, inter):
     first, second = tile_rules.values(("mw_few.h",), tuple("forward_forms(%d, %d, %d, %d).%s" % (n_rows, n, hidden, inter, k) for k in ("first", "second")))
     assert (first == X.FEW) == (second == X.FEW)
+
+
+@pytest.mark.parametrize("case", [c for c in X.CASES if len(c[0]) * c[1] * c[2] * sum(c[0]) < 1e9], ids=str)
+def test_a_lost_term_shows(case, monkeypatch):
+    """What the whole numbers are for: without the last row of a run, the last value of a row, the last inner value, or h's second term, the plain form's results are others."""
+    monkeypatch.setattr(X, "DEV", "cpu")
+    b = X.Block(*case)
+    (y, kept), (dx, dgu, dd, dw) = b.forward(X.few(case)), b.backward()
+    last = case[3] + sum(case[0]) - 1
+    e = max(e for e, c in enumerate(case[0]) if c)
+    other = X.Block(*case)
+    other.dy[last] = 0
+    _, less_gu, less_d, _ = other.backward()
+    assert (less_gu[e] != dgu[e]).any(1).any(1).all() and (less_d[e] != dd[e]).any()
+    other = X.Block(*case)
+    other.x[:, -1] = 0
+    other.dy[:, -1] = 0
+    assert (other.forward(X.few(case))[1][case[3]:last + 1] != kept[case[3]:last + 1]).any(0).any(1).all() and (other.backward()[3] != dw)[case[3]:last + 1].any()
+    other = X.Block(*case)
+    other.down[:, :, -1] = 0
+    other.gate_up[:, 1, -1] = 0
+    assert (other.forward(X.few(case))[0] != y)[case[3]:last + 1].any() and (other.backward()[0] != dx)[case[3]:last + 1].any()
+    if X.few(case):
+        assert (b.forward(False)[0] != y).any()
