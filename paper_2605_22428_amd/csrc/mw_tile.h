@@ -145,7 +145,7 @@ template <int kR, bool kTr, bool kInt8>
 struct tile_frags {
     typedef typename tile_kind<kInt8>::frag frag;
     static constexpr int kN = kR / 64;
-    uint32_t from[4];
+    uint32_t from[kTr ? 1 : 4];
     __device__ __forceinline__ void begin(int half)
     {
         const int lane = threadIdx.x & 63;
@@ -153,14 +153,10 @@ struct tile_frags {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) from[kk] = (uint32_t)(half * (kR / 2) + (lane & 31)) * kStep + (((kk * 2 + (lane >> 5)) ^ exchange(lane & 15)) * 16);
         } else {
-            // sixteen lanes take four rows of 16 values: row (lane / 4) % 4, values (lane % 4) * 4 ..; the rows' 32-byte chunks change places with the row
-            const int k = (lane >> 5) * 8 + ((lane >> 2) & 3), chunk = half * (kR / 32) + ((lane >> 4) & 1);
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                // (k + 4 and k + 16 have the same two bits: one place for each of the piece's two reads and of the four steps)
-                const int s = exchange_lines(k) & (kR / 16 - 1);
-                from[kk] = (uint32_t)(k * kR * 2 + (chunk ^ s) * 32 + (lane & 3) * 8);
-            }
+            // sixteen lanes take four rows of 16 values: row (lane / 4) % 4, values (lane % 4) * 4 ..; the rows' 32-byte chunks change places with the row.  One place serves the piece's two
+            // reads (rows k and k + 4) and the four steps along K (16 rows on): these rows' lowest two bits, by which chunks change places, are k's.
+            const int k = (lane >> 5) * 8 + ((lane >> 2) & 3), chunk = half * (kR / 32) + ((lane >> 4) & 1), s = exchange_lines(k) & (kR / 16 - 1);
+            from[0] = (uint32_t)(k * kR * 2 + (chunk ^ s) * 32 + (lane & 3) * 8);
         }
     }
     __device__ __forceinline__ frag read(const lds_char *stage, int kk, int t) const
