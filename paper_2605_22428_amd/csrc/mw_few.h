@@ -241,9 +241,10 @@ static inline two_forms backward_forms(int64_t n_rows, int64_t n, int64_t hidden
     return {rows_form(n_rows, n, inter, (hidden + 63) / 64, true), rows_form(n_rows, n, hidden, (2 * inter + 63) / 64, true)};
 }
 static inline int int8_form(int64_t n_rows, int64_t n, int64_t columns, int64_t n_in, bool parts) { return rows_form(n_rows, n, columns, (n_in + 127) / 128, parts); }
-// Gradients of matrices by the runs' length and the tiles: sums of a few steps take 128 x 128 with room for one step, long ones over enough tiles 256 x 256.  us of the gradients alone, 128 x 128 /
-// 256 x 256: four experts 7168 x 2048, 512 rows 90 / 117, 2048 200 / 201, 4096 365 / 334, 8192 675 / 596; eight 4096 x 1024, 2048 rows 77 / 82, 4096 115 / 115, 8192 204 / 189;
-// 32 of 2048 x 768, 4096 rows 84 / 109; five 2880 x 1000, 2000 rows 52 / 49; two 1024 x 512 (48 of the larger tiles), 4000 rows 45 / 54.
+// Gradients of matrices by the runs' length and the tiles: sums of a few steps take 128 x 128 with room for one step, long ones over enough tiles 256 x 256.  us of k_ffn_grads without dx before it,
+// medians of a kernel trace, uneven runs, 128 x 128 / 256 x 256: four experts 7168 x 2048, 512 rows 113 / 140, 2048 245 / 248, 4096 391 / 378, 8192 715 / 647, 16384 1565 / 1187; eight
+// 4096 x 1024, 512 rows 44 / 62, 2048 85 / 93, 4096 132 / 130, 8192 226 / 210; 32 of 2048 x 768, 4096 rows 94 / 116; five 2880 x 1000, 333 rows 27 / 33, 2000 56 / 57; two 1024 x 512 (48 of
+// the larger tiles), 4000 rows 48 / 54.
 static inline bool grads_large(int64_t n_rows, int64_t n, int64_t hidden, int64_t inter)
 {
     return n_rows >= 512 * n && ((2 * inter + 255) / 256 + (inter + 255) / 256) * ((hidden + 255) / 256) * n >= kUnits;

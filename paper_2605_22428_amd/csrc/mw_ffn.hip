@@ -9,8 +9,8 @@ namespace {
 // ---- h = silu(x Wg^T) * (x Wu^T) --------------------------------------------------------------------------------
 // Half of a tile's columns are gate rows, half the up rows beside them: a lane then holds both values of an element, and neither product goes to memory unless it is kept.
 // h is rounded to bf16 here, as the next product's matrix instructions take it: at most 2^-8 of h, as the output's own rounding is of y; two terms, as the few rows below have, would
-// double that product.  16384 rows of four experts 7168 x 2048, g and u kept: 860 us (787 the first calls), 1120 TFLOP/s; 512 rows 71 us and a join of 6: 235 MB of weights at 3.1 TB/s, tiles of
-// uneven runs fill three quarters of the CUs.
+// double that product.  Times at these kernels are medians of 33 calls in a kernel trace, the least in brackets; runs are uneven.  16384 rows of four experts 7168 x 2048, g and u kept: 812 us (778), 1180
+// TFLOP/s; 512 rows 71 us (60) and a join of 6: 235 MB of weights at 3.3 TB/s, tiles of uneven runs fill three quarters of the CUs.
 template <int kCols, int kRows>
 struct up_op {
     static constexpr int kP = kCols, kQ = kRows;
@@ -74,8 +74,11 @@ struct up_op {
 };
 
 // ---- rows times a matrix: y = w h Wd^T, dx = [dg du] [Wg; Wu] ---------------------------------------------------
-// dx: the matrices' rows are lines that the sum runs across, so both halves of gate_up are one matrix of 2 I lines, read as it lies.  16384 rows of four experts 7168 x 2048: y 498 us
-// (970 TFLOP/s; sums of 2048 are 32 steps between first loads and results), dx 852 us (1130).
+// dx: the matrices' rows are lines that the sum runs across, so both halves of gate_up are one matrix of 2 I lines, read as it lies.  16384 rows of four experts 7168 x 2048: y 460 us (432),
+// 1050 TFLOP/s (sums of 2048 are 32 steps between first loads and results), dx 841 us (827), 1140.
+// y and dx are stored past the caches, though what follows reads them: the call gains what its reader loses.  us, past / through them, the call, and with a copy of y or dx behind it:
+// mw_ffn, 512 rows of four experts 7168 x 2048 120.0 / 120.3, 123.6 / 123.0; 2048 of eight 4096 x 1024 94.9 / 97.2, 101.6 / 102.1; 16384 of four 7168 x 2048 1223 / 1236, 1287 / 1301; dx of
+// 2048 rows of eight 4096 x 1024 97.6 / 98.7, 103.3 / 103.9.
 template <int kP>
 __device__ __forceinline__ void columns_from(tile_feed<kP, true, false> &fp, const uint16_t *w, int col0, int K, int N)
 {
@@ -133,7 +136,7 @@ struct rows_op {
 
 // ---- da = dy Wd, and what follows from it element by element ------------------------------------------------------
 // da stays in registers: g and u come beside it, and w h, dg and du leave, rounded to bf16 as operands of the products that follow (they are the products' other factors as bf16 dy and x are).
-// dw's sums take da and h unrounded.  16384 rows of four experts 7168 x 2048: 451 us and a join of 11, 1070 TFLOP/s, with 134 MB read and 201 MB written beside the product.
+// dw's sums take da and h unrounded.  16384 rows of four experts 7168 x 2048: 451 us (438) and a join of 13, 1070 TFLOP/s, with 134 MB read and 201 MB written beside the product.
 constexpr int kSum = 64;                        // columns whose da h a row sums up in the tile
 template <int kCols, int kRows>
 struct act_op {
@@ -226,8 +229,8 @@ struct grads_matrix {
 };
 struct grads_args { row_groups g; grads_matrix m[2]; uint32_t first, weights; weights_args w; };          // workgroups of m[0]; of the rows' weights, before all others
 // Tiles of a matrix take as long as its run is: the XCDs get an eighth of every matrix's tiles each, and those of the longest run first.  Both matrices are one launch, and the gate weights'
-// sums, which wait for the same kernel, its first workgroups.  Results are written past the caches: no one reads them soon.  16384 rows of four experts 7168 x 2048: 1165 us, 1240 TFLOP/s; 2048
-// rows of eight 4096 x 1024: 79 us for 52 GFLOP and 201 MB written (writing zeros takes 28).
+// sums, which wait for the same kernel, its first workgroups.  Results are written past the caches: no one reads them soon.  16384 rows of four experts 7168 x 2048: 1162 us (1118), 1240 TFLOP/s;
+// 2048 rows of eight 4096 x 1024: 85 us (80), behind the call's other products 96 (86), for 52 GFLOP and 201 MB written (writing zeros takes 28).
 template <int kP, int kQ>
 __global__ __launch_bounds__(kTileThreads, kP * kQ > 128 * 128 ? 1 : 5) void k_ffn_grads(grads_args a)
 {

@@ -84,7 +84,8 @@ __global__ __launch_bounds__(256) void k_quantize(quant_args a)
 // ---- rows of codes times matrices of codes ------------------------------------------------------------------------
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 // Sums of codes are whole numbers, so their order and parts change nothing; the factors come in once, in fp32, at the end.  kGated: y = silu(gate) * up, columns as in the bf16 experts'.
-// 8192 rows, 7168 -> 7168: 362 (the first calls) to 425 us, 1980 to 2330 TOP/s; 16384 rows of four experts 7168 x 2048, gated: 474 us (2030), back 290 us (1660; 16 steps a tile).
+// Medians of 33 calls in a kernel trace (the least): 8192 rows, 7168 -> 7168, 386 us (366), 2180 TOP/s; 16384 rows of four experts 7168 x 2048, gated, 467 us (457), 2060 TOP/s, and back 276 us
+// (262), 1740 (16 steps a tile).
 template <int kCols, int kRows, bool kGated, bool kF32>
 struct int8_op {
     static constexpr int kP = kCols, kQ = kRows;

@@ -13,7 +13,7 @@
 // the operand.  Neither has a bank conflict (counted).
 //
 // What bounds it: with all CUs busy the matrix instructions and, behind them, the clock that the card holds while they run (a large product's first calls after a pause take a tenth less than
-// those that follow).  16384 rows of codes times 7168 x 7168, 682 us, 2470 TOP/s; bf16 sums of 7168, 16384 x 4096, 740 us, 1300 TFLOP/s; 10 to 18 us a round of tiles go to first loads and to results.
+// those that follow).  16384 rows of codes times 7168 x 7168, 757 us (least 688), 2220 TOP/s (2450); bf16 sums of 7168, 16384 x 4096, 750 us (720), 1280 TFLOP/s (1340); 10 to 18 us a round of tiles go to first loads and to results.
 // Workgroups that stay, and load their next tile's first step before the results of the one before leave, were not faster (sums of 7168 and 2048, 16384 rows, 1240 -> 1246 us; gradients
 // of uneven runs 2429 -> 2526): the hardware hands the next tile to whichever CU is free.
 #ifndef MW_TILE_H_
@@ -280,7 +280,9 @@ struct tile_product {
 };
 
 // The same with room for one step: for sums of a few steps, whose time is waiting for the first loads and writing results, five workgroups a CU that wait for themselves hide
-// more than two that load ahead (gradients of 512 rows over eight experts 4096 x 1024 55 -> 38 us, of 2048 rows 86 -> 69).  Long sums want the room: 512 rows of four experts 7168 x 2048 99 -> 125.
+// more than two that load ahead.  us, room for two / one, medians of a kernel trace over uneven runs: gradients of 512 rows over eight experts 4096 x 1024 59 / 44, 2048 rows 103 / 85, four
+// 7168 x 2048, 512 rows 146 / 113, 2048 rows 268 / 245.  Long sums over few tiles want the room: 4000 rows over two experts 1024 x 512 24 / 48; products of rows, mw_ffn, 512 rows of four
+// 7168 x 2048 120 / 159, 16384 rows 1223 / 1807.
 template <int kP, int kQ, bool kTrP, bool kTrQ, bool kInt8>
 struct tile_product_short {
     typedef tile_kind<kInt8> kind;
@@ -650,7 +652,7 @@ int32_t launch_tiles(typename Op::args a, int columns, hipStream_t s)
 }
 
 __device__ __forceinline__ float tile_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
-// kStreaming: nobody reads it soon.
+// kStreaming: past the caches.
 template <bool kStreaming = false>
 __device__ __forceinline__ void store_bf16(uint16_t *to, const float (&v)[8])
 {
