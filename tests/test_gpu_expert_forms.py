@@ -30,7 +30,7 @@ class Run:
     def __init__(self, counts, hidden, inter, before=0, spare=0, pad=0, seed=1):
         self.b = b = X.Block(counts, hidden, inter, before, spare, seed)
         self.pad, n = pad, len(counts)
-        self.ctx = B.Context(1, n, 1, 0, hidden, B.MW_ROW_BF16, 1, max(b.room, 1), np.zeros(n, dtype=np.int32))
+        self.ctx = B.Context(1, n, 1, 0, hidden, B.MW_ROW_BF16, 1, 1, np.zeros(n, dtype=np.int32))
         self.experts = B.Experts(b.gate_up.bfloat16(), b.down.bfloat16())
         self.offsets = X.offsets_of(counts, before)
         self.x, self.rows, self.dy = padded(b.x, pad), padded(b.rows, pad), padded(b.dy, pad)

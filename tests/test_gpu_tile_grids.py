@@ -12,7 +12,14 @@ from test_gpu_ffn import DEV, host, near, normal
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True, scope="module")
+def _leave_no_cache():
+    yield
+    torch.cuda.empty_cache()
+
+
 def _room(gib):
+    torch.cuda.empty_cache()
     free = torch.cuda.mem_get_info()[0]
     if free < gib << 30:
         pytest.skip("%.0f GiB of device memory free, %d needed" % (free / 2 ** 30, gib))
